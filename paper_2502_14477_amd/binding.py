@@ -15,7 +15,7 @@ from typing import Optional, Tuple
 
 import torch
 
-ESA_F32, ESA_BF16 = 0, 1
+ESA_F32, ESA_BF16, ESA_E4M3 = 0, 1, 2
 ESA_W_ROWMAJOR, ESA_W_PACKED = 0, 1
 _PKG = os.path.dirname(os.path.abspath(__file__))
 
@@ -24,6 +24,19 @@ class EsaError(RuntimeError):
     def __init__(self, code: int, text: str):
         super().__init__("libesa error %d: %s" % (code, text))
         self.code = code
+
+
+class PagedCache(ctypes.Structure):
+    """esa_paged_cache of include/esa_paged.h."""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64), ("tok_stride", ctypes.c_int64),
+                ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int), ("h_kv", ctypes.c_int), ("d", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class PagedBatch(ctypes.Structure):
+    """esa_paged_batch of include/esa_paged.h."""
+    _fields_ = [("cu", ctypes.c_void_p), ("start", ctypes.c_void_p), ("pages", ctypes.c_void_p), ("pages_ld", ctypes.c_int64),
+                ("n_tok", ctypes.c_int64), ("n_seq", ctypes.c_int), ("max_pages", ctypes.c_int)]
 
 
 def lib_path() -> str:
@@ -96,6 +109,13 @@ def _load() -> ctypes.CDLL:
     L.esa_attend_reencoded.restype = i32
     L.esa_attend_reencoded.argtypes = [vp, i32, i32, i32, i32, vp, vp, i64, i64, i64, i64, vp, vp, i32, f32, f64, f64,
                                        vp, vp, i32, i32, i64, i64, i64, i64, vp, sz, vp]
+    batch, cache = ctypes.POINTER(PagedBatch), ctypes.POINTER(PagedCache)
+    L.esa_append_paged.restype = i32
+    L.esa_append_paged.argtypes = [vp, i64, vp, i64, vp, i64, i32, vp, i64, batch, cache, f64, i32, vp]
+    L.esa_attend_paged_workspace_bytes.restype = sz
+    L.esa_attend_paged_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32]
+    L.esa_attend_paged.restype = i32
+    L.esa_attend_paged.argtypes = [vp, i64, i32, batch, cache, i64, i64, vp, i32, i64, f32, f32, vp, i64, vp, i32, vp, sz, vp]
     return L
 
 
@@ -109,6 +129,7 @@ EXPORTS = ("esa_version", "esa_last_error", "esa_segments", "esa_pack_weights", 
            "esa_attend_reencoded_workspace_bytes", "esa_attend_reencoded", "esa_compress_qk",
            "esa_select_topk_static_capacity", "esa_select_topk_static_prepare", "esa_select_topk_static",
            "esa_score_select_gather_workspace_bytes", "esa_score_select_gather")
+PAGED_EXPORTS = ("esa_append_paged", "esa_attend_paged_workspace_bytes", "esa_attend_paged")      # include/esa_paged.h
 
 
 _native.set_error_class(EsaError)
@@ -253,3 +274,25 @@ def esa_attend(q: torch.Tensor, k_cache: torch.Tensor, v_cache: torch.Tensor, t0
     """q [B?, l_c, h, d]; caches [B?, S, h_kv, d] holding the current tokens at rows t0..; gathered
     buffers [B?, n_sel, h_kv, d] -> out [B?, l_c, h, d] (and lse [B?, l_c, h] fp32)."""
     return _native.attend(q, k_cache, v_cache, t0, l_i, l_l, k_sel, v_sel, scale, return_lse, _split)
+
+
+def esa_append_paged(k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, start: torch.Tensor, pages: torch.Tensor,
+                     k_cache: torch.Tensor, v_cache: torch.Tensor, k_scale: Optional[torch.Tensor] = None,
+                     v_scale: Optional[torch.Tensor] = None, q: Optional[torch.Tensor] = None, rope_base: Optional[float] = None,
+                     out_q: Optional[torch.Tensor] = None) -> Optional[torch.Tensor]:
+    """Appends k, v [n_tok, h_kv, d] to a paged cache, keys turned to their positions (rope_base=None: as they are), and returns q
+    [n_tok, h, d] turned likewise (None without q).  Rows cu[b] .. cu[b+1] are sequence b's positions start[b], start[b]+1, ...; cu [n_seq+1],
+    start [n_seq] and pages [n_seq, max_pages] are int32.  Caches [n_pages, h_kv, page_size, d] in any order of strides, of k's type or
+    float8_e4m3fn with scales [n_pages, h_kv] uint8 (exponents: 2^(byte - 127)).  `out_q` may be q itself."""
+    return _native.append_paged(k, v, cu, start, pages, k_cache, v_cache, k_scale, v_scale, q, rope_base, out_q)
+
+
+def esa_attend_paged(q: torch.Tensor, cu: torch.Tensor, start: torch.Tensor, pages: torch.Tensor, k_cache: torch.Tensor,
+                     v_cache: torch.Tensor, k_scale: Optional[torch.Tensor] = None, v_scale: Optional[torch.Tensor] = None,
+                     l_i: Optional[int] = None, l_l: int = 0, idx: Optional[torch.Tensor] = None, scale: Optional[float] = None,
+                     cap: float = 0.0, out: Optional[torch.Tensor] = None, return_lse: bool = False):
+    """Attention of q [n_tok, h, d] over the pages of its sequences, to which the rows' keys and values have been appended (arguments as
+    esa_append_paged, `start` from before it) -> out [n_tok, h, d] (and lse [n_tok, h] fp32).  l_i=None: a token sees everything up to
+    itself; else the initial, the local and the selected positions idx [n_seq, n_sel] int32 (-1: none), segments as esa_segments.
+    cap > 0: scores become cap * tanh(score / cap)."""
+    return _native.attend_paged(q, cu, start, pages, k_cache, v_cache, k_scale, v_scale, l_i, l_l, idx, scale, cap, out, return_lse)

@@ -13,6 +13,7 @@
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
 #include <c10/core/Allocator.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -23,6 +24,7 @@
 #include <utility>
 
 #include "esa.h"
+#include "esa_paged.h"
 
 namespace {
 
@@ -615,6 +617,150 @@ ESA_ENTRY(rope, 5) {
   return a[4];
 }
 
+// ---- the paged cache
+// Rows [n_tok, heads, d], a token's heads contiguous.
+struct Rows {
+  int64_t n, heads, d, ld;
+  void* p;
+};
+Rows rows_of(const at::Tensor& t) {
+  const auto n = t.sizes(), s = t.strides();
+  ESA_ASSERT(n.size() == 3);
+  ESA_ASSERT((s[2] == 1 || n[2] == 1) && (s[1] == n[2] || n[1] == 1));
+  return Rows{n[0], n[1], n[2], n[0] > 1 ? s[0] : n[1] * n[2], ptr(t)};
+}
+
+// The sequences and the pool, checked against each other and to be on `dev`.
+struct Paged {
+  esa_paged_batch b;
+  esa_paged_cache c;
+};
+Paged paged_of(PyObject* cu_obj, PyObject* start_obj, PyObject* pages_obj, PyObject* k_obj, PyObject* v_obj, PyObject* ks_obj, PyObject* vs_obj,
+               const at::Tensor& rows, const Rows& r) {
+  const at::Tensor &cu = tensor_of(cu_obj), &start = tensor_of(start_obj), &pages = tensor_of(pages_obj), &k = tensor_of(k_obj), &v = tensor_of(v_obj);
+  const at::Tensor *ks = tensor_or_none(ks_obj), *vs = tensor_or_none(vs_obj);
+  Paged x;
+  ESA_ASSERT(cu.scalar_type() == at::kInt && start.scalar_type() == at::kInt && pages.scalar_type() == at::kInt);
+  ESA_ASSERT(cu.dim() == 1 && start.dim() == 1 && pages.dim() == 2 && cu.size(0) == start.size(0) + 1 && pages.size(0) == start.size(0));
+  ESA_ASSERT((cu.stride(0) == 1) && (start.stride(0) == 1 || start.size(0) <= 1) && (pages.stride(1) == 1 || pages.size(1) == 1));
+  ESA_ASSERT(start.size(0) <= INT32_MAX && pages.size(1) <= INT32_MAX);
+  x.b.cu = (const int32_t*)ptr(cu);
+  x.b.start = (const int32_t*)ptr(start);
+  x.b.pages = (const int32_t*)ptr(pages);
+  x.b.n_seq = (int)start.size(0);
+  x.b.max_pages = (int)pages.size(1);
+  x.b.pages_ld = x.b.n_seq > 1 ? pages.stride(0) : x.b.max_pages;
+  x.b.n_tok = r.n;
+  const auto n = k.sizes(), s = k.strides();
+  ESA_ASSERT(n.size() == 4 && v.sizes() == n && v.strides() == s && v.scalar_type() == k.scalar_type());
+  ESA_ASSERT((s[3] == 1 || n[3] == 1) && n[3] == r.d && n[0] <= INT32_MAX);
+  x.c.k = ptr(k);
+  x.c.v = ptr(v);
+  x.c.n_pages = (int)n[0];
+  x.c.h_kv = (int)n[1];
+  x.c.page_size = (int)n[2];
+  x.c.d = (int)n[3];
+  x.c.page_stride = n[0] > 1 ? s[0] : n[1] * n[2] * n[3];     // a single page's or head's stride is nobody's
+  x.c.head_stride = n[1] > 1 ? s[1] : n[2] * n[3];
+  x.c.tok_stride = s[2];
+  const bool f8 = k.scalar_type() == at::kFloat8_e4m3fn;
+  ESA_ASSERT(f8 || k.scalar_type() == rows.scalar_type());
+  x.c.dtype = f8 ? ESA_E4M3 : dtype_of(rows);
+  x.c.k_scale = x.c.v_scale = nullptr;
+  ESA_ASSERT((ks != nullptr) == f8 && (vs != nullptr) == f8);
+  if (f8) {
+    ESA_ASSERT(ks->scalar_type() == at::kByte && vs->scalar_type() == at::kByte && ks->is_contiguous() && vs->is_contiguous());
+    ESA_ASSERT(ks->dim() == 2 && ks->size(0) == n[0] && ks->size(1) == n[1] && vs->sizes() == ks->sizes());
+    x.c.k_scale = (uint8_t*)ptr(*ks);
+    x.c.v_scale = (uint8_t*)ptr(*vs);
+  }
+  const at::Device dev = rows.device();
+  ESA_ASSERT(cu.device() == dev && start.device() == dev && pages.device() == dev && k.device() == dev && v.device() == dev &&
+             (!f8 || (ks->device() == dev && vs->device() == dev)) && "tensors of one device");
+  return x;
+}
+void on_gpu(const at::Tensor& t) { ESA_ASSERT(t.is_cuda() && "GPU tensors"); }
+void* stream_on(const at::Device& dev) { return (void*)c10::hip::getCurrentHIPStream(dev.index()).stream(); }
+
+// k, v, cu, start, pages, k_cache, v_cache, k_scale, v_scale, q, rope_base, out_q
+ESA_ENTRY(append_paged, 12) {
+  const at::Tensor &k = tensor_of(a[0]), &v = tensor_of(a[1]);
+  const at::Tensor *q = tensor_or_none(a[9]), *out_q = tensor_or_none(a[11]);
+  const Rows kr = rows_of(k), vr = rows_of(v);
+  const int dt = dtype_of(k);
+  const Paged x = paged_of(a[2], a[3], a[4], a[5], a[6], a[7], a[8], k, kr);
+  ESA_ASSERT(vr.n == kr.n && vr.heads == kr.heads && vr.d == kr.d && kr.heads == x.c.h_kv && v.scalar_type() == k.scalar_type());
+  ESA_ASSERT(v.device() == k.device());
+  const double base = a[10] == Py_None ? 0.0 : float_of(a[10]);
+  if (a[10] != Py_None && !(base > 0.0)) fail_esa(ESA_EINVAL, "esa_append_paged: base must be positive");
+  Rows qr = {}, oq = {};
+  at::Tensor fresh;
+  ESA_ASSERT(q || !out_q);
+  if (q) {
+    qr = rows_of(*q);
+    ESA_ASSERT(qr.n == kr.n && qr.d == kr.d && q->scalar_type() == k.scalar_type() && q->device() == k.device());
+  }
+  on_gpu(k);
+  const c10::DeviceGuard guard(k.device());
+  if (q) {
+    if (!out_q) fresh = new_tensor({qr.n, qr.heads, qr.d}, q->scalar_type(), q->device());
+    const at::Tensor& o = out_q ? *out_q : fresh;
+    oq = rows_of(o);
+    ESA_ASSERT(oq.n == qr.n && oq.heads == qr.heads && oq.d == qr.d && o.scalar_type() == q->scalar_type() && o.device() == q->device());
+  }
+  void* st = stream_on(k.device());
+  launch([&] {
+    return esa_append_paged(kr.p, kr.ld, vr.p, vr.ld, qr.p, qr.ld, (int)qr.heads, oq.p, oq.ld, &x.b, &x.c, base, dt, st);
+  });
+  if (!q) Py_RETURN_NONE;
+  if (!out_q) return wrap(std::move(fresh));
+  Py_INCREF(a[11]);
+  return a[11];
+}
+
+// q, cu, start, pages, k_cache, v_cache, k_scale, v_scale, l_i, l_l, idx, scale, cap, out, return_lse
+ESA_ENTRY(attend_paged, 15) {
+  const at::Tensor& q = tensor_of(a[0]);
+  const Rows qr = rows_of(q);
+  const int dt = dtype_of(q);
+  const Paged x = paged_of(a[1], a[2], a[3], a[4], a[5], a[6], a[7], q, qr);
+  const int64_t l_i = a[8] == Py_None ? INT64_MAX : int_of(a[8]), l_l = int_of(a[9]);
+  const at::Tensor *idx = tensor_or_none(a[10]), *out = tensor_or_none(a[13]);
+  const double scale = a[11] == Py_None ? 1.0 / std::sqrt((double)qr.d) : float_of(a[11]), cap = float_of(a[12]);
+  const bool want_lse = true_of(a[14]);
+  int n_sel = 0;
+  int64_t idx_ld = 0;
+  if (idx) {
+    ESA_ASSERT(idx->scalar_type() == at::kInt && idx->dim() == 2 && idx->size(0) == x.b.n_seq && (idx->size(1) <= 1 || idx->stride(1) == 1));
+    ESA_ASSERT(idx->device() == q.device() && idx->size(1) <= INT32_MAX);
+    n_sel = (int)idx->size(1);
+    idx_ld = x.b.n_seq > 1 ? idx->stride(0) : n_sel;
+  }
+  if (out) ESA_ASSERT(out->sizes() == q.sizes() && out->scalar_type() == q.scalar_type() && out->device() == q.device());
+  on_gpu(q);
+  const c10::DeviceGuard guard(q.device());
+  at::Tensor fresh, lse;
+  if (!out) fresh = new_tensor({qr.n, qr.heads, qr.d}, q.scalar_type(), q.device());
+  if (want_lse) lse = new_tensor({qr.n, qr.heads}, at::kFloat, q.device());
+  const Rows o = rows_of(out ? *out : fresh);
+  const Scratch ws = scratch(esa_attend_paged_workspace_bytes(qr.n, x.b.n_seq, (int)qr.heads, x.c.h_kv, x.c.d, dt));
+  void *st = stream_on(q.device()), *wp = ws.p, *ip = idx && n_sel ? ptr(*idx) : nullptr;
+  float* lp = want_lse ? (float*)ptr(lse) : nullptr;
+  const size_t wn = ws.n;
+  launch([&] {
+    return esa_attend_paged(qr.p, qr.ld, (int)qr.heads, &x.b, &x.c, l_i, l_l, (const int32_t*)ip, n_sel, idx_ld, (float)scale, (float)cap, o.p,
+                            o.ld, lp, dt, wp, wn, st);
+  });
+  PyObject* result;
+  if (out) {
+    Py_INCREF(a[13]);
+    result = a[13];
+  } else {
+    result = wrap(std::move(fresh));
+  }
+  return want_lse ? tuple_of({result, wrap(std::move(lse))}) : result;
+}
+
 // t0, l_i, l_l
 ESA_ENTRY(segments, 3) {
   int64_t i_end = 0, l_start = 0;
@@ -634,7 +780,7 @@ ESA_ENTRY(set_error_class, 1) {
 PyMethodDef methods[] = {ESA_METHOD(compress), ESA_METHOD(compress_qk), ESA_METHOD(score), ESA_METHOD(select_topk),
                          ESA_METHOD(select_topk_static), ESA_METHOD(score_select_gather), ESA_METHOD(gather_kv),
                          ESA_METHOD(attend_indexed), ESA_METHOD(attend_reencoded), ESA_METHOD(attend), ESA_METHOD(attend_local),
-                         ESA_METHOD(rope), ESA_METHOD(segments), ESA_METHOD(set_error_class), {nullptr, nullptr, 0, nullptr}};
+                         ESA_METHOD(rope), ESA_METHOD(append_paged), ESA_METHOD(attend_paged), ESA_METHOD(segments), ESA_METHOD(set_error_class), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "argument marshalling for libesa", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

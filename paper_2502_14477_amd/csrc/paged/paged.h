@@ -1,0 +1,151 @@
+// What the kernels of the paged cache share: a call's sequences, the way from a position to its row, 8-bit blocks.
+#pragma once
+#include "esa_common.h"
+#include "esa_paged.h"
+
+namespace esa {
+namespace paged {
+
+// ---------------------------------------------------------------- the call as the kernels take it
+struct Batch {
+  const int32_t *cu, *start, *pages;
+  int64_t pages_ld;
+  int n_tok, n_seq, max_pages, page_log2;
+};
+struct Cache {
+  char *k, *v;
+  uint8_t *k_scale, *v_scale;               // [n_pages][h_kv]
+  int64_t page_bytes, head_bytes, tok_bytes;
+  int n_pages, h_kv, d;
+};
+
+// A sequence's rows, clamped so that no content of the arrays leads out of the buffers.
+struct Seq {
+  int row0, n, t0;                          // first row, new tokens, position of the first
+};
+__device__ __forceinline__ Seq sequence(const Batch& a, int b) {
+  const int lo = min(max(a.cu[b], 0), a.n_tok), hi = min(max(a.cu[b + 1], lo), a.n_tok);
+  Seq s;
+  s.row0 = lo;
+  s.n = hi - lo;
+  s.t0 = min(max(a.start[b], 0), INT32_MAX - s.n);
+  return s;
+}
+
+// The sequence that has row `tok`, -1: none.  The whole wave takes part with one tok.
+__device__ __forceinline__ int sequence_with(const Batch& a, int tok) {
+  const int lane = threadIdx.x & 63;
+  int b = 0;                                // sequences that end in front of the row
+  for (int b0 = 0; b0 < a.n_seq; b0 += 64) b += __popcll(__ballot(b0 + lane < a.n_seq && a.cu[b0 + lane + 1] <= tok));
+  if (b == a.n_seq) return -1;
+  const Seq s = sequence(a, b);
+  return tok >= s.row0 && tok < s.row0 + s.n ? b : -1;
+}
+
+// The page of a position, -1 where there is none.
+__device__ __forceinline__ int page_of(const Batch& a, int n_pages, int b, int pos) {
+  const int n = pos >> a.page_log2;
+  const int p = a.pages[(int64_t)b * a.pages_ld + min(n, a.max_pages - 1)];
+  return n < a.max_pages && (uint32_t)p < (uint32_t)n_pages ? p : -1;
+}
+
+// ---------------------------------------------------------------- scans over the sequences, a lane to each, 64 at a time
+__device__ __forceinline__ int64_t wave_scan(int64_t x) {       // inclusive
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int64_t y = __shfl_up(x, d);
+    if (lane >= d) x += y;
+  }
+  return x;
+}
+struct Found {
+  int b;              // the sequence, -1: beyond the last
+  int64_t i;          // what is left within it
+};
+// The sequence in which the u-th of count(b) items each falls.  The whole wave takes part with one u.
+template <typename F> __device__ __forceinline__ Found find(int n_seq, int64_t u, F&& count) {
+  const int lane = threadIdx.x & 63;
+  for (int b0 = 0; b0 < n_seq; b0 += 64) {
+    const int b = b0 + lane;
+    const int64_t c = b < n_seq ? count(b) : 0, upto = wave_scan(c);
+    const uint64_t past = __ballot(upto > u);
+    if (past) {
+      const int at = __ffsll((unsigned long long)past) - 1;
+      return Found{b0 + at, u - __shfl(upto - c, at)};
+    }
+    u -= __shfl(upto, 63);
+  }
+  return Found{-1, 0};
+}
+
+// ---------------------------------------------------------------- 8-bit blocks
+constexpr float kF8Max = 448.f;
+constexpr int kScaleLow = 27, kScaleHigh = 239;      // 2^-100, 2^112
+__device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }      // 2^(byte - 127)
+// The byte of the smallest power of two s with amax <= 448 s (448 = 1.75 * 2^8).
+__device__ __forceinline__ int scale_byte(float amax) {
+  const uint32_t u = __float_as_uint(amax);
+  const int byte = (int)(u >> 23) - 8 + ((u & 0x7FFFFFu) > 0x600000u);
+  return min(max(byte, kScaleLow), kScaleHigh);
+}
+__device__ __forceinline__ float f8_clamped(float x) { return x > kF8Max ? kF8Max : x < -kF8Max ? -kF8Max : x; }      // NaN stays
+// Four numbers, rounded to nearest even.
+__device__ __forceinline__ uint32_t f8_pack(float a, float b, float c, float d) {
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(f8_clamped(a), f8_clamped(b), 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(f8_clamped(c), f8_clamped(d), r, true);
+}
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+__device__ __forceinline__ void f8_unpack(uint32_t x, float (&f)[4]) {
+  const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)x, true);
+  f[0] = lo[0];
+  f[1] = lo[1];
+  f[2] = hi[0];
+  f[3] = hi[1];
+}
+
+// ---------------------------------------------------------------- attention
+struct AttendArgs {
+  Batch batch;
+  Cache cache;
+  const char* q;
+  char* out;
+  float* lse;
+  const int32_t* idx;
+  int64_t ldq, ldo, idx_ld;                 // q, out in bytes
+  int h, group, n_sel, l_i, l_l;
+  float scale, cap;
+};
+
+// A sequence's keys, numbered through [0, i_end), the selected entries, [l_start, t0 + n).
+struct Keys {
+  int t0, i_end, n_sel, l_start, n;
+};
+__device__ __forceinline__ Keys keys_of(const AttendArgs& a, const Seq& s) {
+  const int width = a.batch.max_pages << a.batch.page_log2;      // positions from there on have no page
+  Keys k;
+  k.t0 = s.t0;
+  k.i_end = min(min(a.l_i, s.t0), width);
+  k.l_start = min(max(s.t0 - a.l_l, k.i_end), width);
+  k.n_sel = k.l_start > k.i_end ? a.n_sel : 0;
+  k.n = k.i_end + k.n_sel + (min(s.t0 + s.n, width) - k.l_start);
+  return k;
+}
+// The position of key j < k.n, -1 for an entry that is not seen.
+__device__ __forceinline__ int position(const AttendArgs& a, const Keys& k, int b, int j) {
+  if (j < k.i_end) return j;
+  j -= k.i_end;
+  if (j < k.n_sel) {
+    const int p = a.idx[(int64_t)b * a.idx_ld + j];
+    return p >= k.i_end && p < k.l_start ? p : -1;
+  }
+  return j - k.n_sel + k.l_start;
+}
+
+int launch_append(const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq, int h, void* out_q, int64_t ldoq,
+                  const Batch& b, const Cache& c, bool f8, double base, int dtype, hipStream_t st);
+size_t attend_workspace(int64_t n_tok, int n_seq, int h, int h_kv, int d, int dtype);
+int launch_attend(const AttendArgs& a, bool f8, int dtype, void* ws, hipStream_t st);
+
+}  // namespace paged
+}  // namespace esa
