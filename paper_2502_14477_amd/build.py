@@ -14,7 +14,7 @@ LIB = os.path.join(PKG, "libesa.so")
 NATIVE = os.path.join(PKG, "_native.so")
 
 SOURCES = ["esa_api.hip", "compress.hip", "score.hip", "topk.hip", "gather.hip", "attend.hip", "attend_mfma.hip", "attend_split.hip", "rope.hip",
-           "paged/paged_api.hip", "paged/append.hip", "paged/attend_plain.hip"]
+           "../paged/paged_api.hip", "../paged/append.hip", "../paged/attend_plain.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
@@ -69,7 +69,7 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
     hipcc = _hipcc()
 
     def compile_one(src):
-        obj = os.path.join(OBJ, src.replace("/", "_").replace(".hip", ".o"))
+        obj = os.path.join(OBJ, src.replace("../", "").replace("/", "_").replace(".hip", ".o"))
         out = _run([hipcc, *FLAGS, *EXTRA_FLAGS.get(src, []), "-c", os.path.join(CSRC, src), "-o", obj])
         if verbose and out.strip():
             print(out)
