@@ -1,0 +1,432 @@
+// Attention of few rows over a paged cache (decode, drafts; fp32 of any length): 32 rows (new tokens x query heads of a KV head) and a
+// slice of the keys to a workgroup, head sizes 64 and 128.
+//
+// What counts is that many requests are in flight: a decode step reads every key and value once.  A wave takes tiles of 32 keys by
+// itself, with staging space of its own and no barrier in the loop: a tile's rows arrive in registers, 16 bytes a lane and whole rows
+// to neighbouring lanes, are brought to the arithmetic's type (8-bit pages: times the block's scale, a power of two, so exactly) on
+// their way into LDS, and the next tile is requested before the products.  So from LDS on there is one kernel for all cache types.
+//   S^T = K Q^T, O^T += V^T P^T: a lane stands for a row, softmax stays in the lane and its opposite in the other half of the wave, and
+// the layout of S^T's accumulator is the second product's operand layout when key 16 s + 8 (j / 4) + 4 half + j % 4 is operand j of step s.
+// bf16: v_mfma_f32_32x32x16_bf16; a probability enters as two bf16 terms (16 bits), which costs nothing beside the loads.
+// fp32: v_mfma_f32_32x32x2_f32.
+#include "plan.h"
+
+#include <type_traits>
+
+namespace esa {
+namespace paged {
+namespace {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+
+constexpr int kRows = 32, kKeys = 32, kWaves = 4;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// Softmax in base 2 on the hardware's exponential for bf16, in base e and full precision for fp32.
+template <typename T> __device__ __forceinline__ float exp_of(float x) { return sizeof(T) == 2 ? __builtin_amdgcn_exp2f(x) : expf(x); }
+template <typename T> __device__ __forceinline__ float lse_of(float m, float l) { return sizeof(T) == 2 ? __builtin_fmaf(m, kLn2, logf(l)) : m + logf(l); }
+
+__device__ __forceinline__ float halves_max(float v) {
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
+}
+__device__ __forceinline__ float halves_sum(float v) {
+  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
+}
+__device__ __forceinline__ void wave_fence() {      // LDS operations of a wave are in order: only the compiler has to keep it
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+struct FewArgs {
+  AttendArgs a;
+  Shape shape;
+  float* part_o;          // [slot][h_kv][kRows][D], relative to the slice's largest logit
+  float* part_ml;         // [slot][h_kv][kRows][2]: the largest logit, the sum of exponentials
+  float scale;            // bf16: includes log2(e); with a cap: 1 / cap
+  float cap;              // bf16: includes log2(e)
+};
+
+// Scores as the softmax takes them.
+template <typename T, bool CAP> __device__ __forceinline__ float score_of(float dot, float scale, float cap) {
+  const float x = dot * scale;
+  if constexpr (!CAP) return x;
+  if constexpr (sizeof(T) == 4) return cap * tanhf(x);
+  // tanh x = 1 - 2 / (1 + e^(2x)): some 2^-22 of the cap off where x is small, two roundings of a probability to 16 bits less than those
+  const float e = __builtin_amdgcn_exp2f(x * (2.f * kLog2e));
+  return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + e), cap);
+}
+
+template <typename T, bool F8, int D, bool CAP>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D * sizeof(T) > 256 ? 1 : 2))) void attend_few(FewArgs f) {
+  constexpr bool kBf16 = sizeof(T) == 2;
+  constexpr int kRowBytes = D * (int)sizeof(T);                 // of a staged row
+  constexpr int kHeldBytes = F8 ? D : kRowBytes;                // of a row in the pool
+  constexpr int kPieces = kHeldBytes / 16;                      // lanes that fetch a row
+  constexpr int kLoadRows = 64 / kPieces, kLoads = kKeys / kLoadRows;
+  constexpr int kKS = kRowBytes / 32;                           // 16-byte fragments of a half-wave's part of a row
+  constexpr int kMD = D / 32;
+  constexpr int kTileBytes = kKeys * kRowBytes;
+  __shared__ __attribute__((aligned(16))) unsigned char stage[kWaves][2][kTileBytes];
+  __shared__ float ml[kWaves][kRows][2];
+  const AttendArgs& a = f.a;
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, hi = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int g = blockIdx.x % a.cache.h_kv;
+  const int slice = slice_tiles(a, f.shape);
+  const Part at = part_of(a, f.shape, slice, blockIdx.x / a.cache.h_kv);
+  if (at.b < 0) return;
+  const Seq s = sequence(a.batch, at.b);
+  const Keys keys = keys_of(a, s);
+  const int n_rows = s.n * a.group, row0 = at.block * kRows, rows = min(n_rows - row0, kRows);
+  const int n_vis = keys_until(a, s, keys, row0 + rows - 1), tiles = (n_vis + kKeys - 1) / kKeys;
+  const int first = at.slice * slice, end = min(first + slice, tiles);
+  if (at.slice > 0 && first >= end) return;
+  const bool alone = tiles <= slice;
+
+  // a lane's row: both halves of the wave have it; rows behind the last repeat it
+  const int row = row0 + min(r, rows - 1), c = row / a.group, head = g * a.group + row - c * a.group, own = s.t0 + c;
+  const int own_first = s.t0 + row0 / a.group;                  // position of the block's first row
+  u32x4 qf[kKS];
+  {
+    const char* q = a.q + (int64_t)(s.row0 + c) * a.ldq + (int64_t)head * kRowBytes + hi * 16;
+#pragma unroll
+    for (int i = 0; i < kKS; ++i) qf[i] = *(const u32x4*)(q + i * 32);
+  }
+
+  // Lane r stands for key r of a tile: its position (INT32_MAX: not seen), its row's place in the pool, its scales.
+  struct Meta {
+    int pos, page;
+  };
+  auto meta_of = [&](int t) {
+    const int j = t * kKeys + r;
+    Meta m{INT32_MAX, -1};
+    if (j < n_vis) {
+      const int p = position(a, keys, at.b, j);
+      m.page = p >= 0 ? page_of(a.batch, a.cache.n_pages, at.b, p) : -1;
+      if (m.page >= 0) m.pos = p;
+    }
+    return m;
+  };
+  const int slot_mask = (1 << a.batch.page_log2) - 1;
+  u32x4 kr[kLoads], vr[kLoads];
+  float ks = 1.f, vs = 1.f;                                     // of the lane's key
+  auto load = [&](const Meta& m) {
+    const int page = max(m.page, 0);
+    const int64_t place = page * a.cache.page_bytes + g * a.cache.head_bytes + (m.page >= 0 ? m.pos & slot_mask : 0) * a.cache.tok_bytes;
+    if constexpr (F8) {
+      const int kb = a.cache.k_scale[(int64_t)page * a.cache.h_kv + g], vb = a.cache.v_scale[(int64_t)page * a.cache.h_kv + g];
+      ks = scale_of(m.page >= 0 ? kb : 127);                    // (a page that nobody has may hold an infinite one)
+      vs = scale_of(m.page >= 0 ? vb : 127);
+    }
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int64_t from = __shfl(place, i * kLoadRows + lane / kPieces) + lane % kPieces * 16;
+      kr[i] = *(const u32x4*)(a.cache.k + from);
+      vr[i] = *(const u32x4*)(a.cache.v + from);
+    }
+  };
+  // Staged rows are swizzled: 16-byte piece p of a key row lies in place p ^ (row mod 16), of a value row the 64-byte chunks by
+  // row mod 4 (rows of 128 bytes: two share the 256 bytes that the banks cover, and take half the row's number).
+  auto k_swizzle = [](int key) { return kRowBytes >= 256 ? key & 15 : (key >> 1) & 7; };
+  auto v_swizzle = [](int key) { return kRowBytes >= 256 ? (key & 3) << 2 : ((key >> 1) & 1) << 2; };
+  unsigned char* const k_st = stage[wave][0];
+  unsigned char* const v_st = stage[wave][1];
+  auto put = [&](unsigned char* st, const u32x4& x, float scale, int key, int swizzle) {
+    const int piece = lane % kPieces;
+    unsigned char* to = st + key * kRowBytes;
+    if constexpr (!F8) {
+      *(u32x4*)(to + ((piece ^ swizzle) << 4)) = x;
+    } else if constexpr (kBf16) {
+      u32x4 y[2];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        y[i / 2][i % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], scale, false));
+        y[i / 2][i % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[i], scale, true));
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) *(u32x4*)(to + (((piece * 2 + i) ^ swizzle) << 4)) = y[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float y[4];
+        f8_unpack(x[i], y);
+        *(f32x4*)(to + (((piece * 4 + i) ^ swizzle) << 4)) = f32x4{y[0] * scale, y[1] * scale, y[2] * scale, y[3] * scale};
+      }
+    }
+  };
+
+  f32x16 o[kMD];
+#pragma unroll
+  for (int md = 0; md < kMD; ++md)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) o[md][v] = 0.f;
+  float m_run = -INFINITY, l_run = 0.f;
+
+  int t = first + wave;
+  Meta now{INT32_MAX, -1}, next{INT32_MAX, -1};
+  if (t < end) {
+    now = meta_of(t);
+    load(now);
+    if (t + kWaves < end) next = meta_of(t + kWaves);
+  }
+  for (; t < end; t += kWaves) {
+    const uint64_t unseen = __ballot(now.pos == INT32_MAX);
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const int key = i * kLoadRows + lane / kPieces;
+      u32x4 k = kr[i], v = vr[i];
+      if (unseen && ((unseen >> key) & 1)) k = v = u32x4{0, 0, 0, 0};        // whatever lies there: 0 times a NaN is one
+      put(k_st, k, F8 ? __shfl(ks, key) : 1.f, key, k_swizzle(key));
+      put(v_st, v, F8 ? __shfl(vs, key) : 1.f, key, v_swizzle(key));
+    }
+    const int pos = now.pos;
+    now = next;
+    if (t + kWaves < end) load(now);
+    if (t + 2 * kWaves < end) next = meta_of(t + 2 * kWaves);
+    wave_fence();
+
+    f32x16 x, x_odd;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) x[v] = x_odd[v] = 0.f;
+#pragma unroll
+    for (int i = 0; i < kKS; ++i) {
+      const u32x4 kf = *(const u32x4*)(k_st + r * kRowBytes + (((2 * i + hi) ^ k_swizzle(r)) << 4));
+      if constexpr (kBf16) {
+        f32x16& chain = i & 1 ? x_odd : x;
+        chain = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[i]), chain, 0, 0, 0);
+      } else {
+        const f32x4 k4 = __builtin_bit_cast(f32x4, kf), q4 = __builtin_bit_cast(f32x4, qf[i]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(k4[e], q4[e], x, 0, 0, 0);
+      }
+    }
+    if constexpr (kBf16) x += x_odd;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) x[v] = score_of<T, CAP>(x[v], f.scale, f.cap);
+    if (__ballot(pos > own_first)) {                            // some key is not for all rows
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (__shfl(pos, 8 * (v / 4) + 4 * hi + v % 4) > own) x[v] = -INFINITY;
+    }
+    float top = x[0];
+#pragma unroll
+    for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
+    top = fmaxf(m_run, halves_max(top));
+    const float ref = top == -INFINITY ? 0.f : top, less = exp_of<T>(m_run - ref);
+    m_run = top;
+    float sum = 0.f;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) {
+      x[v] = exp_of<T>(x[v] - ref);
+      sum += x[v];
+    }
+    l_run = l_run * less + sum;
+    if (__ballot(less != 1.f)) {
+#pragma unroll
+      for (int md = 0; md < kMD; ++md)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) o[md][v] *= less;
+    }
+    if constexpr (kBf16) {
+      const int tr_key = 4 * hi + ((lane & 15) >> 2), tr_dim = ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
+#pragma unroll
+      for (int kp = 0; kp < 2; ++kp) {
+        bf16x8 p, rest;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          p[e] = (__bf16)x[8 * kp + e];
+          rest[e] = (__bf16)(x[8 * kp + e] - (float)p[e]);
+        }
+#pragma unroll
+        for (int md = 0; md < kMD; ++md) {
+          // lane i of sixteen receives element i % 4 of the 8 bytes that lanes 4 e + i / 4 address: dimension i of keys e = 0 .. 3
+          auto part = [&](int key) {
+            const int piece = (md * 32 + tr_dim) / 8;
+            return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(v_st + key * kRowBytes + ((piece ^ v_swizzle(key)) << 4) + (tr_dim & 4) * 2));
+          };
+          const i16x4 lo = part(16 * kp + tr_key), up = part(16 * kp + 8 + tr_key);
+          const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
+          o[md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p, o[md], 0, 0, 0);
+          o[md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, rest, o[md], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        const int key = 8 * (v / 4) + 4 * hi + v % 4;
+#pragma unroll
+        for (int md = 0; md < kMD; ++md) {
+          const int dim = md * 32 + r;
+          const float vf = *(const float*)(v_st + key * kRowBytes + (((dim / 4) ^ v_swizzle(key)) << 4) + (dim & 3) * 4);
+          o[md] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, x[v], o[md], 0, 0, 0);
+        }
+      }
+    }
+    wave_fence();
+  }
+
+  // ---- the waves' results meet in LDS: a wave's sums of row r, dimensions 4 n ..., at (n * 32 + (r ^ n)) * 16 of its staging space
+  __syncthreads();
+  l_run = halves_sum(l_run);
+  if (hi == 0) {
+    ml[wave][r][0] = m_run;
+    ml[wave][r][1] = l_run;
+  }
+  constexpr int kWaveFloats = 2 * kTileBytes / 4;
+  static_assert(kWaveFloats >= kRows * D, "a wave's staging space holds its sums");
+  float* const sums = (float*)&stage[0][0][0];
+#pragma unroll
+  for (int md = 0; md < kMD; ++md)
+#pragma unroll
+    for (int v = 0; v < 16; v += 4) {
+      const int n = md * 8 + v / 4 * 2 + hi;
+      *(f32x4*)(sums + wave * kWaveFloats + (n * kRows + (r ^ (n & 31))) * 4) = f32x4{o[md][v], o[md][v + 1], o[md][v + 2], o[md][v + 3]};
+    }
+  __syncthreads();
+  for (int e = tid; e < rows * (D / 4); e += 64 * kWaves) {
+    const int n = e % (D / 4), row_in = e / (D / 4);
+    float m = ml[0][row_in][0], l = 0.f;
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) m = fmaxf(m, ml[w][row_in][0]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    f32x4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const float by = exp_of<T>(ml[w][row_in][0] - ref);
+      l = __builtin_fmaf(ml[w][row_in][1], by, l);
+      const f32x4 x = *(const f32x4*)(sums + w * kWaveFloats + (n * kRows + (row_in ^ (n & 31))) * 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum[i] = __builtin_fmaf(x[i], by, sum[i]);
+    }
+    if (alone) {
+      const int rg = row0 + row_in, tok = rg / a.group, hd = g * a.group + rg - tok * a.group;
+      const float inv = l > 0.f ? 1.f / l : 0.f;
+      char* to = a.out + (int64_t)(s.row0 + tok) * a.ldo + (int64_t)hd * kRowBytes;
+      if constexpr (kBf16) {
+        const bf16x2 lo = __builtin_convertvector((f32x2{sum[0] * inv, sum[1] * inv}), bf16x2), up = __builtin_convertvector((f32x2{sum[2] * inv, sum[3] * inv}), bf16x2);
+        *(uint2*)(to + n * 8) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, up));
+      } else {
+        *(f32x4*)(to + n * 16) = f32x4{l > 0.f ? sum[0] / l : 0.f, l > 0.f ? sum[1] / l : 0.f, l > 0.f ? sum[2] / l : 0.f, l > 0.f ? sum[3] / l : 0.f};
+      }
+      if (a.lse && n == 0) a.lse[(int64_t)(s.row0 + tok) * a.h + hd] = l > 0.f ? lse_of<T>(m, l) : -INFINITY;
+    } else {
+      const int64_t part = ((at.slot + (int64_t)at.slice * at.blocks) * a.cache.h_kv + g) * kRows + row_in;
+      *(f32x4*)(f.part_o + part * D + n * 4) = sum;
+      if (n == 0) *(float2*)(f.part_ml + part * 2) = make_float2(m, l);
+    }
+  }
+}
+
+// Slices of a row joined: a wave to a row.
+template <typename T, int D> __global__ __launch_bounds__(256) void attend_join(FewArgs f) {
+  constexpr int kMine = D / 64;
+  typedef __attribute__((ext_vector_type(kMine))) float vec;
+  const AttendArgs& a = f.a;
+  const int lane = threadIdx.x & 63;
+  const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tok = unit / a.h, head = unit % a.h, g = head / a.group;
+  if (tok >= a.batch.n_tok) return;
+  const int b = sequence_with(a.batch, tok);
+  if (b < 0) return;
+  const int slice = slice_tiles(a, f.shape);
+  const Seq s = sequence(a.batch, b);
+  const Keys keys = keys_of(a, s);
+  const int n_rows = s.n * a.group, row = (tok - s.row0) * a.group + head - g * a.group, rows = f.shape.rows;
+  const int block = row / rows, blocks = (n_rows + rows - 1) / rows;
+  const int n_vis = keys_until(a, s, keys, min(block * rows + rows, n_rows) - 1), tiles = (n_vis + f.shape.keys - 1) / f.shape.keys;
+  const int n = (tiles + slice - 1) / slice;
+  if (n <= 1) return;
+  const int64_t slot = parts_before(a, f.shape, slice, b) + block;
+  auto place = [&](int i) { return ((slot + (int64_t)i * blocks) * a.cache.h_kv + g) * rows + row - block * rows; };
+  float m = -INFINITY;
+  for (int i = lane; i < n; i += 64) m = fmaxf(m, f.part_ml[place(i) * 2]);
+  m = wave_max(m);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  vec sum = 0.f;
+  for (int i0 = 0; i0 < n; i0 += 64) {
+    float by = 0.f;
+    if (i0 + lane < n) {
+      const float2 x = *(const float2*)(f.part_ml + place(i0 + lane) * 2);
+      by = exp_of<T>(x.x - ref);
+      l = __builtin_fmaf(x.y, by, l);
+    }
+    const int here = min(n - i0, 64);
+    for (int i = 0; i < here; i += 4) {
+      vec x[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] = *(const vec*)(f.part_o + place(i0 + min(i + u, here - 1)) * D + lane * kMine);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) sum += x[u] * (i + u < here ? __shfl(by, min(i + u, 63)) : 0.f);
+    }
+  }
+  l = wave_sum(l);
+  T* out = (T*)(a.out + (int64_t)tok * a.ldo) + (int64_t)head * D + lane * kMine;
+#pragma unroll
+  for (int i = 0; i < kMine; ++i) store_f32<T>(out + i, l > 0.f ? sum[i] / l : 0.f);
+  if (a.lse && lane == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? lse_of<T>(m, l) : -INFINITY;
+}
+
+// Workgroups that the chip holds: a compute unit has 160 KB of LDS, a workgroup's staging space is 64 KB for rows of up to 256 bytes.
+Shape shape_of(int d, int es) { return Shape{kRows, kKeys, d * es > 256 ? 256 : d * es == 256 ? 512 : 1024, kWaves}; }
+
+template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, hipStream_t st) {
+  if (f.a.cap > 0.f)
+    attend_few<T, F8, D, true><<<grid, 64 * kWaves, 0, st>>>(f);
+  else
+    attend_few<T, F8, D, false><<<grid, 64 * kWaves, 0, st>>>(f);
+  ESA_LAUNCH_CHECK("attend_few");
+  return ESA_OK;
+}
+template <typename T> int launch_all(FewArgs& f, bool f8, void* ws, hipStream_t st) {
+  const AttendArgs& a = f.a;
+  const int d = a.cache.d;
+  f.shape = shape_of(d, sizeof(T));
+  f.part_o = (float*)ws;
+  f.part_ml = f.part_o + most_parts(f.shape, a.cache.h_kv) * a.cache.h_kv * kRows * d;
+  const float base = sizeof(T) == 2 ? kLog2e : 1.f;
+  f.scale = a.cap > 0.f ? a.scale / a.cap : a.scale * base;
+  f.cap = a.cap * base;
+  const int64_t units = most_units(f.shape, a.batch.n_tok, a.batch.n_seq, a.group, a.cache.h_kv) * a.cache.h_kv;
+  if (units > INT32_MAX) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: %lld workgroups", (long long)units);
+  const dim3 grid((unsigned)units);
+  int rc;
+  if (d == 64)
+    rc = f8 ? launch<T, true, 64>(f, grid, st) : launch<T, false, 64>(f, grid, st);
+  else
+    rc = f8 ? launch<T, true, 128>(f, grid, st) : launch<T, false, 128>(f, grid, st);
+  if (rc != ESA_OK) return rc;
+  // (the longest sequence that the table has room for may be a slice)
+  if (((int64_t)a.batch.max_pages << a.batch.page_log2) + a.n_sel <= (int64_t)f.shape.least * kKeys) return ESA_OK;
+  const dim3 join((unsigned)((a.batch.n_tok * (int64_t)a.h + 3) / 4));
+  if (d == 64)
+    attend_join<T, 64><<<join, 256, 0, st>>>(f);
+  else
+    attend_join<T, 128><<<join, 256, 0, st>>>(f);
+  ESA_LAUNCH_CHECK("attend_join");
+  return ESA_OK;
+}
+
+}  // namespace
+
+size_t few_workspace(int h_kv, int d, int dtype) {
+  const Shape sh = shape_of(d, dtype == ESA_F32 ? 4 : 2);
+  return (size_t)(most_parts(sh, h_kv) * h_kv * kRows) * (d + 2) * sizeof(float);
+}
+
+int launch_few(const AttendArgs& a, bool f8, int dtype, void* ws, hipStream_t st) {
+  FewArgs f;
+  f.a = a;
+  return dtype == ESA_F32 ? launch_all<float>(f, f8, ws, st) : launch_all<bf16_t>(f, f8, ws, st);
+}
+
+}  // namespace paged
+}  // namespace esa

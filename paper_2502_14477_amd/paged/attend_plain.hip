@@ -110,9 +110,7 @@ template <typename T, bool F8> __global__ __launch_bounds__(kThreads) void atten
 
 }  // namespace
 
-size_t attend_workspace(int64_t, int, int, int, int, int) { return 256; }
-
-int launch_attend(const AttendArgs& a, bool f8, int dtype, void*, hipStream_t st) {
+int launch_plain(const AttendArgs& a, bool f8, int dtype, hipStream_t st) {
   const dim3 grid((unsigned)(a.batch.n_tok * a.h));
   if (dtype == ESA_BF16) {
     if (f8)

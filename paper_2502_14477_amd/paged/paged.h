@@ -144,8 +144,9 @@ __device__ __forceinline__ int position(const AttendArgs& a, const Keys& k, int 
 
 int launch_append(const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq, int h, void* out_q, int64_t ldoq,
                   const Batch& b, const Cache& c, bool f8, double base, int dtype, hipStream_t st);
-size_t attend_workspace(int64_t n_tok, int n_seq, int h, int h_kv, int d, int dtype);
-int launch_attend(const AttendArgs& a, bool f8, int dtype, void* ws, hipStream_t st);
+int launch_plain(const AttendArgs& a, bool f8, int dtype, hipStream_t st);                     // any head size
+size_t few_workspace(int h_kv, int d, int dtype);
+int launch_few(const AttendArgs& a, bool f8, int dtype, void* ws, hipStream_t st);             // head sizes 64 and 128
 
 }  // namespace paged
 }  // namespace esa

@@ -108,7 +108,7 @@ int esa_append_paged(const void* k, int64_t ldk, const void* v, int64_t ldv, con
 
 size_t esa_attend_paged_workspace_bytes(int64_t n_tok, int n_seq, int h, int h_kv, int d, int dtype) {
   if (n_tok <= 0 || n_seq <= 0 || h <= 0 || h_kv <= 0 || d <= 0 || h % h_kv != 0) return 256;
-  return paged::attend_workspace(n_tok, n_seq, h, h_kv, d, dtype);
+  return d == 64 || d == 128 ? paged::few_workspace(h_kv, d, dtype) : 256;
 }
 
 int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* batch, const esa_paged_cache* cache, int64_t l_i, int64_t l_l,
@@ -145,7 +145,9 @@ int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* b
   a.l_l = (int)(l_l < INT32_MAX ? l_l : INT32_MAX);
   a.scale = scale;
   a.cap = cap;
-  return paged::launch_attend(a, cache->dtype == ESA_E4M3, dtype, workspace, (hipStream_t)stream);
+  const bool f8 = cache->dtype == ESA_E4M3;
+  if (cache->d != 64 && cache->d != 128) return paged::launch_plain(a, f8, dtype, (hipStream_t)stream);
+  return paged::launch_few(a, f8, dtype, workspace, (hipStream_t)stream);
 }
 
 }  // extern "C"
