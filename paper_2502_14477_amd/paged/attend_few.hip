@@ -80,8 +80,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = blockIdx.x % a.cache.h_kv;
-  const int slice = slice_tiles(a, f.shape);
-  const Part at = part_of(a, f.shape, slice, blockIdx.x / a.cache.h_kv);
+  const Plan plan = plan_of(a, f.shape);
+  const int slice = plan.slice;
+  const Part at = part_of(a, f.shape, plan, blockIdx.x / a.cache.h_kv);
   if (at.b < 0) return;
   const Seq s = sequence(a.batch, at.b);
   const Keys keys = keys_of(a, s);
@@ -336,7 +337,8 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attend_join(
   if (tok >= a.batch.n_tok) return;
   const int b = sequence_with(a.batch, tok);
   if (b < 0) return;
-  const int slice = slice_tiles(a, f.shape);
+  const Plan plan = plan_of(a, f.shape);
+  const int slice = plan.slice;
   const Seq s = sequence(a.batch, b);
   const Keys keys = keys_of(a, s);
   const int n_rows = s.n * a.group, row = (tok - s.row0) * a.group + head - g * a.group, rows = f.shape.rows;
@@ -344,7 +346,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void attend_join(
   const int n_vis = keys_until(a, s, keys, min(block * rows + rows, n_rows) - 1), tiles = (n_vis + f.shape.keys - 1) / f.shape.keys;
   const int n = (tiles + slice - 1) / slice;
   if (n <= 1) return;
-  const int64_t slot = parts_before(a, f.shape, slice, b) + block;
+  const int64_t slot = parts_before(a, f.shape, plan, b) + block;
   auto place = [&](int i) { return ((slot + (int64_t)i * blocks) * a.cache.h_kv + g) * rows + row - block * rows; };
   float m = -INFINITY;
   for (int i = lane; i < n; i += 64) m = fmaxf(m, f.part_ml[place(i) * 2]);
