@@ -15,7 +15,7 @@ NATIVE = os.path.join(PKG, "_native.so")
 
 SOURCES = ["esa_api.hip", "compress.hip", "score.hip", "topk.hip", "gather.hip", "attend.hip", "attend_mfma.hip", "attend_split.hip", "rope.hip",
            "../paged/paged_api.hip", "../paged/append.hip", "../paged/attend_plain.hip",
-           "../paged/attend_few.hip"]
+           "../paged/attend_few.hip", "../paged/attend_many.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",

@@ -9,63 +9,15 @@
 // the layout of S^T's accumulator is the second product's operand layout when key 16 s + 8 (j / 4) + 4 half + j % 4 is operand j of step s.
 // bf16: v_mfma_f32_32x32x16_bf16; a probability enters as two bf16 terms (16 bits), which costs nothing beside the loads.
 // fp32: v_mfma_f32_32x32x2_f32.
-#include "plan.h"
-
-#include <type_traits>
+#include "attend_sliced.h"
 
 namespace esa {
 namespace paged {
 namespace {
 
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef __attribute__((ext_vector_type(16))) float f32x16;
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef short i16x8 __attribute__((ext_vector_type(8)));
-typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
-
 constexpr int kRows = 32, kKeys = 32, kWaves = 4;
-constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
-
-// Softmax in base 2 on the hardware's exponential for bf16, in base e and full precision for fp32.
-template <typename T> __device__ __forceinline__ float exp_of(float x) { return sizeof(T) == 2 ? __builtin_amdgcn_exp2f(x) : expf(x); }
-template <typename T> __device__ __forceinline__ float lse_of(float m, float l) { return sizeof(T) == 2 ? __builtin_fmaf(m, kLn2, logf(l)) : m + logf(l); }
-
-__device__ __forceinline__ float halves_max(float v) {
-  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
-}
-__device__ __forceinline__ float halves_sum(float v) {
-  const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-  return __uint_as_float(sw[0]) + __uint_as_float(sw[1]);
-}
-__device__ __forceinline__ void wave_fence() {      // LDS operations of a wave are in order: only the compiler has to keep it
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-}
-
-struct FewArgs {
-  AttendArgs a;
-  Shape shape;
-  float* part_o;          // [slot][h_kv][kRows][D], relative to the slice's largest logit
-  float* part_ml;         // [slot][h_kv][kRows][2]: the largest logit, the sum of exponentials
-  float scale;            // bf16: includes log2(e); with a cap: 1 / cap
-  float cap;              // bf16: includes log2(e)
-};
-
-// Scores as the softmax takes them.
-template <typename T, bool CAP> __device__ __forceinline__ float score_of(float dot, float scale, float cap) {
-  const float x = dot * scale;
-  if constexpr (!CAP) return x;
-  if constexpr (sizeof(T) == 4) return cap * tanhf(x);
-  // tanh x = 1 - 2 / (1 + e^(2x)): some 2^-22 of the cap off where x is small, two roundings of a probability to 16 bits less than those
-  const float e = __builtin_amdgcn_exp2f(x * (2.f * kLog2e));
-  return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + e), cap);
-}
-
 template <typename T, bool F8, int D, bool CAP>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D * sizeof(T) > 256 ? 1 : 2))) void attend_few(FewArgs f) {
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D * sizeof(T) > 256 ? 1 : 2))) void attend_few(SlicedArgs f) {
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int kRowBytes = D * (int)sizeof(T);                 // of a staged row
   constexpr int kHeldBytes = F8 ? D : kRowBytes;                // of a row in the pool
@@ -326,61 +278,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   }
 }
 
-// Slices of a row joined: a wave to a row.
-template <typename T, int D> __global__ __launch_bounds__(256) void attend_join(FewArgs f) {
-  constexpr int kMine = D / 64;
-  typedef __attribute__((ext_vector_type(kMine))) float vec;
-  const AttendArgs& a = f.a;
-  const int lane = threadIdx.x & 63;
-  const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tok = unit / a.h, head = unit % a.h, g = head / a.group;
-  if (tok >= a.batch.n_tok) return;
-  const int b = sequence_with(a.batch, tok);
-  if (b < 0) return;
-  const Plan plan = plan_of(a, f.shape);
-  const int slice = plan.slice;
-  const Seq s = sequence(a.batch, b);
-  const Keys keys = keys_of(a, s);
-  const int n_rows = s.n * a.group, row = (tok - s.row0) * a.group + head - g * a.group, rows = f.shape.rows;
-  const int block = row / rows, blocks = (n_rows + rows - 1) / rows;
-  const int n_vis = keys_until(a, s, keys, min(block * rows + rows, n_rows) - 1), tiles = (n_vis + f.shape.keys - 1) / f.shape.keys;
-  const int n = (tiles + slice - 1) / slice;
-  if (n <= 1) return;
-  const int64_t slot = parts_before(a, f.shape, plan, b) + block;
-  auto place = [&](int i) { return ((slot + (int64_t)i * blocks) * a.cache.h_kv + g) * rows + row - block * rows; };
-  float m = -INFINITY;
-  for (int i = lane; i < n; i += 64) m = fmaxf(m, f.part_ml[place(i) * 2]);
-  m = wave_max(m);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
-  vec sum = 0.f;
-  for (int i0 = 0; i0 < n; i0 += 64) {
-    float by = 0.f;
-    if (i0 + lane < n) {
-      const float2 x = *(const float2*)(f.part_ml + place(i0 + lane) * 2);
-      by = exp_of<T>(x.x - ref);
-      l = __builtin_fmaf(x.y, by, l);
-    }
-    const int here = min(n - i0, 64);
-    for (int i = 0; i < here; i += 4) {
-      vec x[4];
-#pragma unroll
-      for (int u = 0; u < 4; ++u) x[u] = *(const vec*)(f.part_o + place(i0 + min(i + u, here - 1)) * D + lane * kMine);
-#pragma unroll
-      for (int u = 0; u < 4; ++u) sum += x[u] * (i + u < here ? __shfl(by, min(i + u, 63)) : 0.f);
-    }
-  }
-  l = wave_sum(l);
-  T* out = (T*)(a.out + (int64_t)tok * a.ldo) + (int64_t)head * D + lane * kMine;
-#pragma unroll
-  for (int i = 0; i < kMine; ++i) store_f32<T>(out + i, l > 0.f ? sum[i] / l : 0.f);
-  if (a.lse && lane == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? lse_of<T>(m, l) : -INFINITY;
-}
-
 // Workgroups that the chip holds: a compute unit has 160 KB of LDS, a workgroup's staging space is 64 KB for rows of up to 256 bytes.
-Shape shape_of(int d, int es) { return Shape{kRows, kKeys, d * es > 256 ? 256 : d * es == 256 ? 512 : 1024, kWaves}; }
+Shape shape_of(int d, int es, int most_rows) { return Shape{kRows, kKeys, d * es > 256 ? 256 : d * es == 256 ? 512 : 1024, kWaves, 16, 0, most_rows}; }
 
-template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, hipStream_t st) {
+template <typename T, bool F8, int D> int launch(const SlicedArgs& f, dim3 grid, hipStream_t st) {
   if (f.a.cap > 0.f)
     attend_few<T, F8, D, true><<<grid, 64 * kWaves, 0, st>>>(f);
   else
@@ -388,15 +289,10 @@ template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, hi
   ESA_LAUNCH_CHECK("attend_few");
   return ESA_OK;
 }
-template <typename T> int launch_all(FewArgs& f, bool f8, void* ws, hipStream_t st) {
-  const AttendArgs& a = f.a;
+template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows, void* ws, hipStream_t st) {
   const int d = a.cache.d;
-  f.shape = shape_of(d, sizeof(T));
-  f.part_o = (float*)ws;
-  f.part_ml = f.part_o + most_parts(f.shape, a.cache.h_kv) * a.cache.h_kv * kRows * d;
-  const float base = sizeof(T) == 2 ? kLog2e : 1.f;
-  f.scale = a.cap > 0.f ? a.scale / a.cap : a.scale * base;
-  f.cap = a.cap * base;
+  SlicedArgs f;
+  set_sliced<T>(f, a, shape_of(d, sizeof(T), most_rows), ws);
   const int64_t units = most_units(f.shape, a.batch.n_tok, a.batch.n_seq, a.group, a.cache.h_kv) * a.cache.h_kv;
   if (units > INT32_MAX) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: %lld workgroups", (long long)units);
   const dim3 grid((unsigned)units);
@@ -405,29 +301,15 @@ template <typename T> int launch_all(FewArgs& f, bool f8, void* ws, hipStream_t 
     rc = f8 ? launch<T, true, 64>(f, grid, st) : launch<T, false, 64>(f, grid, st);
   else
     rc = f8 ? launch<T, true, 128>(f, grid, st) : launch<T, false, 128>(f, grid, st);
-  if (rc != ESA_OK) return rc;
-  // (the longest sequence that the table has room for may be a slice)
-  if (((int64_t)a.batch.max_pages << a.batch.page_log2) + a.n_sel <= (int64_t)f.shape.least * kKeys) return ESA_OK;
-  const dim3 join((unsigned)((a.batch.n_tok * (int64_t)a.h + 3) / 4));
-  if (d == 64)
-    attend_join<T, 64><<<join, 256, 0, st>>>(f);
-  else
-    attend_join<T, 128><<<join, 256, 0, st>>>(f);
-  ESA_LAUNCH_CHECK("attend_join");
-  return ESA_OK;
+  return rc != ESA_OK ? rc : launch_join<T, true>(f, st);
 }
 
 }  // namespace
 
-size_t few_workspace(int h_kv, int d, int dtype) {
-  const Shape sh = shape_of(d, dtype == ESA_F32 ? 4 : 2);
-  return (size_t)(most_parts(sh, h_kv) * h_kv * kRows) * (d + 2) * sizeof(float);
-}
+size_t few_workspace(int h_kv, int d, int dtype) { return sliced_workspace(shape_of(d, dtype == ESA_F32 ? 4 : 2, INT32_MAX), h_kv, d); }
 
-int launch_few(const AttendArgs& a, bool f8, int dtype, void* ws, hipStream_t st) {
-  FewArgs f;
-  f.a = a;
-  return dtype == ESA_F32 ? launch_all<float>(f, f8, ws, st) : launch_all<bf16_t>(f, f8, ws, st);
+int launch_few(const AttendArgs& a, bool f8, int dtype, int most_rows, void* ws, hipStream_t st) {
+  return dtype == ESA_F32 ? launch_all<float>(a, f8, most_rows, ws, st) : launch_all<bf16_t>(a, f8, most_rows, ws, st);
 }
 
 }  // namespace paged

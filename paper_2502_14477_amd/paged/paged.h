@@ -145,8 +145,11 @@ __device__ __forceinline__ int position(const AttendArgs& a, const Keys& k, int 
 int launch_append(const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq, int h, void* out_q, int64_t ldoq,
                   const Batch& b, const Cache& c, bool f8, double base, int dtype, hipStream_t st);
 int launch_plain(const AttendArgs& a, bool f8, int dtype, hipStream_t st);                     // any head size
+// Head sizes 64 and 128.  Sequences of at most most_rows rows (new tokens x query heads of a KV head), and bf16 ones of more than above.
 size_t few_workspace(int h_kv, int d, int dtype);
-int launch_few(const AttendArgs& a, bool f8, int dtype, void* ws, hipStream_t st);             // head sizes 64 and 128
+int launch_few(const AttendArgs& a, bool f8, int dtype, int most_rows, void* ws, hipStream_t st);
+size_t many_workspace(int h_kv, int d);
+int launch_many(const AttendArgs& a, bool f8, int above, void* ws, hipStream_t st);
 
 }  // namespace paged
 }  // namespace esa

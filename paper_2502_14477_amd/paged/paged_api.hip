@@ -13,6 +13,7 @@ bool head_size_ok(int d) { return d == 32 || d == 64 || d == 128 || d == 256; }
 // Rows of `row` elements of es bytes, `ld` elements apart: on 16-byte boundaries, one behind the other.
 bool rows_ok(const void* p, int64_t ld, int64_t row, int64_t es) { return aligned(p, 16) && ld >= row && ld * es % 16 == 0; }
 
+constexpr int kFewRows = 64;      // of a sequence, new tokens x query heads of a KV head: up to two workgroups' share in the kernel for few rows
 constexpr int64_t kMostKeys = INT32_MAX - 65535;      // counters may run past them by a workgroup's stride
 
 // Whether the pool's three dimensions, in any order, lie behind one another.
@@ -108,7 +109,8 @@ int esa_append_paged(const void* k, int64_t ldk, const void* v, int64_t ldv, con
 
 size_t esa_attend_paged_workspace_bytes(int64_t n_tok, int n_seq, int h, int h_kv, int d, int dtype) {
   if (n_tok <= 0 || n_seq <= 0 || h <= 0 || h_kv <= 0 || d <= 0 || h % h_kv != 0) return 256;
-  return d == 64 || d == 128 ? paged::few_workspace(h_kv, d, dtype) : 256;
+  if (d != 64 && d != 128) return 256;
+  return std::max(paged::few_workspace(h_kv, d, dtype), dtype == ESA_BF16 ? paged::many_workspace(h_kv, d) : 0);
 }
 
 int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* batch, const esa_paged_cache* cache, int64_t l_i, int64_t l_l,
@@ -147,7 +149,18 @@ int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* b
   a.cap = cap;
   const bool f8 = cache->dtype == ESA_E4M3;
   if (cache->d != 64 && cache->d != 128) return paged::launch_plain(a, f8, dtype, (hipStream_t)stream);
-  return paged::launch_few(a, f8, dtype, workspace, (hipStream_t)stream);
+  // The lengths are on the device.  A batch of a few rows a sequence in the mean is served by the kernel for few rows, whatever else
+  // is in it; other batches by both, each of which finds the sequences that are its own (one that finds none: 2 us).  The two run one after the
+  // other and use the same workspace.
+  hipStream_t st = (hipStream_t)stream;
+  const int64_t rows = batch->n_tok * a.group;
+  if (dtype != ESA_BF16 || rows <= (int64_t)kFewRows || rows <= (int64_t)32 * batch->n_seq)
+    return paged::launch_few(a, f8, dtype, INT32_MAX, workspace, st);
+  if (batch->n_seq > 1) {
+    const int rc2 = paged::launch_few(a, f8, dtype, kFewRows, workspace, st);
+    if (rc2 != ESA_OK) return rc2;
+  }
+  return paged::launch_many(a, f8, batch->n_seq > 1 ? kFewRows : 0, workspace, st);
 }
 
 }  // extern "C"
