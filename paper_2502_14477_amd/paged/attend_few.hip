@@ -54,30 +54,31 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
     for (int i = 0; i < kKS; ++i) qf[i] = *(const u32x4*)(q + i * 32);
   }
 
-  // Lane r stands for key r of a tile: its position (INT32_MAX: not seen), its row's place in the pool, its scales.
+  // Lane r stands for key r of a tile: its position (INT32_MAX: not seen), its row's place in the pool, its scales.  Entries of the index list
+  // are requested three tiles ahead, of the page table two, rows one.
   struct Meta {
-    int pos, page;
+    int pos, entry;
   };
-  auto meta_of = [&](int t) {
-    const int j = t * kKeys + r;
-    Meta m{INT32_MAX, -1};
-    if (j < n_vis) {
-      const int p = position(a, keys, at.b, j);
-      m.page = p >= 0 ? page_of(a.batch, a.cache.n_pages, at.b, p) : -1;
-      if (m.page >= 0) m.pos = p;
-    }
+  auto key_at = [&](int t) { return t * kKeys + r; };
+  auto request_entry = [&](int t) { return keys.n_sel && t < end ? entry_of(a, keys, at.b, key_at(t)) : 0; };
+  auto request_page = [&](int t, int entry) {
+    const int j = key_at(t);
+    Meta m;
+    m.pos = j < n_vis ? position(keys, j, entry) : -1;
+    m.entry = page_entry(a.batch, at.b, m.pos);
     return m;
   };
   const int slot_mask = (1 << a.batch.page_log2) - 1;
   u32x4 kr[kLoads], vr[kLoads];
-  float ks = 1.f, vs = 1.f;                                     // of the lane's key
+  int kb = 127, vb = 127, now_pos = INT32_MAX;                  // of the lane's key: exponents of its scales, position
   auto load = [&](const Meta& m) {
-    const int page = max(m.page, 0);
-    const int64_t place = page * a.cache.page_bytes + g * a.cache.head_bytes + (m.page >= 0 ? m.pos & slot_mask : 0) * a.cache.tok_bytes;
+    const bool there = is_page(a.batch, a.cache.n_pages, m.pos, m.entry);
+    const int page = there ? m.entry : 0;
+    now_pos = there ? m.pos : INT32_MAX;
+    const int64_t place = page * a.cache.page_bytes + g * a.cache.head_bytes + (there ? m.pos & slot_mask : 0) * a.cache.tok_bytes;
     if constexpr (F8) {
-      const int kb = a.cache.k_scale[(int64_t)page * a.cache.h_kv + g], vb = a.cache.v_scale[(int64_t)page * a.cache.h_kv + g];
-      ks = scale_of(m.page >= 0 ? kb : 127);                    // (a page that nobody has may hold an infinite one)
-      vs = scale_of(m.page >= 0 ? vb : 127);
+      kb = a.cache.k_scale[(int64_t)page * a.cache.h_kv + g];
+      vb = a.cache.v_scale[(int64_t)page * a.cache.h_kv + g];
     }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
@@ -124,26 +125,31 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   float m_run = -INFINITY, l_run = 0.f;
 
   int t = first + wave;
-  Meta now{INT32_MAX, -1}, next{INT32_MAX, -1};
+  Meta next{-1, 0};
+  int entry = 0;
   if (t < end) {
-    now = meta_of(t);
-    load(now);
-    if (t + kWaves < end) next = meta_of(t + kWaves);
+    const int mine = request_entry(t), after = request_entry(t + kWaves);
+    entry = request_entry(t + 2 * kWaves);
+    const Meta m = request_page(t, mine);
+    next = request_page(t + kWaves, after);
+    load(m);
   }
   for (; t < end; t += kWaves) {
-    const uint64_t unseen = __ballot(now.pos == INT32_MAX);
+    const int pos = now_pos;
+    const uint64_t unseen = __ballot(pos == INT32_MAX);
+    // a page that nobody has may hold an infinite scale; whatever its rows hold: 0 times a NaN is one
+    const float ks = scale_of(pos != INT32_MAX ? kb : 127), vs = scale_of(pos != INT32_MAX ? vb : 127);
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int key = i * kLoadRows + lane / kPieces;
       u32x4 k = kr[i], v = vr[i];
-      if (unseen && ((unseen >> key) & 1)) k = v = u32x4{0, 0, 0, 0};        // whatever lies there: 0 times a NaN is one
+      if (unseen && ((unseen >> key) & 1)) k = v = u32x4{0, 0, 0, 0};
       put(k_st, k, F8 ? __shfl(ks, key) : 1.f, key, k_swizzle(key));
       put(v_st, v, F8 ? __shfl(vs, key) : 1.f, key, v_swizzle(key));
     }
-    const int pos = now.pos;
-    now = next;
-    if (t + kWaves < end) load(now);
-    if (t + 2 * kWaves < end) next = meta_of(t + 2 * kWaves);
+    if (t + kWaves < end) load(next);
+    if (t + 2 * kWaves < end) next = request_page(t + 2 * kWaves, entry);
+    entry = request_entry(t + 3 * kWaves);
     wave_fence();
 
     f32x16 x, x_odd;

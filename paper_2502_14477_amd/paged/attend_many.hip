@@ -58,39 +58,51 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   }
 
   // ---- staging: a thread has piece tid % kPieces of rows tid / kPieces + i kPass of the tile's keys, then values
+  // Entries of the index list are requested three tiles ahead, of the page table two, rows one.
   struct Meta {
-    int pos[kMine], page[kMine];
+    int pos[kMine], entry[kMine];
+  };
+  struct Entries {
+    int x[kMine];
   };
   const int piece = tid % kPieces, my_row = tid / kPieces;
   auto key_of = [&](int i) { return (my_row + i * kPass) % kKeys; };
-  auto position_of = [&](int t, int i) {
-    const int j = t * kKeys + key_of(i);
-    return t < end && j < n_vis ? position(a, keys, at.b, j) : -1;
+  auto request_entries = [&](int t) {
+    Entries e;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) e.x[i] = keys.n_sel && t < end ? entry_of(a, keys, at.b, t * kKeys + key_of(i)) : 0;
+    return e;
   };
-  auto meta_of = [&](int t) {
+  auto request_pages = [&](int t, const Entries& e) {
     Meta m;
 #pragma unroll
     for (int i = 0; i < kMine; ++i) {
-      m.pos[i] = position_of(t, i);
-      m.page[i] = m.pos[i] >= 0 ? page_of(a.batch, a.cache.n_pages, at.b, m.pos[i]) : -1;
+      const int j = t * kKeys + key_of(i);
+      m.pos[i] = j < n_vis ? position(keys, j, e.x[i]) : -1;
+      m.entry[i] = page_entry(a.batch, at.b, m.pos[i]);
     }
     return m;
   };
   const int slot_mask = (1 << a.batch.page_log2) - 1;
   struct Held {
     u32x4 x[kLoads];
-    int scale[kLoads];
-    Meta m;
+    int scale[kLoads], pos[kMine];                              // position: INT32_MAX where nothing is seen
   };
   auto load = [&](Held& h, const Meta& m) {
-    h.m = m;
+    int64_t place[kMine], block[kMine];
+#pragma unroll
+    for (int n = 0; n < kMine; ++n) {
+      const bool there = is_page(a.batch, a.cache.n_pages, m.pos[n], m.entry[n]);
+      const int page = there ? m.entry[n] : 0;
+      h.pos[n] = there ? m.pos[n] : INT32_MAX;
+      place[n] = page * a.cache.page_bytes + g * a.cache.head_bytes + (there ? m.pos[n] & slot_mask : 0) * a.cache.tok_bytes + piece * 16;
+      block[n] = (int64_t)page * a.cache.h_kv + g;
+    }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const bool values = i * kPass + my_row >= kKeys;
-      const int n = kMine == 1 ? 0 : i % kMine, page = max(m.page[n], 0);
-      const int64_t place = page * a.cache.page_bytes + g * a.cache.head_bytes + (m.page[n] >= 0 ? m.pos[n] & slot_mask : 0) * a.cache.tok_bytes;
-      h.x[i] = *(const u32x4*)((values ? a.cache.v : a.cache.k) + place + piece * 16);
-      if constexpr (F8) h.scale[i] = (values ? a.cache.v_scale : a.cache.k_scale)[(int64_t)page * a.cache.h_kv + g];
+      h.x[i] = *(const u32x4*)((values ? a.cache.v : a.cache.k) + place[kMine == 1 ? 0 : i % kMine]);
+      if constexpr (F8) h.scale[i] = (values ? a.cache.v_scale : a.cache.k_scale)[block[kMine == 1 ? 0 : i % kMine]];
     }
   };
   auto k_swizzle = [](int key) { return kRowBytes >= 256 ? key & 15 : (key >> 1) & 7; };
@@ -101,7 +113,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     for (int i = 0; i < kLoads; ++i) {
       const bool values = i * kPass + my_row >= kKeys;
       const int n = kMine == 1 ? 0 : i % kMine, key = key_of(i);
-      const bool there = h.m.page[n] >= 0;
+      const bool there = h.pos[n] != INT32_MAX;
       unsigned char* to = (values ? v_stage[third] : k_stage[j & 1]) + key * kRowBytes;
       const int swizzle = values ? v_swizzle(key) : k_swizzle(key);
       u32x4 x = h.x[i];
@@ -119,7 +131,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       } else {
         *(u32x4*)(to + ((piece ^ swizzle) << 4)) = x;
       }
-      if (piece == 0 && (kLoads == 1 ? !values : i < kMine)) seen[third][key] = there ? h.m.pos[n] : INT32_MAX;
+      if (piece == 0 && (kLoads == 1 ? !values : i < kMine)) seen[third][key] = h.pos[n];
     }
   };
 
@@ -213,14 +225,22 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 
   const int n_tiles = max(end - first, 0);
   Held held;
-  load(held, meta_of(first));
-  Meta next = meta_of(first + 1);
-  // Part of tile j into LDS, the next one's requested.
+  Meta next;
+  Entries entries;
+  {
+    const Entries e0 = request_entries(first), e1 = request_entries(first + 1);
+    entries = request_entries(first + 2);
+    const Meta m = request_pages(first, e0);
+    next = request_pages(first + 1, e1);
+    load(held, m);
+  }
+  // Part of tile j into LDS, the next ones' requested.
   auto stage = [&](int j) __attribute__((always_inline)) {
     if (j >= n_tiles) return;
     put(held, j);
     if (j + 1 < n_tiles) load(held, next);
-    if (j + 2 < n_tiles) next = meta_of(first + j + 2);
+    if (j + 2 < n_tiles) next = request_pages(first + j + 2, entries);
+    entries = request_entries(first + j + 3);
   };
   stage(0);
   phase_end();

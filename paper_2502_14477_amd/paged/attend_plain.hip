@@ -59,7 +59,7 @@ template <typename T, bool F8> __global__ __launch_bounds__(kThreads) void atten
     float x = -INFINITY, by = 1.f;
     int64_t at = 0;
     if (j0 + tid < keys.n) {
-      const int p = position(a, keys, b, j0 + tid);
+      const int p = position(keys, j0 + tid, entry_of(a, keys, b, j0 + tid));
       const int page = p >= 0 && p <= own ? page_of(a.batch, a.cache.n_pages, b, p) : -1;
       if (page >= 0) {
         at = page * a.cache.page_bytes + g * a.cache.head_bytes + (p & ((1 << a.batch.page_log2) - 1)) * a.cache.tok_bytes;

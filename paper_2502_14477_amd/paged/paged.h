@@ -131,15 +131,24 @@ __device__ __forceinline__ Keys keys_of(const AttendArgs& a, const Seq& s) {
   k.n = k.i_end + k.n_sel + (min(s.t0 + s.n, width) - k.l_start);
   return k;
 }
-// The position of key j < k.n, -1 for an entry that is not seen.
-__device__ __forceinline__ int position(const AttendArgs& a, const Keys& k, int b, int j) {
+// The position of key j < k.n, -1 for an entry that is not seen.  In two steps where a kernel requests ahead: a request's result is only
+// looked at when it is needed, so that nothing waits for it in between.
+__device__ __forceinline__ int entry_of(const AttendArgs& a, const Keys& k, int b, int j) {      // as it lies in the list
+  const int i = j - k.i_end;
+  return (uint32_t)i < (uint32_t)k.n_sel ? a.idx[(int64_t)b * a.idx_ld + i] : 0;
+}
+__device__ __forceinline__ int position(const Keys& k, int j, int entry) {
   if (j < k.i_end) return j;
   j -= k.i_end;
-  if (j < k.n_sel) {
-    const int p = a.idx[(int64_t)b * a.idx_ld + j];
-    return p >= k.i_end && p < k.l_start ? p : -1;
-  }
+  if (j < k.n_sel) return entry >= k.i_end && entry < k.l_start ? entry : -1;
   return j - k.n_sel + k.l_start;
+}
+// The table's entry for a position (any: for -1, or one behind the table, some entry), and whether it is a page.
+__device__ __forceinline__ int page_entry(const Batch& a, int b, int pos) {
+  return a.pages[(int64_t)b * a.pages_ld + min(max(pos, 0) >> a.page_log2, a.max_pages - 1)];
+}
+__device__ __forceinline__ bool is_page(const Batch& a, int n_pages, int pos, int entry) {
+  return pos >= 0 && pos >> a.page_log2 < a.max_pages && (uint32_t)entry < (uint32_t)n_pages;
 }
 
 int launch_append(const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq, int h, void* out_q, int64_t ldoq,
