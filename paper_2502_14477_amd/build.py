@@ -9,13 +9,12 @@ from concurrent.futures import ThreadPoolExecutor
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
+PAGED = os.path.join(PKG, "paged")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libesa.so")
 NATIVE = os.path.join(PKG, "_native.so")
 
-SOURCES = ["esa_api.hip", "compress.hip", "score.hip", "topk.hip", "gather.hip", "attend.hip", "attend_mfma.hip", "attend_split.hip", "rope.hip",
-           "../paged/paged_api.hip", "../paged/append.hip", "../paged/attend_plain.hip",
-           "../paged/attend_few.hip", "../paged/attend_many.hip"]
+SOURCES = ["esa_api.hip", "compress.hip", "score.hip", "topk.hip", "gather.hip", "attend.hip", "attend_mfma.hip", "attend_split.hip", "rope.hip"]
 
 FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fvisibility=hidden",
@@ -34,6 +33,15 @@ FLAGS = [
 EXTRA_FLAGS = {
     # plain v_max_f32 for the running maxima of the score sweeps (no NaN handling needed there)
     "score.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"],
+}
+
+
+# The paged cache's sources and what they add.  The kernels that take maxima of matrix-core results: plain v_max_f32 (with NaN handling each
+# operand is quieted by an instruction of its own first); what a pool holds that nobody sees, NaN among it, is left out by integer comparisons.
+PAGED_SOURCES = ["paged_api.hip", "append.hip", "attend_plain.hip", "attend_few.hip", "attend_many.hip"]
+PAGED_FLAGS = {
+    "attend_few.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"],
+    "attend_many.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"],
 }
 
 
@@ -69,9 +77,10 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
     os.makedirs(OBJ, exist_ok=True)
     hipcc = _hipcc()
 
-    def compile_one(src):
-        obj = os.path.join(OBJ, src.replace("../", "").replace("/", "_").replace(".hip", ".o"))
-        out = _run([hipcc, *FLAGS, *EXTRA_FLAGS.get(src, []), "-c", os.path.join(CSRC, src), "-o", obj])
+    def compile_one(job):
+        folder, src, extra = job
+        obj = os.path.join(OBJ, os.path.basename(folder) + "_" + src.replace(".hip", ".o"))
+        out = _run([hipcc, *FLAGS, *extra, "-c", os.path.join(folder, src), "-o", obj])
         if verbose and out.strip():
             print(out)
         return obj
@@ -81,7 +90,8 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
 
     with ThreadPoolExecutor(max_workers=jobs) as pool:
         native = pool.submit(_run, ["g++", *native_compile, "-c", os.path.join(CSRC, "binding.cpp"), "-o", native_obj])
-        objs = list(pool.map(compile_one, SOURCES))
+        jobs = [(PAGED, s, PAGED_FLAGS.get(s, [])) for s in PAGED_SOURCES] + [(CSRC, s, EXTRA_FLAGS.get(s, [])) for s in SOURCES]
+        objs = list(pool.map(compile_one, jobs))
         native.result()
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB])
     _run(["g++", native_obj, *native_link, "-o", NATIVE])

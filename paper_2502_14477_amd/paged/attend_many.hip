@@ -3,14 +3,15 @@
 // A workgroup has 256 rows (new tokens x query heads of a KV head), 32 to each of its eight waves, and a slice of the keys, in tiles of 64
 // that the waves share: every thread fetches its part of a tile into registers ahead, brings it to bf16 (8-bit pages: times the block's
 // scale, exactly) and writes it to LDS.  The products are those of the kernel for few rows: S^T = K Q^T, O^T += V^T P^T, a lane stands for a
-// row; a probability is one bf16 term (its rounding is as large as the output's), and the reference of the softmax stays where it is until a
-// logit exceeds it by 2^8, which spares the sums' rescaling.
+// row; a probability is one bf16 term (its rounding is as large as the output's), and the reference of the softmax stays where it is until
+// probabilities sum up to over 2^8, which spares the maxima and the sums' rescaling.
 //   Here the matrix cores bound: 32 instructions a wave and tile, 2048 cycles of a compute unit's four for all waves, and as many for the LDS
-// reads; the softmax and the staging are about as many cycles of vector instructions, which ran one behind the other when the
-// two waves of a SIMD (w and w + 4) went through a tile together (5600 cycles a tile).  So they take turns: in one phase waves 0 - 3 multiply
-// (scores of tile j, sums of tile j - 1) while waves 4 - 7 do the softmax of tile j - 1 and stage their part of tile j + 1, in the
-// next they change places.  Tile j's keys are read in phases 2 j and 2 j + 1, its values in 2 j + 2 and 2 j + 3, and it is written in
-// 2 j - 2 (by waves 4 - 7) and 2 j - 1: two buffers of keys, three of values and positions.
+// reads.  What else a wave has to do is 250 instructions a tile, so they have to run beside its own matrix instructions: in a step of 32 keys
+// the scores of the next 32 and the sums of the 32 before are multiplied while the probabilities of these are made and a part of the tile
+// after next is staged, slot by slot (one instruction of each product and its share of the rest), in an order that the compiler keeps.
+// (Without that order, products and softmax one behind the other in a wave: 5600 cycles a tile.  Two groups of waves that took turns with
+// products and softmax, a barrier between: the same, as a wave by itself issues a vector instruction every five cycles or so.)
+//   In iteration j keys of tiles j and j + 1 and values of j - 1 and j are read and tile j + 2 is written: four buffers, one barrier.
 #include "attend_sliced.h"
 
 namespace esa {
@@ -18,6 +19,7 @@ namespace paged {
 namespace {
 
 constexpr int kRows = 256, kKeys = 64, kWaves = 8;
+constexpr float kNoReference = -1e30f;      // so low that the first logit exceeds it
 
 template <bool F8, int D, bool CAP>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void attend_many(SlicedArgs f) {
@@ -29,8 +31,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   constexpr int kMine = kPass < kKeys ? kKeys / kPass : 1;      // keys of a thread
   constexpr int kKS = D / 16, kMD = D / 32;
   constexpr int kTileBytes = kKeys * kRowBytes;
-  __shared__ __attribute__((aligned(16))) unsigned char k_stage[2][kTileBytes], v_stage[3][kTileBytes];
-  __shared__ __attribute__((aligned(16))) int seen[3][kKeys];                         // positions, INT32_MAX: not seen
+  constexpr int kBuffers = 4;
+  __shared__ __attribute__((aligned(16))) unsigned char k_stage[kBuffers][kTileBytes], v_stage[kBuffers][kTileBytes];
+  __shared__ __attribute__((aligned(16))) int seen[kBuffers][kKeys];                  // positions, INT32_MAX: not seen
   const AttendArgs& a = f.a;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -58,212 +61,265 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   }
 
   // ---- staging: a thread has piece tid % kPieces of rows tid / kPieces + i kPass of the tile's keys, then values
-  // Entries of the index list are requested three tiles ahead, of the page table two, rows one.
-  struct Meta {
-    int pos[kMine], entry[kMine];
-  };
+  // Entries of the index list are requested three tiles ahead, of the page table two, rows one; behind the slice's last tile something is
+  // fetched that nobody reads.  A tile that lies in one page is found once for the whole workgroup.
+  const int piece = tid % kPieces, my_row = tid / kPieces;
+  auto key_of = [&](int i) { return kPass <= kKeys ? my_row + i * kPass % kKeys : my_row % kKeys; };
+  auto is_value = [&](int i) { return kPass <= kKeys ? i >= kKeys / kPass : my_row >= kKeys; };
+  const int32_t* const list = keys.n_sel ? a.idx + (int64_t)at.b * a.idx_ld : a.batch.pages;
+  const int list_last = max(keys.n_sel - 1, 0);
+  const int slot_mask = (1 << a.batch.page_log2) - 1;
+  const uint32_t tok_bytes = (uint32_t)a.cache.tok_bytes;
   struct Entries {
     int x[kMine];
   };
-  const int piece = tid % kPieces, my_row = tid / kPieces;
-  auto key_of = [&](int i) { return (my_row + i * kPass) % kKeys; };
   auto request_entries = [&](int t) {
     Entries e;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) e.x[i] = keys.n_sel && t < end ? entry_of(a, keys, at.b, t * kKeys + key_of(i)) : 0;
+    for (int i = 0; i < kMine; ++i) e.x[i] = list[min(max(t * kKeys + key_of(i) - keys.i_end, 0), list_last)];
     return e;
+  };
+  struct Meta {
+    int pos0;                                                   // of the tile's first key where it lies in one page, else -1
+    int pos[kMine], entry[kMine];
   };
   auto request_pages = [&](int t, const Entries& e) {
     Meta m;
+    const int j0 = t * kKeys, late = j0 - keys.i_end - keys.n_sel;
+    m.pos0 = j0 + kKeys <= keys.i_end ? j0 : late >= 0 ? late + keys.l_start : -1;
+    if (j0 + kKeys > n_vis || (m.pos0 & (kKeys - 1)) != 0 || slot_mask + 1 < kKeys) m.pos0 = -1;
+    if (m.pos0 >= 0) {
+      m.entry[0] = page_entry(a.batch, at.b, m.pos0);
+    } else {
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) {
-      const int j = t * kKeys + key_of(i);
-      m.pos[i] = j < n_vis ? position(keys, j, e.x[i]) : -1;
-      m.entry[i] = page_entry(a.batch, at.b, m.pos[i]);
+      for (int i = 0; i < kMine; ++i) {
+        const int j = j0 + key_of(i), p = position(keys, j, e.x[i]);
+        m.pos[i] = j < n_vis ? p : -1;
+        m.entry[i] = page_entry(a.batch, at.b, m.pos[i]);
+      }
     }
     return m;
   };
-  const int slot_mask = (1 << a.batch.page_log2) - 1;
   struct Held {
     u32x4 x[kLoads];
     int scale[kLoads], pos[kMine];                              // position: INT32_MAX where nothing is seen
   };
   auto load = [&](Held& h, const Meta& m) {
+    if (m.pos0 >= 0) {
+      const int entry = __builtin_amdgcn_readfirstlane(m.entry[0]);
+      const bool there = is_page(a.batch, a.cache.n_pages, m.pos0, entry);
+      const int page = there ? entry : 0;
+      const int64_t place = page * a.cache.page_bytes + g * a.cache.head_bytes + (int64_t)(m.pos0 & slot_mask) * tok_bytes;
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        h.x[i] = *(const u32x4*)((is_value(i) ? a.cache.v : a.cache.k) + place + ((uint32_t)key_of(i) * tok_bytes + piece * 16));
+      if constexpr (F8) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) h.scale[i] = (is_value(i) ? a.cache.v_scale : a.cache.k_scale)[(int64_t)page * a.cache.h_kv + g];
+      }
+#pragma unroll
+      for (int n = 0; n < kMine; ++n) h.pos[n] = there ? m.pos0 + key_of(n) : INT32_MAX;
+      return;
+    }
     int64_t place[kMine], block[kMine];
 #pragma unroll
     for (int n = 0; n < kMine; ++n) {
       const bool there = is_page(a.batch, a.cache.n_pages, m.pos[n], m.entry[n]);
       const int page = there ? m.entry[n] : 0;
       h.pos[n] = there ? m.pos[n] : INT32_MAX;
-      place[n] = page * a.cache.page_bytes + g * a.cache.head_bytes + (there ? m.pos[n] & slot_mask : 0) * a.cache.tok_bytes + piece * 16;
+      place[n] = page * a.cache.page_bytes + g * a.cache.head_bytes + (int64_t)((there ? m.pos[n] & slot_mask : 0) * (uint64_t)tok_bytes) + piece * 16;
       block[n] = (int64_t)page * a.cache.h_kv + g;
     }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-      const bool values = i * kPass + my_row >= kKeys;
-      h.x[i] = *(const u32x4*)((values ? a.cache.v : a.cache.k) + place[kMine == 1 ? 0 : i % kMine]);
-      if constexpr (F8) h.scale[i] = (values ? a.cache.v_scale : a.cache.k_scale)[block[kMine == 1 ? 0 : i % kMine]];
+      h.x[i] = *(const u32x4*)((is_value(i) ? a.cache.v : a.cache.k) + place[kMine == 1 ? 0 : i % kMine]);
+      if constexpr (F8) h.scale[i] = (is_value(i) ? a.cache.v_scale : a.cache.k_scale)[block[kMine == 1 ? 0 : i % kMine]];
     }
   };
   auto k_swizzle = [](int key) { return kRowBytes >= 256 ? key & 15 : (key >> 1) & 7; };
   auto v_swizzle = [](int key) { return kRowBytes >= 256 ? (key & 3) << 2 : ((key >> 1) & 1) << 2; };
-  auto put = [&](const Held& h, int j) {
-    const int third = j % 3;
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const bool values = i * kPass + my_row >= kKeys;
-      const int n = kMine == 1 ? 0 : i % kMine, key = key_of(i);
-      const bool there = h.pos[n] != INT32_MAX;
-      unsigned char* to = (values ? v_stage[third] : k_stage[j & 1]) + key * kRowBytes;
-      const int swizzle = values ? v_swizzle(key) : k_swizzle(key);
+  // Writing tile j is cut into kParts: 8-bit pages go four bytes of every 16 at a time, others a load at a time.
+  constexpr int kParts = F8 ? 4 * kLoads : kLoads;
+  u32x4 made[2];
+  auto put = [&](const Held& h, int j, int part) __attribute__((always_inline)) {
+    const int i = F8 ? part / 4 : part, e = part % 4;
+    const bool values = is_value(i);
+    const int n = kMine == 1 ? 0 : i % kMine, key = key_of(i);
+    const bool there = h.pos[n] != INT32_MAX;
+    unsigned char* const to = (values ? v_stage[j & 3] : k_stage[j & 3]) + key * kRowBytes;
+    const int swizzle = values ? v_swizzle(key) : k_swizzle(key);
+    // Values that are not there count as 0, whatever lies in their place: 0 times a NaN is one.  (Such keys' scores are masked.)
+    if constexpr (F8) {
+      const uint32_t x = there || (kPass <= kKeys && !values) ? h.x[i][e] : 0;
+      const float by = scale_of(there ? h.scale[i] : 127);
+      made[e / 2][e % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, by, false));
+      made[e / 2][e % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, by, true));
+      if (e % 2) *(u32x4*)(to + (((piece * 2 + e / 2) ^ swizzle) << 4)) = made[e / 2];
+    } else {
       u32x4 x = h.x[i];
-      if (!there) x = u32x4{0, 0, 0, 0};                        // whatever lies there: 0 times a NaN is one
-      if constexpr (F8) {
-        const float by = scale_of(there ? h.scale[i] : 127);
-        u32x4 y[2];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          y[e / 2][e % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[e], by, false));
-          y[e / 2][e % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[e], by, true));
-        }
-#pragma unroll
-        for (int e = 0; e < 2; ++e) *(u32x4*)(to + (((piece * 2 + e) ^ swizzle) << 4)) = y[e];
-      } else {
-        *(u32x4*)(to + ((piece ^ swizzle) << 4)) = x;
-      }
-      if (piece == 0 && (kLoads == 1 ? !values : i < kMine)) seen[third][key] = h.pos[n];
+      for (int w = 0; w < 4; ++w) x[w] = there || !values ? x[w] : 0;
+      *(u32x4*)(to + ((piece ^ swizzle) << 4)) = x;
     }
+    // (several threads write a key's position: the same one)
+    if (part % (kParts / kLoads) == 0 && i < kMine) seen[j & 3][key] = h.pos[n];
   };
 
-  f32x16 o[kMD], x[2];
+  constexpr int kSlots = kKS;                                   // of a step: as many instructions has each product
+  static_assert(kSlots == 2 * kMD, "the products' instructions go in pairs");
+  constexpr int kValues = 16 / kSlots;                          // probabilities of a slot
+  f32x16 o[kMD], x;
 #pragma unroll
   for (int md = 0; md < kMD; ++md)
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[md][v] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
-  bf16x8 p[4];
+  float m_run = kNoReference, l_run = 0.f;
+  bf16x8 p[2];                                                  // of the 32 keys before
+#pragma unroll
+  for (int e = 0; e < 8; ++e) p[0][e] = p[1][e] = (__bf16)0.f;
 
-  // First product of tile j.
-  auto scores = [&](int j) __attribute__((always_inline)) {
-    const unsigned char* const k_st = k_stage[j & 1];
-#pragma unroll
-    for (int n = 0; n < 2; ++n)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) x[n][v] = 0.f;
-#pragma unroll
-    for (int i = 0; i < kKS; ++i)
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const u32x4 kf = *(const u32x4*)(k_st + (n * 32 + r) * kRowBytes + (((2 * i + hi) ^ k_swizzle(r)) << 4));
-        x[n] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[i]), x[n], 0, 0, 0);
-      }
+  const int k_at = r * kRowBytes;
+  auto key_part = [&](const unsigned char* from, int i) __attribute__((always_inline)) {
+    return *(const u32x4*)(from + k_at + (((2 * i + hi) ^ k_swizzle(r)) << 4));
   };
-  // Second product of tile j.
-  auto sums = [&](int buffer) __attribute__((always_inline)) {
-    unsigned char* const v_st = v_stage[buffer];
-    const int tr_key = 4 * hi + ((lane & 15) >> 2), tr_dim = ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
-#pragma unroll
-    for (int kp = 0; kp < 4; ++kp)
-#pragma unroll
-      for (int md = 0; md < kMD; ++md) {
-        // lane i of sixteen receives element i % 4 of the 8 bytes that lanes 4 e + i / 4 address: dimension i of keys e = 0 .. 3
-        auto part = [&](int key) {
-          const int at_piece = (md * 32 + tr_dim) / 8;
-          return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(v_st + key * kRowBytes + ((at_piece ^ v_swizzle(key)) << 4) + (tr_dim & 4) * 2));
-        };
-        const i16x4 lo = part(16 * kp + tr_key), up = part(16 * kp + 8 + tr_key);
-        o[md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7)), p[kp], o[md], 0, 0, 0);
-      }
+  const int tr_key = 4 * hi + ((lane & 15) >> 2), tr_dim = ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
+  // Keys 16 kp + 8 upper + 4 hi + 0 .. 3 of dimension md * 32 + r: lane i of sixteen receives element i % 4 of the 8 bytes that lanes
+  // 4 e + i / 4 address, which is dimension i of keys e = 0 .. 3.
+  auto value_part = [&](unsigned char* from, int kp, int md, int upper) __attribute__((always_inline)) {
+    const int key = 16 * kp + 8 * upper + tr_key, at_piece = (md * 32 + tr_dim) / 8;
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(from + key * kRowBytes + ((at_piece ^ v_swizzle(key)) << 4) + (tr_dim & 4) * 2));
   };
-  // Tile j's probabilities from its scores.
-  auto softmax = [&](int buffer) __attribute__((always_inline)) {
-    if constexpr (CAP) {
+  auto joined = [](const i16x4& lo, const i16x4& up) __attribute__((always_inline)) {
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
+  };
+  const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+
+  Held held;
+  Meta next;
+  Entries entries;
+  {
+    const Entries e0 = request_entries(first), e1 = request_entries(first + 1), e2 = request_entries(first + 2);
+    entries = request_entries(first + 3);
+    const Meta m0 = request_pages(first, e0), m1 = request_pages(first + 1, e1);
+    next = request_pages(first + 2, e2);
+    Held h0;
+    load(h0, m0);
+    load(held, m1);
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+    for (int i = 0; i < kParts; ++i) put(h0, 0, i);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) x[n][v] = score_of<bf16_t, CAP>(x[n][v], f.scale, f.cap);
+    for (int i = 0; i < kParts; ++i) put(held, 1, i);
+    load(held, next);
+    next = request_pages(first + 3, entries);
+    entries = request_entries(first + 4);
+    // the "32 keys before" of the first step: probabilities of 0 times values that are none
+    for (int e = tid; e < 32 * kRowBytes / 16; e += 64 * kWaves) *(u32x4*)(v_stage[3] + 32 * kRowBytes + e * 16) = u32x4{0, 0, 0, 0};
+  }
+  // LDS is settled; loads from memory stay on their way.
+  auto meet = [&]() __attribute__((always_inline)) {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  meet();
+  x = zero;
+#pragma unroll
+  for (int i = 0; i < kKS; ++i)
+    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, key_part(k_stage[0], i)), __builtin_bit_cast(bf16x8, qf[i]), x, 0, 0, 0);
+
+  // Half `n` of tile j, whose scores are in x: leaves the next 32 keys' scores there, and the probabilities in p.
+  auto step = [&](int j, auto half) __attribute__((always_inline)) {
+    constexpr int n = decltype(half)::value;
+    const unsigned char* const k_from = k_stage[(j + n) & 3] + (1 - n) * 32 * kRowBytes;
+    unsigned char* const v_from = v_stage[(j - 1 + n) & 3] + (1 - n) * 32 * kRowBytes;
+    constexpr int kAhead = kSlots < 3 ? kSlots : 3;
+    u32x4 kf[kSlots];
+    i16x4 vf[kSlots][2];
+    auto request = [&](int s) __attribute__((always_inline)) {
+      kf[s] = key_part(k_from, s);
+      vf[s][0] = value_part(v_from, s / kMD, s % kMD, 0);
+      vf[s][1] = value_part(v_from, s / kMD, s % kMD, 1);
+    };
+#pragma unroll
+    for (int s = 0; s < kAhead; ++s) request(s);
+    if (__ballot(seen[j & 3][n * 32 + r] > own_first)) {        // some key is not for all rows of the wave
+#pragma unroll
+      for (int v = 0; v < 16; ++v)
+        if (seen[j & 3][n * 32 + 8 * (v / 4) + 4 * hi + v % 4] > own) x[v] = -INFINITY;
     }
-    const float scale = CAP ? 1.f : f.scale;
-    if (__ballot(seen[buffer][lane] > own_first)) {             // some key is not for all rows of the wave
+    f32x16 x_next;
+    bf16x8 p_next[2];
+    float sum[2] = {0.f, 0.f};
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int n = 0; n < 2; ++n)
+    for (int s = 0; s < kSlots; ++s) {
+      if (s + kAhead < kSlots) request(s + kAhead);
+      x_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[s]), __builtin_bit_cast(bf16x8, qf[s]), s ? x_next : zero, 0, 0, 0);
 #pragma unroll
-        for (int v = 0; v < 16; ++v)
-          if (seen[buffer][n * 32 + 8 * (v / 4) + 4 * hi + v % 4] > own) x[n][v] = -INFINITY;
+      for (int i = 0; i < kValues; ++i) {
+        const int v = s * kValues + i;
+        float e;
+        if constexpr (CAP)
+          e = x[v] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(score_of<bf16_t, CAP>(x[v], f.scale, f.cap) - m_run);
+        else
+          e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v], f.scale, -m_run));
+        sum[i & 1] += e;
+        p_next[v / 8][v % 8] = (__bf16)e;
+      }
+      o[s % kMD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(joined(vf[s][0], vf[s][1]), p[s / kMD], o[s % kMD], 0, 0, 0);
+      if constexpr (n == 0) {
+        if (kParts >= kSlots || s % (kSlots / kParts) == 0) {
+#pragma unroll
+          for (int i = 0; i < (kParts + kSlots - 1) / kSlots; ++i) put(held, j + 2, kParts >= kSlots ? s * (kParts / kSlots) + i : s * kParts / kSlots);
+        }
+      } else {
+        if (s == 0) load(held, next);
+        if (s == kSlots / 2) next = request_pages(first + j + 4, entries);
+        if (s == kSlots - 1) entries = request_entries(first + j + 5);
+      }
+      __builtin_amdgcn_sched_barrier(0);
     }
-    float top = fmaxf(x[0][0], x[1][0]);
+    // The exponentials were taken against the reference as it stands.  Where a row's exceed it by far (and at first) it moves to its largest
+    // logit and they are taken again; the sums so far, those of the 32 keys before among them, come to the new one.
+    if (__ballot(sum[0] + sum[1] > 256.f)) {
+      float top = x[0];
 #pragma unroll
-    for (int v = 1; v < 16; ++v) top = fmaxf(fmaxf(top, x[0][v]), x[1][v]);
-    top = halves_max(top) * scale;
-    if (__ballot(top > m_run + 8.f)) {
-      const float to = fmaxf(m_run, top), less = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m_run - to);
+      for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
+      top = halves_max(top);
+      if (top != -INFINITY) top = score_of<bf16_t, CAP>(top, f.scale, f.cap);
+      const float to = fmaxf(m_run, top), less = __builtin_amdgcn_exp2f(m_run - to);
       m_run = to;
       l_run *= less;
 #pragma unroll
       for (int md = 0; md < kMD; ++md)
 #pragma unroll
         for (int v = 0; v < 16; ++v) o[md][v] *= less;
-    }
-    const float ref = m_run == -INFINITY ? 0.f : m_run;
-    float sum[2] = {0.f, 0.f};
+      sum[0] = sum[1] = 0.f;
 #pragma unroll
-    for (int v = 0; v < 16; ++v)
-#pragma unroll
-      for (int n = 0; n < 2; ++n) {
-        const float e = __builtin_amdgcn_exp2f(CAP ? x[n][v] - ref : __builtin_fmaf(x[n][v], scale, -ref));
-        sum[n] += e;
-        p[2 * n + v / 8][v % 8] = (__bf16)e;
+      for (int v = 0; v < 16; ++v) {
+        const float e = x[v] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(score_of<bf16_t, CAP>(x[v], f.scale, f.cap) - to);
+        sum[v & 1] += e;
+        p_next[v / 8][v % 8] = (__bf16)e;
       }
+    }
     l_run += sum[0] + sum[1];
+    x = x_next;
+    p[0] = p_next[0];
+    p[1] = p_next[1];
   };
-  // Phases end together: LDS is settled, loads from memory stay on their way.
-  auto phase_end = [&]() __attribute__((always_inline)) {
-    __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
-    __builtin_amdgcn_sched_barrier(0);
-  };
-
   const int n_tiles = max(end - first, 0);
-  Held held;
-  Meta next;
-  Entries entries;
-  {
-    const Entries e0 = request_entries(first), e1 = request_entries(first + 1);
-    entries = request_entries(first + 2);
-    const Meta m = request_pages(first, e0);
-    next = request_pages(first + 1, e1);
-    load(held, m);
-  }
-  // Part of tile j into LDS, the next ones' requested.
-  auto stage = [&](int j) __attribute__((always_inline)) {
-    if (j >= n_tiles) return;
-    put(held, j);
-    if (j + 1 < n_tiles) load(held, next);
-    if (j + 2 < n_tiles) next = request_pages(first + j + 2, entries);
-    entries = request_entries(first + j + 3);
-  };
-  stage(0);
-  phase_end();
-  const bool second = wave >= kWaves / 2;
-  if (second) {
-    stage(1);
-    phase_end();
-  }
-  int vb = 2;                                                   // buffer of the tile before
   for (int j = 0; j < n_tiles; ++j) {
-    const int vn = vb == 2 ? 0 : vb + 1;                        // j % 3
-    __builtin_amdgcn_s_setprio(1);
-    scores(j);
-    if (j > 0) sums(vb);
-    __builtin_amdgcn_s_setprio(0);
-    phase_end();
-    softmax(vn);
-    stage(second ? j + 2 : j + 1);
-    vb = vn;
-    phase_end();
+    step(j, std::integral_constant<int, 0>{});
+    step(j, std::integral_constant<int, 1>{});
+    meet();
   }
-  if (n_tiles > 0) sums(vb);
-  if (!second) phase_end();
+  {
+    unsigned char* const v_from = v_stage[(n_tiles - 1) & 3] + 32 * kRowBytes;
+#pragma unroll
+    for (int s = 0; s < kSlots; ++s)
+      o[s % kMD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(joined(value_part(v_from, s / kMD, s % kMD, 0), value_part(v_from, s / kMD, s % kMD, 1)),
+                                                            p[s / kMD], o[s % kMD], 0, 0, 0);
+  }
 
   l_run = halves_sum(l_run);
   if (wave * 32 + r >= rows) return;
