@@ -9,6 +9,8 @@
 // the layout of S^T's accumulator is the second product's operand layout when key 16 s + 8 (j / 4) + 4 half + j % 4 is operand j of step s.
 // bf16: v_mfma_f32_32x32x16_bf16; a probability enters as two bf16 terms (16 bits), which costs nothing beside the loads.
 // fp32: v_mfma_f32_32x32x2_f32.
+#include <algorithm>
+
 #include "attend_sliced.h"
 
 namespace esa {
@@ -34,9 +36,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   const int g = blockIdx.x % a.cache.h_kv;
   const Plan plan = plan_of(a, f.shape);
   const int slice = plan.slice;
-  const Part at = part_of(a, f.shape, plan, blockIdx.x / a.cache.h_kv);
+  const Part at = uniform(part_of(a, f.shape, plan, blockIdx.x / a.cache.h_kv));
   if (at.b < 0) return;
-  const Seq s = sequence(a.batch, at.b);
+  const Seq s = uniform(sequence(a.batch, at.b));
   const Keys keys = keys_of(a, s);
   const int n_rows = s.n * a.group, row0 = at.block * kRows, rows = min(n_rows - row0, kRows);
   const int n_vis = keys_until(a, s, keys, row0 + rows - 1), tiles = (n_vis + kKeys - 1) / kKeys;
@@ -284,8 +286,75 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   }
 }
 
+// Slices of a row joined: a workgroup takes a row, its four waves share the slices.  Only rows of sequences of several slices are gone
+// through, by as many workgroups as the chip holds at most.
+template <typename T, int D> __global__ __launch_bounds__(256) void join_few(SlicedArgs f) {
+  constexpr int kMine = D / 64;
+  typedef __attribute__((ext_vector_type(kMine))) float vec;
+  __shared__ vec sums[4][64];
+  __shared__ float2 ml[4];
+  const AttendArgs& a = f.a;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Plan plan = plan_of(a, f.shape);
+  for (int64_t u = blockIdx.x;; u += gridDim.x) {
+    const int g = (int)(u % a.cache.h_kv);
+    const Split at = uniform(split_of(a, f.shape, plan, u / a.cache.h_kv, [](int rows) { return rows; }));
+    if (at.b < 0) return;
+    const Seq s = uniform(sequence(a.batch, at.b));
+    const Keys keys = keys_of(a, s);
+    const int n_rows = s.n * a.group, block = at.i / kRows, blocks = (n_rows + kRows - 1) / kRows;
+    const int n_vis = keys_until(a, s, keys, min(block * kRows + kRows, n_rows) - 1), tiles = (n_vis + kKeys - 1) / kKeys;
+    const int n = (tiles + plan.slice - 1) / plan.slice;
+    if (n <= 1) continue;
+    auto place = [&](int i) { return ((at.slot + block + (int64_t)i * blocks) * a.cache.h_kv + g) * kRows + at.i - block * kRows; };
+    float m = -INFINITY, l = 0.f;
+    vec sum = 0.f;
+    for (int i0 = wave; i0 < n; i0 += 256) {                    // a lane has the i0 + 4 lane-th slice's weight
+      float mine = -INFINITY, part_l = 0.f;
+      if (i0 + lane * 4 < n) {
+        const float2 x = *(const float2*)(f.part_ml + place(i0 + lane * 4) * 2);
+        mine = x.x;
+        part_l = x.y;
+      }
+      const float top = fmaxf(m, wave_max(mine)), ref = top == -INFINITY ? 0.f : top, less = exp_of<T>(m - ref);
+      m = top;
+      const float by = exp_of<T>(mine - ref);
+      l = l * less + wave_sum(part_l * by);
+      sum *= less;
+      const int here = min((n - i0 + 3) / 4, 64);
+      for (int i = 0; i < here; i += 8) {
+        vec x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = *(const vec*)(f.part_o + place(i0 + min(i + k, here - 1) * 4) * D + lane * kMine);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) sum += x[k] * (i + k < here ? __shfl(by, min(i + k, 63)) : 0.f);
+      }
+    }
+    __syncthreads();
+    sums[wave][lane] = sum;
+    if (lane == 0) ml[wave] = make_float2(m, l);
+    __syncthreads();
+    if (wave != 0) continue;
+    m = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
+    const float ref = m == -INFINITY ? 0.f : m;
+    l = 0.f;
+    sum = 0.f;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float by = exp_of<T>(ml[w].x - ref);
+      l = __builtin_fmaf(ml[w].y, by, l);
+      sum += sums[w][lane] * by;
+    }
+    const int tok = s.row0 + at.i / a.group, head = g * a.group + at.i % a.group;
+    T* out = (T*)(a.out + (int64_t)tok * a.ldo) + (int64_t)head * D + lane * kMine;
+#pragma unroll
+    for (int i = 0; i < kMine; ++i) store_f32<T>(out + i, l > 0.f ? sum[i] / l : 0.f);
+    if (a.lse && lane == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? lse_of<T>(m, l) : -INFINITY;
+  }
+}
+
 // Workgroups that the chip holds: a compute unit has 160 KB of LDS, a workgroup's staging space is 64 KB for rows of up to 256 bytes.
-Shape shape_of(int d, int es, int most_rows) { return Shape{kRows, kKeys, d * es > 256 ? 256 : d * es == 256 ? 512 : 1024, kWaves, 16, 0, most_rows}; }
+Shape shape_of(int d, int es, int most_rows) { return Shape{kRows, kKeys, d * es > 256 ? 256 : d * es == 256 ? 512 : 1024, kWaves, 0, 1, 0, most_rows}; }
 
 template <typename T, bool F8, int D> int launch(const SlicedArgs& f, dim3 grid, hipStream_t st) {
   if (f.a.cap > 0.f)
@@ -307,7 +376,15 @@ template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows
     rc = f8 ? launch<T, true, 64>(f, grid, st) : launch<T, false, 64>(f, grid, st);
   else
     rc = f8 ? launch<T, true, 128>(f, grid, st) : launch<T, false, 128>(f, grid, st);
-  return rc != ESA_OK ? rc : launch_join<T, true>(f, st);
+  if (rc != ESA_OK || !may_split(f)) return rc;
+  const int64_t by_blocks = most_blocks(f.shape, a.batch.n_tok, a.batch.n_seq, a.group) * kRows * a.cache.h_kv, by_tokens = a.batch.n_tok * a.h;
+  const dim3 join((unsigned)std::min<int64_t>(std::min(by_blocks, by_tokens), 2048));
+  if (d == 64)
+    join_few<T, 64><<<join, 256, 0, st>>>(f);
+  else
+    join_few<T, 128><<<join, 256, 0, st>>>(f);
+  ESA_LAUNCH_CHECK("join_few");
+  return ESA_OK;
 }
 
 }  // namespace

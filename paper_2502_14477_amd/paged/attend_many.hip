@@ -12,6 +12,8 @@
 // (Without that order, products and softmax one behind the other in a wave: 5600 cycles a tile.  Two groups of waves that took turns with
 // products and softmax, a barrier between: the same, as a wave by itself issues a vector instruction every five cycles or so.)
 //   In iteration j keys of tiles j and j + 1 and values of j - 1 and j are read and tile j + 2 is written: four buffers, one barrier.
+#include <algorithm>
+
 #include "attend_sliced.h"
 
 namespace esa {
@@ -40,9 +42,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   const int g = blockIdx.x % a.cache.h_kv;
   const Plan plan = plan_of(a, f.shape);
   const int slice = plan.slice;
-  const Part at = part_of(a, f.shape, plan, blockIdx.x / a.cache.h_kv);
+  const Part at = uniform(part_of(a, f.shape, plan, blockIdx.x / a.cache.h_kv));
   if (at.b < 0) return;
-  const Seq s = sequence(a.batch, at.b);
+  const Seq s = uniform(sequence(a.batch, at.b));
   const Keys keys = keys_of(a, s);
   const int n_rows = s.n * a.group, row0 = at.block * kRows, rows = min(n_rows - row0, kRows);
   const int n_vis = keys_until(a, s, keys, row0 + rows - 1), tiles = (n_vis + kKeys - 1) / kKeys;
@@ -322,9 +324,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   }
 
   l_run = halves_sum(l_run);
-  if (wave * 32 + r >= rows) return;
-  const int hd = head;
   if (alone) {
+    if (wave * 32 + r >= rows) return;
+    const int hd = head;
     const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
     char* to = a.out + (int64_t)(s.row0 + c) * a.ldo + (int64_t)hd * kRowBytes;
 #pragma unroll
@@ -337,17 +339,66 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       }
     if (a.lse && hi == 0) a.lse[(int64_t)(s.row0 + c) * a.h + hd] = l_run > 0.f ? lse_of<bf16_t>(m_run, l_run) : -INFINITY;
   } else {
-    const int64_t part = ((at.slot + (int64_t)at.slice * at.blocks) * a.cache.h_kv + g) * kRows + wave * 32 + r;
+    // as the lanes have it: 16 bytes a lane, 1 KB an instruction
+    const int64_t part = ((at.slot + (int64_t)at.slice * at.blocks) * a.cache.h_kv + g) * kWaves + wave;
 #pragma unroll
     for (int md = 0; md < kMD; ++md)
 #pragma unroll
       for (int v = 0; v < 16; v += 4)
-        *(f32x4*)(f.part_o + part * D + md * 32 + v * 2 + 4 * hi) = f32x4{o[md][v], o[md][v + 1], o[md][v + 2], o[md][v + 3]};
-    if (hi == 0) *(float2*)(f.part_ml + part * 2) = make_float2(m_run, l_run);
+        *((f32x4*)f.part_o + (part * (D / 8) + md * 4 + v / 4) * 64 + lane) = f32x4{o[md][v], o[md][v + 1], o[md][v + 2], o[md][v + 3]};
+    if (hi == 0) *(float2*)(f.part_ml + (part * 32 + r) * 2) = make_float2(m_run, l_run);
   }
 }
 
-Shape shape_of(int above) { return Shape{kRows, kKeys, 256, 1, 4, above, INT32_MAX}; }
+// Slices joined: a wave takes a quarter of a wave's 32 rows of a block, as attend_many's lanes have left them, a lane the same row and dimensions.
+template <int D> __global__ __launch_bounds__(256) void join_many(SlicedArgs f) {
+  constexpr int kChunks = D / 8, kMine = kChunks / 4;           // 16 bytes a lane: of 32 rows, and of them a wave's
+  const AttendArgs& a = f.a;
+  const int lane = threadIdx.x & 63, r = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const Plan plan = plan_of(a, f.shape);
+  for (int64_t u = blockIdx.x;; u += gridDim.x) {
+    const int g = (int)(u % a.cache.h_kv);
+    const Split at = uniform(split_of(a, f.shape, plan, u / a.cache.h_kv, [](int rows) { return (rows + 31) / 32; }));
+    if (at.b < 0) return;
+    const Seq s = uniform(sequence(a.batch, at.b));
+    const Keys keys = keys_of(a, s);
+    const int n_rows = s.n * a.group, block = at.i / (kRows / 32), part = at.i % (kRows / 32), blocks = (n_rows + kRows - 1) / kRows;
+    const int n_vis = keys_until(a, s, keys, min(block * kRows + kRows, n_rows) - 1), tiles = (n_vis + kKeys - 1) / kKeys;
+    const int n = (tiles + plan.slice - 1) / plan.slice;
+    if (n <= 1) continue;
+    auto place = [&](int i) { return (at.slot + block + (int64_t)i * blocks) * a.cache.h_kv + g; };
+    float m = kNoReference, l = 0.f;
+    for (int i = 0; i < n; ++i) m = fmaxf(m, f.part_ml[(place(i) * kRows + part * 32 + r) * 2]);
+    f32x4 sum[kMine];
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) sum[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < n; ++i) {
+      const float2 x = *(const float2*)(f.part_ml + (place(i) * kRows + part * 32 + r) * 2);
+      const float by = __builtin_amdgcn_exp2f(x.x - m);
+      l = __builtin_fmaf(x.y, by, l);
+      const f32x4* from = (const f32x4*)f.part_o + (place(i) * (kRows / 32) + part) * kChunks * 64 + wave * kMine * 64 + lane;
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) {
+        const f32x4 y = from[k * 64];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[k][e] = __builtin_fmaf(y[e], by, sum[k][e]);
+      }
+    }
+    const int row = at.i * 32 + r;
+    if (row >= n_rows) continue;
+    const int tok = s.row0 + row / a.group, head = g * a.group + row % a.group;
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    char* to = a.out + (int64_t)tok * a.ldo + (int64_t)head * D * 2;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      const bf16x2 lo = __builtin_convertvector((f32x2{sum[k][0] * inv, sum[k][1] * inv}), bf16x2), up = __builtin_convertvector((f32x2{sum[k][2] * inv, sum[k][3] * inv}), bf16x2);
+      *(uint2*)(to + ((wave * kMine + k) * 8 + 4 * hi) * 2) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, up));
+    }
+    if (a.lse && wave == 0 && hi == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? lse_of<bf16_t>(m, l) : -INFINITY;
+  }
+}
+
+Shape shape_of(int above) { return Shape{kRows, kKeys, 256, 1, 4, 4, above, INT32_MAX}; }
 
 template <bool F8, int D> int launch(const SlicedArgs& f, dim3 grid, hipStream_t st) {
   if (f.a.cap > 0.f)
@@ -373,7 +424,15 @@ int launch_many(const AttendArgs& a, bool f8, int above, void* ws, hipStream_t s
     rc = f8 ? launch<true, 64>(f, grid, st) : launch<false, 64>(f, grid, st);
   else
     rc = f8 ? launch<true, 128>(f, grid, st) : launch<false, 128>(f, grid, st);
-  return rc != ESA_OK ? rc : launch_join<bf16_t, false>(f, st);
+  if (rc != ESA_OK || !may_split(f)) return rc;
+  const int64_t items = most_blocks(f.shape, a.batch.n_tok, a.batch.n_seq, a.group) * (kRows / 32) * a.cache.h_kv;
+  const dim3 join((unsigned)std::min<int64_t>(items, 2048));
+  if (a.cache.d == 64)
+    join_many<64><<<join, 256, 0, st>>>(f);
+  else
+    join_many<128><<<join, 256, 0, st>>>(f);
+  ESA_LAUNCH_CHECK("join_many");
+  return ESA_OK;
 }
 
 }  // namespace paged

@@ -50,15 +50,18 @@ __device__ __forceinline__ int page_of(const Batch& a, int n_pages, int b, int p
 }
 
 // ---------------------------------------------------------------- scans over the sequences, a lane to each, 64 at a time
-__device__ __forceinline__ int64_t wave_scan(int64_t x) {       // inclusive
-  const int lane = threadIdx.x & 63;
-#pragma unroll
-  for (int d = 1; d < 64; d *= 2) {
-    const int64_t y = __shfl_up(x, d);
-    if (lane >= d) x += y;
-  }
+// Sums over the lanes up to each (in the vector unit: DPP shifts within rows of sixteen, then the rows' last lanes passed on).
+__device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false);      // row_shr 1, 2, 4, 8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false);      // row_bcast 15, 31
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
   return x;
 }
+// What a lane may count, so that 64 of them stay within 32 bits (more than any call has).
+__device__ __forceinline__ uint32_t countable(int64_t n) { return (uint32_t)min(n, (int64_t)1 << 24); }
 struct Found {
   int b;              // the sequence, -1: beyond the last
   int64_t i;          // what is left within it
@@ -68,13 +71,13 @@ template <typename F> __device__ __forceinline__ Found find(int n_seq, int64_t u
   const int lane = threadIdx.x & 63;
   for (int b0 = 0; b0 < n_seq; b0 += 64) {
     const int b = b0 + lane;
-    const int64_t c = b < n_seq ? count(b) : 0, upto = wave_scan(c);
+    const uint32_t c = b < n_seq ? countable(count(b)) : 0, upto = wave_scan(c);
     const uint64_t past = __ballot(upto > u);
     if (past) {
       const int at = __ffsll((unsigned long long)past) - 1;
-      return Found{b0 + at, u - __shfl(upto - c, at)};
+      return Found{b0 + at, u - (int64_t)(uint32_t)__builtin_amdgcn_readlane(upto - c, at)};
     }
-    u -= __shfl(upto, 63);
+    u -= (uint32_t)__builtin_amdgcn_readlane(upto, 63);
   }
   return Found{-1, 0};
 }

@@ -12,9 +12,10 @@ namespace esa {
 namespace paged {
 
 // Rows of a block, keys of a tile, workgroups at a time; a slice has a multiple of `least` tiles; a workgroup's beginning and end take
-// as long as `overhead` tiles.  The kernel serves sequences of more than `above` rows, up to `upto`.
+// as long as `overhead` tiles; at most `rounds` units for every place are worth while.  The kernel serves sequences of more than `above`
+// rows, up to `upto`.
 struct Shape {
-  int rows, keys, target, least, overhead, above, upto;
+  int rows, keys, target, least, overhead, rounds, above, upto;
 };
 struct Cost {
   int blocks, tiles;
@@ -25,122 +26,134 @@ __device__ __forceinline__ Cost cost_of(const AttendArgs& a, const Shape& sh, in
   if (rows <= sh.above || rows > sh.upto) return Cost{0, 0};
   return Cost{(rows + sh.rows - 1) / sh.rows, (keys_of(a, s).n + sh.keys - 1) / sh.keys};
 }
+// A value that is the same in every lane, where the compiler does not see it.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) { return (int64_t)(uint32_t)uniform((int)x) | (int64_t)uniform((int)(x >> 32)) << 32; }
+__device__ __forceinline__ Seq uniform(const Seq& s) { return Seq{uniform(s.row0), uniform(s.n), uniform(s.t0)}; }
 struct Plan {
-  Cost mine;      // of the lane's sequence among the first 64
+  Cost mine;      // of the lane's sequence among the first 64; of the only one in every lane
   int slice;      // tiles of a slice
 };
 __device__ __forceinline__ Cost cost_in(const AttendArgs& a, const Shape& sh, const Cost& mine, int b0) {
   const int b = b0 + (int)(threadIdx.x & 63);
   return b0 == 0 ? mine : b < a.batch.n_seq ? cost_of(a, sh, b) : Cost{0, 0};
 }
-// The length of a slice: what the call takes is estimated for slices of which every place of the chip gets one, two, three or four in the
-// mean, and for longer ones of which no more than one round is needed.  (Sixteen sequences of 18 to 66 thousand tokens, cut by their mean,
-// were 600 units for 512 places, and the second round took as long as the first: 497 us, 342 in one.)  Counts are fp32: exact where they
-// decide, and every workgroup comes to the same ones.
+// The length of a slice: so long that no more than one round of units is needed, or, where a call takes long enough, whatever is estimated
+// to be quickest of that and of slices of which every place of the chip gets two, three or four in the mean.  (Sixteen sequences of 18 to
+// 66 thousand tokens, cut by their mean, were 600 units for 512 places, and the second round took as long as the first: 497 us, 342
+// in one.)  Counts are fp32: exact where they decide, and every workgroup comes to the same ones.
 __device__ __forceinline__ Plan plan_of(const AttendArgs& a, const Shape& sh) {
   const int lane = threadIdx.x & 63;
+  const bool one = a.batch.n_seq == 1;
   Plan p;
-  p.mine = lane < a.batch.n_seq ? cost_of(a, sh, lane) : Cost{0, 0};
-  float all = 0.f;
-  for (int b0 = 0; b0 < a.batch.n_seq; b0 += 64) {
-    const Cost c = cost_in(a, sh, p.mine, b0);
-    all += (float)c.blocks * (float)c.tiles;
-  }
-  all = wave_sum(all) * (float)a.cache.h_kv;
-  const float places = (float)sh.target;
-  const float mean = fmaxf(all / places, 1.f);
-  auto rounded = [&](float x) { return (int)fminf(ceilf(x / (float)sh.least), 1e7f) * sh.least; };
-  auto units_of = [&](int slice) {
-    float units = 0.f;
-    for (int b0 = 0; b0 < a.batch.n_seq; b0 += 64) {
-      const Cost c = cost_in(a, sh, p.mine, b0);
-      units += (float)c.blocks * (float)((c.tiles + slice - 1) / slice);
-    }
-    return wave_sum(units) * (float)a.cache.h_kv;
+  p.mine = lane < a.batch.n_seq || one ? cost_of(a, sh, one ? 0 : lane) : Cost{0, 0};
+  auto total = [&](auto&& of) {
+    if (one) return of(p.mine) * (float)a.cache.h_kv;
+    float sum = 0.f;
+    for (int b0 = 0; b0 < a.batch.n_seq; b0 += 64) sum += of(cost_in(a, sh, p.mine, b0));
+    return wave_sum(sum) * (float)a.cache.h_kv;
   };
-  float best = INFINITY;
-  p.slice = 0;
-  auto consider = [&](int slice) {
-    const float units = units_of(slice);
-    const float took = units <= places ? (float)(slice + sh.overhead) : (all + units * (float)sh.overhead) / places + 0.5f * (float)slice;
-    if (took < best) {
-      best = took;
-      p.slice = slice;
-    }
-    return units;
+  const float all = total([](const Cost& c) { return (float)c.blocks * (float)c.tiles; });
+  const float places = (float)sh.target, mean = fmaxf(all / places, 1.f);
+  auto rounded = [&](float x) { return (int)fminf(ceilf(x / (float)sh.least), 1e7f) * sh.least; };
+  auto units_of = [&](int slice) { return total([&](const Cost& c) { return (float)c.blocks * (float)((c.tiles + slice - 1) / slice); }); };
+  auto took = [&](int slice, float units) {
+    return units <= places ? (float)(slice + sh.overhead) : (all + units * (float)sh.overhead) / places + 0.5f * (float)slice;
   };
   int slice = rounded(mean);
-  for (int i = 0; i < 4; ++i) {
-    const float units = consider(slice);
-    if (units <= places) break;
+  float units = units_of(slice);
+  for (int i = 0; i < 4 && units > places; ++i) {
     // every sequence's last slice is half full in the mean: what is over one round is spread over the others
     slice += rounded(fmaxf((float)slice * (units - places) / (2.f * places), 1.f));
+    units = units_of(slice);
   }
-  if (mean > 4.f * (float)sh.overhead) {
-    consider(rounded(mean * 0.5f));
-    consider(rounded(mean * (1.f / 3.f)));
-    consider(rounded(mean * 0.25f));
+  p.slice = uniform(slice);
+  if (sh.rounds > 1 && mean > 4.f * (float)sh.overhead) {
+    float best = took(slice, units);
+    for (int k = 1; k <= sh.rounds; ++k) {
+      const int shorter = rounded(mean / (float)k);
+      const float t = took(shorter, units_of(shorter));
+      if (t < best) {
+        best = t;
+        p.slice = uniform(shorter);
+      }
+    }
   }
   return p;
 }
+__device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane(x, lane); }
 struct Part {
   int b, block, slice;      // b < 0: none
   int64_t slot;             // of the block's first slice among the partial results of a KV head (blocks next to each other), if it has several
   int blocks;
 };
+__device__ __forceinline__ Part uniform(const Part& p) { return Part{uniform(p.b), uniform(p.block), uniform(p.slice), uniform(p.slot), uniform(p.blocks)}; }
 // The u-th unit.  A sequence's units are numbered slice by slice: neighbours read the same keys.
 __device__ __forceinline__ Part part_of(const AttendArgs& a, const Shape& sh, const Plan& plan, int64_t u) {
-  const int slice = plan.slice;
-  int64_t slots = 0;
-  for (int b0 = 0; b0 < a.batch.n_seq; b0 += 64) {
-    const Cost c = cost_in(a, sh, plan.mine, b0);
-    const int n = (c.tiles + slice - 1) / slice;
-    const int64_t units = (int64_t)c.blocks * max(n, 1), parts = n > 1 ? units : 0, upto = wave_scan(units), parts_upto = wave_scan(parts);
-    const uint64_t past = __ballot(upto > u);
-    if (past) {
-      const int at = __ffsll((unsigned long long)past) - 1;
-      const int i = (int)(u - __shfl(upto - units, at)), blocks = __shfl(c.blocks, at);
-      return Part{b0 + at, i % blocks, i / blocks, slots + __shfl(parts_upto - parts, at) + i % blocks, blocks};
-    }
-    u -= __shfl(upto, 63);
-    slots += __shfl(parts_upto, 63);
+  if (a.batch.n_seq == 1) {
+    const int blocks = uniform(plan.mine.blocks), n = max((uniform(plan.mine.tiles) + plan.slice - 1) / plan.slice, 1);
+    if (u >= (int64_t)blocks * n) return Part{-1, 0, 0, 0, 0};
+    return Part{0, (int)u % blocks, (int)u / blocks, (int)u % blocks, blocks};
   }
-  return Part{-1, 0, 0, 0, 0};
-}
-// The u-th row of a KV head among the sequences of several slices.
-struct SplitRow {
-  int b, row;               // b < 0: none
-  int64_t slot;             // of the sequence's first partial result
-};
-__device__ __forceinline__ SplitRow split_row(const AttendArgs& a, const Shape& sh, const Plan& plan, int64_t u) {
-  const int lane = threadIdx.x & 63;
   int64_t slots = 0;
   for (int b0 = 0; b0 < a.batch.n_seq; b0 += 64) {
     const Cost c = cost_in(a, sh, plan.mine, b0);
     const int n = (c.tiles + plan.slice - 1) / plan.slice;
-    const int64_t rows = n > 1 ? (int64_t)sequence(a.batch, b0 + lane).n * a.group : 0, parts = n > 1 ? (int64_t)c.blocks * n : 0;
-    const int64_t upto = wave_scan(rows), parts_upto = wave_scan(parts);
+    const uint32_t units = countable((int64_t)c.blocks * max(n, 1)), parts = n > 1 ? units : 0, upto = wave_scan(units), parts_upto = wave_scan(parts);
     const uint64_t past = __ballot(upto > u);
     if (past) {
       const int at = __ffsll((unsigned long long)past) - 1;
-      return SplitRow{b0 + at, (int)(u - __shfl(upto - rows, at)), slots + __shfl(parts_upto - parts, at)};
+      const int i = (int)(u - lane_value(upto - units, at)), blocks = (int)lane_value(c.blocks, at);
+      return Part{b0 + at, i % blocks, i / blocks, slots + lane_value(parts_upto - parts, at) + i % blocks, blocks};
     }
-    u -= __shfl(upto, 63);
-    slots += __shfl(parts_upto, 63);
+    u -= lane_value(upto, 63);
+    slots += lane_value(parts_upto, 63);
   }
-  return SplitRow{-1, 0, 0};
+  return Part{-1, 0, 0, 0, 0};
+}
+// The u-th of what `count(rows)` makes of the rows of a sequence, among the sequences of several slices.
+struct Split {
+  int b, i;                 // b < 0: none
+  int64_t slot;             // of the sequence's first partial result
+};
+__device__ __forceinline__ Split uniform(const Split& s) { return Split{uniform(s.b), uniform(s.i), uniform(s.slot)}; }
+template <typename F> __device__ __forceinline__ Split split_of(const AttendArgs& a, const Shape& sh, const Plan& plan, int64_t u, F&& count) {
+  const int lane = threadIdx.x & 63;
+  if (a.batch.n_seq == 1) {
+    const bool split = uniform(plan.mine.tiles) > plan.slice && u < count(sequence(a.batch, 0).n * a.group);
+    return Split{split ? 0 : -1, (int)u, 0};
+  }
+  int64_t slots = 0;
+  for (int b0 = 0; b0 < a.batch.n_seq; b0 += 64) {
+    const Cost c = cost_in(a, sh, plan.mine, b0);
+    const int n = (c.tiles + plan.slice - 1) / plan.slice;
+    const uint32_t items = n > 1 ? countable(count(sequence(a.batch, b0 + lane).n * a.group)) : 0, parts = n > 1 ? countable((int64_t)c.blocks * n) : 0;
+    const uint32_t upto = wave_scan(items), parts_upto = wave_scan(parts);
+    const uint64_t past = __ballot(upto > u);
+    if (past) {
+      const int at = __ffsll((unsigned long long)past) - 1;
+      return Split{b0 + at, (int)(u - lane_value(upto - items, at)), slots + lane_value(parts_upto - parts, at)};
+    }
+    u -= lane_value(upto, 63);
+    slots += lane_value(parts_upto, 63);
+  }
+  return Split{-1, 0, 0};
 }
 // Keys that the rows up to `row` of a sequence see at most.
 __device__ __forceinline__ int keys_until(const AttendArgs& a, const Seq& s, const Keys& k, int row) {
   const int width = a.batch.max_pages << a.batch.page_log2;
   return k.n - (min(s.t0 + s.n, width) - min(s.t0 + row / a.group + 1, width));
 }
-// Units of a KV head at most (a slice is a quarter of the mean at least), and partial results among them: a sequence of several slices
-// has more than one slice's tiles, so at most twice as many slices as its tiles fill.
-static inline int64_t most_units(const Shape& sh, int64_t n_tok, int n_seq, int group, int h_kv) {
-  return 4 * ((int64_t)sh.target / h_kv + 1) + n_tok * group / sh.rows + (n_seq < n_tok ? n_seq : n_tok);
+// Blocks, units and partial results of a KV head at most.  A slice is the rounds-th part of the mean at least; a sequence of several
+// slices has more than one slice's tiles, so at most twice as many slices as its tiles fill.
+static inline int64_t most_blocks(const Shape& sh, int64_t n_tok, int n_seq, int group) {
+  const int64_t by_rows = n_tok * group / sh.rows + (n_seq < n_tok ? n_seq : n_tok), by_limit = (int64_t)n_seq * ((sh.upto - 1) / sh.rows + 1);
+  return by_rows < by_limit ? by_rows : by_limit;
 }
-static inline int64_t most_parts(const Shape& sh, int h_kv) { return 8 * ((int64_t)sh.target / h_kv + 1); }
+static inline int64_t most_units(const Shape& sh, int64_t n_tok, int n_seq, int group, int h_kv) {
+  return sh.rounds * ((int64_t)sh.target / h_kv + 1) + most_blocks(sh, n_tok, n_seq, group);
+}
+static inline int64_t most_parts(const Shape& sh, int h_kv) { return 2 * sh.rounds * ((int64_t)sh.target / h_kv + 1); }
 
 }  // namespace paged
 }  // namespace esa
