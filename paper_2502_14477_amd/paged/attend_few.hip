@@ -41,7 +41,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   const Seq s = uniform(sequence(a.batch, at.b));
   const Keys keys = keys_of(a, s);
   const int n_rows = s.n * a.group, row0 = at.block * kRows, rows = min(n_rows - row0, kRows);
-  const int n_vis = keys_until(a, s, keys, row0 + rows - 1), tiles = (n_vis + kKeys - 1) / kKeys;
+  const int n_vis = uniform(keys_until(a, s, keys, row0 + rows - 1)), tiles = (n_vis + kKeys - 1) / kKeys;
   const int first = at.slice * slice, end = min(first + slice, tiles);
   if (at.slice > 0 && first >= end) return;
   const bool alone = tiles <= slice;

@@ -32,9 +32,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   constexpr int kLoads = 2 * kKeys / kPass;
   constexpr int kMine = kPass < kKeys ? kKeys / kPass : 1;      // keys of a thread
   constexpr int kKS = D / 16, kMD = D / 32;
-  constexpr int kTileBytes = kKeys * kRowBytes;
-  constexpr int kBuffers = 4;
-  __shared__ __attribute__((aligned(16))) unsigned char k_stage[kBuffers][kTileBytes], v_stage[kBuffers][kTileBytes];
+  // Rows in LDS are padded so that what lanes read together lies in different banks and every fragment's place is a constant from a lane's
+  // first: 16 bytes behind a key row (eight lanes read 16 bytes of eight rows), 64 behind a value row (64 bytes of four).
+  constexpr int kBuffers = 4, kKeyStride = kRowBytes + 16, kValueStride = kRowBytes + 64;
+  static_assert(kKeyStride % 128 == 16 && (kValueStride % 256 == 64 || kValueStride % 256 == 192), "bank groups");
+  __shared__ __attribute__((aligned(16))) unsigned char k_stage[kBuffers][kKeys * kKeyStride], v_stage[kBuffers][kKeys * kValueStride];
   __shared__ __attribute__((aligned(16))) int seen[kBuffers][kKeys];                  // positions, INT32_MAX: not seen
   const AttendArgs& a = f.a;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, hi = lane >> 5;
@@ -47,7 +49,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   const Seq s = uniform(sequence(a.batch, at.b));
   const Keys keys = keys_of(a, s);
   const int n_rows = s.n * a.group, row0 = at.block * kRows, rows = min(n_rows - row0, kRows);
-  const int n_vis = keys_until(a, s, keys, row0 + rows - 1), tiles = (n_vis + kKeys - 1) / kKeys;
+  const int n_vis = uniform(keys_until(a, s, keys, row0 + rows - 1)), tiles = (n_vis + kKeys - 1) / kKeys;
   const int first = at.slice * slice, end = min(first + slice, tiles);
   if (at.slice > 0 && first >= end) return;
   const bool alone = tiles <= slice;
@@ -105,6 +107,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   struct Held {
     u32x4 x[kLoads];
     int scale[kLoads], pos[kMine];                              // position: INT32_MAX where nothing is seen
+    bool whole;                                                 // a tile in one page
   };
   auto load = [&](Held& h, const Meta& m) {
     if (m.pos0 >= 0) {
@@ -121,8 +124,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       }
 #pragma unroll
       for (int n = 0; n < kMine; ++n) h.pos[n] = there ? m.pos0 + key_of(n) : INT32_MAX;
+      h.whole = there;
       return;
     }
+    h.whole = false;
     int64_t place[kMine], block[kMine];
 #pragma unroll
     for (int n = 0; n < kMine; ++n) {
@@ -138,8 +143,17 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       if constexpr (F8) h.scale[i] = (is_value(i) ? a.cache.v_scale : a.cache.k_scale)[block[kMine == 1 ? 0 : i % kMine]];
     }
   };
-  auto k_swizzle = [](int key) { return kRowBytes >= 256 ? key & 15 : (key >> 1) & 7; };
-  auto v_swizzle = [](int key) { return kRowBytes >= 256 ? (key & 3) << 2 : ((key >> 1) & 1) << 2; };
+  // Values that are not there count as 0, whatever lies in their place and its scale: 0 times a NaN is one.  (Such keys' scores are masked.)
+  auto without_unseen = [&](Held& h) __attribute__((always_inline)) {
+    if (h.whole) return;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      const bool there = h.pos[kMine == 1 ? 0 : i % kMine] != INT32_MAX;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) h.x[i][w] = there ? h.x[i][w] : 0;
+      if constexpr (F8) h.scale[i] = there ? h.scale[i] : 127;
+    }
+  };
   // Writing tile j is cut into kParts: 8-bit pages go four bytes of every 16 at a time, others a load at a time.
   constexpr int kParts = F8 ? 4 * kLoads : kLoads;
   u32x4 made[2];
@@ -147,21 +161,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     const int i = F8 ? part / 4 : part, e = part % 4;
     const bool values = is_value(i);
     const int n = kMine == 1 ? 0 : i % kMine, key = key_of(i);
-    const bool there = h.pos[n] != INT32_MAX;
-    unsigned char* const to = (values ? v_stage[j & 3] : k_stage[j & 3]) + key * kRowBytes;
-    const int swizzle = values ? v_swizzle(key) : k_swizzle(key);
-    // Values that are not there count as 0, whatever lies in their place: 0 times a NaN is one.  (Such keys' scores are masked.)
+    unsigned char* const to = (values ? v_stage[j & 3] + key * kValueStride : k_stage[j & 3] + key * kKeyStride) + piece * (F8 ? 32 : 16);
     if constexpr (F8) {
-      const uint32_t x = there || (kPass <= kKeys && !values) ? h.x[i][e] : 0;
-      const float by = scale_of(there ? h.scale[i] : 127);
-      made[e / 2][e % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, by, false));
-      made[e / 2][e % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x, by, true));
-      if (e % 2) *(u32x4*)(to + (((piece * 2 + e / 2) ^ swizzle) << 4)) = made[e / 2];
+      const float by = scale_of(h.scale[i]);
+      made[e / 2][e % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(h.x[i][e], by, false));
+      made[e / 2][e % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(h.x[i][e], by, true));
+      if (e % 2) *(u32x4*)(to + e / 2 * 16) = made[e / 2];
     } else {
-      u32x4 x = h.x[i];
-#pragma unroll
-      for (int w = 0; w < 4; ++w) x[w] = there || !values ? x[w] : 0;
-      *(u32x4*)(to + ((piece ^ swizzle) << 4)) = x;
+      *(u32x4*)to = h.x[i];
     }
     // (several threads write a key's position: the same one)
     if (part % (kParts / kLoads) == 0 && i < kMine) seen[j & 3][key] = h.pos[n];
@@ -180,16 +187,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
   for (int e = 0; e < 8; ++e) p[0][e] = p[1][e] = (__bf16)0.f;
 
-  const int k_at = r * kRowBytes;
-  auto key_part = [&](const unsigned char* from, int i) __attribute__((always_inline)) {
-    return *(const u32x4*)(from + k_at + (((2 * i + hi) ^ k_swizzle(r)) << 4));
-  };
-  const int tr_key = 4 * hi + ((lane & 15) >> 2), tr_dim = ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
+  const int k_at = r * kKeyStride + hi * 16;
+  auto key_part = [&](const unsigned char* from, int i) __attribute__((always_inline)) { return *(const u32x4*)(from + k_at + i * 32); };
   // Keys 16 kp + 8 upper + 4 hi + 0 .. 3 of dimension md * 32 + r: lane i of sixteen receives element i % 4 of the 8 bytes that lanes
   // 4 e + i / 4 address, which is dimension i of keys e = 0 .. 3.
+  const int v_at = (4 * hi + ((lane & 15) >> 2)) * kValueStride + (((lane >> 4) & 1) * 16 + 4 * (lane & 3)) * 2;
   auto value_part = [&](unsigned char* from, int kp, int md, int upper) __attribute__((always_inline)) {
-    const int key = 16 * kp + 8 * upper + tr_key, at_piece = (md * 32 + tr_dim) / 8;
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(from + key * kRowBytes + ((at_piece ^ v_swizzle(key)) << 4) + (tr_dim & 4) * 2));
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(from + v_at + (16 * kp + 8 * upper) * kValueStride + md * 64));
   };
   auto joined = [](const i16x4& lo, const i16x4& up) __attribute__((always_inline)) {
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
@@ -207,6 +211,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     Held h0;
     load(h0, m0);
     load(held, m1);
+    without_unseen(h0);
+    without_unseen(held);
 #pragma unroll
     for (int i = 0; i < kParts; ++i) put(h0, 0, i);
 #pragma unroll
@@ -215,7 +221,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     next = request_pages(first + 3, entries);
     entries = request_entries(first + 4);
     // the "32 keys before" of the first step: probabilities of 0 times values that are none
-    for (int e = tid; e < 32 * kRowBytes / 16; e += 64 * kWaves) *(u32x4*)(v_stage[3] + 32 * kRowBytes + e * 16) = u32x4{0, 0, 0, 0};
+    for (int e = tid; e < 32 * kValueStride / 16; e += 64 * kWaves) *(u32x4*)(v_stage[3] + 32 * kValueStride + e * 16) = u32x4{0, 0, 0, 0};
   }
   // LDS is settled; loads from memory stay on their way.
   auto meet = [&]() __attribute__((always_inline)) {
@@ -232,9 +238,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   // Half `n` of tile j, whose scores are in x: leaves the next 32 keys' scores there, and the probabilities in p.
   auto step = [&](int j, auto half) __attribute__((always_inline)) {
     constexpr int n = decltype(half)::value;
-    const unsigned char* const k_from = k_stage[(j + n) & 3] + (1 - n) * 32 * kRowBytes;
-    unsigned char* const v_from = v_stage[(j - 1 + n) & 3] + (1 - n) * 32 * kRowBytes;
+    const unsigned char* const k_from = k_stage[(j + n) & 3] + (1 - n) * 32 * kKeyStride;
+    unsigned char* const v_from = v_stage[(j - 1 + n) & 3] + (1 - n) * 32 * kValueStride;
     constexpr int kAhead = kSlots < 3 ? kSlots : 3;
+    if (n == 0) without_unseen(held);
     u32x4 kf[kSlots];
     i16x4 vf[kSlots][2];
     auto request = [&](int s) __attribute__((always_inline)) {
@@ -244,14 +251,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     };
 #pragma unroll
     for (int s = 0; s < kAhead; ++s) request(s);
-    if (__ballot(seen[j & 3][n * 32 + r] > own_first)) {        // some key is not for all rows of the wave
+    const bool masked = __ballot(seen[j & 3][n * 32 + r] > own_first);
+    if (masked) {                                               // some key is not for all rows of the wave
 #pragma unroll
       for (int v = 0; v < 16; ++v)
         if (seen[j & 3][n * 32 + 8 * (v / 4) + 4 * hi + v % 4] > own) x[v] = -INFINITY;
     }
     f32x16 x_next;
     bf16x8 p_next[2];
-    float sum[2] = {0.f, 0.f};
+    float sum[2] = {0.f, 0.f};                                  // of the rounded probabilities: what the second product sees
+    const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
@@ -262,11 +271,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         const int v = s * kValues + i;
         float e;
         if constexpr (CAP)
-          e = x[v] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(score_of<bf16_t, CAP>(x[v], f.scale, f.cap) - m_run);
+          e = __builtin_amdgcn_exp2f(__builtin_fmaf(-2.f * f.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[v] * f.scale)), f.cap - m_run));      // score_of(x) - m_run
         else
           e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v], f.scale, -m_run));
-        sum[i & 1] += e;
         p_next[v / 8][v % 8] = (__bf16)e;
+        if (i & 1) sum[i / 2 & 1] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p_next[v / 8][v % 8 - 1], p_next[v / 8][v % 8]}, ones, sum[i / 2 & 1], false);
       }
       o[s % kMD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(joined(vf[s][0], vf[s][1]), p[s / kMD], o[s % kMD], 0, 0, 0);
       if constexpr (n == 0) {
@@ -277,13 +286,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       } else {
         if (s == 0) load(held, next);
         if (s == kSlots / 2) next = request_pages(first + j + 4, entries);
-        if (s == kSlots - 1) entries = request_entries(first + j + 5);
+        if (s == kSlots - 1 && keys.n_sel) entries = request_entries(first + j + 5);
       }
       __builtin_amdgcn_sched_barrier(0);
     }
     // The exponentials were taken against the reference as it stands.  Where a row's exceed it by far (and at first) it moves to its largest
-    // logit and they are taken again; the sums so far, those of the 32 keys before among them, come to the new one.
-    if (__ballot(sum[0] + sum[1] > 256.f)) {
+    // logit and they are taken again; the sums so far, those of the 32 keys before among them, come to the new one.  (A capped -inf is none:
+    // with masked keys capped scores are taken again too.)
+    if ((CAP && masked) || __ballot(sum[0] + sum[1] > 256.f)) {
       float top = x[0];
 #pragma unroll
       for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
@@ -300,8 +310,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
       for (int v = 0; v < 16; ++v) {
         const float e = x[v] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(score_of<bf16_t, CAP>(x[v], f.scale, f.cap) - to);
-        sum[v & 1] += e;
         p_next[v / 8][v % 8] = (__bf16)e;
+        if (v & 1) sum[0] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p_next[v / 8][v % 8 - 1], p_next[v / 8][v % 8]}, ones, sum[0], false);
       }
     }
     l_run += sum[0] + sum[1];
@@ -316,7 +326,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     meet();
   }
   {
-    unsigned char* const v_from = v_stage[(n_tiles - 1) & 3] + 32 * kRowBytes;
+    unsigned char* const v_from = v_stage[(n_tiles - 1) & 3] + 32 * kValueStride;
 #pragma unroll
     for (int s = 0; s < kSlots; ++s)
       o[s % kMD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(joined(value_part(v_from, s / kMD, s % kMD, 0), value_part(v_from, s / kMD, s % kMD, 1)),

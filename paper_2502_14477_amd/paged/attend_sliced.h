@@ -39,7 +39,7 @@ struct SlicedArgs {
   Shape shape;
   float* part_o;          // [slot][h_kv][shape.rows * D] (in a kernel's own order), relative to the slice's reference
   float* part_ml;         // [slot][h_kv][shape.rows][2]: the reference, the sum of exponentials
-  float scale;            // bf16: includes log2(e); with a cap: 1 / cap
+  float scale;            // bf16: includes log2(e); with a cap: 1 / cap, and bf16: 2 log2(e)
   float cap;              // bf16: includes log2(e)
 };
 
@@ -49,8 +49,7 @@ template <typename T, bool CAP> __device__ __forceinline__ float score_of(float 
   if constexpr (!CAP) return x;
   if constexpr (sizeof(T) == 4) return cap * tanhf(x);
   // tanh x = 1 - 2 / (1 + e^(2x)): some 2^-22 of the cap off where x is small, two roundings of a probability to 16 bits less than those
-  const float e = __builtin_amdgcn_exp2f(x * (2.f * kLog2e));
-  return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + e), cap);
+  return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x)), cap);
 }
 
 // Arguments, workspace.
@@ -60,7 +59,7 @@ template <typename T> static void set_sliced(SlicedArgs& f, const AttendArgs& a,
   f.part_o = (float*)ws;
   f.part_ml = f.part_o + most_parts(shape, a.cache.h_kv) * a.cache.h_kv * shape.rows * a.cache.d;
   const float base = sizeof(T) == 2 ? kLog2e : 1.f;
-  f.scale = a.cap > 0.f ? a.scale / a.cap : a.scale * base;
+  f.scale = a.cap > 0.f ? a.scale / a.cap * (sizeof(T) == 2 ? 2.f * kLog2e : 1.f) : a.scale * base;
   f.cap = a.cap * base;
 }
 static inline size_t sliced_workspace(const Shape& shape, int h_kv, int d) {
