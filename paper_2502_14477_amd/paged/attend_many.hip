@@ -223,35 +223,41 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     // the "32 keys before" of the first step: probabilities of 0 times values that are none
     for (int e = tid; e < 32 * kValueStride / 16; e += 64 * kWaves) *(u32x4*)(v_stage[3] + 32 * kValueStride + e * 16) = u32x4{0, 0, 0, 0};
   }
-  // LDS is settled; loads from memory stay on their way.
+  // What the waves have written to LDS is there; the newest reads, which are behind the writes, and loads from memory stay on their way.
   auto meet = [&]() __attribute__((always_inline)) {
     __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    asm volatile("s_waitcnt lgkmcnt(8)\n\ts_barrier" ::: "memory");
     __builtin_amdgcn_sched_barrier(0);
   };
-  meet();
+  __syncthreads();
   x = zero;
 #pragma unroll
   for (int i = 0; i < kKS; ++i)
     x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, key_part(k_stage[0], i)), __builtin_bit_cast(bf16x8, qf[i]), x, 0, 0, 0);
 
+  // Fragments are requested kAhead slots ahead, across the steps too.  Step (j, n), half n of tile j, multiplies keys 32 behind and values 32
+  // in front of its own.
+  constexpr int kAhead = 4;
+  u32x4 kf[kAhead];
+  i16x4 vf[kAhead][2];
+  auto keys_from = [&](int j, int n) { return (const unsigned char*)k_stage[(j + n) & 3] + (1 - n) * 32 * kKeyStride; };
+  auto values_from = [&](int j, int n) { return (unsigned char*)v_stage[(j - 1 + n) & 3] + (1 - n) * 32 * kValueStride; };
+  auto request = [&](const unsigned char* k_from, unsigned char* v_from, int s) __attribute__((always_inline)) {
+    kf[s % kAhead] = key_part(k_from, s);
+    vf[s % kAhead][0] = value_part(v_from, s / kMD, s % kMD, 0);
+    vf[s % kAhead][1] = value_part(v_from, s / kMD, s % kMD, 1);
+  };
+  int positions = seen[0][r];                                   // of the step's keys
+#pragma unroll
+  for (int s = 0; s < kAhead; ++s) request(keys_from(0, 0), values_from(0, 0), s);
+
   // Half `n` of tile j, whose scores are in x: leaves the next 32 keys' scores there, and the probabilities in p.
   auto step = [&](int j, auto half) __attribute__((always_inline)) {
     constexpr int n = decltype(half)::value;
-    const unsigned char* const k_from = k_stage[(j + n) & 3] + (1 - n) * 32 * kKeyStride;
-    unsigned char* const v_from = v_stage[(j - 1 + n) & 3] + (1 - n) * 32 * kValueStride;
-    constexpr int kAhead = kSlots < 3 ? kSlots : 3;
+    const unsigned char *const k_from = keys_from(j, n), *const k_after = keys_from(j + n, 1 - n);
+    unsigned char *const v_from = values_from(j, n), *const v_after = values_from(j + n, 1 - n);
     if (n == 0) without_unseen(held);
-    u32x4 kf[kSlots];
-    i16x4 vf[kSlots][2];
-    auto request = [&](int s) __attribute__((always_inline)) {
-      kf[s] = key_part(k_from, s);
-      vf[s][0] = value_part(v_from, s / kMD, s % kMD, 0);
-      vf[s][1] = value_part(v_from, s / kMD, s % kMD, 1);
-    };
-#pragma unroll
-    for (int s = 0; s < kAhead; ++s) request(s);
-    const bool masked = __ballot(seen[j & 3][n * 32 + r] > own_first);
+    const bool masked = __ballot(positions > own_first);
     if (masked) {                                               // some key is not for all rows of the wave
 #pragma unroll
       for (int v = 0; v < 16; ++v)
@@ -264,8 +270,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
-      if (s + kAhead < kSlots) request(s + kAhead);
-      x_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[s]), __builtin_bit_cast(bf16x8, qf[s]), s ? x_next : zero, 0, 0, 0);
+      const bf16x8 v_now = joined(vf[s % kAhead][0], vf[s % kAhead][1]);
+      x_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[s % kAhead]), __builtin_bit_cast(bf16x8, qf[s]), s ? x_next : zero, 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < kValues; ++i) {
         const int v = s * kValues + i;
@@ -277,7 +283,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         p_next[v / 8][v % 8] = (__bf16)e;
         if (i & 1) sum[i / 2 & 1] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p_next[v / 8][v % 8 - 1], p_next[v / 8][v % 8]}, ones, sum[i / 2 & 1], false);
       }
-      o[s % kMD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(joined(vf[s][0], vf[s][1]), p[s / kMD], o[s % kMD], 0, 0, 0);
+      o[s % kMD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_now, p[s / kMD], o[s % kMD], 0, 0, 0);
+      if (s + kAhead < kSlots)
+        request(k_from, v_from, s + kAhead);
+      else
+        request(k_after, v_after, s + kAhead - kSlots);
+      if (s == 0) positions = seen[(j + n) & 3][(1 - n) * 32 + r];
       if constexpr (n == 0) {
         if (kParts >= kSlots || s % (kSlots / kParts) == 0) {
 #pragma unroll
