@@ -7,7 +7,8 @@
 // their way into LDS, and the next tile is requested before the products.  So from LDS on there is one kernel for all cache types.
 //   S^T = K Q^T, O^T += V^T P^T: a lane stands for a row, softmax stays in the lane and its opposite in the other half of the wave, and
 // the layout of S^T's accumulator is the second product's operand layout when key 16 s + 8 (j / 4) + 4 half + j % 4 is operand j of step s.
-// bf16: v_mfma_f32_32x32x16_bf16; a probability enters as two bf16 terms (16 bits), which costs nothing beside the loads.
+// bf16: v_mfma_f32_32x32x16_bf16.  A probability enters as two bf16 terms (16 bits) where rows are bf16, which hides behind their loads; as one
+// over 8-bit rows, which come twice as fast: its rounding is then as large as the output's, a sixteenth of a value's in the pool.
 // fp32: v_mfma_f32_32x32x2_f32.
 #include <algorithm>
 
@@ -19,8 +20,9 @@ namespace {
 
 constexpr int kRows = 32, kKeys = 32, kWaves = 4;
 template <typename T, bool F8, int D, bool CAP>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D * sizeof(T) > 256 ? 1 : 2))) void attend_few(SlicedArgs f) {
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D * sizeof(T) > 256 ? 1 : F8 && D * sizeof(T) < 256 ? 3 : 2))) void attend_few(SlicedArgs f) {
   constexpr bool kBf16 = sizeof(T) == 2;
+  constexpr int kTerms = !kBf16 ? 0 : F8 ? 1 : 2;               // bf16 terms of a probability
   constexpr int kRowBytes = D * (int)sizeof(T);                 // of a staged row
   constexpr int kHeldBytes = F8 ? D : kRowBytes;                // of a row in the pool
   constexpr int kPieces = kHeldBytes / 16;                      // lanes that fetch a row
@@ -57,31 +59,66 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   }
 
   // Lane r stands for key r of a tile: its position (INT32_MAX: not seen), its row's place in the pool, its scales.  Entries of the index list
-  // are requested three tiles ahead, of the page table two, rows one.
+  // are requested three tiles ahead, of the page table two, rows one.  A tile that lies in one page is found once for the whole wave.
   struct Meta {
-    int pos, entry;
-  };
-  auto key_at = [&](int t) { return t * kKeys + r; };
-  auto request_entry = [&](int t) { return keys.n_sel && t < end ? entry_of(a, keys, at.b, key_at(t)) : 0; };
-  auto request_page = [&](int t, int entry) {
-    const int j = key_at(t);
-    Meta m;
-    m.pos = j < n_vis ? position(keys, j, entry) : -1;
-    m.entry = page_entry(a.batch, at.b, m.pos);
-    return m;
+    int pos0, pos, entry;                                       // pos0: of the tile's first key where it lies in one page, else -1
   };
   const int slot_mask = (1 << a.batch.page_log2) - 1;
+  const uint32_t tok_bytes = (uint32_t)a.cache.tok_bytes;
+  auto request_entry = [&](int t) { return keys.n_sel && t < end ? entry_of(a, keys, at.b, t * kKeys + r) : 0; };
+  auto request_page = [&](int t, int entry) __attribute__((always_inline)) {
+    const int j0 = t * kKeys, late = j0 - keys.i_end - keys.n_sel;
+    Meta m;
+    m.pos0 = j0 + kKeys <= keys.i_end ? j0 : late >= 0 ? late + keys.l_start : -1;
+    if (j0 + kKeys > n_vis || (m.pos0 & (kKeys - 1)) != 0 || slot_mask + 1 < kKeys) m.pos0 = -1;
+    m.pos = -1;
+    if (m.pos0 >= 0) {
+      m.entry = page_entry(a.batch, at.b, m.pos0);
+    } else {
+      if (j0 + r < n_vis) m.pos = position(keys, j0 + r, entry);
+      m.entry = page_entry(a.batch, at.b, m.pos);
+    }
+    return m;
+  };
   u32x4 kr[kLoads], vr[kLoads];
   int kb = 127, vb = 127, now_pos = INT32_MAX;                  // of the lane's key: exponents of its scales, position
-  auto load = [&](const Meta& m) {
-    const bool there = is_page(a.batch, a.cache.n_pages, m.pos, m.entry);
-    const int page = there ? m.entry : 0;
-    now_pos = there ? m.pos : INT32_MAX;
-    const int64_t place = page * a.cache.page_bytes + g * a.cache.head_bytes + (there ? m.pos & slot_mask : 0) * a.cache.tok_bytes;
-    if constexpr (F8) {
-      kb = a.cache.k_scale[(int64_t)page * a.cache.h_kv + g];
-      vb = a.cache.v_scale[(int64_t)page * a.cache.h_kv + g];
+  int64_t place = 0;                                            // its row; where the tile lies in one page, that of the tile's first
+  bool whole = false;
+  auto find_rows = [&](const Meta& m) __attribute__((always_inline)) {
+    whole = m.pos0 >= 0;
+    const int64_t head = g * a.cache.head_bytes;
+    int64_t block = g;
+    if (whole) {
+      const int entry = uniform(m.entry);
+      const bool there = is_page(a.batch, a.cache.n_pages, m.pos0, entry);
+      const int page = there ? entry : 0;
+      now_pos = there ? m.pos0 + r : INT32_MAX;
+      place = page * a.cache.page_bytes + head + (int64_t)((m.pos0 & slot_mask) * (uint64_t)tok_bytes);
+      block += (int64_t)page * a.cache.h_kv;
+      if constexpr (F8) {
+        kb = a.cache.k_scale[block];
+        vb = a.cache.v_scale[block];
+      }
+    } else {
+      const bool there = is_page(a.batch, a.cache.n_pages, m.pos, m.entry);
+      const int page = there ? m.entry : 0;
+      now_pos = there ? m.pos : INT32_MAX;
+      place = page * a.cache.page_bytes + head + (int64_t)((there ? m.pos & slot_mask : 0) * (uint64_t)tok_bytes);
+      block += (int64_t)page * a.cache.h_kv;
+      if constexpr (F8) {
+        kb = a.cache.k_scale[block];
+        vb = a.cache.v_scale[block];
+      }
     }
+  };
+  // Rows of a tile in one page: keys as soon as those before have left their registers, then values.  Rows that lie anywhere: together.
+  auto load_whole = [&](u32x4 (&x)[kLoads], const char* cache) __attribute__((always_inline)) {
+    const char* const from = cache + uniform(place);
+    const uint32_t mine = (uint32_t)(lane / kPieces) * tok_bytes + lane % kPieces * 16;
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) x[i] = *(const u32x4*)(from + (uint32_t)(i * kLoadRows) * tok_bytes + mine);
+  };
+  auto load_apart = [&]() __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
       const int64_t from = __shfl(place, i * kLoadRows + lane / kPieces) + lane % kPieces * 16;
@@ -124,87 +161,143 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   for (int md = 0; md < kMD; ++md)
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[md][v] = 0.f;
-  float m_run = -INFINITY, l_run = 0.f;
+  float m_run = kNoReference, l_run = 0.f;
 
   int t = first + wave;
-  Meta next{-1, 0};
+  Meta next{-1, -1, 0};
   int entry = 0;
   if (t < end) {
     const int mine = request_entry(t), after = request_entry(t + kWaves);
     entry = request_entry(t + 2 * kWaves);
     const Meta m = request_page(t, mine);
     next = request_page(t + kWaves, after);
-    load(m);
+    find_rows(m);
+    if (whole) {
+      load_whole(kr, a.cache.k);
+      load_whole(vr, a.cache.v);
+    } else {
+      load_apart();
+    }
   }
   for (; t < end; t += kWaves) {
     const int pos = now_pos;
+    const bool one_page = whole, more = t + kWaves < end;
     const uint64_t unseen = __ballot(pos == INT32_MAX);
-    // a page that nobody has may hold an infinite scale; whatever its rows hold: 0 times a NaN is one
-    const float ks = scale_of(pos != INT32_MAX ? kb : 127), vs = scale_of(pos != INT32_MAX ? vb : 127);
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int key = i * kLoadRows + lane / kPieces;
-      u32x4 k = kr[i], v = vr[i];
-      if (unseen && ((unseen >> key) & 1)) k = v = u32x4{0, 0, 0, 0};
-      put(k_st, k, F8 ? __shfl(ks, key) : 1.f, key, k_swizzle(key));
-      put(v_st, v, F8 ? __shfl(vs, key) : 1.f, key, v_swizzle(key));
+    float ks = 1.f, vs = 1.f;
+    if constexpr (F8) {
+      // a page that nobody has may hold an infinite scale; whatever its rows hold: 0 times a NaN is one (scores of such keys are masked)
+      ks = scale_of(pos != INT32_MAX ? kb : 127);
+      vs = scale_of(pos != INT32_MAX ? vb : 127);
     }
-    if (t + kWaves < end) load(next);
-    if (t + 2 * kWaves < end) next = request_page(t + 2 * kWaves, entry);
+    if (unseen) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+        if ((unseen >> (i * kLoadRows + lane / kPieces)) & 1) vr[i] = u32x4{0, 0, 0, 0};
+    }
+    auto put_rows = [&](unsigned char* st, const u32x4 (&x)[kLoads], float scale, auto swizzle) __attribute__((always_inline)) {
+      float of_row[kLoads];
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) of_row[i] = scale;
+      if (F8 && !one_page) {
+#pragma unroll
+        for (int i = 0; i < kLoads; ++i) of_row[i] = __shfl(scale, i * kLoadRows + lane / kPieces);
+      }
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i) {
+        const int key = i * kLoadRows + lane / kPieces;
+        put(st, x[i], of_row[i], key, swizzle(key));
+      }
+    };
+    put_rows(k_st, kr, ks, k_swizzle);
+    if (more) {
+      find_rows(next);
+      if (whole) load_whole(kr, a.cache.k);
+    }
+    if (t + 2 * kWaves < end) next = request_page(t + 2 * kWaves, entry);      // in front of the values: the next tile's keys do not wait for them
     entry = request_entry(t + 3 * kWaves);
+    put_rows(v_st, vr, vs, v_swizzle);
+    if (more) {
+      if (whole)
+        load_whole(vr, a.cache.v);
+      else
+        load_apart();
+    }
     wave_fence();
 
-    f32x16 x, x_odd;
+    f32x16 x;
 #pragma unroll
-    for (int v = 0; v < 16; ++v) x[v] = x_odd[v] = 0.f;
+    for (int v = 0; v < 16; ++v) x[v] = 0.f;
 #pragma unroll
     for (int i = 0; i < kKS; ++i) {
       const u32x4 kf = *(const u32x4*)(k_st + r * kRowBytes + (((2 * i + hi) ^ k_swizzle(r)) << 4));
       if constexpr (kBf16) {
-        f32x16& chain = i & 1 ? x_odd : x;
-        chain = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[i]), chain, 0, 0, 0);
+        x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf), __builtin_bit_cast(bf16x8, qf[i]), x, 0, 0, 0);
       } else {
         const f32x4 k4 = __builtin_bit_cast(f32x4, kf), q4 = __builtin_bit_cast(f32x4, qf[i]);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x = __builtin_amdgcn_mfma_f32_32x32x2f32(k4[e], q4[e], x, 0, 0, 0);
       }
     }
-    if constexpr (kBf16) x += x_odd;
-#pragma unroll
-    for (int v = 0; v < 16; ++v) x[v] = score_of<T, CAP>(x[v], f.scale, f.cap);
-    if (__ballot(pos > own_first)) {                            // some key is not for all rows
+    const bool masked = __ballot(pos > own_first);
+    if (masked) {                                               // some key is not for all rows
 #pragma unroll
       for (int v = 0; v < 16; ++v)
         if (__shfl(pos, 8 * (v / 4) + 4 * hi + v % 4) > own) x[v] = -INFINITY;
     }
-    float top = x[0];
+    f32x16 e;
+    auto to_reference = [&](float to) __attribute__((always_inline)) {       // what the sums so far are relative to
+      const float less = exp_of<T>(m_run - to);
+      m_run = to;
+      l_run *= less;
+      if (__ballot(less != 1.f)) {
 #pragma unroll
-    for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
-    top = fmaxf(m_run, halves_max(top));
-    const float ref = top == -INFINITY ? 0.f : top, less = exp_of<T>(m_run - ref);
-    m_run = top;
-    float sum = 0.f;
+        for (int md = 0; md < kMD; ++md)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) {
-      x[v] = exp_of<T>(x[v] - ref);
-      sum += x[v];
-    }
-    l_run = l_run * less + sum;
-    if (__ballot(less != 1.f)) {
+          for (int v = 0; v < 16; ++v) o[md][v] *= less;
+      }
+    };
+    auto largest = [&]() __attribute__((always_inline)) {
+      float top = x[0];
 #pragma unroll
-      for (int md = 0; md < kMD; ++md)
+      for (int v = 1; v < 16; ++v) top = fmaxf(top, x[v]);
+      top = halves_max(top);
+      return top == -INFINITY ? kNoReference : score_of<T, CAP>(top, f.scale, f.cap);
+    };
+    auto exponentials = [&]() __attribute__((always_inline)) {
+      float sum = 0.f;
 #pragma unroll
-        for (int v = 0; v < 16; ++v) o[md][v] *= less;
+      for (int v = 0; v < 16; ++v) {
+        e[v] = exp_of<T>(score_of<T, CAP>(x[v], f.scale, f.cap) - m_run);
+        if (CAP && x[v] == -INFINITY) e[v] = 0.f;               // (a capped -inf is none)
+        sum += e[v];
+      }
+      return sum;
+    };
+    if constexpr (kTerms == 1) {
+      // Against the reference as it stands.  Where a row's exceed it by far (and at first) it moves to its largest logit, and they are taken again.
+      if (__ballot(exponentials() > 256.f)) {
+        to_reference(fmaxf(m_run, largest()));
+        exponentials();
+      }
+    } else {
+      // (two sets of sixteen registers for them are more than rows of 256 bytes and more on their way leave)
+      to_reference(fmaxf(m_run, largest()));
+      l_run += exponentials();
     }
     if constexpr (kBf16) {
       const int tr_key = 4 * hi + ((lane & 15) >> 2), tr_dim = ((lane >> 4) & 1) * 16 + 4 * (lane & 3);
 #pragma unroll
       for (int kp = 0; kp < 2; ++kp) {
+        __builtin_amdgcn_sched_barrier(0);                      // (fragments of both at once cost registers that rows on their way need)
         bf16x8 p, rest;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          p[e] = (__bf16)x[8 * kp + e];
-          rest[e] = (__bf16)(x[8 * kp + e] - (float)p[e]);
+        for (int i = 0; i < 8; ++i) {
+          p[i] = (__bf16)e[8 * kp + i];
+          if constexpr (kTerms == 2) rest[i] = (__bf16)(e[8 * kp + i] - (float)p[i]);
+        }
+        if constexpr (kTerms == 1) {                            // the sum of what the product sees
+#pragma unroll
+          for (int i = 0; i < 8; i += 2) l_run = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p[i], p[i + 1]}, bf16x2{(__bf16)1.f, (__bf16)1.f}, l_run, false);
         }
 #pragma unroll
         for (int md = 0; md < kMD; ++md) {
@@ -216,7 +309,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
           const i16x4 lo = part(16 * kp + tr_key), up = part(16 * kp + 8 + tr_key);
           const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
           o[md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p, o[md], 0, 0, 0);
-          o[md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, rest, o[md], 0, 0, 0);
+          if constexpr (kTerms == 2) o[md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, rest, o[md], 0, 0, 0);
         }
       }
     } else {
@@ -227,7 +320,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
         for (int md = 0; md < kMD; ++md) {
           const int dim = md * 32 + r;
           const float vf = *(const float*)(v_st + key * kRowBytes + (((dim / 4) ^ v_swizzle(key)) << 4) + (dim & 3) * 4);
-          o[md] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, x[v], o[md], 0, 0, 0);
+          o[md] = __builtin_amdgcn_mfma_f32_32x32x2f32(vf, e[v], o[md], 0, 0, 0);
         }
       }
     }

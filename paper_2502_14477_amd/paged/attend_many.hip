@@ -21,7 +21,6 @@ namespace paged {
 namespace {
 
 constexpr int kRows = 256, kKeys = 64, kWaves = 8;
-constexpr float kNoReference = -1e30f;      // so low that the first logit exceeds it
 
 template <bool F8, int D, bool CAP>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void attend_many(SlicedArgs f) {

@@ -21,6 +21,8 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 template <typename T> __device__ __forceinline__ float exp_of(float x) { return sizeof(T) == 2 ? __builtin_amdgcn_exp2f(x) : expf(x); }
 template <typename T> __device__ __forceinline__ float lse_of(float m, float l) { return sizeof(T) == 2 ? __builtin_fmaf(m, kLn2, logf(l)) : m + logf(l); }
 
+constexpr float kNoReference = -1e30f;      // of a softmax that has seen nothing: so low that the first logit exceeds it
+
 __device__ __forceinline__ float halves_max(float v) {
   const auto sw = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(sw[0]), __uint_as_float(sw[1]));
