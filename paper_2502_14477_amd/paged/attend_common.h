@@ -1,8 +1,8 @@
-// What the matrix-core attention kernels of the paged cache share: arithmetic, arguments, and the kernel that joins slices.
+// What the matrix-core attention kernels of the paged cache share: arithmetic and arguments.
 #pragma once
 #include <type_traits>
 
-#include "plan.h"
+#include "paged.h"
 
 namespace esa {
 namespace paged {
@@ -36,11 +36,12 @@ __device__ __forceinline__ void wave_fence() {      // LDS operations of a wave 
   __builtin_amdgcn_wave_barrier();
 }
 
-struct SlicedArgs {
+// Arguments of a kernel whose blocks' keys are shared among workgroups as SHAPE says.
+template <typename SHAPE> struct SplitArgs {
   AttendArgs a;
-  Shape shape;
-  float* part_o;          // [slot][h_kv][shape.rows * D] (in a kernel's own order), relative to the slice's reference
-  float* part_ml;         // [slot][h_kv][shape.rows][2]: the reference, the sum of exponentials
+  SHAPE shape;
+  float* part_o;          // [slot][shape.rows * D] (in a kernel's own order), relative to the part's reference
+  float* part_ml;         // [slot][shape.rows][2]: the reference, the sum of exponentials
   float scale;            // bf16: includes log2(e); with a cap: 1 / cap, and bf16: 2 log2(e)
   float cap;              // bf16: includes log2(e)
 };
@@ -54,23 +55,19 @@ template <typename T, bool CAP> __device__ __forceinline__ float score_of(float 
   return __builtin_fmaf(-2.f * cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x)), cap);
 }
 
-// Arguments, workspace.
-template <typename T> static void set_sliced(SlicedArgs& f, const AttendArgs& a, const Shape& shape, void* ws) {
+// slots: partial results that the workspace has room for.
+template <typename T, typename SHAPE> static SplitArgs<SHAPE> split_args(const AttendArgs& a, const SHAPE& shape, int64_t slots, void* ws) {
+  const float base = sizeof(T) == 2 ? kLog2e : 1.f;
+  SplitArgs<SHAPE> f;
   f.a = a;
   f.shape = shape;
   f.part_o = (float*)ws;
-  f.part_ml = f.part_o + most_parts(shape, a.cache.h_kv) * a.cache.h_kv * shape.rows * a.cache.d;
-  const float base = sizeof(T) == 2 ? kLog2e : 1.f;
+  f.part_ml = f.part_o + slots * shape.rows * a.cache.d;
   f.scale = a.cap > 0.f ? a.scale / a.cap * (sizeof(T) == 2 ? 2.f * kLog2e : 1.f) : a.scale * base;
   f.cap = a.cap * base;
+  return f;
 }
-static inline size_t sliced_workspace(const Shape& shape, int h_kv, int d) {
-  return (size_t)(most_parts(shape, h_kv) * h_kv * shape.rows) * (d + 2) * sizeof(float);
-}
-// Whether a sequence of the longest that the table has room for may have several slices.
-static inline bool may_split(const SlicedArgs& f) {
-  return ((int64_t)f.a.batch.max_pages << f.a.batch.page_log2) + f.a.n_sel > (int64_t)f.shape.least * f.shape.keys;
-}
+static inline size_t split_workspace(int64_t slots, int rows, int d) { return (size_t)slots * rows * (d + 2) * sizeof(float); }
 
 }  // namespace paged
 }  // namespace esa

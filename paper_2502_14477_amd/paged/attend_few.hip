@@ -12,15 +12,17 @@
 // fp32: v_mfma_f32_32x32x2_f32.
 #include <algorithm>
 
-#include "attend_sliced.h"
+#include "attend_common.h"
+#include "slices.h"
 
 namespace esa {
 namespace paged {
 namespace {
 
 constexpr int kRows = 32, kKeys = 32, kWaves = 4;
+using FewArgs = SplitArgs<SliceShape>;
 template <typename T, bool F8, int D, bool CAP>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D * sizeof(T) > 256 ? 1 : F8 && D * sizeof(T) < 256 ? 3 : 2))) void attend_few(SlicedArgs f) {
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D * sizeof(T) > 256 ? 1 : F8 && D * sizeof(T) < 256 ? 3 : 2))) void attend_few(FewArgs f) {
   constexpr bool kBf16 = sizeof(T) == 2;
   constexpr int kTerms = !kBf16 ? 0 : F8 ? 1 : 2;               // bf16 terms of a probability
   constexpr int kRowBytes = D * (int)sizeof(T);                 // of a staged row
@@ -381,7 +383,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
 
 // Slices of a row joined: a workgroup takes a row, its four waves share the slices.  Only rows of sequences of several slices are gone
 // through, by as many workgroups as the chip holds at most.
-template <typename T, int D> __global__ __launch_bounds__(256) void join_few(SlicedArgs f) {
+template <typename T, int D> __global__ __launch_bounds__(256) void join_few(FewArgs f) {
   constexpr int kMine = D / 64;
   typedef __attribute__((ext_vector_type(kMine))) float vec;
   __shared__ vec sums[4][64];
@@ -447,9 +449,9 @@ template <typename T, int D> __global__ __launch_bounds__(256) void join_few(Sli
 }
 
 // Workgroups that the chip holds: a compute unit has 160 KB of LDS, a workgroup's staging space is 64 KB for rows of up to 256 bytes.
-Shape shape_of(int d, int es, int most_rows) { return Shape{kRows, kKeys, d * es > 256 ? 256 : d * es == 256 ? 512 : 1024, kWaves, 0, 1, 0, most_rows}; }
+SliceShape shape_of(int d, int es, int most_rows) { return SliceShape{kRows, kKeys, d * es > 256 ? 256 : d * es == 256 ? 512 : 1024, kWaves, most_rows}; }
 
-template <typename T, bool F8, int D> int launch(const SlicedArgs& f, dim3 grid, hipStream_t st) {
+template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, hipStream_t st) {
   if (f.a.cap > 0.f)
     attend_few<T, F8, D, true><<<grid, 64 * kWaves, 0, st>>>(f);
   else
@@ -459,8 +461,8 @@ template <typename T, bool F8, int D> int launch(const SlicedArgs& f, dim3 grid,
 }
 template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows, void* ws, hipStream_t st) {
   const int d = a.cache.d;
-  SlicedArgs f;
-  set_sliced<T>(f, a, shape_of(d, sizeof(T), most_rows), ws);
+  const SliceShape shape = shape_of(d, sizeof(T), most_rows);
+  const FewArgs f = split_args<T>(a, shape, most_parts(shape, a.cache.h_kv) * a.cache.h_kv, ws);
   const int64_t units = most_units(f.shape, a.batch.n_tok, a.batch.n_seq, a.group, a.cache.h_kv) * a.cache.h_kv;
   if (units > INT32_MAX) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: %lld workgroups", (long long)units);
   const dim3 grid((unsigned)units);
@@ -469,7 +471,8 @@ template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows
     rc = f8 ? launch<T, true, 64>(f, grid, st) : launch<T, false, 64>(f, grid, st);
   else
     rc = f8 ? launch<T, true, 128>(f, grid, st) : launch<T, false, 128>(f, grid, st);
-  if (rc != ESA_OK || !may_split(f)) return rc;
+  // (the longest sequence that the table has room for may be one slice)
+  if (rc != ESA_OK || ((int64_t)a.batch.max_pages << a.batch.page_log2) + a.n_sel <= (int64_t)shape.least * kKeys) return rc;
   const int64_t by_blocks = most_blocks(f.shape, a.batch.n_tok, a.batch.n_seq, a.group) * kRows * a.cache.h_kv, by_tokens = a.batch.n_tok * a.h;
   const dim3 join((unsigned)std::min<int64_t>(std::min(by_blocks, by_tokens), 2048));
   if (d == 64)
@@ -482,7 +485,9 @@ template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows
 
 }  // namespace
 
-size_t few_workspace(int h_kv, int d, int dtype) { return sliced_workspace(shape_of(d, dtype == ESA_F32 ? 4 : 2, INT32_MAX), h_kv, d); }
+size_t few_workspace(int h_kv, int d, int dtype) {
+  return split_workspace(most_parts(shape_of(d, dtype == ESA_F32 ? 4 : 2, INT32_MAX), h_kv) * h_kv, kRows, d);
+}
 
 int launch_few(const AttendArgs& a, bool f8, int dtype, int most_rows, void* ws, hipStream_t st) {
   return dtype == ESA_F32 ? launch_all<float>(a, f8, most_rows, ws, st) : launch_all<bf16_t>(a, f8, most_rows, ws, st);

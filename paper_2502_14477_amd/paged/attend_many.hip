@@ -14,16 +14,18 @@
 //   In iteration j keys of tiles j and j + 1 and values of j - 1 and j are read and tile j + 2 is written: four buffers, one barrier.
 #include <algorithm>
 
-#include "attend_sliced.h"
+#include "attend_common.h"
+#include "shares.h"
 
 namespace esa {
 namespace paged {
 namespace {
 
 constexpr int kRows = 256, kKeys = 64, kWaves = 8;
+using ManyArgs = SplitArgs<ShareShape>;
 
 template <bool F8, int D, bool CAP>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void attend_many(SlicedArgs f) {
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void attend_many(ManyArgs f) {
   constexpr int kRowBytes = D * 2;                              // of a staged row
   constexpr int kHeldBytes = F8 ? D : kRowBytes;
   constexpr int kPieces = kHeldBytes / 16;                      // threads that fetch a row
@@ -40,18 +42,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   const AttendArgs& a = f.a;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = blockIdx.x % a.cache.h_kv;
-  const Plan plan = plan_of(a, f.shape);
-  const int slice = plan.slice;
-  const Part at = uniform(part_of(a, f.shape, plan, blockIdx.x / a.cache.h_kv));
-  if (at.b < 0) return;
-  const Seq s = uniform(sequence(a.batch, at.b));
-  const Keys keys = keys_of(a, s);
-  const int n_rows = s.n * a.group, row0 = at.block * kRows, rows = min(n_rows - row0, kRows);
-  const int n_vis = uniform(keys_until(a, s, keys, row0 + rows - 1)), tiles = (n_vis + kKeys - 1) / kKeys;
-  const int first = at.slice * slice, end = min(first + slice, tiles);
-  if (at.slice > 0 && first >= end) return;
-  const bool alone = tiles <= slice;
+  const int g = uniform((int)blockIdx.x % a.cache.h_kv);
+  for_parts(a, f.shape, [&](const Part& at) __attribute__((always_inline)) {
+  const Seq& s = at.s;
+  const Keys& keys = at.keys;
+  const int row0 = at.row0, rows = at.rows, n_vis = at.n_vis, first = at.from, end = at.end;
 
   // a lane's row; rows behind the last repeat it
   const int row = row0 + min(wave * 32 + r, rows - 1), c = row / a.group, head = g * a.group + row - c * a.group, own = s.t0 + c;
@@ -344,11 +339,18 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   }
 
   l_run = halves_sum(l_run);
-  if (alone) {
-    if (wave * 32 + r >= rows) return;
-    const int hd = head;
+  if (!at.alone) {
+    // as the lanes have it: 16 bytes a lane, 1 KB an instruction
+    const int64_t part = (int64_t)at.slot * kWaves + wave;
+#pragma unroll
+    for (int md = 0; md < kMD; ++md)
+#pragma unroll
+      for (int v = 0; v < 16; v += 4)
+        *((f32x4*)f.part_o + (part * (D / 8) + md * 4 + v / 4) * 64 + lane) = f32x4{o[md][v], o[md][v + 1], o[md][v + 2], o[md][v + 3]};
+    if (hi == 0) *(float2*)(f.part_ml + (part * 32 + r) * 2) = make_float2(m_run, l_run);
+  } else if (wave * 32 + r < rows) {
     const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
-    char* to = a.out + (int64_t)(s.row0 + c) * a.ldo + (int64_t)hd * kRowBytes;
+    char* to = a.out + (int64_t)(s.row0 + c) * a.ldo + (int64_t)head * kRowBytes;
 #pragma unroll
     for (int md = 0; md < kMD; ++md)
 #pragma unroll
@@ -357,70 +359,62 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         const bf16x2 up = __builtin_convertvector((f32x2{o[md][v + 2] * inv, o[md][v + 3] * inv}), bf16x2);
         *(uint2*)(to + (md * 32 + v * 2 + 4 * hi) * 2) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, up));
       }
-    if (a.lse && hi == 0) a.lse[(int64_t)(s.row0 + c) * a.h + hd] = l_run > 0.f ? lse_of<bf16_t>(m_run, l_run) : -INFINITY;
-  } else {
-    // as the lanes have it: 16 bytes a lane, 1 KB an instruction
-    const int64_t part = ((at.slot + (int64_t)at.slice * at.blocks) * a.cache.h_kv + g) * kWaves + wave;
-#pragma unroll
-    for (int md = 0; md < kMD; ++md)
-#pragma unroll
-      for (int v = 0; v < 16; v += 4)
-        *((f32x4*)f.part_o + (part * (D / 8) + md * 4 + v / 4) * 64 + lane) = f32x4{o[md][v], o[md][v + 1], o[md][v + 2], o[md][v + 3]};
-    if (hi == 0) *(float2*)(f.part_ml + (part * 32 + r) * 2) = make_float2(m_run, l_run);
+    if (a.lse && hi == 0) a.lse[(int64_t)(s.row0 + c) * a.h + head] = l_run > 0.f ? lse_of<bf16_t>(m_run, l_run) : -INFINITY;
   }
+  __syncthreads();                                              // (the next part's tiles go where this one's are)
+  });
 }
 
-// Slices joined: a wave takes a quarter of a wave's 32 rows of a block, as attend_many's lanes have left them, a lane the same row and dimensions.
-template <int D> __global__ __launch_bounds__(256) void join_many(SlicedArgs f) {
+// Cut blocks joined: a workgroup takes 32 rows of a block as a wave has left them, its waves a quarter of the dimensions each.
+template <int D> __global__ __launch_bounds__(256) void join_many(ManyArgs f) {
   constexpr int kChunks = D / 8, kMine = kChunks / 4;           // 16 bytes a lane: of 32 rows, and of them a wave's
+  constexpr int kGroups = kRows / 32;
   const AttendArgs& a = f.a;
   const int lane = threadIdx.x & 63, r = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Plan plan = plan_of(a, f.shape);
-  for (int64_t u = blockIdx.x;; u += gridDim.x) {
-    const int g = (int)(u % a.cache.h_kv);
-    const Split at = uniform(split_of(a, f.shape, plan, u / a.cache.h_kv, [](int rows) { return (rows + 31) / 32; }));
-    if (at.b < 0) return;
-    const Seq s = uniform(sequence(a.batch, at.b));
-    const Keys keys = keys_of(a, s);
-    const int n_rows = s.n * a.group, block = at.i / (kRows / 32), part = at.i % (kRows / 32), blocks = (n_rows + kRows - 1) / kRows;
-    const int n_vis = keys_until(a, s, keys, min(block * kRows + kRows, n_rows) - 1), tiles = (n_vis + kKeys - 1) / kKeys;
-    const int n = (tiles + plan.slice - 1) / plan.slice;
-    if (n <= 1) continue;
-    auto place = [&](int i) { return (at.slot + block + (int64_t)i * blocks) * a.cache.h_kv + g; };
-    float m = kNoReference, l = 0.f;
-    for (int i = 0; i < n; ++i) m = fmaxf(m, f.part_ml[(place(i) * kRows + part * 32 + r) * 2]);
-    f32x4 sum[kMine];
+  const int group = blockIdx.x % kGroups, unit = blockIdx.x / kGroups, g = unit % a.cache.h_kv, w = unit / a.cache.h_kv + 1;
+  const Shares shares(a, f.shape);
+  const Cut c = cut_block(shares, w);
+  if (c.k.b < 0 || group * 32 >= c.block.rows) return;
+  float m = kNoReference, l = 0.f;
+  f32x4 sum[kMine];
 #pragma unroll
-    for (int k = 0; k < kMine; ++k) sum[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int i = 0; i < n; ++i) {
-      const float2 x = *(const float2*)(f.part_ml + (place(i) * kRows + part * 32 + r) * 2);
-      const float by = __builtin_amdgcn_exp2f(x.x - m);
-      l = __builtin_fmaf(x.y, by, l);
-      const f32x4* from = (const f32x4*)f.part_o + (place(i) * (kRows / 32) + part) * kChunks * 64 + wave * kMine * 64 + lane;
+  for (int k = 0; k < kMine; ++k) sum[k] = f32x4{0.f, 0.f, 0.f, 0.f};
+  bool any = false;
+  for (int i0 = 0; i0 < c.n; i0 += 64) {
+    const int slot = slot_of(shares, c, w, i0 + lane, g);
+    uint64_t there = __ballot(slot >= 0);
+    any |= there != 0;
+    for (; there; there &= there - 1) {
+      const int64_t part = (int64_t)__builtin_amdgcn_readlane(slot, __ffsll((unsigned long long)there) - 1) * kGroups + group;
+      const float2 x = *(const float2*)(f.part_ml + (part * 32 + r) * 2);
+      f32x4 y[kMine];
 #pragma unroll
-      for (int k = 0; k < kMine; ++k) {
-        const f32x4 y = from[k * 64];
+      for (int k = 0; k < kMine; ++k) y[k] = ((const f32x4*)f.part_o)[(part * kChunks + wave * kMine + k) * 64 + lane];
+      const float top = fmaxf(m, x.x), less = __builtin_amdgcn_exp2f(m - top), by = __builtin_amdgcn_exp2f(x.x - top);
+      m = top;
+      l = l * less + x.y * by;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) sum[k][e] = __builtin_fmaf(y[e], by, sum[k][e]);
-      }
+      for (int k = 0; k < kMine; ++k)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[k][e] = __builtin_fmaf(y[k][e], by, sum[k][e] * less);
     }
-    const int row = at.i * 32 + r;
-    if (row >= n_rows) continue;
-    const int tok = s.row0 + row / a.group, head = g * a.group + row % a.group;
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    char* to = a.out + (int64_t)tok * a.ldo + (int64_t)head * D * 2;
-#pragma unroll
-    for (int k = 0; k < kMine; ++k) {
-      const bf16x2 lo = __builtin_convertvector((f32x2{sum[k][0] * inv, sum[k][1] * inv}), bf16x2), up = __builtin_convertvector((f32x2{sum[k][2] * inv, sum[k][3] * inv}), bf16x2);
-      *(uint2*)(to + ((wave * kMine + k) * 8 + 4 * hi) * 2) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, up));
-    }
-    if (a.lse && wave == 0 && hi == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? lse_of<bf16_t>(m, l) : -INFINITY;
   }
+  const int in = group * 32 + r, row = c.block.row0 + in;
+  if (!any || in >= c.block.rows) return;                       // (a block of which one part had all tiles)
+  const int tok = c.block.s.row0 + row / a.group, head = g * a.group + row % a.group;
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  char* to = a.out + (int64_t)tok * a.ldo + (int64_t)head * D * 2;
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const bf16x2 lo = __builtin_convertvector((f32x2{sum[k][0] * inv, sum[k][1] * inv}), bf16x2), up = __builtin_convertvector((f32x2{sum[k][2] * inv, sum[k][3] * inv}), bf16x2);
+    *(uint2*)(to + ((wave * kMine + k) * 8 + 4 * hi) * 2) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, up));
+  }
+  if (a.lse && wave == 0 && hi == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? lse_of<bf16_t>(m, l) : -INFINITY;
 }
 
-Shape shape_of(int above) { return Shape{kRows, kKeys, 256, 1, 4, 4, above, INT32_MAX}; }
+ShareShape shape_of(int above) { return ShareShape{kRows, kKeys, 256, 2 * kKeys, 8 * kKeys, 6 * kKeys, above}; }
 
-template <bool F8, int D> int launch(const SlicedArgs& f, dim3 grid, hipStream_t st) {
+template <bool F8, int D> int launch(const ManyArgs& f, dim3 grid, hipStream_t st) {
   if (f.a.cap > 0.f)
     attend_many<F8, D, true><<<grid, 64 * kWaves, 0, st>>>(f);
   else
@@ -431,22 +425,20 @@ template <bool F8, int D> int launch(const SlicedArgs& f, dim3 grid, hipStream_t
 
 }  // namespace
 
-size_t many_workspace(int h_kv, int d) { return sliced_workspace(shape_of(0), h_kv, d); }
+size_t many_workspace(int h_kv, int d) { return split_workspace(2 * (int64_t)grid_of(shape_of(0), h_kv), kRows, d); }
 
 int launch_many(const AttendArgs& a, bool f8, int above, void* ws, hipStream_t st) {
-  SlicedArgs f;
-  set_sliced<bf16_t>(f, a, shape_of(above), ws);
-  const int64_t units = most_units(f.shape, a.batch.n_tok, a.batch.n_seq, a.group, a.cache.h_kv) * a.cache.h_kv;
-  if (units > INT32_MAX) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: %lld workgroups", (long long)units);
-  const dim3 grid((unsigned)units);
+  const ShareShape shape = shape_of(above);
+  const ManyArgs f = split_args<bf16_t>(a, shape, 2 * (int64_t)grid_of(shape, a.cache.h_kv), ws);
+  const dim3 grid((unsigned)grid_of(f.shape, a.cache.h_kv));
   int rc;
   if (a.cache.d == 64)
     rc = f8 ? launch<true, 64>(f, grid, st) : launch<false, 64>(f, grid, st);
   else
     rc = f8 ? launch<true, 128>(f, grid, st) : launch<false, 128>(f, grid, st);
-  if (rc != ESA_OK || !may_split(f)) return rc;
-  const int64_t items = most_blocks(f.shape, a.batch.n_tok, a.batch.n_seq, a.group) * (kRows / 32) * a.cache.h_kv;
-  const dim3 join((unsigned)std::min<int64_t>(items, 2048));
+  // (the longest sequence that the table has room for may be too short to be cut; a block weighs up to a block's tokens more than it sees)
+  if (rc != ESA_OK || ((int64_t)a.batch.max_pages << a.batch.page_log2) + a.n_sel + kRows <= shape.whole) return rc;
+  const dim3 join(grid.x * (kRows / 32));
   if (a.cache.d == 64)
     join_many<64><<<join, 256, 0, st>>>(f);
   else

@@ -154,6 +154,18 @@ __device__ __forceinline__ bool is_page(const Batch& a, int n_pages, int pos, in
   return pos >= 0 && pos >> a.page_log2 < a.max_pages && (uint32_t)entry < (uint32_t)n_pages;
 }
 
+// Keys that the rows up to `row` of a sequence see at most.
+__device__ __forceinline__ int keys_until(const AttendArgs& a, const Seq& s, const Keys& k, int row) {
+  const int width = a.batch.max_pages << a.batch.page_log2;
+  return k.n - (min(s.t0 + s.n, width) - min(s.t0 + row / a.group + 1, width));
+}
+
+// A value that is the same in every lane, where the compiler does not see it.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ int64_t uniform(int64_t x) { return (int64_t)(uint32_t)uniform((int)x) | (int64_t)uniform((int)(x >> 32)) << 32; }
+__device__ __forceinline__ Seq uniform(const Seq& s) { return Seq{uniform(s.row0), uniform(s.n), uniform(s.t0)}; }
+__device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane(x, lane); }
+
 int launch_append(const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq, int h, void* out_q, int64_t ldoq,
                   const Batch& b, const Cache& c, bool f8, double base, int dtype, hipStream_t st);
 int launch_plain(const AttendArgs& a, bool f8, int dtype, hipStream_t st);                     // any head size

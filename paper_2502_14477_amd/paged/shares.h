@@ -1,0 +1,234 @@
+// Which part of the attention a workgroup of the kernel for many rows does.  The lengths lie on the device, so every workgroup finds its part from them: a scan over
+// the sequences, a lane to each.
+//
+// A sequence's rows (new tokens x query heads of a KV head, numbered token by token) are cut into blocks, its keys into tiles.  A block
+// weighs about as much as its last row sees keys.  All blocks of a KV head, one behind the other, are shared out evenly among as many
+// workgroups as the chip has places for (fewer where there is little to do), wherever that cuts a block: a workgroup goes through the end of
+// one block, some whole ones, and the beginning of another.  What it has of a cut block it leaves as a partial result, at most two of them; a
+// second kernel joins these.  Small blocks are not cut.
+// (Slices of one length for all, so long that the units were about one round: with sequences of 18 to 66 thousand keys the last round was
+// often a few units; chunks of prompts took 1.2 to 1.5 times what their tiles did.)
+#pragma once
+#include "paged.h"
+
+namespace esa {
+namespace paged {
+
+// Rows of a block, keys of a tile, workgroups at a time; a share is worth its beginning and end from `least` keys on, blocks of up to `whole`
+// keys are not cut, others not within `near` keys of their begin and end.  The kernel serves sequences of more than `above` rows.
+struct ShareShape {
+  int rows, keys, places, least, whole, near, above;
+};
+
+// A sequence's blocks: block r weighs first + r * step.
+struct Weights {
+  int blocks, first, step;
+  __device__ __forceinline__ int64_t upto(int r) const { return (int64_t)r * first + (int64_t)step * ((int64_t)r * (r - 1) / 2); }      // of r blocks
+  __device__ __forceinline__ int64_t all() const { return upto(blocks); }
+  __device__ __forceinline__ int64_t of(int r) const { return first + (int64_t)r * step; }
+  // The block in which weight x < all() falls.
+  __device__ __forceinline__ int block_at(int64_t x) const {
+    int lo = 0, hi = blocks - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (upto(mid) <= x)
+        lo = mid;
+      else
+        hi = mid - 1;
+    }
+    return lo;
+  }
+};
+__device__ __forceinline__ Weights weights_of(const AttendArgs& a, const ShareShape& sh, const Seq& s) {
+  const int rows = s.n * a.group;
+  if (rows <= sh.above) return Weights{0, 0, 0};
+  return Weights{(rows + sh.rows - 1) / sh.rows, max(keys_until(a, s, keys_of(a, s), min(sh.rows, rows) - 1), 1), max(sh.rows / a.group, 1)};
+}
+
+// Sums over the lanes up to each, of numbers below 2^52: two halves of 26 bits, of which 64 fit into 32.
+__device__ __forceinline__ int64_t wave_scan_long(int64_t x) {
+  return (int64_t)wave_scan((uint32_t)x & 0x3FFFFFFu) + ((int64_t)wave_scan((uint32_t)(x >> 26)) << 26);
+}
+__device__ __forceinline__ int64_t lane_long(int64_t x, int lane) { return (int64_t)lane_value((uint32_t)x, lane) | (int64_t)(int)lane_value((uint32_t)(x >> 32), lane) << 32; }
+
+// The call's blocks of a KV head, and their shares.
+class Shares {
+ public:
+  __device__ __forceinline__ Shares(const AttendArgs& args, const ShareShape& shape) : a(args), sh(shape) {
+    const int lane = threadIdx.x & 63;
+    if (a.batch.n_seq == 1) {
+      total = weights_of(a, sh, uniform(sequence(a.batch, 0))).all();
+    } else {
+      mine = lane < a.batch.n_seq ? weight(lane) : 0;
+      total = lane_long(wave_scan_long(mine), 63);
+      for (int b0 = 64; b0 < a.batch.n_seq; b0 += 64) total += lane_long(wave_scan_long(b0 + lane < a.batch.n_seq ? weight(b0 + lane) : 0), 63);
+    }
+    total = uniform(total);
+    const int64_t worth = (total + sh.least - 1) / sh.least;
+    workers = uniform((int)min(max(worth, (int64_t)1), (int64_t)max(sh.places / a.cache.h_kv, 1)));
+    if (total == 0) workers = 0;
+    share = (double)total / (double)max(workers, 1);
+  }
+
+  // Where share w begins, before small blocks are left whole.  (Doubles: the same ones wherever it is asked.)
+  __device__ __forceinline__ int64_t cut(int w) const { return w >= workers ? total : min((int64_t)(share * (double)w), total); }
+
+  // The block in which weight x < total falls.
+  struct Block {
+    int b, r;               // sequence, block
+    int64_t begin;          // weight in front of it
+    Weights w;
+  };
+  __device__ __forceinline__ Block block_at(int64_t x) const {
+    const int lane = threadIdx.x & 63;
+    int b = 0;
+    int64_t base = 0;
+    if (a.batch.n_seq > 1) {
+      for (int b0 = 0;; b0 += 64) {
+        const int64_t c = b0 == 0 ? mine : b0 + lane < a.batch.n_seq ? weight(b0 + lane) : 0, upto = wave_scan_long(c) + base;
+        const uint64_t past = __ballot(upto > x);
+        if (past) {
+          const int at = __ffsll((unsigned long long)past) - 1;
+          b = b0 + at;
+          base = lane_long(upto - c, at);
+          break;
+        }
+        base = lane_long(upto, 63);
+        if (b0 + 64 >= a.batch.n_seq) return Block{-1, 0, 0, Weights{0, 0, 0}};      // (not with x < total)
+      }
+    }
+    b = uniform(b);
+    Weights w = weights_of(a, sh, uniform(sequence(a.batch, b)));
+    w = Weights{uniform(w.blocks), uniform(w.first), uniform(w.step)};
+    const int r = uniform(w.block_at(x - base));
+    return Block{b, r, uniform(base + w.upto(r)), w};
+  }
+  // A cut in a small block, or near a block's begin or end, is made there instead: a further part of a block costs a workgroup as much as some
+  // tiles.
+  __device__ __forceinline__ int64_t moved(int64_t x, const Block& k) const {
+    const int64_t all = k.w.of(k.r);
+    if (all <= sh.whole || x - k.begin <= sh.near) return k.begin;
+    return k.begin + all - x <= sh.near ? k.begin + all : x;
+  }
+  // The tile of a block of `tiles` at which weight x of its `all` cuts it; each: tiles / all.
+  static __device__ __forceinline__ int tile_at(int64_t x, int64_t all, int tiles, double each) {
+    return x <= 0 ? 0 : x >= all ? tiles : min((int)((double)x * each), tiles);
+  }
+
+  const AttendArgs& a;
+  const ShareShape& sh;
+  int64_t total;
+  int workers;
+  double share;
+
+ private:
+  __device__ __forceinline__ int64_t weight(int b) const { return min(weights_of(a, sh, sequence(a.batch, b)).all(), ((int64_t)1 << 46) - 1); }
+  int64_t mine = 0;
+};
+
+// A part of a block's work: keys of tiles [from, end) for its rows.
+struct Part {
+  Seq s;
+  Keys keys;
+  int b, row0, rows, n_vis, from, end;
+  bool alone;               // all of the block's tiles
+  int slot;                 // else: where the partial result goes
+};
+__device__ __forceinline__ Part part_of(const AttendArgs& a, const ShareShape& sh, const Shares::Block& k, int64_t from, int64_t upto) {
+  Part p;
+  p.b = k.b;
+  p.s = uniform(sequence(a.batch, k.b));
+  const Keys q = keys_of(a, p.s);
+  p.keys = Keys{uniform(q.t0), uniform(q.i_end), uniform(q.n_sel), uniform(q.l_start), uniform(q.n)};
+  p.row0 = k.r * sh.rows;
+  p.rows = min(p.s.n * a.group - p.row0, sh.rows);
+  p.n_vis = uniform(keys_until(a, p.s, p.keys, p.row0 + p.rows - 1));
+  const int tiles = (p.n_vis + sh.keys - 1) / sh.keys;
+  const int64_t all = k.w.of(k.r);
+  const double each = (double)tiles / (double)all;
+  p.from = uniform(Shares::tile_at(from, all, tiles, each));
+  p.end = uniform(Shares::tile_at(upto, all, tiles, each));
+  p.alone = p.from == 0 && p.end == tiles;
+  return p;
+}
+// Every part of the workgroup's share: work(Part).  Parts of no tiles are another one's (or, of a block without keys, its whole).
+template <typename F> __device__ __forceinline__ void for_parts(const AttendArgs& a, const ShareShape& sh, F&& work) {
+  const Shares shares(a, sh);
+  const int w = uniform((int)blockIdx.x / a.cache.h_kv);
+  if (w >= shares.workers) return;
+  int64_t ends[2];          // of the share: its begin and its end
+#pragma unroll 1            // (code that runs once: its instructions come from memory)
+  for (int i = 0; i < 2; ++i) {
+    const int64_t x = uniform(shares.cut(w + i));
+    int64_t y = x;
+    if (x > 0 && x < shares.total) {
+      const Shares::Block k = shares.block_at(x);
+      if (k.b >= 0) y = shares.moved(x, k);
+    }
+    ends[0] = i == 0 ? uniform(y) : ends[0];
+    ends[1] = uniform(y);
+  }
+  const int64_t begin = ends[0], end = ends[1];
+#pragma unroll 1
+  for (int64_t at = begin; at < end;) {
+    const Shares::Block k = shares.block_at(at);
+    if (k.b < 0) return;
+    const int64_t all = k.w.of(k.r), from = at - k.begin, upto = min(all, end - k.begin);
+    Part p = part_of(a, sh, k, from, upto);
+    p.slot = 2 * blockIdx.x + (at == begin ? 0 : 1);
+    if (p.from < p.end || (p.alone && from == 0)) work(p);
+    at = k.begin + upto;
+  }
+}
+
+// A cut block, found from the first cut in it (that in front of share w): its parts are shares w - 1, w, ... 's.
+struct Cut {
+  Shares::Block k;          // k.b < 0: nothing to join
+  Part block;               // with all its tiles
+  int tiles, n;             // n: parts
+  double each;
+  bool begins;              // whether share w - 1 begins with it
+};
+__device__ __forceinline__ Cut cut_block(const Shares& shares, int w) {
+  Cut c;
+  c.k.b = -1;
+  if (w < 1 || w >= shares.workers) return c;
+  const int64_t x = uniform(shares.cut(w)), before = uniform(shares.cut(w - 1));
+  const Shares::Block k = shares.block_at(x);
+  if (k.b < 0) return c;
+  const int64_t all = k.w.of(k.r), end = k.begin + all;
+  auto stays = [&](int64_t y) { return y > k.begin && y < end && shares.moved(y, k) == y; };
+  if (!stays(x) || stays(before)) return c;                     // no cut, or not the first in its block
+  c.k = k;
+  c.block = part_of(shares.a, shares.sh, k, 0, all);
+  c.tiles = c.block.end;
+  c.each = (double)c.tiles / (double)all;
+  // Share w - 1 begins with the block if its cut is at the block's begin or moved there: from inside the block, or from the end of the one before.
+  c.begins = before >= k.begin;
+  if (!c.begins && before > 0) {
+    const Shares::Block b = shares.block_at(before);
+    c.begins = b.b >= 0 && shares.moved(before, b) == k.begin;
+  }
+  if (before <= 0) c.begins = k.begin == 0;
+  int last = w;             // the last share whose cut stays inside
+  for (int step = 1 << 9; step; step >>= 1)
+    if (last + step < shares.workers && shares.cut(last + step) < end && end - shares.cut(last + step) > shares.sh.near) last += step;
+  c.n = last - w + 2;
+  return c;
+}
+// Where part i left its result (lanes ask for different ones), -1: nowhere.
+__device__ __forceinline__ int slot_of(const Shares& shares, const Cut& c, int w, int i, int g) {
+  if (i >= c.n) return -1;
+  const int64_t all = c.k.w.of(c.k.r);
+  const int share = w - 1 + i;
+  const int from = i == 0 ? 0 : Shares::tile_at(shares.cut(share) - c.k.begin, all, c.tiles, c.each);
+  const int end = i == c.n - 1 ? c.tiles : Shares::tile_at(shares.cut(share + 1) - c.k.begin, all, c.tiles, c.each);
+  if (from >= end || (from == 0 && end == c.tiles)) return -1;
+  return 2 * (share * shares.a.cache.h_kv + g) + (i == 0 && !c.begins ? 1 : 0);
+}
+
+// On the host: workgroups, their partial results, and whether there are any.
+static inline int grid_of(const ShareShape& sh, int h_kv) { return (sh.places / h_kv > 1 ? sh.places / h_kv : 1) * h_kv; }
+
+}  // namespace paged
+}  // namespace esa

@@ -1,4 +1,4 @@
-// Which part of the attention a workgroup does.  The lengths lie on the device, so every workgroup finds its part from them: a scan over
+// Which part of the attention a workgroup of the kernel for few rows does.  The lengths lie on the device, so every workgroup finds its part from them: a scan over
 // the sequences, a lane to each.
 //
 // A sequence's rows (new tokens x query heads of a KV head, numbered token by token) are cut into blocks, its keys into tiles, the tiles
@@ -11,38 +11,33 @@
 namespace esa {
 namespace paged {
 
-// Rows of a block, keys of a tile, workgroups at a time; a slice has a multiple of `least` tiles; a workgroup's beginning and end take
-// as long as `overhead` tiles; at most `rounds` units for every place are worth while.  The kernel serves sequences of more than `above`
-// rows, up to `upto`.
-struct Shape {
-  int rows, keys, target, least, overhead, rounds, above, upto;
+// Rows of a block, keys of a tile, workgroups at a time; a slice has a multiple of `least` tiles.  The kernel serves sequences of up to `upto`
+// rows.
+struct SliceShape {
+  int rows, keys, target, least, upto;
 };
 struct Cost {
   int blocks, tiles;
 };
-__device__ __forceinline__ Cost cost_of(const AttendArgs& a, const Shape& sh, int b) {
+__device__ __forceinline__ Cost cost_of(const AttendArgs& a, const SliceShape& sh, int b) {
   const Seq s = sequence(a.batch, b);
   const int rows = s.n * a.group;
-  if (rows <= sh.above || rows > sh.upto) return Cost{0, 0};
+  if (rows > sh.upto) return Cost{0, 0};
   return Cost{(rows + sh.rows - 1) / sh.rows, (keys_of(a, s).n + sh.keys - 1) / sh.keys};
 }
-// A value that is the same in every lane, where the compiler does not see it.
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x) { return (int64_t)(uint32_t)uniform((int)x) | (int64_t)uniform((int)(x >> 32)) << 32; }
-__device__ __forceinline__ Seq uniform(const Seq& s) { return Seq{uniform(s.row0), uniform(s.n), uniform(s.t0)}; }
 struct Plan {
   Cost mine;      // of the lane's sequence among the first 64; of the only one in every lane
   int slice;      // tiles of a slice
 };
-__device__ __forceinline__ Cost cost_in(const AttendArgs& a, const Shape& sh, const Cost& mine, int b0) {
+__device__ __forceinline__ Cost cost_in(const AttendArgs& a, const SliceShape& sh, const Cost& mine, int b0) {
   const int b = b0 + (int)(threadIdx.x & 63);
   return b0 == 0 ? mine : b < a.batch.n_seq ? cost_of(a, sh, b) : Cost{0, 0};
 }
-// The length of a slice: so long that no more than one round of units is needed, or, where a call takes long enough, whatever is estimated
-// to be quickest of that and of slices of which every place of the chip gets two, three or four in the mean.  (Sixteen sequences of 18 to
-// 66 thousand tokens, cut by their mean, were 600 units for 512 places, and the second round took as long as the first: 497 us, 342
-// in one.)  Counts are fp32: exact where they decide, and every workgroup comes to the same ones.
-__device__ __forceinline__ Plan plan_of(const AttendArgs& a, const Shape& sh) {
+// The length of a slice: so long that no more than one round of units is needed.  (Sixteen sequences of 18 to 66 thousand tokens, cut by their
+// mean, were 600 units for 512 places, and the second round took as long as the first: 497 us, 342 in one.  Shorter slices and several
+// rounds were slower, as were shares of the same length that cut sequences anywhere, by what finding them takes in both kernels.)  Counts
+// are fp32: exact where they decide, and every workgroup comes to the same ones.
+__device__ __forceinline__ Plan plan_of(const AttendArgs& a, const SliceShape& sh) {
   const int lane = threadIdx.x & 63;
   const bool one = a.batch.n_seq == 1;
   Plan p;
@@ -57,9 +52,6 @@ __device__ __forceinline__ Plan plan_of(const AttendArgs& a, const Shape& sh) {
   const float places = (float)sh.target, mean = fmaxf(all / places, 1.f);
   auto rounded = [&](float x) { return (int)fminf(ceilf(x / (float)sh.least), 1e7f) * sh.least; };
   auto units_of = [&](int slice) { return total([&](const Cost& c) { return (float)c.blocks * (float)((c.tiles + slice - 1) / slice); }); };
-  auto took = [&](int slice, float units) {
-    return units <= places ? (float)(slice + sh.overhead) : (all + units * (float)sh.overhead) / places + 0.5f * (float)slice;
-  };
   int slice = rounded(mean);
   float units = units_of(slice);
   for (int i = 0; i < 4 && units > places; ++i) {
@@ -68,20 +60,8 @@ __device__ __forceinline__ Plan plan_of(const AttendArgs& a, const Shape& sh) {
     units = units_of(slice);
   }
   p.slice = uniform(slice);
-  if (sh.rounds > 1 && mean > 4.f * (float)sh.overhead) {
-    float best = took(slice, units);
-    for (int k = 1; k <= sh.rounds; ++k) {
-      const int shorter = rounded(mean / (float)k);
-      const float t = took(shorter, units_of(shorter));
-      if (t < best) {
-        best = t;
-        p.slice = uniform(shorter);
-      }
-    }
-  }
   return p;
 }
-__device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane(x, lane); }
 struct Part {
   int b, block, slice;      // b < 0: none
   int64_t slot;             // of the block's first slice among the partial results of a KV head (blocks next to each other), if it has several
@@ -89,7 +69,7 @@ struct Part {
 };
 __device__ __forceinline__ Part uniform(const Part& p) { return Part{uniform(p.b), uniform(p.block), uniform(p.slice), uniform(p.slot), uniform(p.blocks)}; }
 // The u-th unit.  A sequence's units are numbered slice by slice: neighbours read the same keys.
-__device__ __forceinline__ Part part_of(const AttendArgs& a, const Shape& sh, const Plan& plan, int64_t u) {
+__device__ __forceinline__ Part part_of(const AttendArgs& a, const SliceShape& sh, const Plan& plan, int64_t u) {
   if (a.batch.n_seq == 1) {
     const int blocks = uniform(plan.mine.blocks), n = max((uniform(plan.mine.tiles) + plan.slice - 1) / plan.slice, 1);
     if (u >= (int64_t)blocks * n) return Part{-1, 0, 0, 0, 0};
@@ -117,7 +97,7 @@ struct Split {
   int64_t slot;             // of the sequence's first partial result
 };
 __device__ __forceinline__ Split uniform(const Split& s) { return Split{uniform(s.b), uniform(s.i), uniform(s.slot)}; }
-template <typename F> __device__ __forceinline__ Split split_of(const AttendArgs& a, const Shape& sh, const Plan& plan, int64_t u, F&& count) {
+template <typename F> __device__ __forceinline__ Split split_of(const AttendArgs& a, const SliceShape& sh, const Plan& plan, int64_t u, F&& count) {
   const int lane = threadIdx.x & 63;
   if (a.batch.n_seq == 1) {
     const bool split = uniform(plan.mine.tiles) > plan.slice && u < count(sequence(a.batch, 0).n * a.group);
@@ -139,21 +119,16 @@ template <typename F> __device__ __forceinline__ Split split_of(const AttendArgs
   }
   return Split{-1, 0, 0};
 }
-// Keys that the rows up to `row` of a sequence see at most.
-__device__ __forceinline__ int keys_until(const AttendArgs& a, const Seq& s, const Keys& k, int row) {
-  const int width = a.batch.max_pages << a.batch.page_log2;
-  return k.n - (min(s.t0 + s.n, width) - min(s.t0 + row / a.group + 1, width));
-}
-// Blocks, units and partial results of a KV head at most.  A slice is the rounds-th part of the mean at least; a sequence of several
-// slices has more than one slice's tiles, so at most twice as many slices as its tiles fill.
-static inline int64_t most_blocks(const Shape& sh, int64_t n_tok, int n_seq, int group) {
+// Blocks, units and partial results of a KV head at most.  A slice is the mean at least; a sequence of several slices has more than one
+// slice's tiles, so at most twice as many slices as its tiles fill.
+static inline int64_t most_blocks(const SliceShape& sh, int64_t n_tok, int n_seq, int group) {
   const int64_t by_rows = n_tok * group / sh.rows + (n_seq < n_tok ? n_seq : n_tok), by_limit = (int64_t)n_seq * ((sh.upto - 1) / sh.rows + 1);
   return by_rows < by_limit ? by_rows : by_limit;
 }
-static inline int64_t most_units(const Shape& sh, int64_t n_tok, int n_seq, int group, int h_kv) {
-  return sh.rounds * ((int64_t)sh.target / h_kv + 1) + most_blocks(sh, n_tok, n_seq, group);
+static inline int64_t most_units(const SliceShape& sh, int64_t n_tok, int n_seq, int group, int h_kv) {
+  return (int64_t)sh.target / h_kv + 1 + most_blocks(sh, n_tok, n_seq, group);
 }
-static inline int64_t most_parts(const Shape& sh, int h_kv) { return 2 * sh.rounds * ((int64_t)sh.target / h_kv + 1); }
+static inline int64_t most_parts(const SliceShape& sh, int h_kv) { return 2 * ((int64_t)sh.target / h_kv + 1); }
 
 }  // namespace paged
 }  // namespace esa
