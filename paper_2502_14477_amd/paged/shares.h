@@ -15,7 +15,8 @@ namespace esa {
 namespace paged {
 
 // Rows of a block, keys of a tile, workgroups at a time; a share is worth its beginning and end from `least` keys on, blocks of up to `whole`
-// keys are not cut, others not within `near` keys of their begin and end.  The kernel serves sequences of more than `above` rows.
+// keys are not cut, others not within a quarter of a share (`near` keys at least, three times
+// as many at most) of their begin and end.  The kernel serves sequences of more than `above` rows.
 struct ShareShape {
   int rows, keys, places, least, whole, near, above;
 };
@@ -68,6 +69,7 @@ class Shares {
     workers = uniform((int)min(max(worth, (int64_t)1), (int64_t)max(sh.places / a.cache.h_kv, 1)));
     if (total == 0) workers = 0;
     share = (double)total / (double)max(workers, 1);
+    near = (int)fmin(fmax(share * 0.25, (double)sh.near), 3.0 * (double)sh.near);
   }
 
   // Where share w begins, before small blocks are left whole.  (Doubles: the same ones wherever it is asked.)
@@ -107,8 +109,8 @@ class Shares {
   // tiles.
   __device__ __forceinline__ int64_t moved(int64_t x, const Block& k) const {
     const int64_t all = k.w.of(k.r);
-    if (all <= sh.whole || x - k.begin <= sh.near) return k.begin;
-    return k.begin + all - x <= sh.near ? k.begin + all : x;
+    if (all <= sh.whole || x - k.begin <= near) return k.begin;
+    return k.begin + all - x <= near ? k.begin + all : x;
   }
   // The tile of a block of `tiles` at which weight x of its `all` cuts it; each: tiles / all.
   static __device__ __forceinline__ int tile_at(int64_t x, int64_t all, int tiles, double each) {
@@ -118,7 +120,7 @@ class Shares {
   const AttendArgs& a;
   const ShareShape& sh;
   int64_t total;
-  int workers;
+  int workers, near;
   double share;
 
  private:
@@ -212,7 +214,7 @@ __device__ __forceinline__ Cut cut_block(const Shares& shares, int w) {
   if (before <= 0) c.begins = k.begin == 0;
   int last = w;             // the last share whose cut stays inside
   for (int step = 1 << 9; step; step >>= 1)
-    if (last + step < shares.workers && shares.cut(last + step) < end && end - shares.cut(last + step) > shares.sh.near) last += step;
+    if (last + step < shares.workers && shares.cut(last + step) < end && end - shares.cut(last + step) > shares.near) last += step;
   c.n = last - w + 2;
   return c;
 }
