@@ -28,7 +28,8 @@ extern "C" {
  *                     e4m3's subnormals) and its values are bf16 numbers.  NULL for other types.
  * Rows start on 16-byte boundaries (k, v, and every stride in bytes).  Strides may be in any order ([n_pages, page_size, h_kv, d]
  * is as good); two different elements must not overlap.  max_pages * page_size, the tokens, and the tokens times the heads stay
- * below 2^31 - 2^16; offsets into the pool have 64 bits.
+ * below 2^31 - 2^16; offsets into the pool have 64 bits, a stride is below
+ * 2^31 bytes, n_pages * h_kv below 2^31.
  */
 typedef struct {
   void* k;

@@ -103,7 +103,7 @@ template <typename T> __device__ void append_rows(const AppendArgs& a, int block
         const Seq s = sequence(a.batch, b);
         p = s.t0 + tok - s.row0;
         const int page = paged ? page_of(a.batch, a.cache.n_pages, b, p) : -1;
-        if (page >= 0) to = page * a.cache.page_bytes + (p & ((1 << a.batch.page_log2) - 1)) * a.cache.tok_bytes;
+        if (page >= 0) to = place_of(a.cache, page, 0, p & ((1 << a.batch.page_log2) - 1));
       }
       pos[wave] = p;
       at[wave] = to;
@@ -143,7 +143,7 @@ template <typename T> __device__ void append_rows(const AppendArgs& a, int block
         to = a.out_q + (int64_t)(tok0 + r) * a.ldoq + (int64_t)hh * 2 * half_bytes;
       } else {
         if (at[r] < 0) continue;
-        to = (kv < 0 ? a.cache.k : a.cache.v) + at[r] + (kv < 0 ? g : kv) * a.cache.head_bytes;
+        to = (kv < 0 ? a.cache.k : a.cache.v) + at[r] + (int64_t)(kv < 0 ? g : kv) * a.cache.head_bytes;
       }
       store_vec(to + i * 16, x[u]);
       store_vec(to + half_bytes + i * 16, y[u]);
@@ -191,7 +191,7 @@ template <typename T, int J> __global__ __launch_bounds__(kThreads) void append_
   const int lo = max(s.t0 - pos0, 0), hi = min(s.t0 + s.n - pos0, page_size);
   const int page = page_of(a.batch, a.cache.n_pages, f.b, pos0);
   if (page < 0) return;
-  uint8_t* scale = (keys ? a.cache.k_scale : a.cache.v_scale) + (int64_t)page * a.cache.h_kv + g;
+  uint8_t* scale = (keys ? a.cache.k_scale : a.cache.v_scale) + block_of(a.cache, page, g);
   const int old = lo > 0 ? *scale : 0;
   const int d = a.cache.d, half = d >> 1, vecs = half / V, rows = kThreads / vecs, i = tid % vecs, r0 = tid / vecs;
   const int64_t ld = keys ? a.ldk : a.ldv;
@@ -233,7 +233,7 @@ template <typename T, int J> __global__ __launch_bounds__(kThreads) void append_
   __syncthreads();
   m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
   const int byte = max(scale_byte(m), old);
-  char* to = (keys ? a.cache.k : a.cache.v) + page * a.cache.page_bytes + g * a.cache.head_bytes;
+  char* to = (keys ? a.cache.k : a.cache.v) + place_of(a.cache, page, g, 0);
   const float by = scale_of(254 - byte);
 #pragma unroll
   for (int j = 0; j < J; ++j) {

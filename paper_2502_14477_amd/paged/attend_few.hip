@@ -66,7 +66,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
     int pos0, pos, entry;                                       // pos0: of the tile's first key where it lies in one page, else -1
   };
   const int slot_mask = (1 << a.batch.page_log2) - 1;
-  const uint32_t tok_bytes = (uint32_t)a.cache.tok_bytes;
+  const uint32_t tok_bytes = a.cache.tok_bytes;
   auto request_entry = [&](int t) { return keys.n_sel && t < end ? entry_of(a, keys, at.b, t * kKeys + r) : 0; };
   auto request_page = [&](int t, int entry) __attribute__((always_inline)) {
     const int j0 = t * kKeys, late = j0 - keys.i_end - keys.n_sel;
@@ -88,28 +88,24 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   bool whole = false;
   auto find_rows = [&](const Meta& m) __attribute__((always_inline)) {
     whole = m.pos0 >= 0;
-    const int64_t head = g * a.cache.head_bytes;
-    int64_t block = g;
     if (whole) {
       const int entry = uniform(m.entry);
       const bool there = is_page(a.batch, a.cache.n_pages, m.pos0, entry);
       const int page = there ? entry : 0;
       now_pos = there ? m.pos0 + r : INT32_MAX;
-      place = page * a.cache.page_bytes + head + (int64_t)((m.pos0 & slot_mask) * (uint64_t)tok_bytes);
-      block += (int64_t)page * a.cache.h_kv;
+      place = place_of(a.cache, page, g, m.pos0 & slot_mask);
       if constexpr (F8) {
-        kb = a.cache.k_scale[block];
-        vb = a.cache.v_scale[block];
+        kb = a.cache.k_scale[block_of(a.cache, page, g)];
+        vb = a.cache.v_scale[block_of(a.cache, page, g)];
       }
     } else {
       const bool there = is_page(a.batch, a.cache.n_pages, m.pos, m.entry);
       const int page = there ? m.entry : 0;
       now_pos = there ? m.pos : INT32_MAX;
-      place = page * a.cache.page_bytes + head + (int64_t)((there ? m.pos & slot_mask : 0) * (uint64_t)tok_bytes);
-      block += (int64_t)page * a.cache.h_kv;
+      place = place_of(a.cache, page, g, there ? m.pos & slot_mask : 0);
       if constexpr (F8) {
-        kb = a.cache.k_scale[block];
-        vb = a.cache.v_scale[block];
+        kb = a.cache.k_scale[block_of(a.cache, page, g)];
+        vb = a.cache.v_scale[block_of(a.cache, page, g)];
       }
     }
   };

@@ -67,7 +67,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   const int32_t* const list = keys.n_sel ? a.idx + (int64_t)at.b * a.idx_ld : a.batch.pages;
   const int list_last = max(keys.n_sel - 1, 0);
   const int slot_mask = (1 << a.batch.page_log2) - 1;
-  const uint32_t tok_bytes = (uint32_t)a.cache.tok_bytes;
+  const uint32_t tok_bytes = a.cache.tok_bytes;
   struct Entries {
     int x[kMine];
   };
@@ -108,13 +108,13 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       const int entry = __builtin_amdgcn_readfirstlane(m.entry[0]);
       const bool there = is_page(a.batch, a.cache.n_pages, m.pos0, entry);
       const int page = there ? entry : 0;
-      const int64_t place = page * a.cache.page_bytes + g * a.cache.head_bytes + (int64_t)(m.pos0 & slot_mask) * tok_bytes;
+      const int64_t place = place_of(a.cache, page, g, m.pos0 & slot_mask);
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
         h.x[i] = *(const u32x4*)((is_value(i) ? a.cache.v : a.cache.k) + place + ((uint32_t)key_of(i) * tok_bytes + piece * 16));
       if constexpr (F8) {
 #pragma unroll
-        for (int i = 0; i < kLoads; ++i) h.scale[i] = (is_value(i) ? a.cache.v_scale : a.cache.k_scale)[(int64_t)page * a.cache.h_kv + g];
+        for (int i = 0; i < kLoads; ++i) h.scale[i] = (is_value(i) ? a.cache.v_scale : a.cache.k_scale)[block_of(a.cache, page, g)];
       }
 #pragma unroll
       for (int n = 0; n < kMine; ++n) h.pos[n] = there ? m.pos0 + key_of(n) : INT32_MAX;
@@ -122,14 +122,15 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
       return;
     }
     h.whole = false;
-    int64_t place[kMine], block[kMine];
+    int64_t place[kMine];
+    uint32_t block[kMine];
 #pragma unroll
     for (int n = 0; n < kMine; ++n) {
       const bool there = is_page(a.batch, a.cache.n_pages, m.pos[n], m.entry[n]);
       const int page = there ? m.entry[n] : 0;
       h.pos[n] = there ? m.pos[n] : INT32_MAX;
-      place[n] = page * a.cache.page_bytes + g * a.cache.head_bytes + (int64_t)((there ? m.pos[n] & slot_mask : 0) * (uint64_t)tok_bytes) + piece * 16;
-      block[n] = (int64_t)page * a.cache.h_kv + g;
+      place[n] = place_of(a.cache, page, g, there ? m.pos[n] & slot_mask : 0) + piece * 16;
+      block[n] = block_of(a.cache, page, g);
     }
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {

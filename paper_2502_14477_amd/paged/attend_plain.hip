@@ -62,7 +62,7 @@ template <typename T, bool F8> __global__ __launch_bounds__(kThreads) void atten
       const int p = position(keys, j0 + tid, entry_of(a, keys, b, j0 + tid));
       const int page = p >= 0 && p <= own ? page_of(a.batch, a.cache.n_pages, b, p) : -1;
       if (page >= 0) {
-        at = page * a.cache.page_bytes + g * a.cache.head_bytes + (p & ((1 << a.batch.page_log2) - 1)) * a.cache.tok_bytes;
+        at = place_of(a.cache, page, g, p & ((1 << a.batch.page_log2) - 1));
         float dot = 0.f, k[16];
         for (int i = 0; i < d; i += 16) {
           load16_f32<T, F8>(a.cache.k + at + i * (F8 ? 1 : (int)sizeof(T)), k);
@@ -70,8 +70,8 @@ template <typename T, bool F8> __global__ __launch_bounds__(kThreads) void atten
           for (int e = 0; e < 16; ++e) dot = __builtin_fmaf(q[i + e], k[e], dot);
         }
         if (F8) {
-          dot *= scale_of(a.cache.k_scale[(int64_t)page * a.cache.h_kv + g]);
-          by = scale_of(a.cache.v_scale[(int64_t)page * a.cache.h_kv + g]);
+          dot *= scale_of(a.cache.k_scale[block_of(a.cache, page, g)]);
+          by = scale_of(a.cache.v_scale[block_of(a.cache, page, g)]);
         }
         x = dot * a.scale;
         if (a.cap > 0.f) x = a.cap * tanhf(x / a.cap);

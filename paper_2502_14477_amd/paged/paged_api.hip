@@ -50,7 +50,10 @@ int common_ok(const char* name, const esa_paged_batch* b, const esa_paged_cache*
   if (!aligned(b->cu, 4) || !aligned(b->start, 4) || !aligned(b->pages, 4)) ESA_FAIL(ESA_EINVAL, "%s: misaligned pointer", name);
   const int64_t es = c->dtype == ESA_F32 ? 4 : c->dtype == ESA_BF16 ? 2 : 1;
   for (int64_t s : {c->page_stride, c->head_stride, c->tok_stride})
-    if (s < c->d || s * es % 16 != 0) ESA_FAIL(ESA_EINVAL, "%s: a cache stride of %lld elements (at least d, whole 16 bytes)", name, (long long)s);
+    if (s < c->d || s > INT64_MAX / 8 || s * es % 16 != 0) ESA_FAIL(ESA_EINVAL, "%s: a cache stride of %lld elements (at least d, whole 16 bytes)", name, (long long)s);
+  for (int64_t s : {c->page_stride, c->head_stride, c->tok_stride})
+    if (s * es > INT32_MAX) ESA_FAIL(ESA_EINVAL, "%s: a cache stride of %lld elements (below 2^31 bytes)", name, (long long)s);
+  if ((int64_t)c->n_pages * c->h_kv > INT32_MAX) ESA_FAIL(ESA_EINVAL, "%s: more than 2^31 blocks", name);
   if (!apart(*c)) ESA_FAIL(ESA_EINVAL, "%s: elements of the cache overlap", name);
   if (!aligned(c->k, 16) || !aligned(c->v, 16)) ESA_FAIL(ESA_EINVAL, "%s: misaligned cache", name);
   if (c->dtype == ESA_E4M3 && (!c->k_scale || !c->v_scale)) ESA_FAIL(ESA_EINVAL, "%s: an 8-bit cache needs its scales", name);
@@ -76,9 +79,9 @@ paged::Cache cache_of(const esa_paged_cache& c) {
   x.v = (char*)c.v;
   x.k_scale = c.k_scale;
   x.v_scale = c.v_scale;
-  x.page_bytes = c.page_stride * es;
-  x.head_bytes = c.head_stride * es;
-  x.tok_bytes = c.tok_stride * es;
+  x.page_bytes = (uint32_t)(c.page_stride * es);
+  x.head_bytes = (uint32_t)(c.head_stride * es);
+  x.tok_bytes = (uint32_t)(c.tok_stride * es);
   x.n_pages = c.n_pages;
   x.h_kv = c.h_kv;
   x.d = c.d;
