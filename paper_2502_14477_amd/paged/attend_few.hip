@@ -444,8 +444,12 @@ template <typename T, int D> __global__ __launch_bounds__(256) void join_few(Few
   }
 }
 
-// Workgroups that the chip holds: a compute unit has 160 KB of LDS, a workgroup's staging space is 64 KB for rows of up to 256 bytes.
-SliceShape shape_of(int d, int es, int most_rows) { return SliceShape{kRows, kKeys, d * es > 256 ? 256 : d * es == 256 ? 512 : 1024, kWaves, most_rows}; }
+// Workgroups that the chip holds: staging space in LDS and registers leave a compute unit one of fp32 rows of 512 bytes, three of 8-bit rows
+// of 64 elements brought to bf16, two of the others.  (1024 for rows of 64 elements, whatever their registers: eight sequences of 64 thousand
+// keys, 8 bits, 138 us, 1.3 rounds.)
+SliceShape shape_of(int d, int es, bool f8, int most_rows) {
+  return SliceShape{kRows, kKeys, d * es > 256 ? 256 : f8 && d * es < 256 ? 768 : 512, kWaves, most_rows};
+}
 
 template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, hipStream_t st) {
   if (f.a.cap > 0.f)
@@ -457,7 +461,7 @@ template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, hi
 }
 template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows, void* ws, hipStream_t st) {
   const int d = a.cache.d;
-  const SliceShape shape = shape_of(d, sizeof(T), most_rows);
+  const SliceShape shape = shape_of(d, sizeof(T), f8, most_rows);
   const FewArgs f = split_args<T>(a, shape, most_parts(shape, a.cache.h_kv) * a.cache.h_kv, ws);
   const int64_t units = most_units(f.shape, a.batch.n_tok, a.batch.n_seq, a.group, a.cache.h_kv) * a.cache.h_kv;
   if (units > INT32_MAX) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: %lld workgroups", (long long)units);
@@ -482,7 +486,7 @@ template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows
 }  // namespace
 
 size_t few_workspace(int h_kv, int d, int dtype) {
-  return split_workspace(most_parts(shape_of(d, dtype == ESA_F32 ? 4 : 2, INT32_MAX), h_kv) * h_kv, kRows, d);
+  return split_workspace(most_parts(shape_of(d, dtype == ESA_F32 ? 4 : 2, true, INT32_MAX), h_kv) * h_kv, kRows, d);
 }
 
 int launch_few(const AttendArgs& a, bool f8, int dtype, int most_rows, void* ws, hipStream_t st) {
