@@ -6,7 +6,7 @@ import pytest
 import torch
 
 from oracle import paged_oracle as orc
-from paged_support import Pool, check_attention, f64
+from paged_support import TYPES, Pool, check_attention, f64
 
 pytestmark = pytest.mark.gpu
 BASE = 5e5
@@ -217,6 +217,43 @@ def test_attend_chunk(esa, held, l_c, h, h_kv, d):
     check_attention(pool, q, out, lse, l_i=20, l_l=100, idx=idx, cap=5.0, p_half_step=P_STEP["bf16"])
 
 
+# Chunks whose keys are shared out over the workgroups: blocks cut in many places or left whole, blocks of a few rows, groups of heads that
+# do not divide a block, sequences that another kernel serves in between.
+SHARED = {
+    "one long": [(6000, 70)], "from the beginning": [(0, 1300)], "short ones": [(200, 65), (0, 80), (31, 100), (1, 64), (450, 90)],
+    "ragged": [(3000, 300), (40, 600), (0, 33), (2500, 1), (700, 129)], "just over a block": [(1000, 129), (999, 257), (63, 65)],
+}
+
+
+@pytest.mark.parametrize("held", ["e4m3", "same"])
+@pytest.mark.parametrize("h,h_kv,d,page", [(4, 1, 64, 32), (2, 2, 128, 64), (10, 2, 64, 128), (16, 1, 128, 16)])
+@pytest.mark.parametrize("name", sorted(SHARED))
+def test_attend_shares_blocks(esa, held, h, h_kv, d, page, name):
+    print("[case] shares", held, h, h_kv, d, page, name, flush=True)
+    lengths = [(t0, -(-n * 2 // (h // h_kv))) for t0, n in SHARED[name]]      # rows of a KV head: twice n, a block has 256
+    pool = Pool(lengths, h_kv, d, page, "bf16", held, seed=20).fill((1.0, 1.0))
+    q = pool.rows(pool.n_tok, h)
+    out, lse = esa.esa_attend_paged(q, *pool.batch(), return_lse=True)
+    check_attention(pool, q, out, lse, p_half_step=P_STEP["bf16"])
+
+
+@pytest.mark.parametrize("held,cap", [("e4m3", 0.0), ("same", 3.0)])
+def test_attend_of_random_batches(esa, held, cap):
+    for seed in range(12):
+        rng = np.random.default_rng(100 + seed)
+        lengths = [(int(rng.integers(0, 10 ** rng.integers(1, 4))), int(rng.integers(0, 6 if rng.random() < 0.4 else 260))) for _ in range(rng.integers(1, 9))]
+        if sum(n for _, n in lengths) == 0:
+            continue
+        print("[case] random", held, cap, seed, lengths, flush=True)
+        pool = Pool(lengths, 1, 64, int(rng.choice([16, 32, 64, 128])), "bf16", held, seed=seed).fill((1.0, 1.0))
+        q = pool.rows(pool.n_tok, 4)
+        out, lse = esa.esa_attend_paged(q, *pool.batch(), cap=cap, return_lse=True)
+        check_attention(pool, q, out, lse, cap=cap, p_half_step=P_STEP["bf16"])
+        idx = selections(pool, 7, 50, 60, seed=seed)
+        out, lse = esa.esa_attend_paged(q, *pool.batch(), l_i=7, l_l=50, idx=idx, cap=cap, return_lse=True)
+        check_attention(pool, q, out, lse, l_i=7, l_l=50, idx=idx, cap=cap, p_half_step=P_STEP["bf16"])
+
+
 @pytest.mark.parametrize("dtype,held", [("bf16", "e4m3"), ("bf16", "same"), ("f32", "same")])
 def test_attend_with_large_and_far_apart_logits(esa, dtype, held):
     """Logits of some hundreds: the running maximum moves by more than an exponential's range, in both directions."""
@@ -226,6 +263,34 @@ def test_attend_with_large_and_far_apart_logits(esa, dtype, held):
     check_attention(pool, q, out, lse, p_half_step=P_STEP[dtype])
     out, lse = esa.esa_attend_paged(q, *pool.batch(), cap=30.0, return_lse=True)
     check_attention(pool, q, out, lse, cap=30.0, p_half_step=P_STEP[dtype])
+
+
+@pytest.mark.parametrize("dtype,held", [("bf16", "e4m3"), ("bf16", "same"), ("f32", "e4m3")])
+@pytest.mark.parametrize("new", [1, 100])
+def test_attend_with_logits_that_rise_towards_the_end(esa, dtype, held, new):
+    """Every key's logit is larger than those before it: the softmax's reference moves again and again, by more than its lag each time."""
+    pool = Pool([(900, new)], 1, 64, 64, dtype, held, seed=23).fill((0.01, 1.0))
+    direction = torch.zeros(64)
+    direction[5] = 1.0
+    at = torch.arange(900 + new)
+    rise = (at.double() / 4).to(TYPES[dtype])                    # logits 0 .. 250 in steps
+    host = pool.caches[0].cpu()
+    if held == "e4m3":
+        pool.scales[0].fill_(127)
+        x = torch.zeros(pool.caches[0].shape)
+        for p in range(-(-(900 + new) // 64)):
+            rows = rise[p * 64:(p + 1) * 64].float()
+            x[pool.table[0, p], 0, :len(rows), 5] = rows
+        pool.caches[0].view(torch.uint8).copy_(x.to(torch.float8_e4m3fn).view(torch.uint8))
+    else:
+        for p in range(-(-(900 + new) // 64)):
+            rows = rise[p * 64:(p + 1) * 64]
+            host[pool.table[0, p], 0, :len(rows)] = 0
+            host[pool.table[0, p], 0, :len(rows), 5] = rows
+        pool.caches[0].copy_(host)
+    q = (torch.ones(new, 4, 64) * direction).to(TYPES[dtype]).cuda()
+    out, lse = esa.esa_attend_paged(q, *pool.batch(), scale=1.0, return_lse=True)
+    check_attention(pool, q, out, lse, scale=1.0, p_half_step=P_STEP[dtype])
 
 
 @pytest.mark.parametrize("held", ["e4m3", "same"])
