@@ -446,9 +446,10 @@ template <typename T, int D> __global__ __launch_bounds__(256) void join_few(Few
 
 // Workgroups that the chip holds: staging space in LDS and registers leave a compute unit one of fp32 rows of 512 bytes, three of 8-bit rows
 // of 64 elements brought to bf16, two of the others.  (1024 for rows of 64 elements, whatever their registers: eight sequences of 64 thousand
-// keys, 8 bits, 138 us, 1.3 rounds.)
-SliceShape shape_of(int d, int es, bool f8, int most_rows) {
-  return SliceShape{kRows, kKeys, d * es > 256 ? 256 : f8 && d * es < 256 ? 768 : 512, kWaves, most_rows};
+// keys, 8 bits, 138 us, 1.3 rounds.)  A slice has a tile for every wave; where no sequence can have more than 512 keys, four, so that none is
+// cut and nothing is left to join (301 keys: 10.6 us cut in three, 9.1 in one).
+SliceShape shape_of(int d, int es, bool f8, int most_rows, bool shorts) {
+  return SliceShape{kRows, kKeys, d * es > 256 ? 256 : f8 && d * es < 256 ? 768 : 512, shorts ? 4 * kWaves : kWaves, most_rows};
 }
 
 template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, hipStream_t st) {
@@ -461,7 +462,8 @@ template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, hi
 }
 template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows, void* ws, hipStream_t st) {
   const int d = a.cache.d;
-  const SliceShape shape = shape_of(d, sizeof(T), f8, most_rows);
+  const int64_t most_keys = ((int64_t)a.batch.max_pages << a.batch.page_log2) + a.n_sel;      // of a sequence
+  const SliceShape shape = shape_of(d, sizeof(T), f8, most_rows, most_keys <= 4 * kWaves * kKeys);
   const FewArgs f = split_args<T>(a, shape, most_parts(shape, a.cache.h_kv) * a.cache.h_kv, ws);
   const int64_t units = most_units(f.shape, a.batch.n_tok, a.batch.n_seq, a.group, a.cache.h_kv) * a.cache.h_kv;
   if (units > INT32_MAX) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: %lld workgroups", (long long)units);
@@ -471,8 +473,7 @@ template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows
     rc = f8 ? launch<T, true, 64>(f, grid, st) : launch<T, false, 64>(f, grid, st);
   else
     rc = f8 ? launch<T, true, 128>(f, grid, st) : launch<T, false, 128>(f, grid, st);
-  // (the longest sequence that the table has room for may be one slice)
-  if (rc != ESA_OK || ((int64_t)a.batch.max_pages << a.batch.page_log2) + a.n_sel <= (int64_t)shape.least * kKeys) return rc;
+  if (rc != ESA_OK || most_keys <= (int64_t)shape.least * kKeys) return rc;
   const int64_t by_blocks = most_blocks(f.shape, a.batch.n_tok, a.batch.n_seq, a.group) * kRows * a.cache.h_kv, by_tokens = a.batch.n_tok * a.h;
   const dim3 join((unsigned)std::min<int64_t>(std::min(by_blocks, by_tokens), 2048));
   if (d == 64)
@@ -486,7 +487,7 @@ template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows
 }  // namespace
 
 size_t few_workspace(int h_kv, int d, int dtype) {
-  return split_workspace(most_parts(shape_of(d, dtype == ESA_F32 ? 4 : 2, true, INT32_MAX), h_kv) * h_kv, kRows, d);
+  return split_workspace(most_parts(shape_of(d, dtype == ESA_F32 ? 4 : 2, true, INT32_MAX, false), h_kv) * h_kv, kRows, d);
 }
 
 int launch_few(const AttendArgs& a, bool f8, int dtype, int most_rows, void* ws, hipStream_t st) {

@@ -152,18 +152,22 @@ int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* b
   a.cap = cap;
   const bool f8 = cache->dtype == ESA_E4M3;
   if (cache->d != 64 && cache->d != 128) return paged::launch_plain(a, f8, dtype, (hipStream_t)stream);
-  // The lengths are on the device.  A batch of a few rows a sequence in the mean is served by the kernel for few rows, whatever else
-  // is in it; other batches by both, each of which finds the sequences that are its own (one that finds none: 2 us).  The two run one after the
-  // other and use the same workspace.
+  // The lengths are on the device, the mean is known.  A batch of few rows a sequence in the mean is served by the kernel for few rows, whatever
+  // else is in it; other batches by both, one after the other in the same workspace, each of which finds the sequences that are its own.  One that
+  // finds none takes 5 us and its join 5 more, while short sequences in the kernel for many rows cost no more than twice their time: where the
+  // table has no room for more than 2^17 keys over all heads (8 tiles of 64 a workgroup, 15 us), that one serves them all.  (Chunks of 333 and 117
+  // tokens over 5000 keys, 8 heads: 75.6 us by both, 68.2 by one.  Sixteen tokens of 16 thousand keys beside a long prompt: twice 270 us.)
   hipStream_t st = (hipStream_t)stream;
   const int64_t rows = batch->n_tok * a.group;
   if (dtype != ESA_BF16 || rows <= (int64_t)kFewRows || rows <= (int64_t)32 * batch->n_seq)
     return paged::launch_few(a, f8, dtype, INT32_MAX, workspace, st);
-  if (batch->n_seq > 1) {
-    const int rc2 = paged::launch_few(a, f8, dtype, kFewRows, workspace, st);
-    if (rc2 != ESA_OK) return rc2;
+  const int64_t most_keys = ((int64_t)batch->max_pages << a.batch.page_log2) + a.n_sel;
+  const bool both = batch->n_seq > 1 && most_keys > (1 << 17) / ((int64_t)batch->n_seq * cache->h_kv);
+  if (both) {
+    const int few = paged::launch_few(a, f8, dtype, kFewRows, workspace, st);
+    if (few != ESA_OK) return few;
   }
-  return paged::launch_many(a, f8, batch->n_seq > 1 ? kFewRows : 0, workspace, st);
+  return paged::launch_many(a, f8, both ? kFewRows : 0, workspace, st);
 }
 
 }  // extern "C"
