@@ -22,7 +22,9 @@ namespace paged {
 namespace {
 
 constexpr int kRows = 256, kKeys = 64, kWaves = 8;
-using ManyArgs = SplitArgs<ShareShape>;
+struct ManyArgs : SplitArgs<ShareShape> {
+  Record* records;          // [slot]
+};
 
 template <bool F8, int D, bool CAP>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void attend_many(ManyArgs f) {
@@ -43,7 +45,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = uniform((int)blockIdx.x % a.cache.h_kv);
-  for_parts(a, f.shape, [&](const Part& at) __attribute__((always_inline)) {
+  for_parts(a, f.shape, f.records, [&](const Part& at) __attribute__((always_inline)) {
   const Seq& s = at.s;
   const Keys& keys = at.keys;
   const int row0 = at.row0, rows = at.rows, n_vis = at.n_vis, first = at.from, end = at.end;
@@ -366,48 +368,67 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   });
 }
 
-// Cut blocks joined: a workgroup takes 32 rows of a block as a wave has left them, its waves a quarter of the dimensions each.
+// Cut blocks joined: a workgroup takes 32 rows of a block as a wave has left them, its waves a quarter of the dimensions each.  A block's first
+// part is the last thing that a share leaves, the others are the first that the shares behind it leave.  The next part is requested before one is added.
 template <int D> __global__ __launch_bounds__(256) void join_many(ManyArgs f) {
   constexpr int kChunks = D / 8, kMine = kChunks / 4;           // 16 bytes a lane: of 32 rows, and of them a wave's
   constexpr int kGroups = kRows / 32;
   const AttendArgs& a = f.a;
   const int lane = threadIdx.x & 63, r = lane & 31, hi = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int group = blockIdx.x % kGroups, unit = blockIdx.x / kGroups, g = unit % a.cache.h_kv, w = unit / a.cache.h_kv + 1;
-  const Shares shares(a, f.shape);
-  const Cut c = cut_block(shares, w);
-  if (c.k.b < 0 || group * 32 >= c.block.rows) return;
-  float m = kNoReference, l = 0.f;
-  f32x4 sum[kMine];
+  const int group = blockIdx.x % kGroups, unit = blockIdx.x / kGroups, h_kv = a.cache.h_kv, g = unit % h_kv, units = (int)gridDim.x / kGroups;
+  const bool second = f.records[2 * unit + 1].rows > 0;
+  const int slot0 = 2 * unit + (second ? 1 : 0);
+  const Record block = f.records[slot0];
+  if (!block.begins || group * 32 >= block.rows) return;
+  struct Partial {
+    float2 ml;
+    f32x4 x[kMine];
+  };
+  auto load = [&](int slot) {
+    const int64_t part = (int64_t)slot * kGroups + group;
+    Partial p;
+    p.ml = *(const float2*)(f.part_ml + (part * 32 + r) * 2);
 #pragma unroll
-  for (int k = 0; k < kMine; ++k) sum[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-  bool any = false;
-  for (int i0 = 0; i0 < c.n; i0 += 64) {
-    const int slot = slot_of(shares, c, w, i0 + lane, g);
-    uint64_t there = __ballot(slot >= 0);
-    any |= there != 0;
-    for (; there; there &= there - 1) {
-      const int64_t part = (int64_t)__builtin_amdgcn_readlane(slot, __ffsll((unsigned long long)there) - 1) * kGroups + group;
-      const float2 x = *(const float2*)(f.part_ml + (part * 32 + r) * 2);
-      f32x4 y[kMine];
+    for (int k = 0; k < kMine; ++k) p.x[k] = ((const f32x4*)f.part_o)[(part * kChunks + wave * kMine + k) * 64 + lane];
+    return p;
+  };
+  Partial sum = load(slot0);
+  for (int u0 = unit + h_kv; u0 < units; u0 += 64 * h_kv) {     // shares behind this one, a lane to each
+    const int u = u0 + lane * h_kv, slot = 2 * min(u, units - 1);
+    const Record mine = f.records[slot];
+    const bool same = u < units && mine.rows > 0 && mine.b == block.b && mine.row0 == block.row0 && !mine.begins;
+    uint64_t there = __ballot(same);
+    const bool done = __ballot(same && mine.ends) != 0;
+    auto next = [&] {
+      const int slot = 2 * (u0 + (__ffsll((unsigned long long)there) - 1) * h_kv);
+      there &= there - 1;
+      return slot;
+    };
+    if (there) {
+      Partial p = load(next());
+      for (bool more = true; more;) {
+        more = there != 0;
+        const Partial behind = more ? load(next()) : p;
+        const float top = fmaxf(sum.ml.x, p.ml.x), less = __builtin_amdgcn_exp2f(sum.ml.x - top), by = __builtin_amdgcn_exp2f(p.ml.x - top);
+        sum.ml = make_float2(top, sum.ml.y * less + p.ml.y * by);
 #pragma unroll
-      for (int k = 0; k < kMine; ++k) y[k] = ((const f32x4*)f.part_o)[(part * kChunks + wave * kMine + k) * 64 + lane];
-      const float top = fmaxf(m, x.x), less = __builtin_amdgcn_exp2f(m - top), by = __builtin_amdgcn_exp2f(x.x - top);
-      m = top;
-      l = l * less + x.y * by;
+        for (int k = 0; k < kMine; ++k)
 #pragma unroll
-      for (int k = 0; k < kMine; ++k)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sum[k][e] = __builtin_fmaf(y[k][e], by, sum[k][e] * less);
+          for (int e = 0; e < 4; ++e) sum.x[k][e] = __builtin_fmaf(p.x[k][e], by, sum.x[k][e] * less);
+        p = behind;
+      }
     }
+    if (done) break;
   }
-  const int in = group * 32 + r, row = c.block.row0 + in;
-  if (!any || in >= c.block.rows) return;                       // (a block of which one part had all tiles)
-  const int tok = c.block.s.row0 + row / a.group, head = g * a.group + row % a.group;
+  const int in = group * 32 + r, row = block.row0 + in;
+  if (in >= block.rows) return;
+  const float m = sum.ml.x, l = sum.ml.y;
+  const int tok = block.tok0 + row / a.group, head = g * a.group + row % a.group;
   const float inv = l > 0.f ? 1.f / l : 0.f;
   char* to = a.out + (int64_t)tok * a.ldo + (int64_t)head * D * 2;
 #pragma unroll
   for (int k = 0; k < kMine; ++k) {
-    const bf16x2 lo = __builtin_convertvector((f32x2{sum[k][0] * inv, sum[k][1] * inv}), bf16x2), up = __builtin_convertvector((f32x2{sum[k][2] * inv, sum[k][3] * inv}), bf16x2);
+    const bf16x2 lo = __builtin_convertvector((f32x2{sum.x[k][0] * inv, sum.x[k][1] * inv}), bf16x2), up = __builtin_convertvector((f32x2{sum.x[k][2] * inv, sum.x[k][3] * inv}), bf16x2);
     *(uint2*)(to + ((wave * kMine + k) * 8 + 4 * hi) * 2) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, up));
   }
   if (a.lse && wave == 0 && hi == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? lse_of<bf16_t>(m, l) : -INFINITY;
@@ -426,11 +447,16 @@ template <bool F8, int D> int launch(const ManyArgs& f, dim3 grid, hipStream_t s
 
 }  // namespace
 
-size_t many_workspace(int h_kv, int d) { return split_workspace(2 * (int64_t)grid_of(shape_of(0), h_kv), kRows, d); }
+size_t many_workspace(int h_kv, int d) {
+  const int64_t slots = 2 * (int64_t)grid_of(shape_of(0), h_kv);
+  return split_workspace(slots, kRows, d) + slots * sizeof(Record);
+}
 
 int launch_many(const AttendArgs& a, bool f8, int above, void* ws, hipStream_t st) {
   const ShareShape shape = shape_of(above);
-  const ManyArgs f = split_args<bf16_t>(a, shape, 2 * (int64_t)grid_of(shape, a.cache.h_kv), ws);
+  const int64_t slots = 2 * (int64_t)grid_of(shape, a.cache.h_kv);
+  const SplitArgs<ShareShape> split = split_args<bf16_t>(a, shape, slots, ws);
+  const ManyArgs f{split, (Record*)(split.part_ml + slots * kRows * 2)};
   const dim3 grid((unsigned)grid_of(f.shape, a.cache.h_kv));
   int rc;
   if (a.cache.d == 64)

@@ -133,7 +133,7 @@ struct Part {
   Seq s;
   Keys keys;
   int b, row0, rows, n_vis, from, end;
-  bool alone;               // all of the block's tiles
+  bool ends, alone;         // the block's last tile; all of its tiles
   int slot;                 // else: where the partial result goes
 };
 __device__ __forceinline__ Part part_of(const AttendArgs& a, const ShareShape& sh, const Shares::Block& k, int64_t from, int64_t upto) {
@@ -150,11 +150,20 @@ __device__ __forceinline__ Part part_of(const AttendArgs& a, const ShareShape& s
   const double each = (double)tiles / (double)all;
   p.from = uniform(Shares::tile_at(from, all, tiles, each));
   p.end = uniform(Shares::tile_at(upto, all, tiles, each));
-  p.alone = p.from == 0 && p.end == tiles;
+  p.ends = p.end == tiles;
+  p.alone = p.from == 0 && p.ends;
   return p;
 }
+// What a slot's partial result is of, for the kernel that joins them.  (Found from the lengths there too, that kernel took 5 us more.)
+struct Record {
+  int rows;                 // of the block; 0: the slot holds nothing
+  int b, row0, tok0;        // sequence, the block's first row, the sequence's first token
+  int begins, ends;         // the part has the block's first tile, its last one
+  int pad[2];
+};
 // Every part of the workgroup's share: work(Part).  Parts of no tiles are another one's (or, of a block without keys, its whole).
-template <typename F> __device__ __forceinline__ void for_parts(const AttendArgs& a, const ShareShape& sh, F&& work) {
+template <typename F> __device__ __forceinline__ void for_parts(const AttendArgs& a, const ShareShape& sh, Record* records, F&& work) {
+  if (threadIdx.x == 0) records[2 * blockIdx.x].rows = records[2 * blockIdx.x + 1].rows = 0;
   const Shares shares(a, sh);
   const int w = uniform((int)blockIdx.x / a.cache.h_kv);
   if (w >= shares.workers) return;
@@ -178,55 +187,12 @@ template <typename F> __device__ __forceinline__ void for_parts(const AttendArgs
     const int64_t all = k.w.of(k.r), from = at - k.begin, upto = min(all, end - k.begin);
     Part p = part_of(a, sh, k, from, upto);
     p.slot = 2 * blockIdx.x + (at == begin ? 0 : 1);
-    if (p.from < p.end || (p.alone && from == 0)) work(p);
+    if (p.from < p.end || (p.alone && from == 0)) {
+      if (!p.alone && threadIdx.x == 0) records[p.slot] = Record{p.rows, p.b, p.row0, p.s.row0, p.from == 0, p.ends, {0, 0}};
+      work(p);
+    }
     at = k.begin + upto;
   }
-}
-
-// A cut block, found from the first cut in it (that in front of share w): its parts are shares w - 1, w, ... 's.
-struct Cut {
-  Shares::Block k;          // k.b < 0: nothing to join
-  Part block;               // with all its tiles
-  int tiles, n;             // n: parts
-  double each;
-  bool begins;              // whether share w - 1 begins with it
-};
-__device__ __forceinline__ Cut cut_block(const Shares& shares, int w) {
-  Cut c;
-  c.k.b = -1;
-  if (w < 1 || w >= shares.workers) return c;
-  const int64_t x = uniform(shares.cut(w)), before = uniform(shares.cut(w - 1));
-  const Shares::Block k = shares.block_at(x);
-  if (k.b < 0) return c;
-  const int64_t all = k.w.of(k.r), end = k.begin + all;
-  auto stays = [&](int64_t y) { return y > k.begin && y < end && shares.moved(y, k) == y; };
-  if (!stays(x) || stays(before)) return c;                     // no cut, or not the first in its block
-  c.k = k;
-  c.block = part_of(shares.a, shares.sh, k, 0, all);
-  c.tiles = c.block.end;
-  c.each = (double)c.tiles / (double)all;
-  // Share w - 1 begins with the block if its cut is at the block's begin or moved there: from inside the block, or from the end of the one before.
-  c.begins = before >= k.begin;
-  if (!c.begins && before > 0) {
-    const Shares::Block b = shares.block_at(before);
-    c.begins = b.b >= 0 && shares.moved(before, b) == k.begin;
-  }
-  if (before <= 0) c.begins = k.begin == 0;
-  int last = w;             // the last share whose cut stays inside
-  for (int step = 1 << 9; step; step >>= 1)
-    if (last + step < shares.workers && shares.cut(last + step) < end && end - shares.cut(last + step) > shares.near) last += step;
-  c.n = last - w + 2;
-  return c;
-}
-// Where part i left its result (lanes ask for different ones), -1: nowhere.
-__device__ __forceinline__ int slot_of(const Shares& shares, const Cut& c, int w, int i, int g) {
-  if (i >= c.n) return -1;
-  const int64_t all = c.k.w.of(c.k.r);
-  const int share = w - 1 + i;
-  const int from = i == 0 ? 0 : Shares::tile_at(shares.cut(share) - c.k.begin, all, c.tiles, c.each);
-  const int end = i == c.n - 1 ? c.tiles : Shares::tile_at(shares.cut(share + 1) - c.k.begin, all, c.tiles, c.each);
-  if (from >= end || (from == 0 && end == c.tiles)) return -1;
-  return 2 * (share * shares.a.cache.h_kv + g) + (i == 0 && !c.begins ? 1 : 0);
 }
 
 // On the host: workgroups, their partial results, and whether there are any.
