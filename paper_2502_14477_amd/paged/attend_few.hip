@@ -20,7 +20,43 @@ namespace paged {
 namespace {
 
 constexpr int kRows = 32, kKeys = 32, kWaves = 4;
-using FewArgs = SplitArgs<SliceShape>;
+struct FewArgs : SplitArgs<SliceShape> {
+  Made made;
+};
+// The plan of a call of more than 64 sequences, by one workgroup.
+__global__ __launch_bounds__(1024) void plan_few(FewArgs f) {
+  __shared__ float sums[16];
+  const AttendArgs& a = f.a;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, n_seq = a.batch.n_seq, groups = (n_seq + 63) / 64;
+  const int slice = slice_of(f.shape, a.cache.h_kv, [&](auto&& of) {
+    float sum = 0.f;
+    for (int b = tid; b < n_seq; b += 1024) sum += of(cost_of(a, f.shape, b));
+    sum = wave_sum(sum);
+    __syncthreads();
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    sum = 0.f;
+    for (int w = 0; w < 16; ++w) sum += sums[w];
+    return sum;
+  });
+  if (tid == 0) *f.made.slice = slice;
+  for (int c = wave; c < groups; c += 16) {
+    const int b = c * 64 + lane;
+    const Counts x = b < n_seq ? counts_of(a, cost_of(a, f.shape, b), slice, b) : Counts{0, 0, 0};
+    const uint32_t units = wave_scan(x.units), parts = wave_scan(x.parts), rows = wave_scan(x.rows);
+    if (lane == 63) f.made.upto[c] = Upto{units, parts, rows};
+  }
+  __threadfence_block();
+  __syncthreads();
+  if (wave != 0) return;
+  Upto before{0, 0, 0};
+  for (int c0 = 0; c0 < groups; c0 += 64) {
+    const Upto x = c0 + lane < groups ? f.made.upto[c0 + lane] : Upto{0, 0, 0};
+    const Upto upto{before.units + wave_scan_long(x.units), before.parts + wave_scan_long(x.parts), before.rows + wave_scan_long(x.rows)};
+    if (c0 + lane < groups) f.made.upto[c0 + lane] = upto;
+    before = Upto{lane_long(upto.units, 63), lane_long(upto.parts, 63), lane_long(upto.rows, 63)};
+  }
+}
 template <typename T, bool F8, int D, bool CAP>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D * sizeof(T) > 256 ? 1 : F8 && D * sizeof(T) < 256 ? 3 : 2))) void attend_few(FewArgs f) {
   constexpr bool kBf16 = sizeof(T) == 2;
@@ -38,9 +74,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int g = blockIdx.x % a.cache.h_kv;
-  const Plan plan = plan_of(a, f.shape);
+  const Plan plan = plan_of(a, f.shape, f.made);
   const int slice = plan.slice;
-  const Part at = uniform(part_of(a, f.shape, plan, blockIdx.x / a.cache.h_kv));
+  const Part at = uniform(part_of(a, f.shape, plan, f.made, blockIdx.x / a.cache.h_kv));
   if (at.b < 0) return;
   const Seq s = uniform(sequence(a.batch, at.b));
   const Keys keys = keys_of(a, s);
@@ -386,10 +422,10 @@ template <typename T, int D> __global__ __launch_bounds__(256) void join_few(Few
   __shared__ float2 ml[4];
   const AttendArgs& a = f.a;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const Plan plan = plan_of(a, f.shape);
+  const Plan plan = plan_of(a, f.shape, f.made);
   for (int64_t u = blockIdx.x;; u += gridDim.x) {
     const int g = (int)(u % a.cache.h_kv);
-    const Split at = uniform(split_of(a, f.shape, plan, u / a.cache.h_kv, [](int rows) { return rows; }));
+    const Split at = uniform(split_of(a, f.shape, plan, f.made, u / a.cache.h_kv));
     if (at.b < 0) return;
     const Seq s = uniform(sequence(a.batch, at.b));
     const Keys keys = keys_of(a, s);
@@ -464,10 +500,17 @@ template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows
   const int d = a.cache.d;
   const int64_t most_keys = ((int64_t)a.batch.max_pages << a.batch.page_log2) + a.n_sel;      // of a sequence
   const SliceShape shape = shape_of(d, sizeof(T), f8, most_rows, most_keys <= 4 * kWaves * kKeys);
-  const FewArgs f = split_args<T>(a, shape, most_parts(shape, a.cache.h_kv) * a.cache.h_kv, ws);
+  const int64_t parts = most_parts(shape, a.cache.h_kv) * a.cache.h_kv;
+  const SplitArgs<SliceShape> split = split_args<T>(a, shape, parts, ws);
+  char* const made = (char*)ws + (split_workspace(parts, kRows, d) + kPlanBytes - 1) / kPlanBytes * kPlanBytes;
+  const FewArgs f{split, Made{(int*)made, (Upto*)(made + kPlanBytes)}};
   const int64_t units = most_units(f.shape, a.batch.n_tok, a.batch.n_seq, a.group, a.cache.h_kv) * a.cache.h_kv;
   if (units > INT32_MAX) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: %lld workgroups", (long long)units);
   const dim3 grid((unsigned)units);
+  if (a.batch.n_seq > 64) {
+    plan_few<<<1, 1024, 0, st>>>(f);
+    ESA_LAUNCH_CHECK("plan_few");
+  }
   int rc;
   if (d == 64)
     rc = f8 ? launch<T, true, 64>(f, grid, st) : launch<T, false, 64>(f, grid, st);
@@ -486,8 +529,9 @@ template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows
 
 }  // namespace
 
-size_t few_workspace(int h_kv, int d, int dtype) {
-  return split_workspace(most_parts(shape_of(d, dtype == ESA_F32 ? 4 : 2, true, INT32_MAX, false), h_kv) * h_kv, kRows, d);
+size_t few_workspace(int n_seq, int h_kv, int d, int dtype) {
+  const int64_t parts = most_parts(shape_of(d, dtype == ESA_F32 ? 4 : 2, true, INT32_MAX, false), h_kv) * h_kv;
+  return split_workspace(parts, kRows, d) + 2 * kPlanBytes + ((size_t)n_seq + 63) / 64 * sizeof(Upto);
 }
 
 int launch_few(const AttendArgs& a, bool f8, int dtype, int most_rows, void* ws, hipStream_t st) {

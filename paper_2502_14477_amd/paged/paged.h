@@ -65,6 +65,12 @@ __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false);
   return x;
 }
+__device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane(x, lane); }
+// Sums over the lanes up to each, of numbers below 2^52: two halves of 26 bits, of which 64 fit into 32.
+__device__ __forceinline__ int64_t wave_scan_long(int64_t x) {
+  return (int64_t)wave_scan((uint32_t)x & 0x3FFFFFFu) + ((int64_t)wave_scan((uint32_t)(x >> 26)) << 26);
+}
+__device__ __forceinline__ int64_t lane_long(int64_t x, int lane) { return (int64_t)lane_value((uint32_t)x, lane) | (int64_t)(int)lane_value((uint32_t)(x >> 32), lane) << 32; }
 // What a lane may count, so that 64 of them stay within 32 bits (more than any call has).
 __device__ __forceinline__ uint32_t countable(int64_t n) { return (uint32_t)min(n, (int64_t)1 << 24); }
 struct Found {
@@ -169,13 +175,12 @@ __device__ __forceinline__ int keys_until(const AttendArgs& a, const Seq& s, con
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int64_t uniform(int64_t x) { return (int64_t)(uint32_t)uniform((int)x) | (int64_t)uniform((int)(x >> 32)) << 32; }
 __device__ __forceinline__ Seq uniform(const Seq& s) { return Seq{uniform(s.row0), uniform(s.n), uniform(s.t0)}; }
-__device__ __forceinline__ uint32_t lane_value(uint32_t x, int lane) { return (uint32_t)__builtin_amdgcn_readlane(x, lane); }
 
 int launch_append(const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq, int h, void* out_q, int64_t ldoq,
                   const Batch& b, const Cache& c, bool f8, double base, int dtype, hipStream_t st);
 int launch_plain(const AttendArgs& a, bool f8, int dtype, hipStream_t st);                     // any head size
 // Head sizes 64 and 128.  Sequences of at most most_rows rows (new tokens x query heads of a KV head), and bf16 ones of more than above.
-size_t few_workspace(int h_kv, int d, int dtype);
+size_t few_workspace(int n_seq, int h_kv, int d, int dtype);
 int launch_few(const AttendArgs& a, bool f8, int dtype, int most_rows, void* ws, hipStream_t st);
 size_t many_workspace(int h_kv, int d);
 int launch_many(const AttendArgs& a, bool f8, int above, void* ws, hipStream_t st);

@@ -113,7 +113,7 @@ int esa_append_paged(const void* k, int64_t ldk, const void* v, int64_t ldv, con
 size_t esa_attend_paged_workspace_bytes(int64_t n_tok, int n_seq, int h, int h_kv, int d, int dtype) {
   if (n_tok <= 0 || n_seq <= 0 || h <= 0 || h_kv <= 0 || d <= 0 || h % h_kv != 0) return 256;
   if (d != 64 && d != 128) return 256;
-  return std::max(paged::few_workspace(h_kv, d, dtype), dtype == ESA_BF16 ? paged::many_workspace(h_kv, d) : 0);
+  return std::max(paged::few_workspace(n_seq, h_kv, d, dtype), dtype == ESA_BF16 ? paged::many_workspace(h_kv, d) : 0);
 }
 
 int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* batch, const esa_paged_cache* cache, int64_t l_i, int64_t l_l,

@@ -46,12 +46,6 @@ __device__ __forceinline__ Weights weights_of(const AttendArgs& a, const ShareSh
   return Weights{(rows + sh.rows - 1) / sh.rows, max(keys_until(a, s, keys_of(a, s), min(sh.rows, rows) - 1), 1), max(sh.rows / a.group, 1)};
 }
 
-// Sums over the lanes up to each, of numbers below 2^52: two halves of 26 bits, of which 64 fit into 32.
-__device__ __forceinline__ int64_t wave_scan_long(int64_t x) {
-  return (int64_t)wave_scan((uint32_t)x & 0x3FFFFFFu) + ((int64_t)wave_scan((uint32_t)(x >> 26)) << 26);
-}
-__device__ __forceinline__ int64_t lane_long(int64_t x, int lane) { return (int64_t)lane_value((uint32_t)x, lane) | (int64_t)(int)lane_value((uint32_t)(x >> 32), lane) << 32; }
-
 // The call's blocks of a KV head, and their shares.
 class Shares {
  public:
@@ -75,28 +69,28 @@ class Shares {
   // Where share w begins, before small blocks are left whole.  (Doubles: the same ones wherever it is asked.)
   __device__ __forceinline__ int64_t cut(int w) const { return w >= workers ? total : min((int64_t)(share * (double)w), total); }
 
-  // The block in which weight x < total falls.
+  // The block in which weight x < total falls, from where the last one was found.
   struct Block {
     int b, r;               // sequence, block
     int64_t begin;          // weight in front of it
     Weights w;
   };
-  __device__ __forceinline__ Block block_at(int64_t x) const {
-    const int lane = threadIdx.x & 63;
+  __device__ __forceinline__ Block block_at(int64_t x) {
     int b = 0;
     int64_t base = 0;
     if (a.batch.n_seq > 1) {
-      for (int b0 = 0;; b0 += 64) {
-        const int64_t c = b0 == 0 ? mine : b0 + lane < a.batch.n_seq ? weight(b0 + lane) : 0, upto = wave_scan_long(c) + base;
+      if (x < seen) go_to(0, 0);
+      for (;;) {
+        const int64_t upto = wave_scan_long(mine) + seen;
         const uint64_t past = __ballot(upto > x);
         if (past) {
           const int at = __ffsll((unsigned long long)past) - 1;
           b = b0 + at;
-          base = lane_long(upto - c, at);
+          base = lane_long(upto - mine, at);
           break;
         }
-        base = lane_long(upto, 63);
         if (b0 + 64 >= a.batch.n_seq) return Block{-1, 0, 0, Weights{0, 0, 0}};      // (not with x < total)
+        go_to(b0 + 64, lane_long(upto, 63));
       }
     }
     b = uniform(b);
@@ -124,8 +118,14 @@ class Shares {
   double share;
 
  private:
+  __device__ __forceinline__ void go_to(int first, int64_t in_front) {
+    if (first != b0) mine = first + (int)(threadIdx.x & 63) < a.batch.n_seq ? weight(first + (int)(threadIdx.x & 63)) : 0;
+    b0 = first;
+    seen = uniform(in_front);
+  }
   __device__ __forceinline__ int64_t weight(int b) const { return min(weights_of(a, sh, sequence(a.batch, b)).all(), ((int64_t)1 << 46) - 1); }
-  int64_t mine = 0;
+  int b0 = 0;               // the sequences that the lanes hold, and what weighs in front of them
+  int64_t mine = 0, seen = 0;
 };
 
 // A part of a block's work: keys of tiles [from, end) for its rows.
@@ -164,7 +164,7 @@ struct Record {
 // Every part of the workgroup's share: work(Part).  Parts of no tiles are another one's (or, of a block without keys, its whole).
 template <typename F> __device__ __forceinline__ void for_parts(const AttendArgs& a, const ShareShape& sh, Record* records, F&& work) {
   if (threadIdx.x == 0) records[2 * blockIdx.x].rows = records[2 * blockIdx.x + 1].rows = 0;
-  const Shares shares(a, sh);
+  Shares shares(a, sh);
   const int w = uniform((int)blockIdx.x / a.cache.h_kv);
   if (w >= shares.workers) return;
   int64_t ends[2];          // of the share: its begin and its end

@@ -358,6 +358,35 @@ def test_many_sequences(esa):
     check_attention(pool, turned, out, lse, p_half_step=P_STEP["bf16"])
 
 
+@pytest.mark.parametrize("dtype,held", [("bf16", "e4m3"), ("f32", "same")])
+@pytest.mark.parametrize("n_seq", [64, 65, 128, 1000, 4200])
+def test_sequences_in_groups_of_64(esa, dtype, held, n_seq):
+    """Single tokens, most of them with few keys or idle, some with so many that they are cut."""
+    print("[case] groups", dtype, held, n_seq, flush=True)
+    rng = np.random.default_rng(n_seq)
+    lengths = [(int(rng.integers(0, 40)), int(rng.random() < 0.8)) for _ in range(n_seq)]
+    for b in (0, 3, 62, 63, n_seq // 2, n_seq - 1):
+        lengths[b] = (int(rng.integers(600, 4000)), 1)
+    pool = Pool(lengths, 2, 64, 64, dtype, held, seed=21).fill((1.0, 1.0))
+    q = pool.rows(pool.n_tok, 4)
+    out, lse = esa.esa_attend_paged(q, *pool.batch(), return_lse=True)
+    check_attention(pool, q, out, lse, p_half_step=P_STEP[dtype])
+
+
+@pytest.mark.parametrize("held", ["e4m3", "same"])
+@pytest.mark.parametrize("n_seq", [65, 150, 300])
+def test_chunks_in_groups_of_64(esa, held, n_seq):
+    print("[case] chunk groups", held, n_seq, flush=True)
+    rng = np.random.default_rng(n_seq)
+    lengths = [(int(rng.integers(0, 60)), int(rng.integers(0, 2 if b % 3 else 50))) for b in range(n_seq)]
+    for b in (1, 63, 64, n_seq - 1):
+        lengths[b] = (int(rng.integers(600, 2000)), int(rng.integers(1, 200)))
+    pool = Pool(lengths, 1, 64, 32, "bf16", held, seed=22).fill((1.0, 1.0))
+    q = pool.rows(pool.n_tok, 8)
+    out, lse = esa.esa_attend_paged(q, *pool.batch(), return_lse=True)
+    check_attention(pool, q, out, lse, p_half_step=P_STEP["bf16"])
+
+
 # ---------------------------------------------------------------- as a program uses them
 def test_results_are_the_same_every_time_and_on_every_stream(esa):
     pool = Pool([(3000, 1), (100, 64), (1, 1)], 8, 128, 64, "bf16", "e4m3", seed=16).fill()
