@@ -145,20 +145,22 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
       }
     }
   };
-  // Rows of a tile in one page: keys as soon as those before have left their registers, then values.  Rows that lie anywhere: together.
+  // Keys are requested as soon as those before have left their registers, then values.
   auto load_whole = [&](u32x4 (&x)[kLoads], const char* cache) __attribute__((always_inline)) {
     const char* const from = cache + uniform(place);
     const uint32_t mine = (uint32_t)(lane / kPieces) * tok_bytes + lane % kPieces * 16;
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) x[i] = *(const u32x4*)(from + (uint32_t)(i * kLoadRows) * tok_bytes + mine);
   };
-  auto load_apart = [&]() __attribute__((always_inline)) {
+  auto load_apart = [&](u32x4 (&x)[kLoads], const char* cache) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) {
-      const int64_t from = __shfl(place, i * kLoadRows + lane / kPieces) + lane % kPieces * 16;
-      kr[i] = *(const u32x4*)(a.cache.k + from);
-      vr[i] = *(const u32x4*)(a.cache.v + from);
-    }
+    for (int i = 0; i < kLoads; ++i) x[i] = *(const u32x4*)(cache + __shfl(place, i * kLoadRows + lane / kPieces) + lane % kPieces * 16);
+  };
+  auto load = [&](u32x4 (&x)[kLoads], const char* cache) __attribute__((always_inline)) {
+    if (whole)
+      load_whole(x, cache);
+    else
+      load_apart(x, cache);
   };
   // Staged rows are swizzled: 16-byte piece p of a key row lies in place p ^ (row mod 16), of a value row the 64-byte chunks by
   // row mod 4 (rows of 128 bytes: two share the 256 bytes that the banks cover, and take half the row's number).
@@ -206,12 +208,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
     const Meta m = request_page(t, mine);
     next = request_page(t + kWaves, after);
     find_rows(m);
-    if (whole) {
-      load_whole(kr, a.cache.k);
-      load_whole(vr, a.cache.v);
-    } else {
-      load_apart();
-    }
+    load(kr, a.cache.k);
+    load(vr, a.cache.v);
   }
   for (; t < end; t += kWaves) {
     const int pos = now_pos;
@@ -245,17 +243,12 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
     put_rows(k_st, kr, ks, k_swizzle);
     if (more) {
       find_rows(next);
-      if (whole) load_whole(kr, a.cache.k);
+      load(kr, a.cache.k);
     }
     if (t + 2 * kWaves < end) next = request_page(t + 2 * kWaves, entry);      // in front of the values: the next tile's keys do not wait for them
     entry = request_entry(t + 3 * kWaves);
     put_rows(v_st, vr, vs, v_swizzle);
-    if (more) {
-      if (whole)
-        load_whole(vr, a.cache.v);
-      else
-        load_apart();
-    }
+    if (more) load(vr, a.cache.v);
     wave_fence();
 
     f32x16 x;
