@@ -1,5 +1,5 @@
 // Attention of few rows over a paged cache (decode, drafts; fp32 of any length): 32 rows (new tokens x query heads of a KV head) and a
-// slice of the keys to a workgroup, head sizes 64 and 128.
+// slice of the keys to a workgroup, rows of up to 512 bytes.
 //
 // What counts is that many requests are in flight: a decode step reads every key and value once.  A wave takes tiles of 32 keys by
 // itself, with staging space of its own and no barrier in the loop: a tile's rows arrive in registers, 16 bytes a lane and whole rows
@@ -163,9 +163,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
       load_apart(x, cache);
   };
   // Staged rows are swizzled: 16-byte piece p of a key row lies in place p ^ (row mod 16), of a value row the 64-byte chunks by
-  // row mod 4 (rows of 128 bytes: two share the 256 bytes that the banks cover, and take half the row's number).
-  auto k_swizzle = [](int key) { return kRowBytes >= 256 ? key & 15 : (key >> 1) & 7; };
-  auto v_swizzle = [](int key) { return kRowBytes >= 256 ? (key & 3) << 2 : ((key >> 1) & 1) << 2; };
+  // row mod 4 (of rows of 128 or 64 bytes two or four share the 256 bytes that the banks cover, and take a half or a quarter of the row's number).
+  auto k_swizzle = [](int key) { return kRowBytes >= 256 ? key & 15 : kRowBytes == 128 ? (key >> 1) & 7 : (key >> 2) & 3; };
+  auto v_swizzle = [](int key) { return kRowBytes >= 256 ? (key & 3) << 2 : kRowBytes == 128 ? ((key >> 1) & 1) << 2 : 0; };
   unsigned char* const k_st = stage[wave][0];
   unsigned char* const v_st = stage[wave][1];
   auto put = [&](unsigned char* st, const u32x4& x, float scale, int key, int swizzle) {
@@ -409,7 +409,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
 // Slices of a row joined: a workgroup takes a row, its four waves share the slices.  Only rows of sequences of several slices are gone
 // through, by as many workgroups as the chip holds at most.
 template <typename T, int D> __global__ __launch_bounds__(256) void join_few(FewArgs f) {
-  constexpr int kMine = D / 64;
+  constexpr int kMine = D > 64 ? D / 64 : 1, kLanes = D / kMine;      // a lane's dimensions; lanes that have some
   typedef __attribute__((ext_vector_type(kMine))) float vec;
   __shared__ vec sums[4][64];
   __shared__ float2 ml[4];
@@ -445,7 +445,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void join_few(Few
       for (int i = 0; i < here; i += 8) {
         vec x[8];
 #pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = *(const vec*)(f.part_o + place(i0 + min(i + k, here - 1) * 4) * D + lane * kMine);
+        for (int k = 0; k < 8; ++k) x[k] = *(const vec*)(f.part_o + place(i0 + min(i + k, here - 1) * 4) * D + lane % kLanes * kMine);
 #pragma unroll
         for (int k = 0; k < 8; ++k) sum += x[k] * (i + k < here ? __shfl(by, min(i + k, 63)) : 0.f);
       }
@@ -467,6 +467,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void join_few(Few
     }
     const int tok = s.row0 + at.i / a.group, head = g * a.group + at.i % a.group;
     T* out = (T*)(a.out + (int64_t)tok * a.ldo) + (int64_t)head * D + lane * kMine;
+    if (lane >= kLanes) continue;
 #pragma unroll
     for (int i = 0; i < kMine; ++i) store_f32<T>(out + i, l > 0.f ? sum[i] / l : 0.f);
     if (a.lse && lane == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? lse_of<T>(m, l) : -INFINITY;
@@ -481,12 +482,15 @@ SliceShape shape_of(int d, int es, bool f8, int most_rows, bool shorts) {
   return SliceShape{kRows, kKeys, d * es > 256 ? 256 : f8 && d * es < 256 ? 768 : 512, shorts ? 4 * kWaves : kWaves, most_rows};
 }
 
-template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, hipStream_t st) {
+template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, dim3 join, hipStream_t st) {
   if (f.a.cap > 0.f)
     attend_few<T, F8, D, true><<<grid, 64 * kWaves, 0, st>>>(f);
   else
     attend_few<T, F8, D, false><<<grid, 64 * kWaves, 0, st>>>(f);
   ESA_LAUNCH_CHECK("attend_few");
+  if (join.x == 0) return ESA_OK;
+  join_few<T, D><<<join, 256, 0, st>>>(f);
+  ESA_LAUNCH_CHECK("join_few");
   return ESA_OK;
 }
 template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows, void* ws, hipStream_t st) {
@@ -504,20 +508,15 @@ template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows
     plan_few<<<1, 1024, 0, st>>>(f);
     ESA_LAUNCH_CHECK("plan_few");
   }
-  int rc;
-  if (d == 64)
-    rc = f8 ? launch<T, true, 64>(f, grid, st) : launch<T, false, 64>(f, grid, st);
-  else
-    rc = f8 ? launch<T, true, 128>(f, grid, st) : launch<T, false, 128>(f, grid, st);
-  if (rc != ESA_OK || most_keys <= (int64_t)shape.least * kKeys) return rc;
   const int64_t by_blocks = most_blocks(f.shape, a.batch.n_tok, a.batch.n_seq, a.group) * kRows * a.cache.h_kv, by_tokens = a.batch.n_tok * a.h;
-  const dim3 join((unsigned)std::min<int64_t>(std::min(by_blocks, by_tokens), 2048));
-  if (d == 64)
-    join_few<T, 64><<<join, 256, 0, st>>>(f);
-  else
-    join_few<T, 128><<<join, 256, 0, st>>>(f);
-  ESA_LAUNCH_CHECK("join_few");
-  return ESA_OK;
+  const bool none_cut = most_keys <= (int64_t)shape.least * kKeys;
+  const dim3 join(none_cut ? 0 : (unsigned)std::min<int64_t>(std::min(by_blocks, by_tokens), 2048));
+  if (d == 32) return f8 ? launch<T, true, 32>(f, grid, join, st) : launch<T, false, 32>(f, grid, join, st);
+  if (d == 64) return f8 ? launch<T, true, 64>(f, grid, join, st) : launch<T, false, 64>(f, grid, join, st);
+  if constexpr (sizeof(T) == 2) {
+    if (d == 256) return f8 ? launch<T, true, 256>(f, grid, join, st) : launch<T, false, 256>(f, grid, join, st);
+  }
+  return f8 ? launch<T, true, 128>(f, grid, join, st) : launch<T, false, 128>(f, grid, join, st);
 }
 
 }  // namespace

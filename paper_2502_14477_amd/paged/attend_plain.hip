@@ -1,128 +1,110 @@
-// Attention over a paged cache, plainly: a workgroup has one token and query head and goes through the keys 256 at a time, a thread to a
-// key for the logits, a thread to a dimension for the values.  Any head size, type and shape; reads keys and values once for every
-// query head and token.
+// Attention over a paged cache, plainly: fp32 rows of 256 elements, which leave the matrix-core kernels neither registers nor LDS for a tile.
+// A workgroup has one token and query head, its four waves 64 keys at a time each: a lane finds a key's row, then the wave takes the rows
+// eight at a time, a lane to four dimensions.  Keys and values are read once for every query head and token, out of L2 in the main: that bounds
+// chunks (512 tokens of 32 heads over 4608 keys 16 ms, 5.2 from 8-bit pages); one wave's path through its keys bounds single tokens (one over 32
+// thousand keys 1.6 ms, sixteen over 8 thousand 1.2 ms or 1.7 TB/s, 0.57 from 8-bit pages).  (A thread to a key, for its whole row: 15 ms and 4.1.)
 #include "paged.h"
 
 namespace esa {
 namespace paged {
 namespace {
 
-constexpr int kThreads = 256;
+constexpr int kWaves = 4, kD = 256, kAtOnce = 8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 
-template <typename T, bool F8> __device__ __forceinline__ void load16_f32(const char* p, float (&x)[16]) {
-  if constexpr (F8) {
-    const u32x4 w = *(const u32x4*)p;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float f[4];
-      f8_unpack(w[i], f);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) x[4 * i + j] = f[j];
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = load_f32<T>((const T*)p + i);
-  }
+template <bool F8> __device__ __forceinline__ f32x4 four(const char* row, int lane) {
+  if constexpr (!F8) return ((const f32x4*)row)[lane];
+  float x[4];
+  f8_unpack(((const uint32_t*)row)[lane], x);
+  return f32x4{x[0], x[1], x[2], x[3]};
 }
 
-__device__ __forceinline__ float block_max(float v, float* part) {
-  v = wave_max(v);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = fmaxf(fmaxf(part[0], part[1]), fmaxf(part[2], part[3]));
-  __syncthreads();
-  return v;
-}
-__device__ __forceinline__ float block_sum(float v, float* part) {
-  v = wave_sum(v);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = (part[0] + part[1]) + (part[2] + part[3]);
-  __syncthreads();
-  return v;
-}
-
-template <typename T, bool F8> __global__ __launch_bounds__(kThreads) void attend_plain(AttendArgs a) {
-  __shared__ float q[256], part[4], weight[kThreads], sums[kThreads];
-  __shared__ int64_t place[kThreads];
-  const int tid = threadIdx.x, head = blockIdx.x % a.h, tok = blockIdx.x / a.h, d = a.cache.d, g = head / a.group;
+template <bool F8> __global__ __launch_bounds__(64 * kWaves) void attend_plain(AttendArgs a) {
+  __shared__ f32x4 sums[kWaves][64];
+  __shared__ float2 ml[kWaves];
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), head = blockIdx.x % a.h, tok = blockIdx.x / a.h, g = head / a.group;
   const int b = sequence_with(a.batch, tok);
   if (b < 0) return;
   const Seq s = sequence(a.batch, b);
   const Keys keys = keys_of(a, s);
   const int own = s.t0 + tok - s.row0;
-  if (tid < d) q[tid] = load_f32<T>((const T*)(a.q + tok * a.ldq) + head * d + tid);
-  __syncthreads();
-  const int dim = tid % d, lane_group = tid / d, groups = kThreads / d;
-  float m = -INFINITY, l = 0.f, o = 0.f;
-  for (int j0 = 0; j0 < keys.n; j0 += kThreads) {
-    float x = -INFINITY, by = 1.f;
+  const f32x4 q = ((const f32x4*)(a.q + tok * a.ldq))[head * (kD / 4) + lane];
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  for (int j0 = wave * 64; j0 < keys.n; j0 += 64 * kWaves) {
     int64_t at = 0;
-    if (j0 + tid < keys.n) {
-      const int p = position(keys, j0 + tid, entry_of(a, keys, b, j0 + tid));
+    float k_by = 1.f, v_by = 1.f;
+    bool seen = false;
+    if (j0 + lane < keys.n) {
+      const int p = position(keys, j0 + lane, entry_of(a, keys, b, j0 + lane));
       const int page = p >= 0 && p <= own ? page_of(a.batch, a.cache.n_pages, b, p) : -1;
-      if (page >= 0) {
+      seen = page >= 0;
+      if (seen) {
         at = place_of(a.cache, page, g, p & ((1 << a.batch.page_log2) - 1));
-        float dot = 0.f, k[16];
-        for (int i = 0; i < d; i += 16) {
-          load16_f32<T, F8>(a.cache.k + at + i * (F8 ? 1 : (int)sizeof(T)), k);
-#pragma unroll
-          for (int e = 0; e < 16; ++e) dot = __builtin_fmaf(q[i + e], k[e], dot);
-        }
         if (F8) {
-          dot *= scale_of(a.cache.k_scale[block_of(a.cache, page, g)]);
-          by = scale_of(a.cache.v_scale[block_of(a.cache, page, g)]);
+          k_by = scale_of(a.cache.k_scale[block_of(a.cache, page, g)]);
+          v_by = scale_of(a.cache.v_scale[block_of(a.cache, page, g)]);
         }
-        x = dot * a.scale;
-        if (a.cap > 0.f) x = a.cap * tanhf(x / a.cap);
       }
     }
-    const float top = fmaxf(m, block_max(x, part));
-    if (top == -INFINITY) continue;
-    const float w = x == -INFINITY ? 0.f : expf(x - top), less = m == -INFINITY ? 0.f : expf(m - top);
-    l = l * less + block_sum(w, part);
-    m = top;
-    weight[tid] = w == 0.f ? 0.f : w * by;
-    place[tid] = at;
-    __syncthreads();
-    o *= less;
-    for (int j = lane_group; j < min(kThreads, keys.n - j0); j += groups) {
-      const float p = weight[j];
-      if (p == 0.f) continue;
-      const char* v = a.cache.v + place[j];
-      float x1;
-      if constexpr (F8)
-        x1 = __builtin_amdgcn_cvt_f32_fp8((int)(uint8_t)v[dim], 0);
-      else
-        x1 = load_f32<T>((const T*)v + dim);
-      o = __builtin_fmaf(p, x1, o);
+    const uint64_t all = __ballot(seen);
+    for (int k0 = 0; k0 < 64; k0 += kAtOnce) {
+      if (((all >> k0) & ((1u << kAtOnce) - 1)) == 0) continue;
+      f32x4 k[kAtOnce], v[kAtOnce];
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {                       // (of a key that is not seen: row 0 of the pool, left out below)
+        const int64_t row = lane_long(at, k0 + i);
+        k[i] = four<F8>(a.cache.k + row, lane);
+        v[i] = four<F8>(a.cache.v + row, lane);
+      }
+      float x[kAtOnce], top = m;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        const float dot = wave_sum(__builtin_fmaf(k[i][0], q[0], __builtin_fmaf(k[i][1], q[1], __builtin_fmaf(k[i][2], q[2], k[i][3] * q[3]))));
+        x[i] = dot * (F8 ? __shfl(k_by, k0 + i) : 1.f) * a.scale;
+        if (a.cap > 0.f) x[i] = a.cap * tanhf(x[i] / a.cap);
+        if (!((all >> (k0 + i)) & 1)) x[i] = -INFINITY;
+        top = fmaxf(top, x[i]);
+      }
+      const float less = m == -INFINITY ? 0.f : expf(m - top);
+      m = top;
+      l *= less;
+      o *= less;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        if (!((all >> (k0 + i)) & 1)) continue;                 // whatever its row holds
+        const float p = expf(x[i] - top), by = F8 ? p * __shfl(v_by, k0 + i) : p;
+        l += p;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(by, v[i][e], o[e]);
+      }
     }
-    __syncthreads();
   }
-  sums[tid] = o;
+  sums[wave][lane] = o;
+  if (lane == 0) ml[wave] = make_float2(m, l);
   __syncthreads();
-  if (tid < d) {
-    for (int i = 1; i < groups; ++i) o += sums[tid + i * d];
-    store_f32<T>((T*)(a.out + tok * a.ldo) + head * d + tid, l > 0.f ? o / l : 0.f);
-    if (a.lse && tid == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? m + logf(l) : -INFINITY;
+  if (wave != 0) return;
+  m = fmaxf(fmaxf(ml[0].x, ml[1].x), fmaxf(ml[2].x, ml[3].x));
+  l = 0.f;
+  o = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    const float by = ml[w].x == -INFINITY ? 0.f : expf(ml[w].x - m);
+    l = __builtin_fmaf(ml[w].y, by, l);
+    o += sums[w][lane] * by;
   }
+  ((f32x4*)(a.out + tok * a.ldo))[head * (kD / 4) + lane] = l > 0.f ? o / l : f32x4{0.f, 0.f, 0.f, 0.f};
+  if (a.lse && lane == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? m + logf(l) : -INFINITY;
 }
 
 }  // namespace
 
-int launch_plain(const AttendArgs& a, bool f8, int dtype, hipStream_t st) {
+int launch_plain(const AttendArgs& a, bool f8, hipStream_t st) {
   const dim3 grid((unsigned)(a.batch.n_tok * a.h));
-  if (dtype == ESA_BF16) {
-    if (f8)
-      attend_plain<bf16_t, true><<<grid, kThreads, 0, st>>>(a);
-    else
-      attend_plain<bf16_t, false><<<grid, kThreads, 0, st>>>(a);
-  } else {
-    if (f8)
-      attend_plain<float, true><<<grid, kThreads, 0, st>>>(a);
-    else
-      attend_plain<float, false><<<grid, kThreads, 0, st>>>(a);
-  }
+  if (f8)
+    attend_plain<true><<<grid, 64 * kWaves, 0, st>>>(a);
+  else
+    attend_plain<false><<<grid, 64 * kWaves, 0, st>>>(a);
   ESA_LAUNCH_CHECK("attend_plain");
   return ESA_OK;
 }

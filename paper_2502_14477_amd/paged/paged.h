@@ -178,8 +178,8 @@ __device__ __forceinline__ Seq uniform(const Seq& s) { return Seq{uniform(s.row0
 
 int launch_append(const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq, int h, void* out_q, int64_t ldoq,
                   const Batch& b, const Cache& c, bool f8, double base, int dtype, hipStream_t st);
-int launch_plain(const AttendArgs& a, bool f8, int dtype, hipStream_t st);                     // any head size
-// Head sizes 64 and 128.  Sequences of at most most_rows rows (new tokens x query heads of a KV head), and bf16 ones of more than above.
+int launch_plain(const AttendArgs& a, bool f8, hipStream_t st);                                // fp32
+// Sequences of at most most_rows rows (new tokens x query heads of a KV head), rows of up to 512 bytes; bf16 ones of more than above, head sizes 64 and 128.
 size_t few_workspace(int n_seq, int h_kv, int d, int dtype);
 int launch_few(const AttendArgs& a, bool f8, int dtype, int most_rows, void* ws, hipStream_t st);
 size_t many_workspace(int h_kv, int d);

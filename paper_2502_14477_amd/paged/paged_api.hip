@@ -14,6 +14,8 @@ bool head_size_ok(int d) { return d == 32 || d == 64 || d == 128 || d == 256; }
 bool rows_ok(const void* p, int64_t ld, int64_t row, int64_t es) { return aligned(p, 16) && ld >= row && ld * es % 16 == 0; }
 
 constexpr int kFewRows = 64;      // of a sequence, new tokens x query heads of a KV head: up to two workgroups' share in the kernel for few rows
+bool served_plainly(int d, int dtype) { return dtype == ESA_F32 && d == 256; }
+bool in_many(int d, int dtype) { return dtype == ESA_BF16 && (d == 64 || d == 128); }      // whether the kernel for many rows takes it
 constexpr int64_t kMostKeys = INT32_MAX - 65535;      // counters may run past them by a workgroup's stride
 
 // Whether the pool's three dimensions, in any order, lie behind one another.
@@ -112,8 +114,8 @@ int esa_append_paged(const void* k, int64_t ldk, const void* v, int64_t ldv, con
 
 size_t esa_attend_paged_workspace_bytes(int64_t n_tok, int n_seq, int h, int h_kv, int d, int dtype) {
   if (n_tok <= 0 || n_seq <= 0 || h <= 0 || h_kv <= 0 || d <= 0 || h % h_kv != 0) return 256;
-  if (d != 64 && d != 128) return 256;
-  return std::max(paged::few_workspace(n_seq, h_kv, d, dtype), dtype == ESA_BF16 ? paged::many_workspace(h_kv, d) : 0);
+  if (served_plainly(d, dtype)) return 256;
+  return std::max(paged::few_workspace(n_seq, h_kv, d, dtype), in_many(d, dtype) ? paged::many_workspace(h_kv, d) : 0);
 }
 
 int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* batch, const esa_paged_cache* cache, int64_t l_i, int64_t l_l,
@@ -151,7 +153,7 @@ int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* b
   a.scale = scale;
   a.cap = cap;
   const bool f8 = cache->dtype == ESA_E4M3;
-  if (cache->d != 64 && cache->d != 128) return paged::launch_plain(a, f8, dtype, (hipStream_t)stream);
+  if (served_plainly(cache->d, dtype)) return paged::launch_plain(a, f8, (hipStream_t)stream);
   // The lengths are on the device, the mean is known.  A batch of few rows a sequence in the mean is served by the kernel for few rows, whatever
   // else is in it; other batches by both, one after the other in the same workspace, each of which finds the sequences that are its own.  One that
   // finds none takes 5 us and its join 5 more, while short sequences in the kernel for many rows cost no more than twice their time: where the
@@ -159,7 +161,7 @@ int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* b
   // tokens over 5000 keys, 8 heads: 75.6 us by both, 68.2 by one.  Sixteen tokens of 16 thousand keys beside a long prompt: twice 270 us.)
   hipStream_t st = (hipStream_t)stream;
   const int64_t rows = batch->n_tok * a.group;
-  if (dtype != ESA_BF16 || rows <= (int64_t)kFewRows || rows <= (int64_t)32 * batch->n_seq)
+  if (!in_many(cache->d, dtype) || rows <= (int64_t)kFewRows || rows <= (int64_t)32 * batch->n_seq)
     return paged::launch_few(a, f8, dtype, INT32_MAX, workspace, st);
   const int64_t most_keys = ((int64_t)batch->max_pages << a.batch.page_log2) + a.n_sel;
   const bool both = batch->n_seq > 1 && most_keys > (1 << 17) / ((int64_t)batch->n_seq * cache->h_kv);

@@ -217,6 +217,20 @@ def test_attend_chunk(esa, held, l_c, h, h_kv, d):
     check_attention(pool, q, out, lse, l_i=20, l_l=100, idx=idx, cap=5.0, p_half_step=P_STEP["bf16"])
 
 
+@pytest.mark.parametrize("dtype,held", [("bf16", "e4m3"), ("bf16", "same"), ("f32", "e4m3"), ("f32", "same")])
+@pytest.mark.parametrize("h,h_kv,d", [(8, 2, 32), (4, 1, 256)])
+def test_attend_other_head_sizes(esa, dtype, held, h, h_kv, d):
+    """Head sizes 32 and 256 with sequences that are cut, a chunk among them, and a view."""
+    print("[case] head size", dtype, held, h, h_kv, d, flush=True)
+    pool = Pool([(3500, 1), (0, 0), (700, 70), (40, 3)], h_kv, d, 32, dtype, held, seed=23).fill((1.0, 1.0))
+    q = pool.rows(pool.n_tok, h)
+    out, lse = esa.esa_attend_paged(q, *pool.batch(), return_lse=True)
+    check_attention(pool, q, out, lse, p_half_step=P_STEP[dtype])
+    idx = selections(pool, 20, 100, 333)
+    out, lse = esa.esa_attend_paged(q, *pool.batch(), l_i=20, l_l=100, idx=idx, cap=5.0, return_lse=True)
+    check_attention(pool, q, out, lse, l_i=20, l_l=100, idx=idx, cap=5.0, p_half_step=P_STEP[dtype])
+
+
 # Chunks whose keys are shared out over the workgroups: blocks cut in many places or left whole, blocks of a few rows, groups of heads that
 # do not divide a block, sequences that another kernel serves in between.
 SHARED = {
