@@ -438,7 +438,7 @@ template <int D> __global__ __launch_bounds__(256) void join_many(ManyArgs f) {
   if (a.lse && wave == 0 && hi == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? lse_of<bf16_t>(m, l) : -INFINITY;
 }
 
-ShareShape shape_of(int above) { return ShareShape{kRows, kKeys, 256, 2 * kKeys, 8 * kKeys, 6 * kKeys, above}; }
+ShareShape shape_of(int above) { return ShareShape{kRows, kKeys, 256, 2 * kKeys, 5 * kKeys, 6 * kKeys, above}; }
 
 template <bool F8, int D> int launch(const ManyArgs& f, dim3 grid, hipStream_t st) {
   if (f.a.cap > 0.f)

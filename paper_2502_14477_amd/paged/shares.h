@@ -15,8 +15,9 @@ namespace esa {
 namespace paged {
 
 // Rows of a block, keys of a tile, workgroups at a time; a share is worth its beginning and end from `least` keys on, blocks of up to `whole`
-// keys are not cut, others not within a quarter of a share (`near` keys at least, three times
-// as many at most) of their begin and end.  The kernel serves sequences of more than `above` rows.
+// keys are not cut, others not within a quarter of a share (`near` keys at least, three times as many and half a share at most) of their begin
+// and end.  The kernel serves sequences of more than `above` rows.  (Five tiles for `whole`: with eight and no half a share, 64 tokens behind 300
+// to 2500, 8 heads, took 27 to 37 us, now 21 to 28; 512 behind as many 39 to 54, now 33 to 56.)
 struct ShareShape {
   int rows, keys, places, least, whole, near, above;
 };
@@ -63,7 +64,7 @@ class Shares {
     workers = uniform((int)min(max(worth, (int64_t)1), (int64_t)max(sh.places / a.cache.h_kv, 1)));
     if (total == 0) workers = 0;
     share = (double)total / (double)max(workers, 1);
-    near = (int)fmin(fmax(share * 0.25, (double)sh.near), 3.0 * (double)sh.near);
+    near = (int)fmin(fmin(fmax(share * 0.25, (double)sh.near), 3.0 * (double)sh.near), share * 0.5);
   }
 
   // Where share w begins, before small blocks are left whole.  (Doubles: the same ones wherever it is asked.)
