@@ -70,7 +70,7 @@ typedef struct {
  * (within 2^-100 ... 2^112; what is larger is held as the largest number, NaN as NaN).  A block whose earlier rows belong to the
  * sequence keeps its scale if that is larger and is brought to the new one otherwise; a block that begins with the first appended
  * row takes no heed of what the page held before.  Rows in `dtype` are rounded to the nearest e4m3 number, ties to even.
- * A page that is written to belongs to one sequence of the call (pages that are only read may be shared): rows [start[b],
+ * A page that is written to belongs to one sequence of the call and is listed once (pages that are only read may be shared): rows [start[b],
  * start[b] + new) of it are written, earlier ones only where the scale grows, later ones never.
  * n_tok == 0 or n_seq == 0 is a no-op.  d: 32, 64, 128 or 256.  Rows of k, v, q and out_q start on 16-byte boundaries.
  */
@@ -85,14 +85,14 @@ ESA_API int esa_append_paged(const void* k, int64_t ldk, const void* v, int64_t 
  *   otherwise              [0, i_end), the selected ones and [l_start, p], with i_end and l_start of esa_segments for t0 = start[b]
  *   idx  [n_seq][n_sel] int32, row stride idx_ld: the selected positions; an entry outside [i_end, l_start) is not seen (rows of
  *        different lengths end in -1), one that is listed twice counts twice.  NULL with n_sel = 0.
- *   cap  0: scores as they are; positive: capped
+ *   cap  0: scores as they are; positive: capped (ESA_BF16: at most 4096, as a capped score is off by up to 2^-21 cap)
  *   q, out  [n_tok][h, d], row strides ldq, ldo; rows start on 16-byte boundaries; out does not overlap q
  *   lse  [n_tok][h] fp32 natural-log normaliser, or NULL
  *   workspace esa_attend_paged_workspace_bytes(n_tok, n_seq, h, h_kv, d, dtype) bytes, 256-byte aligned
  * A token that sees nothing (its pages are missing) has out = 0 and lse = -inf.  Rows of out and lse behind cu[n_seq] are left as
  * they were.  Keys and values that are seen must be finite, everything else in the pool may hold anything.
- * n_tok == 0 or n_seq == 0 is a no-op.  d: 32, 64, 128 or 256.  bf16 values may use the whole finite range as long as the products
- * and sums stay finite in fp32.
+ * Scores scale * q.k stay below 2^90 in magnitude, values below 2^90.
+ * n_tok == 0 or n_seq == 0 is a no-op.  d: 32, 64, 128 or 256 (ESA_F32 with 256 by a plain kernel, far slower than the others).
  */
 ESA_API size_t esa_attend_paged_workspace_bytes(int64_t n_tok, int n_seq, int h, int h_kv, int d, int dtype);
 ESA_API int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* batch, const esa_paged_cache* cache, int64_t l_i,

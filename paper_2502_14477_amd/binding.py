@@ -283,7 +283,8 @@ def esa_append_paged(k: torch.Tensor, v: torch.Tensor, cu: torch.Tensor, start: 
     """Appends k, v [n_tok, h_kv, d] to a paged cache, keys turned to their positions (rope_base=None: as they are), and returns q
     [n_tok, h, d] turned likewise (None without q).  Rows cu[b] .. cu[b+1] are sequence b's positions start[b], start[b]+1, ...; cu [n_seq+1],
     start [n_seq] and pages [n_seq, max_pages] are int32.  Caches [n_pages, h_kv, page_size, d] in any order of strides, of k's type or
-    float8_e4m3fn with scales [n_pages, h_kv] uint8 (exponents: 2^(byte - 127)).  `out_q` may be q itself."""
+    float8_e4m3fn with scales [n_pages, h_kv] uint8 (exponents: 2^(byte - 127)).  `out_q` may be q itself.  Rows behind cu[n_seq] are left
+    as they are, undefined in a new tensor."""
     return _native.append_paged(k, v, cu, start, pages, k_cache, v_cache, k_scale, v_scale, q, rope_base, out_q)
 
 
@@ -294,5 +295,5 @@ def esa_attend_paged(q: torch.Tensor, cu: torch.Tensor, start: torch.Tensor, pag
     """Attention of q [n_tok, h, d] over the pages of its sequences, to which the rows' keys and values have been appended (arguments as
     esa_append_paged, `start` from before it) -> out [n_tok, h, d] (and lse [n_tok, h] fp32).  l_i=None: a token sees everything up to
     itself; else the initial, the local and the selected positions idx [n_seq, n_sel] int32 (-1: none), segments as esa_segments.
-    cap > 0: scores become cap * tanh(score / cap)."""
+    cap > 0: scores become cap * tanh(score / cap).  Rows behind cu[n_seq] are left as they are, undefined in new tensors."""
     return _native.attend_paged(q, cu, start, pages, k_cache, v_cache, k_scale, v_scale, l_i, l_l, idx, scale, cap, out, return_lse)

@@ -124,8 +124,11 @@ int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* b
   if (n_sel < 0 || l_i < 0 || l_l < 0) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: negative argument");
   const int rc = common_ok("esa_attend_paged", batch, cache, h, true, n_sel, dtype);
   if (rc != ESA_OK) return rc;
-  if (!(scale > 0.f) || !(scale < 3.0e38f)) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: scale must be positive and finite");
+  // (times log2(e), and divided by a cap, it has to stay finite; the capped scores of bf16 are 2^-22 of the cap off)
+  if (!(scale > 0.f) || !(scale < 1.0e38f)) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: scale must be positive and finite");
   if (!(cap >= 0.f) || !(cap < 3.0e38f)) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: cap must be finite and not negative");
+  if (cap > 0.f && !(scale / cap < 1.0e38f)) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: a cap of %g with a scale of %g", (double)cap, (double)scale);
+  if (cap > 4096.f && dtype == ESA_BF16) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: a cap of %g (bf16: at most 4096)", (double)cap);
   if (batch->n_tok == 0 || batch->n_seq == 0) return ESA_OK;
   if (!q || !out || q == out || (n_sel > 0 && !idx)) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: null pointer, or out over q");
   if (n_sel > 0 && (!aligned(idx, 4) || idx_ld < n_sel)) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: misaligned index list, or rows that overlap");

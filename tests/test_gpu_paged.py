@@ -279,6 +279,16 @@ def test_attend_with_large_and_far_apart_logits(esa, dtype, held):
     check_attention(pool, q, out, lse, cap=30.0, p_half_step=P_STEP[dtype])
 
 
+@pytest.mark.parametrize("dtype,held", [("bf16", "e4m3"), ("bf16", "same"), ("f32", "same")])
+def test_attend_with_large_values_and_caps(esa, dtype, held):
+    """Values of some 2^87, and the largest cap."""
+    pool = Pool([(700, 1), (500, 90)], 2, 128, 64, dtype, held, seed=24).fill((4.0, 2.0 ** 85))
+    q = pool.rows(pool.n_tok, 8, 3.0)
+    for cap in (0.0, 4096.0):
+        out, lse = esa.esa_attend_paged(q, *pool.batch(), cap=cap, return_lse=True)
+        check_attention(pool, q, out, lse, cap=cap, p_half_step=P_STEP[dtype])
+
+
 @pytest.mark.parametrize("dtype,held", [("bf16", "e4m3"), ("bf16", "same"), ("f32", "e4m3")])
 @pytest.mark.parametrize("new", [1, 100])
 def test_attend_with_logits_that_rise_towards_the_end(esa, dtype, held, new):

@@ -104,6 +104,11 @@ def test_attend_refuses():
         assert attend(**change) == -3, change
 
 
+def test_attend_refuses_caps_that_its_arithmetic_cannot_hold():
+    for change in (dict(cap=4097.0), dict(cap=1e-38, scale=1.0), dict(scale=2e38)):
+        assert attend(**change) == -1, change
+
+
 def test_nothing_to_do():
     for b in (batch(n_tok=0, cu=None, start=None, pages=None), batch(n_seq=0, cu=None, start=None, pages=None)):
         assert append(b=b, k=None, v=None, q=None, out_q=None) == 0
