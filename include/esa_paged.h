@@ -27,9 +27,8 @@ extern "C" {
  *                     Powers of two, so that a block grows to a larger scale without its numbers being rounded again (but for
  *                     e4m3's subnormals) and its values are bf16 numbers.  NULL for other types.
  * Rows start on 16-byte boundaries (k, v, and every stride in bytes).  Strides may be in any order ([n_pages, page_size, h_kv, d]
- * is as good); two different elements must not overlap.  max_pages * page_size, the tokens, and the tokens times the heads stay
- * below 2^31 - 2^16; offsets into the pool have 64 bits, a stride is below
- * 2^31 bytes, n_pages * h_kv below 2^31.
+ * is as good); two different elements must not overlap.  max_pages * page_size stays below 2^31 - 2^16, the tokens times the heads
+ * below 2^28 - 2^16; offsets into the pool have 64 bits, a stride is below 2^31 bytes, n_pages * h_kv below 2^31.
  */
 typedef struct {
   void* k;
@@ -72,6 +71,7 @@ typedef struct {
  * row takes no heed of what the page held before.  Rows in `dtype` are rounded to the nearest e4m3 number, ties to even.
  * A page that is written to belongs to one sequence of the call and is listed once (pages that are only read may be shared): rows [start[b],
  * start[b] + new) of it are written, earlier ones only where the scale grows, later ones never.
+ * The cache's k and v are two places, as are its scales (esa_attend_paged reads one place as both as well).
  * n_tok == 0 or n_seq == 0 is a no-op.  d: 32, 64, 128 or 256.  Rows of k, v, q and out_q start on 16-byte boundaries.
  */
 ESA_API int esa_append_paged(const void* k, int64_t ldk, const void* v, int64_t ldv, const void* q, int64_t ldq, int h, void* out_q,

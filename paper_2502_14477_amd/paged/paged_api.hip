@@ -17,6 +17,7 @@ constexpr int kFewRows = 64;      // of a sequence, new tokens x query heads of 
 bool served_plainly(int d, int dtype) { return dtype == ESA_F32 && d == 256; }
 bool in_many(int d, int dtype) { return dtype == ESA_BF16 && (d == 64 || d == 128); }      // whether the kernel for many rows takes it
 constexpr int64_t kMostKeys = INT32_MAX - 65535;      // counters may run past them by a workgroup's stride
+constexpr int64_t kMostRows = (1 << 28) - 65536;      // tokens x heads: what scans over the sequences count stays below 2^24 each
 
 // Whether the pool's three dimensions, in any order, lie behind one another.
 bool apart(const esa_paged_cache& c) {
@@ -45,8 +46,8 @@ int common_ok(const char* name, const esa_paged_batch* b, const esa_paged_cache*
   if (c->page_size != 16 && c->page_size != 32 && c->page_size != 64 && c->page_size != 128)
     ESA_FAIL(ESA_EUNSUPPORTED, "%s: page_size %d (16, 32, 64 or 128)", name, c->page_size);
   if (queries && (h <= 0 || h > 65535 || h % c->h_kv != 0)) ESA_FAIL(ESA_EINVAL, "%s: h=%d is not a multiple of h_kv=%d", name, h, c->h_kv);
-  if ((int64_t)b->max_pages * c->page_size + n_sel > kMostKeys || b->n_tok > kMostKeys / (queries && h > c->h_kv ? h : c->h_kv))
-    ESA_FAIL(ESA_EINVAL, "%s: more than 2^31-2^16 positions or rows", name);
+  if ((int64_t)b->max_pages * c->page_size + n_sel > kMostKeys || b->n_tok > kMostRows / (queries && h > c->h_kv ? h : c->h_kv))
+    ESA_FAIL(ESA_EINVAL, "%s: more than 2^31-2^16 positions, or 2^28-2^16 tokens times heads", name);
   if (b->n_tok == 0 || b->n_seq == 0) return ESA_OK;
   if (!b->cu || !b->start || !b->pages || !c->k || !c->v) ESA_FAIL(ESA_EINVAL, "%s: null pointer", name);
   if (!aligned(b->cu, 4) || !aligned(b->start, 4) || !aligned(b->pages, 4)) ESA_FAIL(ESA_EINVAL, "%s: misaligned pointer", name);
@@ -108,6 +109,8 @@ int esa_append_paged(const void* k, int64_t ldk, const void* v, int64_t ldv, con
   if (q && (!rows_ok(q, ldq, (int64_t)h * cache->d, es) || !rows_ok(out_q, ldoq, (int64_t)h * cache->d, es)))
     ESA_FAIL(ESA_EINVAL, "esa_append_paged: rows of queries start on 16-byte boundaries and do not overlap");
   if (q && q == out_q && ldq != ldoq) ESA_FAIL(ESA_EINVAL, "esa_append_paged: in place needs equal strides");
+  if (cache->k == cache->v || (cache->dtype == ESA_E4M3 && cache->k_scale == cache->v_scale))
+    ESA_FAIL(ESA_EINVAL, "esa_append_paged: keys and values in one place");
   return paged::launch_append(k, ldk, v, ldv, q, ldq, h, out_q, ldoq, batch_of(*batch, cache->page_size), cache_of(*cache),
                               cache->dtype == ESA_E4M3, rope_base, dtype, (hipStream_t)stream);
 }

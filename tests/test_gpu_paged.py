@@ -371,6 +371,35 @@ def test_offsets_beyond_32_bits(esa):
     assert torch.equal(got[0], got[2]) and torch.equal(got[1], got[3])
 
 
+@pytest.mark.parametrize("lengths", [[(2000, 1), (500, 3)], [(100, 90), (40, 70)]], ids=["few rows", "many"])
+def test_attend_with_more_heads_than_workgroups_at_a_time(esa, lengths):
+    pool = Pool(lengths, 600, 64, 64, "bf16", "same", seed=25).fill((1.0, 1.0))
+    q = pool.rows(pool.n_tok, 600)
+    out, lse = esa.esa_attend_paged(q, *pool.batch(), return_lse=True)
+    check_attention(pool, q, out, lse, p_half_step=P_STEP["bf16"])
+
+
+@pytest.mark.parametrize("dtype,held,d", [("bf16", "e4m3", 128), ("bf16", "same", 64), ("f32", "same", 256), ("f32", "e4m3", 32)])
+def test_attend_takes_and_writes_parts_of_larger_tensors(esa, dtype, held, d):
+    """Queries out of a fused projection, results into it, index list and table out of wider ones, another scale; the rest stays as it is."""
+    pool = Pool([(900, 1), (300, 80), (0, 0)], 2, d, 32, dtype, held, seed=26).fill((1.0, 1.0))
+    h, n = 8, pool.n_tok + 3                                      # rows behind the last sequence
+    fused = pool.rows(n, 3 * h)
+    q, out = fused[:, :h], fused[:, h:2 * h]
+    before = fused.clone()
+    idx = selections(pool, 20, 50, 60)
+    wide = torch.full((3, 100), -1, dtype=torch.int32, device="cuda")
+    wide[:, :60] = idx
+    table = torch.full((3, pool.pages.shape[1] + 5), -1, dtype=torch.int32, device="cuda")
+    table[:, :pool.pages.shape[1]] = pool.pages
+    batch = list(pool.batch())
+    batch[2] = table[:, :pool.pages.shape[1]]
+    got, lse = esa.esa_attend_paged(q, *batch, l_i=20, l_l=50, idx=wide[:, :60], scale=0.03, out=out, return_lse=True)
+    assert got is out
+    check_attention(pool, q[:pool.n_tok], out[:pool.n_tok], lse[:pool.n_tok], l_i=20, l_l=50, idx=idx, scale=0.03, p_half_step=P_STEP[dtype])
+    assert torch.equal(fused[:, :h], before[:, :h]) and torch.equal(fused[:, 2 * h:], before[:, 2 * h:]) and torch.equal(out[pool.n_tok:], before[pool.n_tok:, h:2 * h])
+
+
 def test_many_sequences(esa):
     """More sequences than a wave has lanes, some of them idle."""
     rng = np.random.default_rng(14)

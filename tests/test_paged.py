@@ -95,6 +95,18 @@ def test_append_refuses():
         assert b"esa_append_paged" in esa.lib.esa_last_error()
 
 
+def test_both_refuse_more_rows_than_they_count():
+    assert append(b=batch(n_tok=1 << 26)) == -1 and attend(b=batch(n_tok=1 << 26)) == -1
+    assert b"2^28" in esa.lib.esa_last_error()
+
+
+def test_append_refuses_keys_and_values_in_one_place():
+    there = dict(v=2 * FAKE, v_scale=2 * FAKE)
+    for c in (cache(**{**there, "v": FAKE}), cache(**{**there, "v_scale": FAKE})):
+        assert append(c=c) == -1
+        assert b"one place" in esa.lib.esa_last_error()
+
+
 def test_attend_refuses():
     for change in (dict(scale=0.0), dict(scale=float("inf")), dict(scale=float("nan")), dict(cap=-1.0), dict(cap=float("nan")), dict(cap=float("inf")),
                    dict(l_i=-1), dict(l_l=-1), dict(n_sel=-1), dict(n_sel=4, idx=None, idx_ld=4), dict(n_sel=4, idx=FAKE + 2, idx_ld=4),
