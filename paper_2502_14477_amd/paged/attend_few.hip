@@ -21,7 +21,7 @@ namespace esa {
 namespace paged {
 namespace {
 
-constexpr int kRows = 32, kKeys = 32, kWaves = 4;
+constexpr int kRows = SliceShape::rows, kKeys = SliceShape::keys, kWaves = 4;
 struct FewArgs : SplitArgs<SliceShape> {
   Made made;
 };
@@ -481,7 +481,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void join_few(Few
 // keys, 8 bits, 138 us, 1.3 rounds.)  A slice has a tile for every wave; where no sequence can have more than 512 keys, four, so that none is
 // cut and nothing is left to join (301 keys: 10.6 us cut in three, 9.1 in one).
 SliceShape shape_of(int d, int es, bool f8, int most_rows, bool shorts) {
-  return SliceShape{kRows, kKeys, d * es > 256 ? 256 : f8 && d * es < 256 ? 768 : 512, shorts ? 4 * kWaves : kWaves, most_rows};
+  return SliceShape{d * es > 256 ? 256 : f8 && d * es < 256 ? 768 : 512, shorts ? 4 * kWaves : kWaves, most_rows};
 }
 
 template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, dim3 join, hipStream_t st) {

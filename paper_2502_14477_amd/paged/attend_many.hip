@@ -23,7 +23,7 @@ namespace esa {
 namespace paged {
 namespace {
 
-constexpr int kRows = 256, kKeys = 64, kWaves = 8;
+constexpr int kRows = ShareShape::rows, kKeys = ShareShape::keys, kWaves = kRows / 32;
 struct ManyArgs : SplitArgs<ShareShape> {
   Record* records;          // [slot]
   int units;                // workgroups that share the work
@@ -440,7 +440,6 @@ template <int D> __global__ __launch_bounds__(256) void join_many(ManyArgs f) {
   if (a.lse && wave == 0 && hi == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? lse_of<bf16_t>(m, l) : -INFINITY;
 }
 
-ShareShape shape_of(int above) { return ShareShape{kRows, kKeys, 256, 2 * kKeys, 5 * kKeys, 6 * kKeys, above}; }
 
 template <bool F8, int D> int launch(const ManyArgs& f, dim3 grid, hipStream_t st) {
   if (f.a.cap > 0.f)
@@ -454,15 +453,15 @@ template <bool F8, int D> int launch(const ManyArgs& f, dim3 grid, hipStream_t s
 }  // namespace
 
 size_t many_workspace(int h_kv, int d) {
-  const int64_t slots = 2 * (int64_t)grid_of(shape_of(0), h_kv);
+  const int64_t slots = 2 * (int64_t)grid_of(h_kv);
   return split_workspace(slots, kRows, d) + slots * sizeof(Record);
 }
 
 int launch_many(const AttendArgs& a, bool f8, int above, void* ws, hipStream_t st) {
-  const ShareShape shape = shape_of(above);
-  const int64_t slots = 2 * (int64_t)grid_of(shape, a.cache.h_kv);
+  const ShareShape shape{above};
+  const int64_t slots = 2 * (int64_t)grid_of(a.cache.h_kv);
   const SplitArgs<ShareShape> split = split_args<bf16_t>(a, shape, slots, ws);
-  const ManyArgs f{split, (Record*)(split.part_ml + slots * kRows * 2), grid_of(shape, a.cache.h_kv)};
+  const ManyArgs f{split, (Record*)(split.part_ml + slots * kRows * 2), grid_of(a.cache.h_kv)};
   const dim3 grid((unsigned)f.units);
   int rc;
   if (a.cache.d == 64)

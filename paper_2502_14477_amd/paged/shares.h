@@ -5,7 +5,9 @@
 // weighs about as much as its last row sees keys.  All blocks of a KV head, one behind the other, are shared out evenly among as many
 // workgroups as the chip has places for (fewer where there is little to do), wherever that cuts a block: a workgroup goes through the end of
 // one block, some whole ones, and the beginning of another.  What it has of a cut block it leaves as a partial result, at most two of them; a
-// second kernel joins these.  Small blocks are not cut.
+// second kernel joins these.  Small blocks are not cut.  Where there are three workgroups to a block and more, each block is shared out by itself
+// among as many as its weight is worth, evenly: no workgroup has parts of two, and none more than its share by what makes a cut give way
+// otherwise (%s).
 // (Slices of one length for all, so long that the units were about one round: with sequences of 18 to 66 thousand keys the last round was
 // often a few units; chunks of prompts took 1.2 to 1.5 times what their tiles did.)
 #pragma once
@@ -19,7 +21,8 @@ namespace paged {
 // and end.  The kernel serves sequences of more than `above` rows.  (Five tiles for `whole`: with eight and no half a share, 64 tokens behind 300
 // to 2500, 8 heads, took 27 to 37 us, now 21 to 28; 512 behind as many 39 to 54, now 33 to 56.)
 struct ShareShape {
-  int rows, keys, places, least, whole, near, above;
+  static constexpr int rows = 256, keys = 64, places = 256, least = 2 * keys, whole = 5 * keys, near = 6 * keys;
+  int above;
 };
 
 // A sequence's blocks: block r weighs first + r * step.
@@ -52,23 +55,30 @@ class Shares {
  public:
   __device__ __forceinline__ Shares(const AttendArgs& args, const ShareShape& shape) : a(args), sh(shape) {
     const int lane = threadIdx.x & 63;
+    int64_t blocks;
     if (a.batch.n_seq == 1) {
-      total = weights_of(a, sh, uniform(sequence(a.batch, 0))).all();
+      const Weights w = weights_of(a, sh, uniform(sequence(a.batch, 0)));
+      total = w.all();
+      blocks = w.blocks;
     } else {
-      mine = lane < a.batch.n_seq ? weight(lane) : 0;
-      total = lane_long(wave_scan_long(mine), 63);
-      for (int b0 = 64; b0 < a.batch.n_seq; b0 += 64) total += lane_long(wave_scan_long(b0 + lane < a.batch.n_seq ? weight(b0 + lane) : 0), 63);
+      total = blocks = 0;
+      for (int b0 = 0; b0 < a.batch.n_seq; b0 += 64) {
+        const Weights w = b0 + lane < a.batch.n_seq ? weights(b0 + lane) : Weights{0, 0, 0};
+        const int64_t weight = weight_of(w);
+        if (b0 == 0) mine = weight;
+        total += lane_long(wave_scan_long(weight), 63);
+        blocks += lane_value(wave_scan((uint32_t)w.blocks), 63);
+      }
     }
     total = uniform(total);
     const int64_t worth = (total + sh.least - 1) / sh.least;
     workers = uniform((int)min(max(worth, (int64_t)1), (int64_t)max(sh.places / a.cache.h_kv, 1)));
     if (total == 0) workers = 0;
     share = (double)total / (double)max(workers, 1);
+    per_weight = (double)workers / (double)max(total, (int64_t)1);
+    by_block = uniform((int)(3 * blocks <= workers));
     near = (int)fmin(fmin(fmax(share * 0.25, (double)sh.near), 3.0 * (double)sh.near), share * 0.5);
   }
-
-  // Where share w begins, before small blocks are left whole.  (Doubles: the same ones wherever it is asked.)
-  __device__ __forceinline__ int64_t cut(int w) const { return w >= workers ? total : min((int64_t)(share * (double)w), total); }
 
   // The block in which weight x < total falls, from where the last one was found.
   struct Block {
@@ -100,10 +110,22 @@ class Shares {
     const int r = uniform(w.block_at(x - base));
     return Block{b, r, uniform(base + w.upto(r)), w};
   }
-  // A cut in a small block, or near a block's begin or end, is made there instead: a further part of a block costs a workgroup as much as some
-  // tiles.
-  __device__ __forceinline__ int64_t moved(int64_t x, const Block& k) const {
+  // Where share w begins.  (Doubles: the same ones wherever it is asked.)
+  __device__ __forceinline__ int64_t begin_of(int w) {
+    if (w <= 0) return 0;
+    if (w >= workers) return total;
+    const int64_t x = by_block ? middle_of(w) : min((int64_t)(share * (double)w), total);
+    if (x <= 0 || x >= total) return x;
+    const Block k = block_at(x);
+    if (k.b < 0) return x;
     const int64_t all = k.w.of(k.r);
+    if (by_block) {
+      const int first = first_in(k.begin), n = first_in(k.begin + all) - first, i = w - first;
+      if (i <= 0) return k.begin;
+      return i >= n || all <= sh.whole ? k.begin + all : k.begin + (int64_t)((double)all * (double)((float)i * __builtin_amdgcn_rcpf((float)n)));
+    }
+    // A cut in a small block, or near a block's begin or end, is made there instead: a further part of a block costs a workgroup as much as
+    // some tiles.
     if (all <= sh.whole || x - k.begin <= near) return k.begin;
     return k.begin + all - x <= near ? k.begin + all : x;
   }
@@ -115,8 +137,8 @@ class Shares {
   const AttendArgs& a;
   const ShareShape& sh;
   int64_t total;
-  int workers, near;
-  double share;
+  int workers, near, by_block;
+  double share, per_weight;
 
  private:
   __device__ __forceinline__ void go_to(int first, int64_t in_front) {
@@ -124,7 +146,15 @@ class Shares {
     b0 = first;
     seen = uniform(in_front);
   }
-  __device__ __forceinline__ int64_t weight(int b) const { return min(weights_of(a, sh, sequence(a.batch, b)).all(), ((int64_t)1 << 46) - 1); }
+  __device__ __forceinline__ Weights weights(int b) const { return weights_of(a, sh, sequence(a.batch, b)); }
+  static __device__ __forceinline__ int64_t weight_of(const Weights& w) { return min(w.all(), ((int64_t)1 << 46) - 1); }
+  __device__ __forceinline__ int64_t weight(int b) const { return weight_of(weights(b)); }
+  // Where blocks are dealt with one by one: a share belongs to the block that has its middle.  The first share whose middle is not in front of x
+  // (or one beside it, by a rounding: the same one wherever it is asked, and cuts stay in order).
+  __device__ __forceinline__ int64_t middle_of(int w) const { return min((int64_t)(share * ((double)w + 0.5)), total - 1); }
+  __device__ __forceinline__ int first_in(int64_t x) const {
+    return min(max((int)ceil((double)x * per_weight - 0.5), 0), workers);
+  }
   int b0 = 0;               // the sequences that the lanes hold, and what weighs in front of them
   int64_t mine = 0, seen = 0;
 };
@@ -171,12 +201,7 @@ template <typename F> __device__ __forceinline__ void for_parts(const AttendArgs
   int64_t ends[2];          // of the share: its begin and its end
 #pragma unroll 1            // (code that runs once: its instructions come from memory)
   for (int i = 0; i < 2; ++i) {
-    const int64_t x = uniform(shares.cut(w + i));
-    int64_t y = x;
-    if (x > 0 && x < shares.total) {
-      const Shares::Block k = shares.block_at(x);
-      if (k.b >= 0) y = shares.moved(x, k);
-    }
+    const int64_t y = shares.begin_of(w + i);
     ends[0] = i == 0 ? uniform(y) : ends[0];
     ends[1] = uniform(y);
   }
@@ -197,7 +222,7 @@ template <typename F> __device__ __forceinline__ void for_parts(const AttendArgs
 }
 
 // On the host: workgroups, their partial results, and whether there are any.
-static inline int grid_of(const ShareShape& sh, int h_kv) { return (sh.places / h_kv > 1 ? sh.places / h_kv : 1) * h_kv; }
+static inline int grid_of(int h_kv) { return (ShareShape::places / h_kv > 1 ? ShareShape::places / h_kv : 1) * h_kv; }
 
 }  // namespace paged
 }  // namespace esa

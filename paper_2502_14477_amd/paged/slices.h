@@ -14,7 +14,8 @@ namespace paged {
 // Rows of a block, keys of a tile, workgroups at a time; a slice has a multiple of `least` tiles.  The kernel serves sequences of up to `upto`
 // rows.
 struct SliceShape {
-  int rows, keys, target, least, upto;
+  static constexpr int rows = 32, keys = 32;
+  int target, least, upto;
 };
 struct Cost {
   int blocks, tiles;
