@@ -458,7 +458,7 @@ size_t many_workspace(int h_kv, int d) {
 }
 
 int launch_many(const AttendArgs& a, bool f8, int above, void* ws, hipStream_t st) {
-  const ShareShape shape{above};
+  const ShareShape shape{above, std::max(kRows / a.group, 1), (kRows - 1) / a.group};
   const int64_t slots = 2 * (int64_t)grid_of(a.cache.h_kv);
   const SplitArgs<ShareShape> split = split_args<bf16_t>(a, shape, slots, ws);
   const ManyArgs f{split, (Record*)(split.part_ml + slots * kRows * 2), grid_of(a.cache.h_kv)};

@@ -165,11 +165,12 @@ __device__ __forceinline__ bool is_page(const Batch& a, int n_pages, int pos, in
   return pos >= 0 && pos >> a.page_log2 < a.max_pages && (uint32_t)entry < (uint32_t)n_pages;
 }
 
-// Keys that the rows up to `row` of a sequence see at most.
-__device__ __forceinline__ int keys_until(const AttendArgs& a, const Seq& s, const Keys& k, int row) {
+// Keys that the tokens up to `token`, or the rows up to `row`, of a sequence see at most.
+__device__ __forceinline__ int keys_up_to(const AttendArgs& a, const Seq& s, const Keys& k, int token) {
   const int width = a.batch.max_pages << a.batch.page_log2;
-  return k.n - (min(s.t0 + s.n, width) - min(s.t0 + row / a.group + 1, width));
+  return k.n - (min(s.t0 + s.n, width) - min(s.t0 + token + 1, width));
 }
+__device__ __forceinline__ int keys_until(const AttendArgs& a, const Seq& s, const Keys& k, int row) { return keys_up_to(a, s, k, row / a.group); }
 
 // A value that is the same in every lane, where the compiler does not see it.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }

@@ -23,6 +23,7 @@ namespace paged {
 struct ShareShape {
   static constexpr int rows = 256, keys = 64, places = 256, least = 2 * keys, whole = 5 * keys, near = 6 * keys;
   int above;
+  int step, last;           // tokens from a block's first row to the next one's, about, and to its last row's
 };
 
 // A sequence's blocks: block r weighs first + r * step.
@@ -47,7 +48,7 @@ struct Weights {
 __device__ __forceinline__ Weights weights_of(const AttendArgs& a, const ShareShape& sh, const Seq& s) {
   const int rows = s.n * a.group;
   if (rows <= sh.above) return Weights{0, 0, 0};
-  return Weights{(rows + sh.rows - 1) / sh.rows, max(keys_until(a, s, keys_of(a, s), min(sh.rows, rows) - 1), 1), max(sh.rows / a.group, 1)};
+  return Weights{(rows + sh.rows - 1) / sh.rows, max(keys_up_to(a, s, keys_of(a, s), min(sh.last, s.n - 1)), 1), sh.step};
 }
 
 // The call's blocks of a KV head, and their shares.
@@ -74,8 +75,8 @@ class Shares {
     const int64_t worth = (total + sh.least - 1) / sh.least;
     workers = uniform((int)min(max(worth, (int64_t)1), (int64_t)max(sh.places / a.cache.h_kv, 1)));
     if (total == 0) workers = 0;
-    share = (double)total / (double)max(workers, 1);
-    per_weight = (double)workers / (double)max(total, (int64_t)1);
+    share = (double)total * __builtin_amdgcn_rcp((double)max(workers, 1));      // (reciprocals: what is found here in front of all work counts)
+    per_weight = (double)workers * __builtin_amdgcn_rcp((double)max(total, (int64_t)1));
     by_block = uniform((int)(3 * blocks <= workers));
     near = (int)fmin(fmin(fmax(share * 0.25, (double)sh.near), 3.0 * (double)sh.near), share * 0.5);
   }
@@ -178,7 +179,7 @@ __device__ __forceinline__ Part part_of(const AttendArgs& a, const ShareShape& s
   p.n_vis = uniform(keys_until(a, p.s, p.keys, p.row0 + p.rows - 1));
   const int tiles = (p.n_vis + sh.keys - 1) / sh.keys;
   const int64_t all = k.w.of(k.r);
-  const double each = (double)tiles / (double)all;
+  const double each = (double)tiles * __builtin_amdgcn_rcp((double)all);
   p.from = uniform(Shares::tile_at(from, all, tiles, each));
   p.end = uniform(Shares::tile_at(upto, all, tiles, each));
   p.ends = p.end == tiles;
