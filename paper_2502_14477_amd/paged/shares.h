@@ -6,8 +6,8 @@
 // workgroups as the chip has places for (fewer where there is little to do), wherever that cuts a block: a workgroup goes through the end of
 // one block, some whole ones, and the beginning of another.  What it has of a cut block it leaves as a partial result, at most two of them; a
 // second kernel joins these.  Small blocks are not cut.  Where there are three workgroups to a block and more, each block is shared out by itself
-// among as many as its weight is worth, evenly: no workgroup has parts of two, and none more than its share by what makes a cut give way
-// otherwise (%s).
+// among as many as its weight is worth, evenly: no workgroup has parts of two.  (512 tokens over 128, 2048 selected and 2048 local ones, 8 heads of
+// eight blocks: 61.0 us, 66.4 with cuts wherever they fall; 1024 tokens from the beginning, two heads of 32 blocks that grow: 38.7 and 48.3.)
 // (Slices of one length for all, so long that the units were about one round: with sequences of 18 to 66 thousand keys the last round was
 // often a few units; chunks of prompts took 1.2 to 1.5 times what their tiles did.)
 #pragma once
@@ -28,8 +28,10 @@ struct ShareShape {
 
 // A sequence's blocks: block r weighs first + r * step.
 struct Weights {
-  int blocks, first, step;
-  __device__ __forceinline__ int64_t upto(int r) const { return (int64_t)r * first + (int64_t)step * ((int64_t)r * (r - 1) / 2); }      // of r blocks
+  int blocks;
+  int64_t first;
+  int step;
+  __device__ __forceinline__ int64_t upto(int r) const { return r * first + (int64_t)step * ((int64_t)r * (r - 1) / 2); }      // of r blocks
   __device__ __forceinline__ int64_t all() const { return upto(blocks); }
   __device__ __forceinline__ int64_t of(int r) const { return first + (int64_t)r * step; }
   // The block in which weight x < all() falls.
@@ -57,6 +59,7 @@ class Shares {
   __device__ __forceinline__ Shares(const AttendArgs& args, const ShareShape& shape) : a(args), sh(shape) {
     const int lane = threadIdx.x & 63;
     int64_t blocks;
+    int my_blocks = 0;
     if (a.batch.n_seq == 1) {
       const Weights w = weights_of(a, sh, uniform(sequence(a.batch, 0)));
       total = w.all();
@@ -66,7 +69,10 @@ class Shares {
       for (int b0 = 0; b0 < a.batch.n_seq; b0 += 64) {
         const Weights w = b0 + lane < a.batch.n_seq ? weights(b0 + lane) : Weights{0, 0, 0};
         const int64_t weight = weight_of(w);
-        if (b0 == 0) mine = weight;
+        if (b0 == 0) {
+          mine = weight;
+          my_blocks = w.blocks;
+        }
         total += lane_long(wave_scan_long(weight), 63);
         blocks += lane_value(wave_scan((uint32_t)w.blocks), 63);
       }
@@ -75,9 +81,14 @@ class Shares {
     const int64_t worth = (total + sh.least - 1) / sh.least;
     workers = uniform((int)min(max(worth, (int64_t)1), (int64_t)max(sh.places / a.cache.h_kv, 1)));
     if (total == 0) workers = 0;
+    by_block = uniform((int)(3 * blocks <= workers));
+    if (by_block) {
+      extra = uniform((int64_t)((double)total * __builtin_amdgcn_rcp((double)(2 * workers - (int)blocks))));
+      total = uniform(total + blocks * extra);
+      mine += my_blocks * extra;
+    }
     share = (double)total * __builtin_amdgcn_rcp((double)max(workers, 1));      // (reciprocals: what is found here in front of all work counts)
     per_weight = (double)workers * __builtin_amdgcn_rcp((double)max(total, (int64_t)1));
-    by_block = uniform((int)(3 * blocks <= workers));
     near = (int)fmin(fmin(fmax(share * 0.25, (double)sh.near), 3.0 * (double)sh.near), share * 0.5);
   }
 
@@ -107,7 +118,7 @@ class Shares {
     }
     b = uniform(b);
     Weights w = weights_of(a, sh, uniform(sequence(a.batch, b)));
-    w = Weights{uniform(w.blocks), uniform(w.first), uniform(w.step)};
+    w = Weights{uniform(w.blocks), uniform(w.first) + extra, uniform(w.step)};
     const int r = uniform(w.block_at(x - base));
     return Block{b, r, uniform(base + w.upto(r)), w};
   }
@@ -123,7 +134,7 @@ class Shares {
     if (by_block) {
       const int first = first_in(k.begin), n = first_in(k.begin + all) - first, i = w - first;
       if (i <= 0) return k.begin;
-      return i >= n || all <= sh.whole ? k.begin + all : k.begin + (int64_t)((double)all * (double)((float)i * __builtin_amdgcn_rcpf((float)n)));
+      return i >= n || all - extra <= sh.whole ? k.begin + all : k.begin + (int64_t)((double)all * (double)((float)i * __builtin_amdgcn_rcpf((float)n)));
     }
     // A cut in a small block, or near a block's begin or end, is made there instead: a further part of a block costs a workgroup as much as
     // some tiles.
@@ -149,15 +160,20 @@ class Shares {
   }
   __device__ __forceinline__ Weights weights(int b) const { return weights_of(a, sh, sequence(a.batch, b)); }
   static __device__ __forceinline__ int64_t weight_of(const Weights& w) { return min(w.all(), ((int64_t)1 << 46) - 1); }
-  __device__ __forceinline__ int64_t weight(int b) const { return weight_of(weights(b)); }
-  // Where blocks are dealt with one by one: a share belongs to the block that has its middle.  The first share whose middle is not in front of x
-  // (or one beside it, by a rounding: the same one wherever it is asked, and cuts stay in order).
+  __device__ __forceinline__ int64_t weight(int b) const {
+    Weights w = weights(b);
+    w.first += extra;
+    return weight_of(w);
+  }
+  // Where blocks are shared out one by one, each weighs half a share more, so that small ones have one for themselves as well.  A share belongs
+  // to the block that has its middle.  The first share whose middle is not in front of x (or one beside it, by a rounding: the same one wherever
+  // it is asked, and cuts stay in order).
   __device__ __forceinline__ int64_t middle_of(int w) const { return min((int64_t)(share * ((double)w + 0.5)), total - 1); }
   __device__ __forceinline__ int first_in(int64_t x) const {
     return min(max((int)ceil((double)x * per_weight - 0.5), 0), workers);
   }
   int b0 = 0;               // the sequences that the lanes hold, and what weighs in front of them
-  int64_t mine = 0, seen = 0;
+  int64_t mine = 0, seen = 0, extra = 0;
 };
 
 // A part of a block's work: keys of tiles [from, end) for its rows.
