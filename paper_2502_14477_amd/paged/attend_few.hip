@@ -479,7 +479,8 @@ template <typename T, int D> __global__ __launch_bounds__(256) void join_few(Few
 // Workgroups that the chip holds: staging space in LDS and registers leave a compute unit one of fp32 rows of 512 bytes, three of 8-bit rows
 // of 64 elements brought to bf16, two of the others.  (1024 for rows of 64 elements, whatever their registers: eight sequences of 64 thousand
 // keys, 8 bits, 138 us, 1.3 rounds.)  A slice has a tile for every wave; where no sequence can have more than 512 keys, four, so that none is
-// cut and nothing is left to join (301 keys: 10.6 us cut in three, 9.1 in one).
+// cut and nothing is left to join (301 keys: 10.6 us cut in three, 9.1 in one).  Not so fp32, whose products take 3.4 us a tile, where there are few blocks (four
+// sequences of 455 keys, 8 heads: 33 us uncut, 18.6 cut; two of 468 tokens 34 and 40).
 SliceShape shape_of(int d, int es, bool f8, int most_rows, bool shorts) {
   return SliceShape{d * es > 256 ? 256 : f8 && d * es < 256 ? 768 : 512, shorts ? 4 * kWaves : kWaves, most_rows};
 }
@@ -498,7 +499,8 @@ template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, di
 template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows, void* ws, hipStream_t st) {
   const int d = a.cache.d;
   const int64_t most_keys = ((int64_t)a.batch.max_pages << a.batch.page_log2) + a.n_sel;      // of a sequence
-  const SliceShape shape = shape_of(d, sizeof(T), f8, most_rows, most_keys <= 4 * kWaves * kKeys);
+  const bool shorts = most_keys <= 4 * kWaves * kKeys && (sizeof(T) == 2 || a.batch.n_tok * a.h >= 128 * kRows);
+  const SliceShape shape = shape_of(d, sizeof(T), f8, most_rows, shorts);
   const int64_t parts = most_parts(shape, a.cache.h_kv) * a.cache.h_kv;
   const SplitArgs<SliceShape> split = split_args<T>(a, shape, parts, ws);
   char* const made = (char*)ws + (split_workspace(parts, kRows, d) + kPlanBytes - 1) / kPlanBytes * kPlanBytes;

@@ -372,7 +372,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 }
 
 // Cut blocks joined: a workgroup takes 32 rows of a block as a wave has left them, its waves a quarter of the dimensions each.  A block's first
-// part is the last thing that a share leaves, the others are the first that the shares behind it leave.  The next part is requested before one is added.
+// part is the last thing that a share leaves, the others are the first that the shares behind it leave.
 // Workgroups b and b + 8 n share an L2: what one of eight shares has left is read where it was written (33 MB in 9.7 us, 11.3 the other way round).
 template <int D> __global__ __launch_bounds__(256) void join_many(ManyArgs f) {
   constexpr int kChunks = D / 8, kMine = kChunks / 4;           // 16 bytes a lane: of 32 rows, and of them a wave's
@@ -399,6 +399,7 @@ template <int D> __global__ __launch_bounds__(256) void join_many(ManyArgs f) {
     return p;
   };
   Partial sum = load(slot0);
+  constexpr int kAtOnce = 4;                                    // parts on their way together
   for (int u0 = unit + h_kv; u0 < units; u0 += 64 * h_kv) {     // shares behind this one, a lane to each
     const int u = u0 + lane * h_kv, slot = 2 * min(u, units - 1);
     const Record mine = f.records[slot];
@@ -410,18 +411,31 @@ template <int D> __global__ __launch_bounds__(256) void join_many(ManyArgs f) {
       there &= there - 1;
       return slot;
     };
-    if (there) {
-      Partial p = load(next());
-      for (bool more = true; more;) {
-        more = there != 0;
-        const Partial behind = more ? load(next()) : p;
-        const float top = fmaxf(sum.ml.x, p.ml.x), less = __builtin_amdgcn_exp2f(sum.ml.x - top), by = __builtin_amdgcn_exp2f(p.ml.x - top);
-        sum.ml = make_float2(top, sum.ml.y * less + p.ml.y * by);
+    while (there) {
+      Partial p[kAtOnce];
+      bool has[kAtOnce];
+      float top = sum.ml.x;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        has[i] = there != 0;
+        p[i] = load(has[i] ? next() : slot0);
+      }
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i)
+        if (has[i]) top = fmaxf(top, p[i].ml.x);
+      const float less = __builtin_amdgcn_exp2f(sum.ml.x - top);
+      sum.ml = make_float2(top, sum.ml.y * less);
+#pragma unroll
+      for (int k = 0; k < kMine; ++k) sum.x[k] *= less;
+#pragma unroll
+      for (int i = 0; i < kAtOnce; ++i) {
+        if (!has[i]) break;
+        const float by = __builtin_amdgcn_exp2f(p[i].ml.x - top);
+        sum.ml.y = __builtin_fmaf(p[i].ml.y, by, sum.ml.y);
 #pragma unroll
         for (int k = 0; k < kMine; ++k)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) sum.x[k][e] = __builtin_fmaf(p.x[k][e], by, sum.x[k][e] * less);
-        p = behind;
+          for (int e = 0; e < 4; ++e) sum.x[k][e] = __builtin_fmaf(p[i].x[k][e], by, sum.x[k][e]);
       }
     }
     if (done) break;

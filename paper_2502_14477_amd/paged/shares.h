@@ -1,12 +1,13 @@
-// Which part of the attention a workgroup of the kernel for many rows does.  The lengths lie on the device, so every workgroup finds its part from them: a scan over
-// the sequences, a lane to each.
+// Which part of the attention a workgroup of the kernel for many rows does.  The lengths lie on the device, so every workgroup finds its part
+// from them: a scan over the sequences, a lane to each.
 //
 // A sequence's rows (new tokens x query heads of a KV head, numbered token by token) are cut into blocks, its keys into tiles.  A block
 // weighs about as much as its last row sees keys.  All blocks of a KV head, one behind the other, are shared out evenly among as many
 // workgroups as the chip has places for (fewer where there is little to do), wherever that cuts a block: a workgroup goes through the end of
 // one block, some whole ones, and the beginning of another.  What it has of a cut block it leaves as a partial result, at most two of them; a
-// second kernel joins these.  Small blocks are not cut.  Where there are three workgroups to a block and more, each block is shared out by itself
-// among as many as its weight is worth, evenly: no workgroup has parts of two.  (512 tokens over 128, 2048 selected and 2048 local ones, 8 heads of
+// second kernel joins these.  Small blocks are not cut.  Where there are three workgroups to a block and more, or little to do, each block is
+// shared out by itself among as many as its weight is worth, evenly: no workgroup has parts of two.  (512 tokens over 128, 2048 selected and
+// 2048 local ones, 8 heads of
 // eight blocks: 61.0 us, 66.4 with cuts wherever they fall; 1024 tokens from the beginning, two heads of 32 blocks that grow: 38.7 and 48.3.)
 // (Slices of one length for all, so long that the units were about one round: with sequences of 18 to 66 thousand keys the last round was
 // often a few units; chunks of prompts took 1.2 to 1.5 times what their tiles did.)
@@ -16,12 +17,14 @@
 namespace esa {
 namespace paged {
 
-// Rows of a block, keys of a tile, workgroups at a time; a share is worth its beginning and end from `least` keys on, blocks of up to `whole`
-// keys are not cut, others not within a quarter of a share (`near` keys at least, three times as many and half a share at most) of their begin
-// and end.  The kernel serves sequences of more than `above` rows.  (Five tiles for `whole`: with eight and no half a share, 64 tokens behind 300
-// to 2500, 8 heads, took 27 to 37 us, now 21 to 28; 512 behind as many 39 to 54, now 33 to 56.)
+// Rows of a block, keys of a tile, workgroups at a time; a share is worth its beginning and end from `least` keys on, and a block as much besides.
+// Blocks are shared out by themselves where there are three workgroups to each, or one and no more than `little` keys to a workgroup (248 and
+// 100 tokens from the beginning, two heads, capped: 40 us otherwise, now 30).  Blocks of up to `whole` keys are not cut; others, where they are not
+// shared out by themselves, not within a quarter of a share (`near` keys at least, three times as many and half a share at most) of their begin
+// and end.  (Five tiles for `whole`: with eight and no half a share, 64 tokens behind 300 to 2500, 8 heads, took 27 to 37 us, now 21 to 28; 512
+// behind as many 39 to 54, now 31 to 52.)  The kernel serves sequences of more than `above` rows.
 struct ShareShape {
-  static constexpr int rows = 256, keys = 64, places = 256, least = 2 * keys, whole = 5 * keys, near = 6 * keys;
+  static constexpr int rows = 256, keys = 64, places = 256, least = 2 * keys, whole = 5 * keys, near = 6 * keys, little = 8 * keys;
   int above;
   int step, last;           // tokens from a block's first row to the next one's, about, and to its last row's
 };
@@ -78,10 +81,10 @@ class Shares {
       }
     }
     total = uniform(total);
-    const int64_t worth = (total + sh.least - 1) / sh.least;
+    const int64_t worth = (total + sh.least - 1) / sh.least + blocks;
     workers = uniform((int)min(max(worth, (int64_t)1), (int64_t)max(sh.places / a.cache.h_kv, 1)));
     if (total == 0) workers = 0;
-    by_block = uniform((int)(3 * blocks <= workers));
+    by_block = uniform((int)(3 * blocks <= workers || (blocks <= workers && total <= (int64_t)sh.little * workers)));
     if (by_block) {
       extra = uniform((int64_t)((double)total * __builtin_amdgcn_rcp((double)(2 * workers - (int)blocks))));
       total = uniform(total + blocks * extra);
