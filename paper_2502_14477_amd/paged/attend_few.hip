@@ -107,7 +107,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   const uint32_t tok_bytes = a.cache.tok_bytes;
   auto request_entry = [&](int t) { return keys.n_sel && t < end ? entry_of(a, keys, at.b, t * kKeys + r) : 0; };
   auto request_page = [&](int t, int entry) __attribute__((always_inline)) {
-    const int j0 = t * kKeys, late = j0 - keys.i_end - keys.n_sel;
+    const int j0 = t * kKeys, late = j0 - keys.i_end - keys.late;
     Meta m;
     m.pos0 = j0 + kKeys <= keys.i_end ? j0 : late >= 0 ? late + keys.l_start : -1;
     if (j0 + kKeys > n_vis || (m.pos0 & (kKeys - 1)) != 0 || slot_mask + 1 < kKeys) m.pos0 = -1;
@@ -498,7 +498,7 @@ template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, di
 }
 template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows, void* ws, hipStream_t st) {
   const int d = a.cache.d;
-  const int64_t most_keys = ((int64_t)a.batch.max_pages << a.batch.page_log2) + a.n_sel;      // of a sequence
+  const int64_t most_keys = most_keys_of(a);
   const bool shorts = most_keys <= 4 * kWaves * kKeys && (sizeof(T) == 2 || a.batch.n_tok * a.h >= 128 * kRows);
   const SliceShape shape = shape_of(d, sizeof(T), f8, most_rows, shorts);
   const int64_t parts = most_parts(shape, a.cache.h_kv) * a.cache.h_kv;

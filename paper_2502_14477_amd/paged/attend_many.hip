@@ -88,7 +88,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   };
   auto request_pages = [&](int t, const Entries& e) {
     Meta m;
-    const int j0 = t * kKeys, late = j0 - keys.i_end - keys.n_sel;
+    const int j0 = t * kKeys, late = j0 - keys.i_end - keys.late;
     m.pos0 = j0 + kKeys <= keys.i_end ? j0 : late >= 0 ? late + keys.l_start : -1;
     if (j0 + kKeys > n_vis || (m.pos0 & (kKeys - 1)) != 0 || slot_mask + 1 < kKeys) m.pos0 = -1;
     if (m.pos0 >= 0) {
@@ -483,7 +483,7 @@ int launch_many(const AttendArgs& a, bool f8, int above, void* ws, hipStream_t s
   else
     rc = f8 ? launch<true, 128>(f, grid, st) : launch<false, 128>(f, grid, st);
   // (the longest sequence that the table has room for may be too short to be cut; a block weighs up to a block's tokens more than it sees)
-  if (rc != ESA_OK || ((int64_t)a.batch.max_pages << a.batch.page_log2) + a.n_sel + kRows <= shape.whole) return rc;
+  if (rc != ESA_OK || most_keys_of(a) + kRows <= shape.whole) return rc;
   const dim3 join((unsigned)((f.units + 7) / 8 * 8 * (kRows / 32)));
   if (a.cache.d == 64)
     join_many<64><<<join, 256, 0, st>>>(f);

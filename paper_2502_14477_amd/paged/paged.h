@@ -131,9 +131,10 @@ struct AttendArgs {
   float scale, cap;
 };
 
-// A sequence's keys, numbered through [0, i_end), the selected entries, [l_start, t0 + n).
+// A sequence's keys, numbered through [0, i_end), the selected entries, [l_start, t0 + n); in front of the last a gap of numbers that are no
+// keys, so that a multiple of 64 of them is one of the positions too and tiles lie in one page there (sixteen tokens over 128 and 4097 8-bit ones: 35.5 us without, 32.5).
 struct Keys {
-  int t0, i_end, n_sel, l_start, n;
+  int t0, i_end, n_sel, late, l_start, n;      // late: the list's and the gap's
 };
 __device__ __forceinline__ Keys keys_of(const AttendArgs& a, const Seq& s) {
   const int width = a.batch.max_pages << a.batch.page_log2;      // positions from there on have no page
@@ -142,9 +143,12 @@ __device__ __forceinline__ Keys keys_of(const AttendArgs& a, const Seq& s) {
   k.i_end = min(min(a.l_i, s.t0), width);
   k.l_start = min(max(s.t0 - a.l_l, k.i_end), width);
   k.n_sel = k.l_start > k.i_end ? a.n_sel : 0;
-  k.n = k.i_end + k.n_sel + (min(s.t0 + s.n, width) - k.l_start);
+  k.late = k.n_sel + ((k.l_start - k.i_end - k.n_sel) & 63);
+  k.n = k.i_end + k.late + (min(s.t0 + s.n, width) - k.l_start);
   return k;
 }
+// Numbers that a sequence has at most.
+inline int64_t most_keys_of(const AttendArgs& a) { return ((int64_t)a.batch.max_pages << a.batch.page_log2) + (a.n_sel ? a.n_sel + 63 : 0); }
 // The position of key j < k.n, -1 for an entry that is not seen.  In two steps where a kernel requests ahead: a request's result is only
 // looked at when it is needed, so that nothing waits for it in between.
 __device__ __forceinline__ int entry_of(const AttendArgs& a, const Keys& k, int b, int j) {      // as it lies in the list
@@ -155,7 +159,7 @@ __device__ __forceinline__ int position(const Keys& k, int j, int entry) {
   if (j < k.i_end) return j;
   j -= k.i_end;
   if (j < k.n_sel) return entry >= k.i_end && entry < k.l_start ? entry : -1;
-  return j - k.n_sel + k.l_start;
+  return j < k.late ? -1 : j - k.late + k.l_start;
 }
 // The table's entry for a position (any: for -1, or one behind the table, some entry), and whether it is a page.
 __device__ __forceinline__ int page_entry(const Batch& a, int b, int pos) {

@@ -169,8 +169,7 @@ int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* b
   const int64_t rows = batch->n_tok * a.group;
   if (!in_many(cache->d, dtype) || rows <= (int64_t)kFewRows || rows <= (int64_t)32 * batch->n_seq)
     return paged::launch_few(a, f8, dtype, INT32_MAX, workspace, st);
-  const int64_t most_keys = ((int64_t)batch->max_pages << a.batch.page_log2) + a.n_sel;
-  const bool both = batch->n_seq > 1 && most_keys > (1 << 17) / ((int64_t)batch->n_seq * cache->h_kv);
+  const bool both = batch->n_seq > 1 && paged::most_keys_of(a) > (1 << 17) / ((int64_t)batch->n_seq * cache->h_kv);
   if (both) {
     const int few = paged::launch_few(a, f8, dtype, kFewRows, workspace, st);
     if (few != ESA_OK) return few;

@@ -192,7 +192,7 @@ __device__ __forceinline__ Part part_of(const AttendArgs& a, const ShareShape& s
   p.b = k.b;
   p.s = uniform(sequence(a.batch, k.b));
   const Keys q = keys_of(a, p.s);
-  p.keys = Keys{uniform(q.t0), uniform(q.i_end), uniform(q.n_sel), uniform(q.l_start), uniform(q.n)};
+  p.keys = Keys{uniform(q.t0), uniform(q.i_end), uniform(q.n_sel), uniform(q.late), uniform(q.l_start), uniform(q.n)};
   p.row0 = k.r * sh.rows;
   p.rows = min(p.s.n * a.group - p.row0, sh.rows);
   p.n_vis = uniform(keys_until(a, p.s, p.keys, p.row0 + p.rows - 1));
