@@ -479,10 +479,10 @@ template <typename T, int D> __global__ __launch_bounds__(256) void join_few(Few
 // Workgroups that the chip holds: staging space in LDS and registers leave a compute unit one of fp32 rows of 512 bytes, three of 8-bit rows
 // of 64 elements brought to bf16, two of the others.  (1024 for rows of 64 elements, whatever their registers: eight sequences of 64 thousand
 // keys, 8 bits, 138 us, 1.3 rounds.)  A slice has a tile for every wave; where no sequence can have more than 512 keys, four, so that none is
-// cut and nothing is left to join (301 keys: 10.6 us cut in three, 9.1 in one).  Not so fp32, whose products take 3.4 us a tile, where there are few blocks (four
+// cut and nothing is left to join (301 keys: 10.6 us cut in three, 9.3 in one, 9.1 without a look at what slices would come to).  Not so fp32, whose products take 3.4 us a tile, where there are few blocks (four
 // sequences of 455 keys, 8 heads: 33 us uncut, 18.6 cut; two of 468 tokens 34 and 40).
 SliceShape shape_of(int d, int es, bool f8, int most_rows, bool shorts) {
-  return SliceShape{d * es > 256 ? 256 : f8 && d * es < 256 ? 768 : 512, shorts ? 4 * kWaves : kWaves, most_rows};
+  return SliceShape{d * es > 256 ? 256 : f8 && d * es < 256 ? 768 : 512, shorts ? 4 * kWaves : kWaves, most_rows, shorts};
 }
 
 template <typename T, bool F8, int D> int launch(const FewArgs& f, dim3 grid, dim3 join, hipStream_t st) {

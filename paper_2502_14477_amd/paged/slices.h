@@ -16,6 +16,7 @@ namespace paged {
 struct SliceShape {
   static constexpr int rows = 32, keys = 32;
   int target, least, upto;
+  bool uncut;      // no sequence can have more than `least` tiles
 };
 struct Cost {
   int blocks, tiles;
@@ -31,6 +32,7 @@ __device__ __forceinline__ Cost cost_of(const AttendArgs& a, const SliceShape& s
 // rounds were slower, as were shares of the same length that cut sequences anywhere, by what finding them takes in both kernels.)  Counts
 // are fp32: exact where they decide, and every workgroup comes to the same ones.  total(of): the sum of of(cost) over all sequences.
 template <typename F> __device__ __forceinline__ int slice_of(const SliceShape& sh, int h_kv, F&& total) {
+  if (sh.uncut) return sh.least;
   const float all = total([](const Cost& c) { return (float)c.blocks * (float)c.tiles; }) * (float)h_kv;
   const float places = (float)sh.target, mean = fmaxf(all / places, 1.f);
   auto rounded = [&](float x) { return (int)fminf(ceilf(x / (float)sh.least), 1e7f) * sh.least; };
