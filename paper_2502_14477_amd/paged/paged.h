@@ -132,7 +132,8 @@ struct AttendArgs {
 };
 
 // A sequence's keys, numbered through [0, i_end), the selected entries, [l_start, t0 + n); in front of the last a gap of numbers that are no
-// keys, so that a multiple of 64 of them is one of the positions too and tiles lie in one page there (sixteen tokens over 128 and 4097 8-bit ones: 35.5 us without, 32.5).
+// keys, so that a multiple of 64 of them is one of the positions too and tiles lie in one page there (sixteen tokens over 128 and 4097 8-bit
+// ones: 35.5 us without, 32.5).
 struct Keys {
   int t0, i_end, n_sel, late, l_start, n;      // late: the list's and the gap's
 };

@@ -7,8 +7,8 @@
 // one block, some whole ones, and the beginning of another.  What it has of a cut block it leaves as a partial result, at most two of them; a
 // second kernel joins these.  Small blocks are not cut.  Where there are three workgroups to a block and more, or little to do, each block is
 // shared out by itself among as many as its weight is worth, evenly: no workgroup has parts of two.  (512 tokens over 128, 2048 selected and
-// 2048 local ones, 8 heads of
-// eight blocks: 61.0 us, 66.4 with cuts wherever they fall; 1024 tokens from the beginning, two heads of 32 blocks that grow: 38.7 and 48.3.)
+// 2048 local ones, 8 heads of eight blocks: 61.0 us, 66.4 with cuts wherever they fall; 1024 tokens from the beginning, two heads of 32 blocks
+// that grow: 38.7 and 48.3.)
 // (Slices of one length for all, so long that the units were about one round: with sequences of 18 to 66 thousand keys the last round was
 // often a few units; chunks of prompts took 1.2 to 1.5 times what their tiles did.)
 #pragma once
