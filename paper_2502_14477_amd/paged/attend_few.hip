@@ -7,8 +7,9 @@
 // their way into LDS, and the next tile is requested before the products.  So from LDS on there is one kernel for all cache types.
 //   S^T = K Q^T, O^T += V^T P^T: a lane stands for a row, softmax stays in the lane and its opposite in the other half of the wave, and
 // the layout of S^T's accumulator is the second product's operand layout when key 16 s + 8 (j / 4) + 4 half + j % 4 is operand j of step s.
-// bf16: v_mfma_f32_32x32x16_bf16.  A probability enters as two bf16 terms (16 bits) where rows are bf16, which hides behind their loads; as one
-// over 8-bit rows, which come twice as fast: its rounding is then as large as the output's, a sixteenth of a value's in the pool.
+// bf16: v_mfma_f32_32x32x16_bf16.  A probability enters as two bf16 terms (16 bits), so that outputs are as near the exact ones as rounding them
+// to bf16 leaves them: 1.66e-3 rms, 2.5e-3 of them are not the nearest number.  One term: 2.3e-3 and 0.42, which over 8-bit rows takes 271 us
+// for 288 with two (sixteen sequences of 18 to 66 thousand keys) and 104 for 113 (one of 262144); behind bf16 rows two cost nothing.
 // fp32: v_mfma_f32_32x32x2_f32.
 //   HBM bounds: a token over 262144 8-bit keys of 8 heads of 128 elements 100.5 us, 537 MB at 5.6 TB/s but for the join's 5.8 us; sixteen over 18 to 66
 // thousand 271 us, 1500 MB.  Eight over 8 thousand take 24 us and 5.3 (95 MB): some 8 us of it start and end.
@@ -62,7 +63,7 @@ __global__ __launch_bounds__(1024) void plan_few(FewArgs f) {
 template <typename T, bool F8, int D, bool CAP>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D * sizeof(T) > 256 ? 1 : F8 && D * sizeof(T) < 256 ? 3 : 2))) void attend_few(FewArgs f) {
   constexpr bool kBf16 = sizeof(T) == 2;
-  constexpr int kTerms = !kBf16 ? 0 : F8 ? 1 : 2;               // bf16 terms of a probability
+  constexpr bool kLags = kBf16 && F8;                           // the softmax's reference
   constexpr int kRowBytes = D * (int)sizeof(T);                 // of a staged row
   constexpr int kHeldBytes = F8 ? D : kRowBytes;                // of a row in the pool
   constexpr int kPieces = kHeldBytes / 16;                      // lanes that fetch a row
@@ -302,12 +303,14 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
       }
       return sum;
     };
-    if constexpr (kTerms == 1) {
+    if constexpr (kLags) {
       // Against the reference as it stands.  Where a row's exceed it by far (and at first) it moves to its largest logit, and they are taken again.
-      if (__ballot(exponentials() > 256.f)) {
+      float sum = exponentials();
+      if (__ballot(sum > 256.f)) {
         to_reference(fmaxf(m_run, largest()));
-        exponentials();
+        sum = exponentials();
       }
+      l_run += sum;
     } else {
       // (two sets of sixteen registers for them are more than rows of 256 bytes and more on their way leave)
       to_reference(fmaxf(m_run, largest()));
@@ -322,11 +325,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           p[i] = (__bf16)e[8 * kp + i];
-          if constexpr (kTerms == 2) rest[i] = (__bf16)(e[8 * kp + i] - (float)p[i]);
-        }
-        if constexpr (kTerms == 1) {                            // the sum of what the product sees
-#pragma unroll
-          for (int i = 0; i < 8; i += 2) l_run = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p[i], p[i + 1]}, bf16x2{(__bf16)1.f, (__bf16)1.f}, l_run, false);
+          rest[i] = (__bf16)(e[8 * kp + i] - (float)p[i]);
         }
 #pragma unroll
         for (int md = 0; md < kMD; ++md) {
@@ -338,7 +337,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
           const i16x4 lo = part(16 * kp + tr_key), up = part(16 * kp + 8 + tr_key);
           const bf16x8 vf = __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, up, 0, 1, 2, 3, 4, 5, 6, 7));
           o[md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, p, o[md], 0, 0, 0);
-          if constexpr (kTerms == 2) o[md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, rest, o[md], 0, 0, 0);
+          o[md] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, rest, o[md], 0, 0, 0);
         }
       }
     } else {
