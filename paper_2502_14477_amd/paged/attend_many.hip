@@ -3,8 +3,11 @@
 // A workgroup has 256 rows (new tokens x query heads of a KV head), 32 to each of its eight waves, and a slice of the keys, in tiles of 64
 // that the waves share: every thread fetches its part of a tile into registers ahead, brings it to bf16 (8-bit pages: times the block's
 // scale, exactly) and writes it to LDS.  The products are those of the kernel for few rows: S^T = K Q^T, O^T += V^T P^T, a lane stands for a
-// row; a probability is one bf16 term (its rounding is as large as the output's), and the reference of the softmax stays where it is until
-// probabilities sum up to over 2^8, which spares the maxima and the sums' rescaling.
+// row; the reference of the softmax stays where it is until probabilities sum up to over 2^8, which spares the maxima and the sums'
+// rescaling.  A probability enters as one bf16 term at head size 128, whose rounding is as large as the output's, and as two at 64 (16 bits), as
+// the contiguous chunks' do: 2.3e-3 and 1.66e-3 from the exact result.  The second term is half more matrix instructions and a third
+// more vector ones: prompts of up to 1024 tokens behind 16 thousand 420 us (bf16 pages, head size 64; 318 with one);
+// at 128 490 would be 673.
 //   Here the matrix cores bound: 32 instructions a wave and tile, 2048 cycles of a compute unit's four for all waves, and as many for the LDS
 // reads.  What else a wave has to do is 250 instructions a tile, so they have to run beside its own matrix instructions: in a step of 32 keys
 // the scores of the next 32 and the sums of the 32 before are multiplied while the probabilities of these are made and a part of the tile
@@ -24,6 +27,7 @@ namespace paged {
 namespace {
 
 constexpr int kRows = ShareShape::rows, kKeys = ShareShape::keys, kWaves = kRows / 32;
+constexpr int terms_of(int d) { return d == 64 ? 2 : 1; }      // bf16 terms of a probability
 struct ManyArgs : SplitArgs<ShareShape> {
   Record* records;          // [slot]
   int units;                // workgroups that share the work
@@ -177,15 +181,35 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   constexpr int kSlots = kKS;                                   // of a step: as many instructions has each product
   static_assert(kSlots == 2 * kMD, "the products' instructions go in pairs");
   constexpr int kValues = 16 / kSlots;                          // probabilities of a slot
+  constexpr int kTerms = terms_of(D);
+  struct Probabilities {                                        // of 32 keys
+    bf16x8 x[2][kTerms];
+    // Sets a pair of them and adds it to the sum: the sum of what the second product sees.
+    __device__ __forceinline__ void set(int v, float e0, float e1, float& sum) {
+      const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+#pragma unroll
+      for (int n = 0; n < kTerms; ++n) {
+        const __bf16 t0 = (__bf16)e0, t1 = (__bf16)e1;
+        x[v / 8][n][v % 8] = t0;
+        x[v / 8][n][v % 8 + 1] = t1;
+        if constexpr (kTerms == 1) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{t0, t1}, ones, sum, false);
+        if constexpr (kTerms > 1) {
+          if (n == 0) sum += e0 + e1;                           // (all but their last bits)
+          e0 -= (float)t0;
+          e1 -= (float)t1;
+        }
+      }
+    }
+  };
   f32x16 o[kMD], x;
 #pragma unroll
   for (int md = 0; md < kMD; ++md)
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[md][v] = 0.f;
   float m_run = kNoReference, l_run = 0.f;
-  bf16x8 p[2];                                                  // of the 32 keys before
+  Probabilities p;                                              // of the 32 keys before
 #pragma unroll
-  for (int e = 0; e < 8; ++e) p[0][e] = p[1][e] = (__bf16)0.f;
+  for (int v = 0; v < 16; v += 2) p.set(v, 0.f, 0.f, l_run);
 
   const int k_at = r * kKeyStride + hi * 16;
   auto key_part = [&](const unsigned char* from, int i) __attribute__((always_inline)) { return *(const u32x4*)(from + k_at + i * 32); };
@@ -264,26 +288,25 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         if (seen[j & 3][n * 32 + 8 * (v / 4) + 4 * hi + v % 4] > own) x[v] = -INFINITY;
     }
     f32x16 x_next;
-    bf16x8 p_next[2];
-    float sum[2] = {0.f, 0.f};                                  // of the rounded probabilities: what the second product sees
-    const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+    Probabilities p_next;
+    float sum[2] = {0.f, 0.f};
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int s = 0; s < kSlots; ++s) {
       const bf16x8 v_now = joined(vf[s % kAhead][0], vf[s % kAhead][1]);
+      float e[kValues];
       x_next = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, kf[s % kAhead]), __builtin_bit_cast(bf16x8, qf[s]), s ? x_next : zero, 0, 0, 0);
 #pragma unroll
       for (int i = 0; i < kValues; ++i) {
         const int v = s * kValues + i;
-        float e;
         if constexpr (CAP)
-          e = __builtin_amdgcn_exp2f(__builtin_fmaf(-2.f * f.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[v] * f.scale)), f.cap - m_run));      // score_of(x) - m_run
+          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(-2.f * f.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[v] * f.scale)), f.cap - m_run));      // score_of(x) - m_run
         else
-          e = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v], f.scale, -m_run));
-        p_next[v / 8][v % 8] = (__bf16)e;
-        if (i & 1) sum[i / 2 & 1] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p_next[v / 8][v % 8 - 1], p_next[v / 8][v % 8]}, ones, sum[i / 2 & 1], false);
+          e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v], f.scale, -m_run));
+        if (i & 1) p_next.set(v - 1, e[i - 1], e[i], sum[i / 2 & 1]);
       }
-      o[s % kMD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_now, p[s / kMD], o[s % kMD], 0, 0, 0);
+#pragma unroll
+      for (int u = 0; u < kTerms; ++u) o[s % kMD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_now, p.x[s / kMD][u], o[s % kMD], 0, 0, 0);
       if (s + kAhead < kSlots)
         request(k_from, v_from, s + kAhead);
       else
@@ -319,16 +342,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         for (int v = 0; v < 16; ++v) o[md][v] *= less;
       sum[0] = sum[1] = 0.f;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const float e = x[v] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(score_of<bf16_t, CAP>(x[v], f.scale, f.cap) - to);
-        p_next[v / 8][v % 8] = (__bf16)e;
-        if (v & 1) sum[0] = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{p_next[v / 8][v % 8 - 1], p_next[v / 8][v % 8]}, ones, sum[0], false);
+      for (int v = 0; v < 16; v += 2) {
+        float e[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) e[u] = x[v + u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(score_of<bf16_t, CAP>(x[v + u], f.scale, f.cap) - to);
+        p_next.set(v, e[0], e[1], sum[0]);
       }
     }
     l_run += sum[0] + sum[1];
     x = x_next;
-    p[0] = p_next[0];
-    p[1] = p_next[1];
+    p = p_next;
   };
   const int n_tiles = max(end - first, 0);
   for (int j = 0; j < n_tiles; ++j) {
@@ -339,9 +362,11 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   {
     unsigned char* const v_from = v_stage[(n_tiles - 1) & 3] + 32 * kValueStride;
 #pragma unroll
-    for (int s = 0; s < kSlots; ++s)
-      o[s % kMD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(joined(value_part(v_from, s / kMD, s % kMD, 0), value_part(v_from, s / kMD, s % kMD, 1)),
-                                                            p[s / kMD], o[s % kMD], 0, 0, 0);
+    for (int s = 0; s < kSlots; ++s) {
+      const bf16x8 v_now = joined(value_part(v_from, s / kMD, s % kMD, 0), value_part(v_from, s / kMD, s % kMD, 1));
+#pragma unroll
+      for (int u = 0; u < kTerms; ++u) o[s % kMD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_now, p.x[s / kMD][u], o[s % kMD], 0, 0, 0);
+    }
   }
 
   l_run = halves_sum(l_run);
