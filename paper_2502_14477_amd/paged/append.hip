@@ -241,15 +241,16 @@ template <typename T, int J> __global__ __launch_bounds__(kThreads) void append_
   for (int j = 0; j < J; ++j) {
     const int r = j * rows + r0;
     if (r >= lo && r < hi) {
-      store_f8<T>(to + r * a.cache.tok_bytes + i * V, x[j], by);
-      store_f8<T>(to + r * a.cache.tok_bytes + half + i * V, y[j], by);
+      char* const row = to + row_at(a.cache, r);
+      store_f8<T>(row + i * V, x[j], by);
+      store_f8<T>(row + half + i * V, y[j], by);
     }
   }
   if (lo > 0 && byte > old) {               // the sequence's earlier rows come to the larger scale
     const float less = scale_of(max(127 - (byte - old), 1));
     const int pieces = d / 16;
     for (int e = tid; e < lo * pieces; e += kThreads) {
-      u32x4* p = (u32x4*)(to + (e / pieces) * a.cache.tok_bytes + e % pieces * 16);
+      u32x4* p = (u32x4*)(to + row_at(a.cache, e / pieces) + e % pieces * 16);
       u32x4 w = *p;
 #pragma unroll
       for (int n = 0; n < 4; ++n) {

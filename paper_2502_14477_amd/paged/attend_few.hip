@@ -100,7 +100,8 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   }
 
   // Lane r stands for key r of a tile: its position (INT32_MAX: not seen), its row's place in the pool, its scales.  Entries of the index list
-  // are requested three tiles ahead, of the page table two, rows one.  A tile that lies in one page is found once for the whole wave.
+  // are requested three tiles ahead, of the page table two, rows one.  A tile that lies in one page, its rows within 32 bits of each other, is
+  // found once for the whole wave.
   struct Meta {
     int pos0, pos, entry;                                       // pos0: of the tile's first key where it lies in one page, else -1
   };
@@ -111,7 +112,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
     const int j0 = t * kKeys, late = j0 - keys.i_end - keys.late;
     Meta m;
     m.pos0 = j0 + kKeys <= keys.i_end ? j0 : late >= 0 ? late + keys.l_start : -1;
-    if (j0 + kKeys > n_vis || (m.pos0 & (kKeys - 1)) != 0 || slot_mask + 1 < kKeys) m.pos0 = -1;
+    if (j0 + kKeys > n_vis || (m.pos0 & (kKeys - 1)) != 0 || a.cache.close < kKeys) m.pos0 = -1;
     m.pos = -1;
     if (m.pos0 >= 0) {
       m.entry = page_entry(a.batch, at.b, m.pos0);

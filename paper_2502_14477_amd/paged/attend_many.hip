@@ -69,7 +69,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 
   // ---- staging: a thread has piece tid % kPieces of rows tid / kPieces + i kPass of the tile's keys, then values
   // Entries of the index list are requested three tiles ahead, of the page table two, rows one; behind the slice's last tile something is
-  // fetched that nobody reads.  A tile that lies in one page is found once for the whole workgroup.
+  // fetched that nobody reads.  A tile that lies in one page, its rows within 32 bits of each other, is found once for the whole workgroup.
   const int piece = tid % kPieces, my_row = tid / kPieces;
   auto key_of = [&](int i) { return kPass <= kKeys ? my_row + i * kPass % kKeys : my_row % kKeys; };
   auto is_value = [&](int i) { return kPass <= kKeys ? i >= kKeys / kPass : my_row >= kKeys; };
@@ -94,7 +94,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     Meta m;
     const int j0 = t * kKeys, late = j0 - keys.i_end - keys.late;
     m.pos0 = j0 + kKeys <= keys.i_end ? j0 : late >= 0 ? late + keys.l_start : -1;
-    if (j0 + kKeys > n_vis || (m.pos0 & (kKeys - 1)) != 0 || slot_mask + 1 < kKeys) m.pos0 = -1;
+    if (j0 + kKeys > n_vis || (m.pos0 & (kKeys - 1)) != 0 || a.cache.close < kKeys) m.pos0 = -1;
     if (m.pos0 >= 0) {
       m.entry[0] = page_entry(a.batch, at.b, m.pos0);
     } else {

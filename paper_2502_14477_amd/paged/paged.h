@@ -17,11 +17,14 @@ struct Cache {
   uint8_t *k_scale, *v_scale;               // [n_pages][h_kv]
   uint32_t page_bytes, head_bytes, tok_bytes;
   int n_pages, h_kv, d;
+  int close;                                // positions of a page whose rows lie within 2^32 bytes: all of them, or 0 where they span more
 };
 // A row's place in the pool, and a block's number (the host keeps strides and the number of blocks within 32 bits; one instruction each).
 __device__ __forceinline__ int64_t place_of(const Cache& c, int page, int g, int slot) {
   return (int64_t)((uint64_t)(uint32_t)page * c.page_bytes + (uint64_t)(uint32_t)g * c.head_bytes + (uint64_t)(uint32_t)slot * c.tok_bytes);
 }
+// What a row lies behind its block's first.
+__device__ __forceinline__ int64_t row_at(const Cache& c, int slot) { return (int64_t)((uint64_t)(uint32_t)slot * c.tok_bytes); }
 __device__ __forceinline__ uint32_t block_of(const Cache& c, int page, int g) { return (uint32_t)page * (uint32_t)c.h_kv + (uint32_t)g; }
 
 // A sequence's rows, clamped so that no content of the arrays leads out of the buffers.

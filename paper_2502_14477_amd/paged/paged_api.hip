@@ -85,6 +85,7 @@ paged::Cache cache_of(const esa_paged_cache& c) {
   x.page_bytes = (uint32_t)(c.page_stride * es);
   x.head_bytes = (uint32_t)(c.head_stride * es);
   x.tok_bytes = (uint32_t)(c.tok_stride * es);
+  x.close = c.tok_stride * es * c.page_size <= (int64_t)UINT32_MAX ? c.page_size : 0;
   x.n_pages = c.n_pages;
   x.h_kv = c.h_kv;
   x.d = c.d;

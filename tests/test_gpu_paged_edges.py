@@ -1,0 +1,73 @@
+"""Calls of the paged cache at the ends of what its header allows."""
+import pytest
+import torch
+
+from paged_support import TYPES, Pool
+
+pytestmark = pytest.mark.gpu
+BASE = 5e5
+
+
+@pytest.fixture(scope="module")
+def esa():
+    import paper_2502_14477_amd as lib
+    return lib
+
+
+def step_and_look(esa, batch, k, v, q, lengths):
+    """A chunk of every sequence, then a token of each: turned queries, the attention of both."""
+    turned = esa.esa_append_paged(k, v, *batch, q=q, rope_base=BASE)
+    out, lse = esa.esa_attend_paged(turned, *batch, return_lse=True)
+    ends = torch.tensor(lengths).cumsum(0) - 1
+    cu = torch.arange(len(lengths) + 1, dtype=torch.int32, device="cuda")
+    start = torch.tensor([n - 1 for n in lengths], dtype=torch.int32, device="cuda")
+    one, one_lse = esa.esa_attend_paged(turned[ends.tolist()].contiguous(), cu, start, *batch[2:], return_lse=True)
+    return turned, out, lse, one, one_lse
+
+
+@pytest.mark.parametrize("dtype,held,d", [("bf16", "e4m3", 128), ("bf16", "same", 64), ("f32", "e4m3", 64)])
+@pytest.mark.parametrize("order", ["tokens", "heads"])
+def test_rows_and_heads_beyond_32_bits(esa, dtype, held, d, order):
+    """A pool whose outermost dimension is a page's positions, or its heads: rows of one page lie up to 12 GB apart."""
+    print("[case] far rows", dtype, held, d, order, flush=True)
+    lengths, page, h_kv = [300, 200], 64, 8
+    pool = Pool([(0, n) for n in lengths], h_kv, d, page, dtype, held, seed=41)
+    at = torch.uint8 if held == "e4m3" else TYPES[dtype]
+    tok_bytes = 190 << 20                                        # 24 of them are more than 2^32
+    n_pages = tok_bytes // (h_kv * d * torch.empty(0, dtype=at).element_size())
+    shape, back = {"tokens": ((page, n_pages, h_kv, d), (1, 2, 0, 3)), "heads": ((h_kv, n_pages, page, d), (1, 0, 2, 3))}[order]
+    caches = [torch.empty(shape, dtype=at, device="cuda").permute(back) for _ in "kv"]
+    if held == "e4m3":
+        caches = [c.view(torch.float8_e4m3fn) for c in caches]
+    scales = [torch.empty((n_pages, h_kv), dtype=torch.uint8, device="cuda") if held == "e4m3" else None for _ in "kv"]
+    far = torch.where(pool.pages < pool.n_pages, n_pages - 1 - pool.pages, pool.pages)
+    k, v, q = pool.rows(pool.n_tok, h_kv), pool.rows(pool.n_tok, h_kv), pool.rows(pool.n_tok, 16)
+    near = step_and_look(esa, pool.batch(), k, v, q, lengths)
+    there = step_and_look(esa, (pool.cu, pool.start, far, *caches, *scales), k, v, q, lengths)
+    # one order of summation, whichever way a tile's rows are found
+    for a, b in zip(near, there):
+        assert torch.equal(a, b)
+    used = pool.table[0, :len(range(0, lengths[0], page)) - 1]   # whole pages of the first sequence: what the pools hold is the same
+    for a, b in zip(pool.caches, caches):
+        raw = [c.view(torch.uint8) if held == "e4m3" else c for c in (a, b)]
+        rows = torch.from_numpy(used).long().cuda()
+        assert torch.equal(raw[0][rows], raw[1][n_pages - 1 - rows])
+
+
+def test_a_growing_scale_reaches_rows_beyond_32_bits(esa):
+    """Earlier rows of a block are brought to a larger scale wherever they lie."""
+    page, h_kv, d = 64, 8, 128
+    pool = Pool([(0, 60)], h_kv, d, page, "bf16", "e4m3", seed=42)
+    n_pages = (190 << 20) // (h_kv * d)
+    caches = [torch.empty((page, n_pages, h_kv, d), dtype=torch.uint8, device="cuda").permute(1, 2, 0, 3).view(torch.float8_e4m3fn) for _ in "kv"]
+    scales = [torch.empty((n_pages, h_kv), dtype=torch.uint8, device="cuda") for _ in "kv"]
+    far = torch.where(pool.pages < pool.n_pages, n_pages - 1 - pool.pages, pool.pages)
+    k, v = pool.rows(60, h_kv), pool.rows(60, h_kv)
+    k[55:] *= 64
+    for cu, start, rows in (([0, 50], [0], slice(0, 50)), ([0, 10], [50], slice(50, 60))):
+        cu, start = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (cu, start))
+        for batch in ((cu, start, *pool.batch()[2:]), (cu, start, far, *caches, *scales)):
+            esa.esa_append_paged(k[rows], v[rows], *batch, rope_base=BASE)
+    at = int(pool.table[0, 0])
+    for a, b, sa, sb in zip(pool.caches, caches, pool.scales, scales):
+        assert torch.equal(a.view(torch.uint8)[at, :, :60], b.view(torch.uint8)[n_pages - 1 - at, :, :60]) and torch.equal(sa[at], sb[n_pages - 1 - at])
