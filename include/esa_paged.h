@@ -25,7 +25,8 @@ extern "C" {
  *   page_size  16, 32, 64 or 128
  *   k_scale, v_scale  ESA_E4M3: [n_pages, h_kv] bytes (E8M0): a block's values are its e4m3 numbers times 2^(byte - 127).
  *                     Powers of two, so that a block grows to a larger scale without its numbers being rounded again (but for
- *                     e4m3's subnormals) and its values are bf16 numbers.  NULL for other types.
+ *                     e4m3's subnormals) and its values are bf16 numbers (those below 2^-126, of bytes 0 to 9, may count as 0 where
+ *                     rows are bf16).  255: the block holds nothing.  NULL for other types.
  * Rows start on 16-byte boundaries (k, v, and every stride in bytes).  Strides may be in any order ([n_pages, page_size, h_kv, d]
  * is as good); two different elements must not overlap.  max_pages * page_size stays below 2^31 - 2^16, the tokens times the heads
  * below 2^28 - 2^16; offsets into the pool have 64 bits, a stride is below 2^31 bytes, n_pages * h_kv below 2^31.
@@ -68,7 +69,7 @@ typedef struct {
  * ESA_E4M3: a block's scale is the smallest power of two with which 448, e4m3's largest number, covers the rows appended to it
  * (within 2^-100 ... 2^112; what is larger is held as the largest number, NaN as NaN).  A block whose earlier rows belong to the
  * sequence keeps its scale if that is larger and is brought to the new one otherwise; a block that begins with the first appended
- * row takes no heed of what the page held before.  Rows in `dtype` are rounded to the nearest e4m3 number, ties to even.
+ * row, or whose byte is 255, takes no heed of what the page held before.  Rows in `dtype` are rounded to the nearest e4m3 number, ties to even.
  * A page that is written to belongs to one sequence of the call and is listed once (pages that are only read may be shared): rows [start[b],
  * start[b] + new) of it are written, earlier ones only where the scale grows, later ones never.
  * The cache's k and v are two places, as are its scales (esa_attend_paged reads one place as both as well).

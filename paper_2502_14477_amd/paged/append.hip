@@ -194,7 +194,7 @@ template <typename T, int J> __global__ __launch_bounds__(kThreads) void append_
   const int page = page_of(a.batch, a.cache.n_pages, f.b, pos0);
   if (page < 0) return;
   uint8_t* scale = (keys ? a.cache.k_scale : a.cache.v_scale) + block_of(a.cache, page, g);
-  const int old = lo > 0 ? *scale : 0;
+  const int held = lo > 0 ? *scale : kNoScale, old = held == kNoScale ? 0 : held;
   const int d = a.cache.d, half = d >> 1, vecs = half / V, rows = kThreads / vecs, i = tid % vecs, r0 = tid / vecs;
   const int64_t ld = keys ? a.ldk : a.ldv;
   const char* from = (keys ? a.k : a.v) + ((int64_t)s.row0 + pos0 - s.t0) * ld + ((int64_t)g * d + i * V) * (int)sizeof(T);
@@ -236,7 +236,7 @@ template <typename T, int J> __global__ __launch_bounds__(kThreads) void append_
   m = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3]));
   const int byte = max(scale_byte(m), old);
   char* to = (keys ? a.cache.k : a.cache.v) + place_of(a.cache, page, g, 0);
-  const float by = scale_of(254 - byte);
+  const float by = power_of(254 - byte);
 #pragma unroll
   for (int j = 0; j < J; ++j) {
     const int r = j * rows + r0;
@@ -246,7 +246,7 @@ template <typename T, int J> __global__ __launch_bounds__(kThreads) void append_
       store_f8<T>(row + half + i * V, y[j], by);
     }
   }
-  if (lo > 0 && byte > old) {               // the sequence's earlier rows come to the larger scale
+  if (held != kNoScale && byte > old) {     // the sequence's earlier rows come to the larger scale
     const float less = scale_of(max(127 - (byte - old), 1));
     const int pieces = d / 16;
     for (int e = tid; e < lo * pieces; e += kThreads) {

@@ -99,7 +99,10 @@ template <typename F> __device__ __forceinline__ Found find(int n_seq, int64_t u
 // ---------------------------------------------------------------- 8-bit blocks
 constexpr float kF8Max = 448.f;
 constexpr int kScaleLow = 27, kScaleHigh = 239;      // 2^-100, 2^112
-__device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }      // 2^(byte - 127)
+constexpr int kNoScale = 255;                        // a block that holds nothing
+// 2^(byte - 127) as the conversions take it: by its exponent's bits alone; and as a number, 2^-127 a subnormal one.
+__device__ __forceinline__ float scale_of(int byte) { return __uint_as_float((uint32_t)byte << 23); }
+__device__ __forceinline__ float power_of(int byte) { return byte > 0 ? scale_of(byte) : __uint_as_float(0x400000u); }
 // The byte of the smallest power of two s with amax <= 448 s (448 = 1.75 * 2^8).
 __device__ __forceinline__ int scale_byte(float amax) {
   const uint32_t u = __float_as_uint(amax);

@@ -1,8 +1,10 @@
 """Calls of the paged cache at the ends of what its header allows."""
+import numpy as np
 import pytest
 import torch
 
-from paged_support import TYPES, Pool
+from oracle import paged_oracle as orc
+from paged_support import TYPES, Pool, f64
 
 pytestmark = pytest.mark.gpu
 BASE = 5e5
@@ -71,3 +73,36 @@ def test_a_growing_scale_reaches_rows_beyond_32_bits(esa):
     at = int(pool.table[0, 0])
     for a, b, sa, sb in zip(pool.caches, caches, pool.scales, scales):
         assert torch.equal(a.view(torch.uint8)[at, :, :60], b.view(torch.uint8)[n_pages - 1 - at, :, :60]) and torch.equal(sa[at], sb[n_pages - 1 - at])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_append_to_blocks_of_any_scale(esa, dtype):
+    """Every exponent byte that a page may hold before a sequence goes on in it; 255 is a block that holds nothing."""
+    bytes_held, first, new, page, h_kv, d = [0, 1, 26, 27, 120, 239, 240, 253, 254, 255], 7, 5, 16, 2, 64
+    pool = Pool([(first, new)] * len(bytes_held), h_kv, d, page, dtype, "e4m3", seed=43)
+    values, _, scale, _ = [None if x is None else x.copy() for x in pool.values()]
+    rows, raw = [], pool.caches[0].view(torch.uint8).cpu()
+    for b, byte in enumerate(bytes_held):
+        at = pool.table[b, 0]
+        # rows some of which the block's own scale can hold
+        rows.append(torch.from_numpy(pool.rng.standard_normal((new, h_kv, d)) * 2.0 ** (min(max(byte, 40), 250) - 127)))
+        if byte != 255:
+            x = orc.to_e4m3(pool.rng.standard_normal((h_kv, first, d)) * 100)
+            values[at, :, :first] = x
+            raw[at, :, :first] = torch.from_numpy(x).to(torch.float8_e4m3fn).view(torch.uint8)
+        scale[at] = byte
+    for cache, s in zip(pool.caches, pool.scales):
+        cache.view(torch.uint8).copy_(raw)
+        s.copy_(torch.from_numpy(scale))
+    k = torch.cat(rows).to(TYPES[dtype]).cuda()
+    esa.esa_append_paged(k, k, *pool.batch())
+    for b, byte in enumerate(bytes_held):
+        at, mine = pool.table[b, 0], f64(k[b * new:(b + 1) * new])
+        earlier = values[at, :, :first].copy()
+        if byte == 255:
+            scale[at], values[at, :, :first] = 0, 0.0
+        orc.append_blocks(values, scale, mine, first, pool.table[b], page)
+        if byte == 255:
+            values[at, :, :first] = earlier
+    for got, want in zip(pool.values(), (values, values, scale, scale)):
+        assert np.array_equal(got, want, equal_nan=want.ndim == 4)
