@@ -222,8 +222,9 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
     float ks = 1.f, vs = 1.f;
     if constexpr (F8) {
       // a page that nobody has may hold an infinite scale; whatever its rows hold: 0 times a NaN is one (scores of such keys are masked)
-      ks = scale_of(pos != INT32_MAX ? kb : 127);
-      vs = scale_of(pos != INT32_MAX ? vb : 127);
+      const int k_byte = pos != INT32_MAX ? kb : 127, v_byte = pos != INT32_MAX ? vb : 127;
+      ks = kBf16 ? scale_of(k_byte) : power_of(k_byte);
+      vs = kBf16 ? scale_of(v_byte) : power_of(v_byte);
     }
     if (unseen) {
 #pragma unroll

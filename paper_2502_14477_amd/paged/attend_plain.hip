@@ -42,8 +42,8 @@ template <bool F8> __global__ __launch_bounds__(64 * kWaves) void attend_plain(A
       if (seen) {
         at = place_of(a.cache, page, g, p & ((1 << a.batch.page_log2) - 1));
         if (F8) {
-          k_by = scale_of(a.cache.k_scale[block_of(a.cache, page, g)]);
-          v_by = scale_of(a.cache.v_scale[block_of(a.cache, page, g)]);
+          k_by = power_of(a.cache.k_scale[block_of(a.cache, page, g)]);
+          v_by = power_of(a.cache.v_scale[block_of(a.cache, page, g)]);
         }
       }
     }
@@ -73,10 +73,10 @@ template <bool F8> __global__ __launch_bounds__(64 * kWaves) void attend_plain(A
 #pragma unroll
       for (int i = 0; i < kAtOnce; ++i) {
         if (!((all >> (k0 + i)) & 1)) continue;                 // whatever its row holds
-        const float p = expf(x[i] - top), by = F8 ? p * __shfl(v_by, k0 + i) : p;
+        const float p = expf(x[i] - top), by = F8 ? __shfl(v_by, k0 + i) : 1.f;      // (of the value: beside a small scale p would be subnormal)
         l += p;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(by, v[i][e], o[e]);
+        for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(p, v[i][e] * by, o[e]);
       }
     }
   }

@@ -106,3 +106,20 @@ def test_append_to_blocks_of_any_scale(esa, dtype):
             values[at, :, :first] = earlier
     for got, want in zip(pool.values(), (values, values, scale, scale)):
         assert np.array_equal(got, want, equal_nan=want.ndim == 4)
+
+
+@pytest.mark.parametrize("dtype,d,new", [("bf16", 64, 1), ("bf16", 128, 100), ("f32", 64, 1), ("f32", 256, 1)])
+def test_attend_reads_every_scale(esa, dtype, d, new):
+    """Values of a block are its numbers times 2^(byte - 127) from the first byte to the last: outputs grow by that power of two."""
+    pool = Pool([(300, new)], 1, d, 64, dtype, "e4m3", seed=44).fill()
+    # numbers from 256 to 448 and probabilities of about one: no value or product is subnormal under byte 0 but for what a probability's second
+    # term adds, so fp32 outputs are the same but for the power of two, bf16 ones within a rounding of each
+    q = pool.rows(new, 4, 0.01)
+    raw = pool.caches[1].view(torch.uint8)
+    raw.copy_((raw & 0x7F).clamp(0x78, 0x7E))
+    got = []
+    for byte in (127, 0, 1, 200):
+        pool.scales[1].fill_(byte)
+        got.append(esa.esa_attend_paged(q, *pool.batch()).double() * 2.0 ** (127 - byte))
+    for x in got[1:]:
+        assert torch.equal(x, got[0]) if dtype == "f32" else torch.all((x - got[0]).abs() <= 2.0 ** -7 * got[0])
