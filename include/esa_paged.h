@@ -91,7 +91,8 @@ ESA_API int esa_append_paged(const void* k, int64_t ldk, const void* v, int64_t 
  *   lse  [n_tok][h] fp32 natural-log normaliser, or NULL
  *   workspace esa_attend_paged_workspace_bytes(n_tok, n_seq, h, h_kv, d, dtype) bytes, 256-byte aligned
  * A token that sees nothing (its pages are missing) has out = 0 and lse = -inf.  Rows of out and lse behind cu[n_seq] are left as
- * they were.  Keys and values that are seen must be finite, everything else in the pool may hold anything.
+ * they were.  Keys and values that are seen must be finite, everything else in the pool may hold anything.  So must queries be, but that
+ * the rows of one that holds a NaN are NaN, out and lse, and no other row is.
  * Scores scale * q.k stay below 2^90 in magnitude, values below 2^90.
  * n_tok == 0 or n_seq == 0 is a no-op.  d: 32, 64, 128 or 256 (ESA_F32 with 256 by a plain kernel, far slower than the others).
  */

@@ -21,6 +21,25 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 template <typename T> __device__ __forceinline__ float exp_of(float x) { return sizeof(T) == 2 ? __builtin_amdgcn_exp2f(x) : expf(x); }
 template <typename T> __device__ __forceinline__ float lse_of(float m, float l) { return sizeof(T) == 2 ? __builtin_fmaf(m, kLn2, logf(l)) : m + logf(l); }
 
+// Whether a lane's row of queries, of which it and its opposite have 16 bytes in turn, holds a NaN.  By their bits: the kernels are compiled without
+// heed of NaN, and comparisons, maxima and selections may take one for anything.  The row's sum of exponentials is made NaN at its end, which the
+// arithmetic behind it passes on.
+template <typename T, int N> __device__ __forceinline__ bool holds_nan(const u32x4 (&q)[N]) {
+  constexpr uint32_t kMagnitude = sizeof(T) == 2 ? 0x7FFF7FFFu : 0x7FFFFFFFu, kToSign = sizeof(T) == 2 ? 0x007F007Fu : 0x007FFFFFu;
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int w = 0; w < 4; ++w) any |= (q[i][w] & kMagnitude) + kToSign;      // past infinity: over into the sign
+  const auto both = __builtin_amdgcn_permlane32_swap(any, any, false, false);
+  return ((both[0] | both[1]) & ~kMagnitude) != 0;
+}
+__device__ __forceinline__ float nan_if(bool is, float x) {
+  uint32_t bits = is ? 0x7FC00000u : __float_as_uint(x);
+  asm("" : "+v"(bits));                     // (a NaN that the compiler sees it leaves out)
+  return __uint_as_float(bits);
+}
+
 constexpr float kNoReference = -1e30f;      // of a softmax that has seen nothing: so low that the first logit exceeds it
 
 __device__ __forceinline__ float halves_max(float v) {

@@ -98,6 +98,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
 #pragma unroll
     for (int i = 0; i < kKS; ++i) qf[i] = *(const u32x4*)(q + i * 32);
   }
+  const bool ill = holds_nan<T>(qf);
 
   // Lane r stands for key r of a tile: its position (INT32_MAX: not seen), its row's place in the pool, its scales.  Entries of the index list
   // are requested three tiles ahead, of the page table two, rows one.  A tile that lies in one page, its rows within 32 bits of each other, is
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
 
   // ---- the waves' results meet in LDS: a wave's sums of row r, dimensions 4 n ..., at (n * 32 + (r ^ n)) * 16 of its staging space
   __syncthreads();
-  l_run = halves_sum(l_run);
+  l_run = nan_if(ill, halves_sum(l_run));
   if (hi == 0) {
     ml[wave][r][0] = m_run;
     ml[wave][r][1] = l_run;
@@ -392,15 +393,16 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
     }
     if (alone) {
       const int rg = row0 + row_in, tok = rg / a.group, hd = g * a.group + rg - tok * a.group;
-      const float inv = l > 0.f ? 1.f / l : 0.f;
+      const bool nothing = nothing_seen(l);
+      const float inv = nothing ? 0.f : 1.f / l;
       char* to = a.out + (int64_t)(s.row0 + tok) * a.ldo + (int64_t)hd * kRowBytes;
       if constexpr (kBf16) {
         const bf16x2 lo = __builtin_convertvector((f32x2{sum[0] * inv, sum[1] * inv}), bf16x2), up = __builtin_convertvector((f32x2{sum[2] * inv, sum[3] * inv}), bf16x2);
         *(uint2*)(to + n * 8) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, up));
       } else {
-        *(f32x4*)(to + n * 16) = f32x4{l > 0.f ? sum[0] / l : 0.f, l > 0.f ? sum[1] / l : 0.f, l > 0.f ? sum[2] / l : 0.f, l > 0.f ? sum[3] / l : 0.f};
+        *(f32x4*)(to + n * 16) = nothing ? f32x4{0.f, 0.f, 0.f, 0.f} : sum / l;
       }
-      if (a.lse && n == 0) a.lse[(int64_t)(s.row0 + tok) * a.h + hd] = l > 0.f ? lse_of<T>(m, l) : -INFINITY;
+      if (a.lse && n == 0) a.lse[(int64_t)(s.row0 + tok) * a.h + hd] = nothing ? -INFINITY : lse_of<T>(m, l);
     } else {
       const int64_t part = ((at.slot + (int64_t)at.slice * at.blocks) * a.cache.h_kv + g) * kRows + row_in;
       *(f32x4*)(f.part_o + part * D + n * 4) = sum;
@@ -472,8 +474,8 @@ template <typename T, int D> __global__ __launch_bounds__(256) void join_few(Few
     T* out = (T*)(a.out + (int64_t)tok * a.ldo) + (int64_t)head * D + lane * kMine;
     if (lane >= kLanes) continue;
 #pragma unroll
-    for (int i = 0; i < kMine; ++i) store_f32<T>(out + i, l > 0.f ? sum[i] / l : 0.f);
-    if (a.lse && lane == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? lse_of<T>(m, l) : -INFINITY;
+    for (int i = 0; i < kMine; ++i) store_f32<T>(out + i, nothing_seen(l) ? 0.f : sum[i] / l);
+    if (a.lse && lane == 0) a.lse[(int64_t)tok * a.h + head] = nothing_seen(l) ? -INFINITY : lse_of<T>(m, l);
   }
 }
 

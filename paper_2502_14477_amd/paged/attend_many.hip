@@ -369,7 +369,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
     }
   }
 
-  l_run = halves_sum(l_run);
+  l_run = nan_if(holds_nan<bf16_t>(qf), halves_sum(l_run));
   if (!at.alone) {
     // as the lanes have it: 16 bytes a lane, 1 KB an instruction
     const int64_t part = (int64_t)at.slot * kWaves + wave;
@@ -380,7 +380,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         *((f32x4*)f.part_o + (part * (D / 8) + md * 4 + v / 4) * 64 + lane) = f32x4{o[md][v], o[md][v + 1], o[md][v + 2], o[md][v + 3]};
     if (hi == 0) *(float2*)(f.part_ml + (part * 32 + r) * 2) = make_float2(m_run, l_run);
   } else if (wave * 32 + r < rows) {
-    const float inv = l_run > 0.f ? 1.f / l_run : 0.f;
+    const float inv = nothing_seen(l_run) ? 0.f : 1.f / l_run;
     char* to = a.out + (int64_t)(s.row0 + c) * a.ldo + (int64_t)head * kRowBytes;
 #pragma unroll
     for (int md = 0; md < kMD; ++md)
@@ -390,7 +390,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         const bf16x2 up = __builtin_convertvector((f32x2{o[md][v + 2] * inv, o[md][v + 3] * inv}), bf16x2);
         *(uint2*)(to + (md * 32 + v * 2 + 4 * hi) * 2) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, up));
       }
-    if (a.lse && hi == 0) a.lse[(int64_t)(s.row0 + c) * a.h + head] = l_run > 0.f ? lse_of<bf16_t>(m_run, l_run) : -INFINITY;
+    if (a.lse && hi == 0) a.lse[(int64_t)(s.row0 + c) * a.h + head] = nothing_seen(l_run) ? -INFINITY : lse_of<bf16_t>(m_run, l_run);
   }
   __syncthreads();                                              // (the next part's tiles go where this one's are)
   });
@@ -469,14 +469,14 @@ template <int D> __global__ __launch_bounds__(256) void join_many(ManyArgs f) {
   if (in >= block.rows) return;
   const float m = sum.ml.x, l = sum.ml.y;
   const int tok = block.tok0 + row / a.group, head = g * a.group + row % a.group;
-  const float inv = l > 0.f ? 1.f / l : 0.f;
+  const float inv = nothing_seen(l) ? 0.f : 1.f / l;
   char* to = a.out + (int64_t)tok * a.ldo + (int64_t)head * D * 2;
 #pragma unroll
   for (int k = 0; k < kMine; ++k) {
     const bf16x2 lo = __builtin_convertvector((f32x2{sum.x[k][0] * inv, sum.x[k][1] * inv}), bf16x2), up = __builtin_convertvector((f32x2{sum.x[k][2] * inv, sum.x[k][3] * inv}), bf16x2);
     *(uint2*)(to + ((wave * kMine + k) * 8 + 4 * hi) * 2) = make_uint2(__builtin_bit_cast(uint32_t, lo), __builtin_bit_cast(uint32_t, up));
   }
-  if (a.lse && wave == 0 && hi == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? lse_of<bf16_t>(m, l) : -INFINITY;
+  if (a.lse && wave == 0 && hi == 0) a.lse[(int64_t)tok * a.h + head] = nothing_seen(l) ? -INFINITY : lse_of<bf16_t>(m, l);
 }
 
 

@@ -93,8 +93,8 @@ template <bool F8> __global__ __launch_bounds__(64 * kWaves) void attend_plain(A
     l = __builtin_fmaf(ml[w].y, by, l);
     o += sums[w][lane] * by;
   }
-  ((f32x4*)(a.out + tok * a.ldo))[head * (kD / 4) + lane] = l > 0.f ? o / l : f32x4{0.f, 0.f, 0.f, 0.f};
-  if (a.lse && lane == 0) a.lse[(int64_t)tok * a.h + head] = l > 0.f ? m + logf(l) : -INFINITY;
+  ((f32x4*)(a.out + tok * a.ldo))[head * (kD / 4) + lane] = nothing_seen(l) ? f32x4{0.f, 0.f, 0.f, 0.f} : o / l;
+  if (a.lse && lane == 0) a.lse[(int64_t)tok * a.h + head] = nothing_seen(l) ? -INFINITY : m + logf(l);
 }
 
 }  // namespace

@@ -183,6 +183,10 @@ __device__ __forceinline__ int keys_up_to(const AttendArgs& a, const Seq& s, con
 }
 __device__ __forceinline__ int keys_until(const AttendArgs& a, const Seq& s, const Keys& k, int row) { return keys_up_to(a, s, k, row / a.group); }
 
+// Whether a row whose exponentials sum up to l has seen nothing: the largest of what it sees is one or nearly so.  By its bits: l is NaN where the
+// query is.
+__device__ __forceinline__ bool nothing_seen(float l) { return __float_as_uint(l) == 0; }
+
 // A value that is the same in every lane, where the compiler does not see it.
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int64_t uniform(int64_t x) { return (int64_t)(uint32_t)uniform((int)x) | (int64_t)uniform((int)(x >> 32)) << 32; }

@@ -123,3 +123,21 @@ def test_attend_reads_every_scale(esa, dtype, d, new):
         got.append(esa.esa_attend_paged(q, *pool.batch()).double() * 2.0 ** (127 - byte))
     for x in got[1:]:
         assert torch.equal(x, got[0]) if dtype == "f32" else torch.all((x - got[0]).abs() <= 2.0 ** -7 * got[0])
+
+
+@pytest.mark.parametrize("dtype,held,d", [("bf16", "e4m3", 128), ("bf16", "same", 64), ("bf16", "same", 256), ("f32", "same", 64), ("f32", "e4m3", 128), ("f32", "same", 256)])
+@pytest.mark.parametrize("cap", [0.0, 30.0])
+@pytest.mark.parametrize("lengths", [[(100, 2), (20, 1)], [(5000, 2), (20, 1)], [(100, 90), (0, 40)], [(3000, 300), (20, 1)]], ids=["short", "cut", "chunk", "cut chunk"])
+def test_a_query_that_is_nan_shows(esa, dtype, held, d, cap, lengths):
+    """Its rows are NaN however their keys are shared out, and every other row is what it would be."""
+    print("[case] NaN query", dtype, held, d, cap, lengths, flush=True)
+    pool = Pool(lengths, 2, d, 64, dtype, held, seed=45).fill()
+    q = pool.rows(pool.n_tok, 8)
+    want, want_lse = esa.esa_attend_paged(q, *pool.batch(), cap=cap, return_lse=True)
+    ill = torch.zeros(pool.n_tok, 8, dtype=torch.bool, device="cuda")
+    for tok, head in ((0, 3), (lengths[0][1] - 1, 0), (pool.n_tok - 1, 7)):
+        ill[tok, head] = True
+        q[tok, head, 5 + head] = float("nan")
+    out, lse = esa.esa_attend_paged(q, *pool.batch(), cap=cap, return_lse=True)
+    assert torch.all(torch.isnan(out[ill])) and torch.all(torch.isnan(lse[ill]))
+    assert torch.equal(out[~ill], want[~ill]) and torch.equal(lse[~ill], want_lse[~ill])
