@@ -155,7 +155,7 @@ template <typename T> __device__ void append_rows(const AppendArgs& a, int block
 
 template <typename T> __global__ __launch_bounds__(kThreads) void append_same(AppendArgs a) {
   extern __shared__ f64x2 table[];          // [kRowTokens][d / 2]
-  append_rows<T>(a, blockIdx.x, true, table);
+  append_rows<T>(a, block_index(), true, table);
 }
 
 template <typename T> __device__ __forceinline__ float largest(const Vec<T>& v) {
@@ -176,11 +176,12 @@ template <typename T, int J> __global__ __launch_bounds__(kThreads) void append_
   constexpr int V = Vec<T>::n;
   __shared__ f64x2 cs[kThreads * V];        // a round's rows' turns: [rows][d / 2]
   __shared__ float most[kThreads / 64];
-  if ((int)blockIdx.x < a.row_blocks) {
-    append_rows<T>(a, blockIdx.x, false, cs);
+  const int block = block_index();
+  if (block < a.row_blocks) {
+    append_rows<T>(a, block, false, cs);
     return;
   }
-  const int unit = blockIdx.x - a.row_blocks, tid = threadIdx.x;
+  const int unit = block - a.row_blocks, tid = threadIdx.x;
   const bool keys = (unit & 1) == 0;
   const int g = (unit >> 1) % a.cache.h_kv, log2 = a.batch.page_log2, page_size = 1 << log2;
   const Found f = find(a.batch.n_seq, (unit >> 1) / a.cache.h_kv, [&](int b) -> int64_t {
@@ -287,7 +288,7 @@ template <typename T> int launch(AppendArgs& a, bool f8, hipStream_t st) {
   a.row_tokens = a.batch.n_tok <= 512 ? 1 : kRowTokens;
   const int row_blocks = (a.batch.n_tok + a.row_tokens - 1) / a.row_tokens;
   if (!f8) {
-    append_same<T><<<row_blocks, kThreads, kRowTokens * (a.cache.d / 2) * sizeof(f64x2), st>>>(a);
+    append_same<T><<<grid_for(row_blocks), kThreads, kRowTokens * (a.cache.d / 2) * sizeof(f64x2), st>>>(a);
     ESA_LAUNCH_CHECK("append_same");
     return ESA_OK;
   }
@@ -297,9 +298,8 @@ template <typename T> int launch(AppendArgs& a, bool f8, hipStream_t st) {
   int64_t parts = a.batch.n_tok / page_size + 2 * (int64_t)used;
   if (parts > a.batch.n_tok) parts = a.batch.n_tok;
   const int64_t grid = a.row_blocks + parts * 2 * a.cache.h_kv;
-  if (grid > INT32_MAX) ESA_FAIL(ESA_EINVAL, "esa_append_paged: %lld workgroups", (long long)grid);
   const int rows = kThreads / (a.cache.d / 2 / Vec<T>::n), j = (page_size + rows - 1) / rows;
-  const dim3 g((unsigned)grid);
+  const dim3 g = grid_for(grid);
   if (j <= 1)
     append_blocks<T, 1><<<g, kThreads, 0, st>>>(a);
   else if (j == 2)

@@ -76,10 +76,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
   const AttendArgs& a = f.a;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, hi = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int g = blockIdx.x % a.cache.h_kv;
+  const int unit = block_index(), g = unit % a.cache.h_kv;
   const Plan plan = plan_of(a, f.shape, f.made);
   const int slice = plan.slice;
-  const Part at = uniform(part_of(a, f.shape, plan, f.made, blockIdx.x / a.cache.h_kv));
+  const Part at = uniform(part_of(a, f.shape, plan, f.made, unit / a.cache.h_kv));
   if (at.b < 0) return;
   const Seq s = uniform(sequence(a.batch, at.b));
   const Keys keys = keys_of(a, s);
@@ -509,8 +509,7 @@ template <typename T> int launch_all(const AttendArgs& a, bool f8, int most_rows
   char* const made = (char*)ws + (split_workspace(parts, kRows, d) + kPlanBytes - 1) / kPlanBytes * kPlanBytes;
   const FewArgs f{split, Made{(int*)made, (Upto*)(made + kPlanBytes)}};
   const int64_t units = most_units(f.shape, a.batch.n_tok, a.batch.n_seq, a.group, a.cache.h_kv) * a.cache.h_kv;
-  if (units > INT32_MAX) ESA_FAIL(ESA_EINVAL, "esa_attend_paged: %lld workgroups", (long long)units);
-  const dim3 grid((unsigned)units);
+  const dim3 grid = grid_for(units);
   if (a.batch.n_seq > 64) {
     plan_few<<<1, 1024, 0, st>>>(f);
     ESA_LAUNCH_CHECK("plan_few");

@@ -22,7 +22,7 @@ template <bool F8> __device__ __forceinline__ f32x4 four(const char* row, int la
 template <bool F8> __global__ __launch_bounds__(64 * kWaves) void attend_plain(AttendArgs a) {
   __shared__ f32x4 sums[kWaves][64];
   __shared__ float2 ml[kWaves];
-  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), head = blockIdx.x % a.h, tok = blockIdx.x / a.h, g = head / a.group;
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), block = block_index(), head = block % a.h, tok = block / a.h, g = head / a.group;
   const int b = sequence_with(a.batch, tok);
   if (b < 0) return;
   const Seq s = sequence(a.batch, b);
@@ -100,7 +100,7 @@ template <bool F8> __global__ __launch_bounds__(64 * kWaves) void attend_plain(A
 }  // namespace
 
 int launch_plain(const AttendArgs& a, bool f8, hipStream_t st) {
-  const dim3 grid((unsigned)(a.batch.n_tok * a.h));
+  const dim3 grid = grid_for((int64_t)a.batch.n_tok * a.h);
   if (f8)
     attend_plain<true><<<grid, 64 * kWaves, 0, st>>>(a);
   else

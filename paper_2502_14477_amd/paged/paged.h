@@ -57,6 +57,15 @@ __device__ __forceinline__ int page_of(const Batch& a, int n_pages, int b, int p
   return n < a.max_pages && (uint32_t)p < (uint32_t)n_pages ? p : -1;
 }
 
+// ---------------------------------------------------------------- workgroups
+// A launch has fewer than 2^32 threads a dimension: more workgroups than that leaves room for lie in rows of 2^22.  The last row's may have nothing
+// to do.
+constexpr int kGridRow = 1 << 22;
+inline dim3 grid_for(int64_t blocks) {
+  return blocks <= kGridRow ? dim3((unsigned)blocks) : dim3(kGridRow, (unsigned)((blocks + kGridRow - 1) / kGridRow));
+}
+__device__ __forceinline__ int block_index() { return (int)(blockIdx.y * kGridRow + blockIdx.x); }
+
 // ---------------------------------------------------------------- scans over the sequences, a lane to each, 64 at a time
 // Sums over the lanes up to each (in the vector unit: DPP shifts within rows of sixteen, then the rows' last lanes passed on).
 __device__ __forceinline__ uint32_t wave_scan(uint32_t x) {

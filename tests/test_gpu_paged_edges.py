@@ -141,3 +141,56 @@ def test_a_query_that_is_nan_shows(esa, dtype, held, d, cap, lengths):
     out, lse = esa.esa_attend_paged(q, *pool.batch(), cap=cap, return_lse=True)
     assert torch.all(torch.isnan(out[ill])) and torch.all(torch.isnan(lse[ill]))
     assert torch.equal(out[~ill], want[~ill]) and torch.equal(lse[~ill], want_lse[~ill])
+
+
+# ---------------------------------------------------------------- more workgroups than a dimension of a launch takes (2^24 of 256 threads)
+@pytest.fixture
+def memory():
+    yield
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("held,n_tok,h_kv", [("same", (1 << 26) + 70, 1), ("e4m3", (1 << 24) + 70, 8)])
+def test_append_of_millions_of_tokens(esa, memory, held, n_tok, h_kv):
+    """A prompt all but whose last rows have no page; those are the rows that they are by themselves."""
+    print("[case] long append", held, n_tok, h_kv, flush=True)
+    d, page, last = 32, 16, 50
+    pool = Pool([(0, last)], h_kv, d, page, "bf16", held, seed=46, spare=20)
+    k = torch.empty((n_tok, h_kv, d), dtype=torch.bfloat16, device="cuda")
+    k[-last:] = pool.rows(last, h_kv)
+    first = n_tok - last
+    table = torch.full((1, -(-n_tok // page)), -1, dtype=torch.int32, device="cuda")
+    n = table.shape[1] - first // page
+    got = []
+    for at, cu, start, rows in ((0, [0, n_tok], [0], k), (8, [0, last], [first], k[-last:])):
+        table[0, -n:] = torch.arange(at, at + n, dtype=torch.int32)
+        # the page in which the last rows begin has earlier ones too where they belong to the call
+        table[0, first // page] = -1
+        cu, start = (torch.tensor(x, dtype=torch.int32, device="cuda") for x in (cu, start))
+        esa.esa_append_paged(rows, rows, cu, start, table, *pool.batch()[3:], rope_base=BASE)
+        got.append([c.view(torch.uint8)[at + 1:at + n].clone() if held == "e4m3" else c[at + 1:at + n].clone() for c in pool.caches]
+                   + [s[at + 1:at + n].clone() for s in pool.scales if s is not None])
+    for a, b in zip(*got):
+        if a.dtype == torch.bfloat16:
+            a, b = a.view(torch.int16), b.view(torch.int16)
+        assert torch.equal(a, b)
+    assert held == "e4m3" or not torch.all(torch.isnan(got[0][0]))
+
+
+@pytest.mark.parametrize("dtype,h,h_kv,d,lengths", [("f32", 65535, 1, 256, [(0, 257)]), ("bf16", 65535, 65535, 32, [(b % 16, 1) for b in range(257)])],
+                         ids=["plain", "few rows"])
+def test_attend_with_millions_of_workgroups(esa, memory, dtype, h, h_kv, d, lengths):
+    print("[case] workgroups", dtype, h, h_kv, d, flush=True)
+    n_tok, n_seq, page = sum(n for _, n in lengths), len(lengths), 16
+    width = -(-max(t0 + n for t0, n in lengths) // page)
+    caches = [torch.randn((width, h_kv, page, d), device="cuda").to(TYPES[dtype]) for _ in "kv"]
+    table = torch.arange(width, dtype=torch.int32, device="cuda").expand(n_seq, -1).contiguous()      # pages that all sequences read
+    cu = torch.tensor([0] + [n for _, n in lengths], dtype=torch.int32).cumsum(0).to(torch.int32).cuda()
+    start = torch.tensor([t0 for t0, _ in lengths], dtype=torch.int32, device="cuda")
+    q = torch.zeros((n_tok, h, d), dtype=TYPES[dtype], device="cuda")
+    q[-1] = torch.randn((h, d), device="cuda").to(q.dtype)
+    out, lse = esa.esa_attend_paged(q, cu, start, table, *caches, return_lse=True)
+    one = (torch.tensor([0, 1], dtype=torch.int32, device="cuda"), (start + cu[1:] - cu[:-1] - 1)[-1:].contiguous(), table[-1:], *caches)
+    want, want_lse = esa.esa_attend_paged(q[-1:].contiguous(), *one, return_lse=True)
+    assert torch.equal(out[-1:], want) and torch.equal(lse[-1:], want_lse)
+    assert torch.all(lse[0] == torch.log(torch.tensor(1.0 + lengths[0][0])).item())       # one key, a query of zeros
