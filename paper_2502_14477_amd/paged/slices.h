@@ -30,13 +30,24 @@ __device__ __forceinline__ Cost cost_of(const AttendArgs& a, const SliceShape& s
 // The length of a slice: so long that no more than one round of units is needed.  (Sixteen sequences of 18 to 66 thousand tokens, cut by their
 // mean, were 600 units for 512 places, and the second round took as long as the first: 497 us, 342 in one.  Shorter slices and several
 // rounds were slower, as were shares of the same length that cut sequences anywhere, by what finding them takes in both kernels.)  Counts
-// are fp32: exact where they decide, and every workgroup comes to the same ones.  total(of): the sum of of(cost) over all sequences.
+// are fp32, rounded from 2^24 on, and both kernels have to come to the same slice: nothing is contracted, so that every operation is rounded as it
+// stands wherever it is compiled.  total(of): the sum of of(cost) over all sequences.
 template <typename F> __device__ __forceinline__ int slice_of(const SliceShape& sh, int h_kv, F&& total) {
+#pragma clang fp contract(off)
   if (sh.uncut) return sh.least;
-  const float all = total([](const Cost& c) { return (float)c.blocks * (float)c.tiles; }) * (float)h_kv;
+  const float all = total([](const Cost& c) {
+#pragma clang fp contract(off)
+    return (float)c.blocks * (float)c.tiles;
+  }) * (float)h_kv;
   const float places = (float)sh.target, mean = fmaxf(all / places, 1.f);
   auto rounded = [&](float x) { return (int)fminf(ceilf(x / (float)sh.least), 1e7f) * sh.least; };
-  auto units_of = [&](int slice) { return total([&](const Cost& c) { return (float)c.blocks * (float)((c.tiles + slice - 1) / slice); }) * (float)h_kv; };
+  auto units_of = [&](int slice) {
+#pragma clang fp contract(off)
+    return total([&](const Cost& c) {
+#pragma clang fp contract(off)
+      return (float)c.blocks * (float)((c.tiles + slice - 1) / slice);
+    }) * (float)h_kv;
+  };
   int slice = rounded(mean);
   float units = units_of(slice);
   for (int i = 0; i < 4 && units > places; ++i) {

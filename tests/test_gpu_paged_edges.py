@@ -194,3 +194,23 @@ def test_attend_with_millions_of_workgroups(esa, memory, dtype, h, h_kv, d, leng
     want, want_lse = esa.esa_attend_paged(q[-1:].contiguous(), *one, return_lse=True)
     assert torch.equal(out[-1:], want) and torch.equal(lse[-1:], want_lse)
     assert torch.all(lse[0] == torch.log(torch.tensor(1.0 + lengths[0][0])).item())       # one key, a query of zeros
+
+
+def test_one_token_of_millions_beside_a_chunk(esa, memory):
+    """More blocks times tiles than fp32 counts exactly: the kernels cut the long sequence alike.  Its table repeats eight pages, so its softmax is theirs."""
+    page, d, h, chunk, repeats = 128, 32, 32, 2050, 8192
+    caches = [torch.randn((8, 1, page, d), device="cuda") for _ in "kv"]
+    width = 8 * repeats
+    table = torch.arange(width, dtype=torch.int32, device="cuda").remainder(8).expand(2, -1).contiguous()
+    total = [width * page, 1 << 18]
+    cu = torch.tensor([0, 1, 1 + chunk], dtype=torch.int32, device="cuda")
+    start = torch.tensor([total[0] - 1, total[1] - chunk], dtype=torch.int32, device="cuda")
+    q = torch.randn((1 + chunk, h, d), device="cuda")
+    out, lse = esa.esa_attend_paged(q, cu, start, table, *caches, return_lse=True)
+    k, v = (f64(c)[:, 0].reshape(-1, d) for c in caches)
+    for row, n in ((0, repeats), (-1, total[1] // (8 * page))):
+        want, want_lse, spread, _ = orc.attend(f64(q[row])[None], 8 * page, k[:, None], v[:, None], range(8 * page), d ** -0.5)
+        # sums of a wave run over up to 2^16 tiles, one rounding each, of the exponentials and of their products; 2^-20 for the rest
+        tol = 2 * (2.0 ** -8 + 2.0 ** -20)
+        assert np.all(np.abs(f64(out[row]) - want[0]) <= tol * spread[0])
+        assert np.all(np.abs(f64(lse[row]) - want_lse[0] - np.log(n)) <= tol)
