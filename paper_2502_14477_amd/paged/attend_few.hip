@@ -98,7 +98,6 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
 #pragma unroll
     for (int i = 0; i < kKS; ++i) qf[i] = *(const u32x4*)(q + i * 32);
   }
-  const bool ill = holds_nan<T>(qf);
 
   // Lane r stands for key r of a tile: its position (INT32_MAX: not seen), its row's place in the pool, its scales.  Entries of the index list
   // are requested three tiles ahead, of the page table two, rows one.  A tile that lies in one page, its rows within 32 bits of each other, is
@@ -360,7 +359,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(D *
 
   // ---- the waves' results meet in LDS: a wave's sums of row r, dimensions 4 n ..., at (n * 32 + (r ^ n)) * 16 of its staging space
   __syncthreads();
-  l_run = nan_if(ill, halves_sum(l_run));
+  l_run = nan_if(holds_nan<T>(qf), halves_sum(l_run));
   if (hi == 0) {
     ml[wave][r][0] = m_run;
     ml[wave][r][1] = l_run;
