@@ -1,13 +1,16 @@
 """Calls of the paged cache at the ends of what its header allows."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
 
 from oracle import paged_oracle as orc
-from paged_support import TYPES, Pool, f64
+from paged_support import TYPES, Pool, check_attention, f64
 
 pytestmark = pytest.mark.gpu
 BASE = 5e5
+P_STEP = {"bf16": 2.0 ** -8, "f32": 0.0}      # probabilities of chunks of head size 128 are rounded to bf16
 
 
 @pytest.fixture(scope="module")
@@ -214,3 +217,83 @@ def test_one_token_of_millions_beside_a_chunk(esa, memory):
         tol = 2 * (2.0 ** -8 + 2.0 ** -20)
         assert np.all(np.abs(f64(out[row]) - want[0]) <= tol * spread[0])
         assert np.all(np.abs(f64(lse[row]) - want_lse[0] - np.log(n)) <= tol)
+
+
+# ---------------------------------------------------------------- what the arrays on the device may hold
+BAD = {
+    "descending": ([0, 40, 10, 60, 20, 70], [0, 5, 0, 700, 3]), "behind the rows": ([0, 500, 3, 10 ** 9, 2 ** 31 - 1, 90], [0, 0, 100, 0, 0]),
+    "negative": ([-5, 7, -2 ** 31, 30, 30, 69], [-1, -2 ** 31, 4, 50, 0]), "positions at the end": ([0, 1, 2, 40, 50, 70], [2 ** 31 - 1, 2 ** 31 - 2, 2 ** 31 - 30, 899, 10 ** 9]),
+    "one sequence has all": ([0, 70, 70, 70, 70, 70], [900, -7, 5, 2 ** 30, 0]),
+}
+
+
+@pytest.mark.parametrize("dtype,held,d", [("bf16", "e4m3", 128), ("bf16", "same", 64), ("bf16", "e4m3", 32), ("f32", "same", 64), ("f32", "e4m3", 256)])
+@pytest.mark.parametrize("name", sorted(BAD))
+@pytest.mark.parametrize("times", [1, 20], ids=["5 sequences", "100"])
+def test_nothing_in_the_arrays_leads_out_of_the_buffers(esa, dtype, held, d, name, times):
+    """Offsets, positions, pages and selected entries of any content: what lies around the pool, the outputs and the workspace stays as it is."""
+    print("[case] bad arrays", dtype, held, d, name, times, flush=True)
+    rng = np.random.default_rng(47)
+    h, h_kv, page, n_pages, width, n_tok, n_sel, edge = 8, 2, 16, 12, 64, 70, 33, 64
+    t, at = TYPES[dtype], torch.uint8 if held == "e4m3" else TYPES[dtype]
+    ints = lambda *shape: torch.from_numpy(rng.integers(-2 ** 31, 2 ** 31, shape, dtype=np.int64).astype(np.int32))
+    cu = torch.tensor((BAD[name][0][:-1] * times + BAD[name][0][-1:]), dtype=torch.int64).to(torch.int32).cuda()
+    start = torch.tensor(BAD[name][1] * times, dtype=torch.int64).to(torch.int32).cuda()
+    n_seq = len(start)
+    pages = torch.where(torch.from_numpy(rng.random((n_seq, width)) < 0.5), ints(n_seq, width), torch.from_numpy(rng.integers(0, n_pages, (n_seq, width)).astype(np.int32))).cuda()
+    idx = torch.where(torch.from_numpy(rng.random((n_seq, n_sel)) < 0.5), ints(n_seq, n_sel), torch.from_numpy(rng.integers(0, 1000, (n_seq, n_sel)).astype(np.int32))).cuda()
+    pool = [torch.full((n_pages + 2, h_kv, page, d), 1, dtype=at, device="cuda") for _ in "kv"]
+    scales = [torch.full((n_pages + 2, h_kv), 127, dtype=torch.uint8, device="cuda") for _ in "kv"]
+    inner = [p[1:-1].view(torch.float8_e4m3fn) if held == "e4m3" else p[1:-1] for p in pool] + [s[1:-1] if held == "e4m3" else None for s in scales]
+    q, k, v = (torch.from_numpy(rng.standard_normal((n_tok, n, d))).to(t).cuda() for n in (h, h_kv, h_kv))
+    out, turned = (torch.full((n_tok + 2, h, d), 3.0, dtype=t, device="cuda") for _ in range(2))
+    esa.esa_append_paged(k, v, cu, start, pages, *inner, q=q, rope_base=BASE, out_q=turned[1:-1])
+    for l_i, l_l, chosen in ((None, 0, None), (20, 100, idx)):
+        esa.esa_attend_paged(q, cu, start, pages, *inner, l_i=l_i, l_l=l_l, idx=chosen, out=out[1:-1], return_lse=True)
+    # the C entry, whose workspace is the caller's
+    need = esa.lib.esa_attend_paged_workspace_bytes(n_tok, n_seq, h, h_kv, d, 0 if dtype == "f32" else 1)
+    ws = torch.full((need + edge * 1024,), 0x5A, dtype=torch.uint8, device="cuda")
+    lse = torch.full((n_tok + 2, h), 3.0, device="cuda")
+    batch = esa.PagedBatch(cu=cu.data_ptr(), start=start.data_ptr(), pages=pages.data_ptr(), pages_ld=width, n_tok=n_tok, n_seq=n_seq, max_pages=width)
+    e = {"e4m3": 2, "same": 0 if dtype == "f32" else 1}[held]
+    cache = esa.PagedCache(k=inner[0].data_ptr(), v=inner[1].data_ptr(), k_scale=inner[2].data_ptr() if e == 2 else None, v_scale=inner[3].data_ptr() if e == 2 else None,
+                           page_stride=h_kv * page * d, head_stride=page * d, tok_stride=d, n_pages=n_pages, page_size=page, h_kv=h_kv, d=d, dtype=e)
+    assert esa.lib.esa_attend_paged(q.data_ptr(), h * d, h, ctypes.byref(batch), ctypes.byref(cache), 1 << 40, 0, None, 0, 0, 0.1, 0.0, out[1:].data_ptr(), h * d,
+                                    lse[1:].data_ptr(), 0 if dtype == "f32" else 1, ws.data_ptr(), need, torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    for x, same in [(p, 1) for p in pool] + [(s, 127) for s in scales] + [(out, 3.0), (turned, 3.0), (lse, 3.0)]:
+        assert torch.all(x[0] == same) and torch.all(x[-1] == same)
+    assert torch.all(ws[need:] == 0x5A)
+
+
+@pytest.mark.parametrize("dtype,held,d", [("bf16", "e4m3", 128), ("bf16", "same", 64), ("f32", "e4m3", 256)])
+@pytest.mark.parametrize("new", [1, 80])
+def test_pages_that_several_sequences_read(esa, dtype, held, d, new):
+    """A common beginning lies in the pool once."""
+    print("[case] shared pages", dtype, held, d, new, flush=True)
+    page, shared = 32, 6
+    pool = Pool([(300, new), (200, new), (shared * page, new)], 2, d, page, dtype, held, seed=48)
+    pool.table[1:, :shared] = pool.table[0, :shared]
+    pool.pages = torch.tensor(pool.table, device="cuda")
+    pool.fill()
+    k, v, q = pool.rows(pool.n_tok, 2), pool.rows(pool.n_tok, 2), pool.rows(pool.n_tok, 8)
+    turned = esa.esa_append_paged(k, v, *pool.batch(), q=q, rope_base=BASE)
+    out, lse = esa.esa_attend_paged(turned, *pool.batch(), return_lse=True)
+    check_attention(pool, turned, out, lse, p_half_step=P_STEP[dtype])
+
+
+WIDE = {"one short": [(301, 1)], "chunks": [(40, 90), (200, 33)], "mixed": [(0, 1), (63, 40), (513, 7), (7, 0), (31, 1)], "drafts": [(455, 5)] * 4}
+
+
+@pytest.mark.parametrize("dtype,held,d", [("bf16", "e4m3", 128), ("bf16", "same", 64), ("f32", "same", 64), ("f32", "e4m3", 128), ("bf16", "same", 256)])
+@pytest.mark.parametrize("name", sorted(WIDE))
+def test_short_sequences_under_a_wide_table(esa, dtype, held, d, name):
+    """A table with room for 131072 positions: sequences are cut and joined otherwise than under one of their own length."""
+    print("[case] wide table", dtype, held, d, name, flush=True)
+    pool = Pool(WIDE[name], 2, d, 64, dtype, held, seed=49).fill()
+    wide = torch.full((len(WIDE[name]), 2048), -1, dtype=torch.int32, device="cuda")
+    wide[:, :pool.pages.shape[1]] = pool.pages
+    q = pool.rows(pool.n_tok, 8)
+    for l_i, l_l in ((None, 0), (20, 100)):
+        out, lse = esa.esa_attend_paged(q, *pool.batch()[:2], wide, *pool.batch()[3:], l_i=l_i, l_l=l_l, return_lse=True)
+        check_attention(pool, q, out, lse, l_i=l_i, l_l=l_l, p_half_step=P_STEP[dtype])
