@@ -92,8 +92,11 @@ ESA_API int esa_append_paged(const void* k, int64_t ldk, const void* v, int64_t 
  *   workspace esa_attend_paged_workspace_bytes(n_tok, n_seq, h, h_kv, d, dtype) bytes, 256-byte aligned
  * A token that sees nothing (its pages are missing) has out = 0 and lse = -inf.  Rows of out and lse behind cu[n_seq] are left as
  * they were.  Keys and values that are seen must be finite, everything else in the pool may hold anything.  So must queries be, but that
- * the rows of one that holds a NaN are NaN, out and lse, and no other row is.
+ * one which holds a NaN makes its own row NaN, out and lse, if it sees anything, and no other.
  * Scores scale * q.k stay below 2^90 in magnitude, values below 2^90.
+ * ESA_BF16: probabilities keep 16 bits, but 8 with d = 128 in a batch of more than 64 rows (tokens x h / h_kv) and more than 32 a sequence
+ * in the mean, where only sequences of up to 64 may keep 16: outputs are then 2.3e-3 from the exact ones (relative, rms) instead of 1.66e-3,
+ * as those of esa_attend's chunks with d = 128 are.
  * n_tok == 0 or n_seq == 0 is a no-op.  d: 32, 64, 128 or 256 (ESA_F32 with 256 by a plain kernel, far slower than the others).
  */
 ESA_API size_t esa_attend_paged_workspace_bytes(int64_t n_tok, int n_seq, int h, int h_kv, int d, int dtype);

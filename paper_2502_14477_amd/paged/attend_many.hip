@@ -5,9 +5,9 @@
 // scale, exactly) and writes it to LDS.  The products are those of the kernel for few rows: S^T = K Q^T, O^T += V^T P^T, a lane stands for a
 // row; the reference of the softmax stays where it is until probabilities sum up to over 2^8, which spares the maxima and the sums'
 // rescaling.  A probability enters as one bf16 term at head size 128, whose rounding is as large as the output's, and as two at 64 (16 bits), as
-// the contiguous chunks' do: 2.3e-3 and 1.66e-3 from the exact result.  The second term is half more matrix instructions and a third
-// more vector ones: prompts of up to 1024 tokens behind 16 thousand 420 us (bf16 pages, head size 64; 318 with one);
-// at 128 490 would be 673.
+// contiguous chunks take one at 128 and more at 64: outputs are 2.3e-3 and 1.66e-3 from the exact ones.  The second term is half more matrix
+// instructions and a third more vector ones: prompts of up to 1024 tokens behind 16 thousand 428 us at 64 (bf16 pages; 325 with one term), 673 at
+// 128 (8-bit ones; 490).
 //   Here the matrix cores bound: 32 instructions a wave and tile, 2048 cycles of a compute unit's four for all waves, and as many for the LDS
 // reads.  What else a wave has to do is 250 instructions a tile, so they have to run beside its own matrix instructions: in a step of 32 keys
 // the scores of the next 32 and the sums of the 32 before are multiplied while the probabilities of these are made and a part of the tile
@@ -28,6 +28,15 @@ namespace {
 
 constexpr int kRows = ShareShape::rows, kKeys = ShareShape::keys, kWaves = kRows / 32;
 constexpr int terms_of(int d) { return d == 64 ? 2 : 1; }      // bf16 terms of a probability
+// What the lower or the upper one of a pair of bf16 numbers leaves of x, exactly, in one instruction (capped chunks of 333 and 117 tokens over 5000 keys:
+// 68 us with the number brought to fp32 and taken away, 63.5 so).  The factors are registers that the compiler does not see through: as constants
+// they came out wrong.
+struct Leaves {
+  uint32_t minus_lower = 0x0000BF80u, minus_upper = 0xBF800000u;
+  __device__ __forceinline__ Leaves() { asm("" : "+s"(minus_lower), "+s"(minus_upper)); }
+  __device__ __forceinline__ float lower(bf16x2 p, float x) const { return __builtin_amdgcn_fdot2_f32_bf16(p, __builtin_bit_cast(bf16x2, minus_lower), x, false); }
+  __device__ __forceinline__ float upper(bf16x2 p, float x) const { return __builtin_amdgcn_fdot2_f32_bf16(p, __builtin_bit_cast(bf16x2, minus_upper), x, false); }
+};
 struct ManyArgs : SplitArgs<ShareShape> {
   Record* records;          // [slot]
   int units;                // workgroups that share the work
@@ -184,20 +193,18 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
   constexpr int kTerms = terms_of(D);
   struct Probabilities {                                        // of 32 keys
     bf16x8 x[2][kTerms];
-    // Sets a pair of them and adds it to the sum: the sum of what the second product sees.
-    __device__ __forceinline__ void set(int v, float e0, float e1, float& sum) {
+    // Sets a pair of them and adds it to the sum: the sum of what the second product sees (but for a second term's last bits).
+    __device__ __forceinline__ void set(const Leaves& leaves, int v, float e0, float e1, float& sum) {
       const bf16x2 ones = {(__bf16)1.f, (__bf16)1.f};
+      if constexpr (kTerms > 1) sum += e0 + e1;
 #pragma unroll
       for (int n = 0; n < kTerms; ++n) {
-        const __bf16 t0 = (__bf16)e0, t1 = (__bf16)e1;
-        x[v / 8][n][v % 8] = t0;
-        x[v / 8][n][v % 8 + 1] = t1;
-        if constexpr (kTerms == 1) sum = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{t0, t1}, ones, sum, false);
-        if constexpr (kTerms > 1) {
-          if (n == 0) sum += e0 + e1;                           // (all but their last bits)
-          e0 -= (float)t0;
-          e1 -= (float)t1;
-        }
+        const bf16x2 t = {(__bf16)e0, (__bf16)e1};
+        x[v / 8][n][v % 8] = t[0];
+        x[v / 8][n][v % 8 + 1] = t[1];
+        if constexpr (kTerms == 1) sum = __builtin_amdgcn_fdot2_f32_bf16(t, ones, sum, false);
+        e0 = leaves.lower(t, e0);
+        e1 = leaves.upper(t, e1);
       }
     }
   };
@@ -207,9 +214,10 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
     for (int v = 0; v < 16; ++v) o[md][v] = 0.f;
   float m_run = kNoReference, l_run = 0.f;
+  const Leaves leaves;
   Probabilities p;                                              // of the 32 keys before
 #pragma unroll
-  for (int v = 0; v < 16; v += 2) p.set(v, 0.f, 0.f, l_run);
+  for (int v = 0; v < 16; v += 2) p.set(leaves, v, 0.f, 0.f, l_run);
 
   const int k_at = r * kKeyStride + hi * 16;
   auto key_part = [&](const unsigned char* from, int i) __attribute__((always_inline)) { return *(const u32x4*)(from + k_at + i * 32); };
@@ -303,7 +311,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
           e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(-2.f * f.cap, __builtin_amdgcn_rcpf(1.f + __builtin_amdgcn_exp2f(x[v] * f.scale)), f.cap - m_run));      // score_of(x) - m_run
         else
           e[i] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[v], f.scale, -m_run));
-        if (i & 1) p_next.set(v - 1, e[i - 1], e[i], sum[i / 2 & 1]);
+        if (i & 1) p_next.set(leaves, v - 1, e[i - 1], e[i], sum[i / 2 & 1]);
       }
 #pragma unroll
       for (int u = 0; u < kTerms; ++u) o[s % kMD] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(v_now, p.x[s / kMD][u], o[s % kMD], 0, 0, 0);
@@ -346,7 +354,7 @@ __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 
         float e[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) e[u] = x[v + u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(score_of<bf16_t, CAP>(x[v + u], f.scale, f.cap) - to);
-        p_next.set(v, e[0], e[1], sum[0]);
+        p_next.set(leaves, v, e[0], e[1], sum[0]);
       }
     }
     l_run += sum[0] + sum[1];
