@@ -8,11 +8,11 @@
 //   S^T = K Q^T, O^T += V^T P^T: a lane stands for a row, softmax stays in the lane and its opposite in the other half of the wave, and
 // the layout of S^T's accumulator is the second product's operand layout when key 16 s + 8 (j / 4) + 4 half + j % 4 is operand j of step s.
 // bf16: v_mfma_f32_32x32x16_bf16.  A probability enters as two bf16 terms (16 bits), so that outputs are as near the exact ones as rounding them
-// to bf16 leaves them: 1.66e-3 rms, 2.5e-3 of them are not the nearest number.  One term: 2.3e-3 and 0.42, which over 8-bit rows takes 271 us
-// for 288 with two (sixteen sequences of 18 to 66 thousand keys) and 104 for 113 (one of 262144); behind bf16 rows two cost nothing.
+// to bf16 leaves them: 1.66e-3 rms, 2.5e-3 of them are not the nearest number.  One term: 2.3e-3 and 0.42, which over 8-bit rows takes 272 us
+// for 290 with two (sixteen sequences of 18 to 66 thousand keys) and 104 for 112 (one of 262144); behind bf16 rows two cost nothing.
 // fp32: v_mfma_f32_32x32x2_f32.
-//   HBM bounds: a token over 262144 8-bit keys of 8 heads of 128 elements 100.5 us, 537 MB at 5.6 TB/s but for the join's 5.8 us; sixteen over 18 to 66
-// thousand 271 us, 1500 MB.  Eight over 8 thousand take 24 us and 5.3 (95 MB): some 8 us of it start and end.
+//   HBM bounds, over 8-bit rows beside a wave's instructions: a token over 262144 8-bit keys of 8 heads of 128 elements 105 us, 537 MB at 5.4 TB/s but for
+// the join's 5.5 us; sixteen over 18 to 66 thousand 292 us, 1500 MB.  Eight over 8 thousand take 26 us and 5.2 (95 MB): some 8 us of it start and end.
 #include <algorithm>
 
 #include "attend_common.h"
@@ -482,7 +482,7 @@ template <typename T, int D> __global__ __launch_bounds__(256) void join_few(Few
 // Workgroups that the chip holds: staging space in LDS and registers leave a compute unit one of fp32 rows of 512 bytes, three of 8-bit rows
 // of 64 elements brought to bf16, two of the others.  (1024 for rows of 64 elements, whatever their registers: eight sequences of 64 thousand
 // keys, 8 bits, 138 us, 1.3 rounds.)  A slice has a tile for every wave; where no sequence can have more than 512 keys, four, so that none is
-// cut and nothing is left to join (301 keys: 10.6 us cut in three, 9.3 in one, 9.1 without a look at what slices would come to).  Not so fp32, whose products take 3.4 us a tile, where there are few blocks (four
+// cut and nothing is left to join (301 keys: 11.2 us cut and joined, 9.6 so).  Not so fp32, whose products take 3.4 us a tile, where there are few blocks (four
 // sequences of 455 keys, 8 heads: 33 us uncut, 18.6 cut; two of 468 tokens 34 and 40).
 SliceShape shape_of(int d, int es, bool f8, int most_rows, bool shorts) {
   return SliceShape{d * es > 256 ? 256 : f8 && d * es < 256 ? 768 : 512, shorts ? 4 * kWaves : kWaves, most_rows, shorts};

@@ -8,15 +8,15 @@
 // contiguous chunks take one at 128 and more at 64: outputs are 2.3e-3 and 1.66e-3 from the exact ones.  The second term is half more matrix
 // instructions and a third more vector ones: prompts of up to 1024 tokens behind 16 thousand 428 us at 64 (bf16 pages; 325 with one term), 673 at
 // 128 (8-bit ones; 490).
-//   Here the matrix cores bound: 32 instructions a wave and tile, 2048 cycles of a compute unit's four for all waves, and as many for the LDS
+//   Here the matrix cores bound: 32 instructions a wave and tile (24 with 64 elements a row), 2048 cycles of a compute unit's four for all waves, and as many for the LDS
 // reads.  What else a wave has to do is 250 instructions a tile, so they have to run beside its own matrix instructions: in a step of 32 keys
 // the scores of the next 32 and the sums of the 32 before are multiplied while the probabilities of these are made and a part of the tile
 // after next is staged, slot by slot (one instruction of each product and its share of the rest), in an order that the compiler keeps.
 // (Without that order, products and softmax one behind the other in a wave: 5600 cycles a tile.  Two groups of waves that took turns with
 // products and softmax, a barrier between: the same, as a wave by itself issues a vector instruction every five cycles or so.)
 //   In iteration j keys of tiles j and j + 1 and values of j - 1 and j are read and tile j + 2 is written: four buffers, one barrier.
-//   A tile takes 1.9 us (1.2 with 64 elements a row, 2.3 with a cap); four chunks of up to 1024 tokens behind 16 thousand, 32 and 8 heads, 8-bit
-// pages, 485 us or 0.96 PFLOP/s.  A workgroup's way to its first tile and its partial sums take 14 to 20 us more.
+//   A tile takes 1.8 us with 8-bit pages, 2.0 with bf16 ones, 2.4 with a cap, 1.65 with 64 elements a row; four chunks of up to 1024 tokens behind 16
+// thousand, 32 and 8 heads, 8-bit pages, 480 to 504 us or 0.93 to 0.97 PFLOP/s.  A workgroup's way to its first tile and its partial sums take 14 to 20 us more.
 #include <algorithm>
 
 #include "attend_common.h"

@@ -165,9 +165,9 @@ int esa_attend_paged(const void* q, int64_t ldq, int h, const esa_paged_batch* b
   // else is in it; other batches by both, one after the other in the same workspace, each of which finds the sequences that are its own.  One that
   // finds none takes 5 us and its join 5 more, while short sequences in the kernel for many rows cost no more than twice their time: where the
   // table has no room for more than 2^17 keys over all heads (8 tiles of 64 a workgroup, 15 us), that one serves them all.  (Chunks of 333 and 117
-  // tokens over 5000 keys, 8 heads: 75.6 us by both, 68.2 by one.  Sixteen tokens of 16 thousand keys beside a long prompt: twice 270 us.)
+  // tokens over 5000 keys, 8 heads: 71 us by both, 63 by one.  Sixteen tokens of 16 thousand keys beside a long prompt: twice 270 us.)
   // Few rows in the mean with a chunk among them, 8-bit pages, 32 and 8 heads of 128 elements: 127 single tokens of 4000 keys beside a chunk of 896
-  // 327 us by the kernel for few rows, 294 by both; 159 of 1000 beside a prompt of 1024 120 and 135, 255 of 500 beside a chunk of 100 80 and 101, 31
+  // 330 us by the kernel for few rows, 294 by both; 159 of 1000 beside a prompt of 1024 118 and 135, 255 of 500 beside a chunk of 100 79 and 101, 31
   // of 16 thousand beside a chunk of 220 264 and 261, eight of 4 tokens beside eight of 12 60 and 65.
   hipStream_t st = (hipStream_t)stream;
   const int64_t rows = batch->n_tok * a.group;
