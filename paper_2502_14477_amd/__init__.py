@@ -10,6 +10,8 @@ _BINDING_NAMES = (
     "esa_version", "esa_segments", "esa_pack_weights", "esa_compress", "esa_score", "esa_select_topk", "esa_gather_kv", "esa_attend", "esa_attend_local", "esa_attend_finish", "esa_attend_indexed", "esa_rope", "esa_attend_reencoded", "esa_compress_qk",
     "esa_select_topk_static", "esa_select_topk_static_capacity", "esa_select_topk_static_prepare", "esa_score_select_gather",
     "ESA_E4M3", "PAGED_EXPORTS", "PagedBatch", "PagedCache", "esa_append_paged", "esa_attend_paged",
+    "ESA_PAIRS_HALVES", "ESA_PAIRS_NEIGHBOURS", "ESA_SCALE_NONE", "ESA_SCALE_LINEAR", "ESA_SCALE_NTK", "ESA_SCALE_YARN", "SERVE_EXPORTS", "RopeRows",
+    "PageState", "PagePlan", "esa_rope_frequencies", "esa_rope_at", "esa_plan_paged", "esa_verify_drafts",
 )
 __all__ = list(_BINDING_NAMES)
 

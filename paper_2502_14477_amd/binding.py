@@ -11,12 +11,14 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import NamedTuple, Optional, Tuple
 
 import torch
 
 ESA_F32, ESA_BF16, ESA_E4M3 = 0, 1, 2
 ESA_W_ROWMAJOR, ESA_W_PACKED = 0, 1
+ESA_PAIRS_HALVES, ESA_PAIRS_NEIGHBOURS = 0, 1
+ESA_SCALE_NONE, ESA_SCALE_LINEAR, ESA_SCALE_NTK, ESA_SCALE_YARN = 0, 1, 2, 3
 _PKG = os.path.dirname(os.path.abspath(__file__))
 
 
@@ -37,6 +39,19 @@ class PagedBatch(ctypes.Structure):
     """esa_paged_batch of include/esa_paged.h."""
     _fields_ = [("cu", ctypes.c_void_p), ("start", ctypes.c_void_p), ("pages", ctypes.c_void_p), ("pages_ld", ctypes.c_int64),
                 ("n_tok", ctypes.c_int64), ("n_seq", ctypes.c_int), ("max_pages", ctypes.c_int)]
+
+
+class RopeRows(ctypes.Structure):
+    """esa_rope_rows of include/esa_serve.h."""
+    _fields_ = [("x", ctypes.c_void_p), ("out", ctypes.c_void_p), ("x_tok", ctypes.c_int64), ("x_head", ctypes.c_int64),
+                ("out_tok", ctypes.c_int64), ("out_head", ctypes.c_int64), ("heads", ctypes.c_int)]
+
+
+class PageState(ctypes.Structure):
+    """esa_page_state of include/esa_serve.h."""
+    _fields_ = [("start_in", ctypes.c_void_p), ("held_in", ctypes.c_void_p), ("ring_at_in", ctypes.c_void_p), ("start", ctypes.c_void_p),
+                ("held", ctypes.c_void_p), ("ring_at", ctypes.c_void_p), ("pages", ctypes.c_void_p), ("pages_ld", ctypes.c_int64),
+                ("ring", ctypes.c_void_p), ("n_seq", ctypes.c_int), ("max_pages", ctypes.c_int), ("n_pages", ctypes.c_int), ("page_size", ctypes.c_int)]
 
 
 def lib_path() -> str:
@@ -116,6 +131,18 @@ def _load() -> ctypes.CDLL:
     L.esa_attend_paged_workspace_bytes.argtypes = [i64, i32, i32, i32, i32, i32]
     L.esa_attend_paged.restype = i32
     L.esa_attend_paged.argtypes = [vp, i64, i32, batch, cache, i64, i64, vp, i32, i64, f32, f32, vp, i64, vp, i32, vp, sz, vp]
+    L.esa_rope_frequencies.restype = i32
+    L.esa_rope_frequencies.argtypes = [f64, i32, i32, f64, f64, f64, f64, ctypes.POINTER(f64)]
+    L.esa_rope_at.restype = i32
+    L.esa_rope_at.argtypes = [ctypes.POINTER(RopeRows), i32, vp, i64, i32, i32, ctypes.POINTER(f64), i32, f64, i32, i32, vp]
+    L.esa_plan_paged_workspace_bytes.restype = sz
+    L.esa_plan_paged_workspace_bytes.argtypes = [i32]
+    L.esa_plan_paged.restype = i32
+    L.esa_plan_paged.argtypes = [ctypes.POINTER(PageState), vp, vp, i64, vp, vp, vp, vp, vp, sz, vp]
+    L.esa_verify_drafts_workspace_bytes.restype = sz
+    L.esa_verify_drafts_workspace_bytes.argtypes = [i32, i64]
+    L.esa_verify_drafts.restype = i32
+    L.esa_verify_drafts.argtypes = [vp, i64, vp, i64, vp, vp, vp, i64, i32, i64, vp, vp, i32, vp, sz, vp]
     return L
 
 
@@ -130,6 +157,8 @@ EXPORTS = ("esa_version", "esa_last_error", "esa_segments", "esa_pack_weights", 
            "esa_select_topk_static_capacity", "esa_select_topk_static_prepare", "esa_select_topk_static",
            "esa_score_select_gather_workspace_bytes", "esa_score_select_gather")
 PAGED_EXPORTS = ("esa_append_paged", "esa_attend_paged_workspace_bytes", "esa_attend_paged")      # include/esa_paged.h
+SERVE_EXPORTS = ("esa_rope_frequencies", "esa_rope_at", "esa_plan_paged_workspace_bytes", "esa_plan_paged",
+                 "esa_verify_drafts_workspace_bytes", "esa_verify_drafts")      # include/esa_serve.h
 
 
 _native.set_error_class(EsaError)
@@ -297,3 +326,60 @@ def esa_attend_paged(q: torch.Tensor, cu: torch.Tensor, start: torch.Tensor, pag
     itself; else the initial, the local and the selected positions idx [n_seq, n_sel] int32 (-1: none), segments as esa_segments.
     cap > 0: scores become cap * tanh(score / cap).  Rows behind cu[n_seq] are left as they are, undefined in new tensors."""
     return _native.attend_paged(q, cu, start, pages, k_cache, v_cache, k_scale, v_scale, l_i, l_l, idx, scale, cap, out, return_lse)
+
+
+def esa_rope_frequencies(base: float, rot: int, scaling: int = ESA_SCALE_NONE, factor: float = 1.0, length: float = 0.0, fast: float = 32.0,
+                         slow: float = 1.0) -> torch.Tensor:
+    """Angles a position of the rot/2 pairs, float64 in host memory: base^(-2j/rot), or scaled for contexts `factor` times as long
+    (ESA_SCALE_YARN: pairs that make more than `fast` turns in `length` tokens stay, those that make less than `slow` are divided)."""
+    return _native.rope_frequencies(base, rot, scaling, factor, length, fast, slow)
+
+
+def esa_rope_at(q: torch.Tensor, pos: torch.Tensor, freq: torch.Tensor, k: Optional[torch.Tensor] = None, pairs: int = ESA_PAIRS_HALVES,
+                gain: float = 1.0, transposed: bool = False, out_q: Optional[torch.Tensor] = None, out_k: Optional[torch.Tensor] = None):
+    """Rotary encoding of q [n_tok, h, d], and k [n_tok, h_kv, d] in the same call, at positions pos [n_tok] int32 on the GPU; tokens and heads may
+    lie in any order of strides.  freq: esa_rope_frequencies' or any float64 in host memory; the first 2 * len(freq) elements of a head
+    turn, the others are copied.  transposed=True takes gradients of the outputs to gradients of the inputs.  Rows of negative
+    position are left as they are, undefined in a new tensor.  `out_q`, `out_k` may be q and k.  Returns q, or (q, k)."""
+    return _native.rope_at(q, pos, freq, k, pairs, gain, transposed, out_q, out_k)
+
+
+class PagePlan(NamedTuple):
+    """What esa_plan_paged writes: cu [n_seq + 1], start, held [n_seq], ring_at [2], pos [n_tok], lack [1] int32, slot [n_tok] int64."""
+    cu: torch.Tensor
+    start: torch.Tensor
+    held: torch.Tensor
+    ring_at: torch.Tensor
+    pos: torch.Tensor
+    slot: torch.Tensor
+    lack: torch.Tensor
+
+    @staticmethod
+    def empty(n_seq: int, n_tok: int, device) -> "PagePlan":
+        def ints(n, dtype=torch.int32):
+            return torch.empty(n, dtype=dtype, device=device)
+        return PagePlan(ints(n_seq + 1), ints(n_seq), ints(n_seq), ints(2), ints(n_tok), ints(n_tok, torch.int64), ints(1))
+
+
+def esa_plan_paged(new: torch.Tensor, start: torch.Tensor, held: torch.Tensor, pages: torch.Tensor, ring: torch.Tensor, ring_at: torch.Tensor,
+                   page_size: int, n_tok: int, grow: Optional[torch.Tensor] = None, out: Optional[PagePlan] = None) -> PagePlan:
+    """Begins a step of new[b] tokens of sequence b [n_seq], which has start[b] (+ grow[b]) in the cache and holds the pages pages[b, :held[b]] of a
+    pool of len(ring) pages; ring holds those that nobody holds, ring_at[1] of them from place ring_at[0] on.  Pages that are no longer needed go
+    back to the ring, those that are needed come from it: pages [n_seq, max_pages] and ring are changed in place.  n_tok is the number of
+    rows that there is room for.  Returns cu, start and (with pages) what esa_append_paged and esa_attend_paged take, pos as esa_rope_at
+    takes it, slot = page * page_size + pos % page_size (-1: none), the next call's held and ring_at, and lack, the pages that were not to be
+    had.  `out` is written into and returned; its start, held and ring_at may be the arguments of these names."""
+    if out is None:
+        out = PagePlan.empty(pages.shape[0], n_tok, pages.device)
+    _native.plan_paged(new, start, held, pages, ring, ring_at, page_size, n_tok, grow, *out)
+    return out
+
+
+def esa_verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu: torch.Tensor, u: torch.Tensor, draft: Optional[torch.Tensor] = None,
+                      out: Optional[torch.Tensor] = None, count: Optional[torch.Tensor] = None):
+    """Rows cu[b] .. cu[b+1] are sequence b's last token and the drafted ones behind it: tokens [n_tok] int32, target [n_tok, vocab] the target's
+    probabilities behind each row, draft [n_tok, vocab] those that the row's token was drawn from (None: it was looked up), u [n_tok] fp32 random numbers
+    (a drafted row's decides whether it stands, the first row's draws the token behind the last that stands).  Returns (out [n_tok],
+    count [n_seq]) int32: the token behind each row, -1 behind the drawn one, and how many there are.  Rows behind cu[n_seq] are left as they are,
+    undefined in a new tensor."""
+    return _native.verify_drafts(target, tokens, cu, u, draft, out, count)

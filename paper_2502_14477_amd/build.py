@@ -10,6 +10,7 @@ PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 PAGED = os.path.join(PKG, "paged")
+SERVE = os.path.join(PKG, "serve")
 OBJ = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libesa.so")
 NATIVE = os.path.join(PKG, "_native.so")
@@ -43,6 +44,9 @@ PAGED_FLAGS = {
     "attend_few.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"],
     "attend_many.hip": ["-mno-amdgpu-ieee", "-fno-honor-nans"],
 }
+
+# The calls around the paged cache.
+SERVE_SOURCES = ["serve_api.hip", "rope_at.hip", "plan.hip", "verify.hip"]
 
 
 def _hipcc() -> str:
@@ -90,7 +94,7 @@ def build(verbose: bool = False, jobs: int = 8) -> str:
 
     with ThreadPoolExecutor(max_workers=jobs) as pool:
         native = pool.submit(_run, ["g++", *native_compile, "-c", os.path.join(CSRC, "binding.cpp"), "-o", native_obj])
-        jobs = [(PAGED, s, PAGED_FLAGS.get(s, [])) for s in PAGED_SOURCES] + [(CSRC, s, EXTRA_FLAGS.get(s, [])) for s in SOURCES]
+        jobs = [(PAGED, s, PAGED_FLAGS.get(s, [])) for s in PAGED_SOURCES] + [(SERVE, s, []) for s in SERVE_SOURCES] + [(CSRC, s, EXTRA_FLAGS.get(s, [])) for s in SOURCES]
         objs = list(pool.map(compile_one, jobs))
         native.result()
     _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", *objs, "-o", LIB])

@@ -25,6 +25,7 @@
 
 #include "esa.h"
 #include "esa_paged.h"
+#include "esa_serve.h"
 
 namespace {
 
@@ -761,6 +762,132 @@ ESA_ENTRY(attend_paged, 15) {
   return want_lse ? tuple_of({result, wrap(std::move(lse))}) : result;
 }
 
+// ---- around the paged cache
+// A tensor of whole numbers in one dimension, its elements one behind the other.
+const at::Tensor& list_of(PyObject* o, at::ScalarType type, const at::Device& dev, int64_t n) {
+  const at::Tensor& t = tensor_of(o);
+  ESA_ASSERT(t.scalar_type() == type && t.dim() == 1 && t.size(0) == n && (n <= 1 || t.stride(0) == 1) && t.device() == dev && "lists that fit each other");
+  return t;
+}
+PyObject* given_or(PyObject* given, at::Tensor fresh) {
+  if (given == Py_None) return wrap(std::move(fresh));
+  Py_INCREF(given);
+  return given;
+}
+
+// base, rot, scaling, factor, length, fast, slow
+ESA_ENTRY(rope_frequencies, 7) {
+  const int rot = int32_of(a[1]);
+  at::Tensor f = new_tensor({rot > 0 ? rot / 2 : 0}, at::kDouble, at::Device(at::kCPU));
+  check(esa_rope_frequencies(float_of(a[0]), rot, int32_of(a[2]), float_of(a[3]), float_of(a[4]), float_of(a[5]), float_of(a[6]), (double*)ptr(f)));
+  return wrap(std::move(f));
+}
+
+// One tensor of a rotation: rows and where they go.
+esa_rope_rows rope_rows_of(const at::Tensor& x, const at::Tensor& out) {
+  const auto n = x.sizes(), s = x.strides(), so = out.strides();
+  ESA_ASSERT(n.size() == 3 && out.sizes() == n && out.scalar_type() == x.scalar_type() && out.device() == x.device());
+  ESA_ASSERT((s[2] == 1 || n[2] == 1) && (so[2] == 1 || n[2] == 1) && n[1] <= INT32_MAX && n[2] <= INT32_MAX);
+  return esa_rope_rows{ptr(x), ptr(out), s[0], s[1], so[0], so[1], (int)n[1]};
+}
+
+// q, pos, freq, k, pairs, gain, transposed, out_q, out_k
+ESA_ENTRY(rope_at, 9) {
+  const at::Tensor &q = tensor_of(a[0]), &freq = tensor_of(a[2]);
+  const at::Tensor *k = tensor_or_none(a[3]), *oq = tensor_or_none(a[7]), *ok = tensor_or_none(a[8]);
+  ESA_ASSERT(q.dim() == 3 && (!k || (k->dim() == 3 && k->size(0) == q.size(0) && k->size(2) == q.size(2) && k->scalar_type() == q.scalar_type() && k->device() == q.device())));
+  ESA_ASSERT(k || !ok);
+  ESA_ASSERT(freq.device().is_cpu() && freq.scalar_type() == at::kDouble && freq.dim() == 1 && freq.is_contiguous() && freq.size(0) <= 65536);
+  const at::Tensor& pos = list_of(a[1], at::kInt, q.device(), q.size(0));
+  const int dt = dtype_of(q), pairs = int32_of(a[4]), transposed = true_of(a[6]);
+  const double gain = float_of(a[5]);
+  on_gpu(q);
+  const c10::DeviceGuard guard(q.device());
+  at::Tensor fresh_q, fresh_k;
+  if (!oq) fresh_q = new_tensor(q.sizes(), q.scalar_type(), q.device());
+  if (k && !ok) fresh_k = new_tensor(k->sizes(), k->scalar_type(), k->device());
+  esa_rope_rows rows[2] = {rope_rows_of(q, oq ? *oq : fresh_q), {}};
+  if (k) rows[1] = rope_rows_of(*k, ok ? *ok : fresh_k);
+  void* st = stream_on(q.device());
+  const int64_t n = q.size(0), d = q.size(2), rot = 2 * freq.size(0);
+  launch([&] {
+    return esa_rope_at(rows, k ? 2 : 1, (const int32_t*)ptr(pos), n, (int)d, (int)rot, (const double*)ptr(freq), pairs, gain, transposed, dt, st);
+  });
+  PyObject* first = given_or(a[7], std::move(fresh_q));
+  if (!k) return first;
+  return tuple_of({first, given_or(a[8], std::move(fresh_k))});
+}
+
+// new, start, held, pages, ring, ring_at, page_size, n_tok, grow, then the outputs: cu, start, held, ring_at, pos, slot, lack
+ESA_ENTRY(plan_paged, 16) {
+  const at::Tensor &pages = tensor_of(a[3]), &ring = tensor_of(a[4]);
+  const at::Device dev = pages.device();
+  ESA_ASSERT(pages.scalar_type() == at::kInt && pages.dim() == 2 && (pages.stride(1) == 1 || pages.size(1) == 1) && pages.size(0) <= INT32_MAX && pages.size(1) <= INT32_MAX);
+  ESA_ASSERT(ring.dim() == 1 && ring.size(0) <= INT32_MAX);
+  const int64_t n_seq = pages.size(0), n_tok = int_of(a[7]);
+  if (n_tok < 0) fail_esa(ESA_EINVAL, "esa_plan_paged: negative n_tok");
+  esa_page_state s;
+  const int32_t* fresh = (const int32_t*)ptr(list_of(a[0], at::kInt, dev, n_seq));
+  s.start_in = (const int32_t*)ptr(list_of(a[1], at::kInt, dev, n_seq));
+  s.held_in = (const int32_t*)ptr(list_of(a[2], at::kInt, dev, n_seq));
+  s.ring = (int32_t*)ptr(list_of(a[4], at::kInt, dev, ring.size(0)));
+  s.ring_at_in = (const int32_t*)ptr(list_of(a[5], at::kInt, dev, 2));
+  const int32_t* grow = a[8] == Py_None ? nullptr : (const int32_t*)ptr(list_of(a[8], at::kInt, dev, n_seq));
+  int32_t* cu = (int32_t*)ptr(list_of(a[9], at::kInt, dev, n_seq + 1));
+  s.start = (int32_t*)ptr(list_of(a[10], at::kInt, dev, n_seq));
+  s.held = (int32_t*)ptr(list_of(a[11], at::kInt, dev, n_seq));
+  s.ring_at = (int32_t*)ptr(list_of(a[12], at::kInt, dev, 2));
+  int32_t* pos = (int32_t*)ptr(list_of(a[13], at::kInt, dev, n_tok));
+  int64_t* slot = (int64_t*)ptr(list_of(a[14], at::kLong, dev, n_tok));
+  int32_t* lack = (int32_t*)ptr(list_of(a[15], at::kInt, dev, 1));
+  s.pages = (int32_t*)ptr(pages);
+  s.n_seq = (int)n_seq;
+  s.max_pages = (int)pages.size(1);
+  s.pages_ld = n_seq > 1 ? pages.stride(0) : s.max_pages;
+  s.n_pages = (int)ring.size(0);
+  s.page_size = int32_of(a[6]);
+  on_gpu(pages);
+  const c10::DeviceGuard guard(dev);
+  const Scratch ws = scratch(esa_plan_paged_workspace_bytes(s.n_seq));
+  void *st = stream_on(dev), *wp = ws.p;
+  const size_t wn = ws.n;
+  launch([&] { return esa_plan_paged(&s, grow, fresh, n_tok, cu, pos, slot, lack, wp, wn, st); });
+  Py_RETURN_NONE;
+}
+
+// target, tokens, cu, u, draft, out, count
+ESA_ENTRY(verify_drafts, 7) {
+  const at::Tensor &target = tensor_of(a[0]), &cu = tensor_of(a[2]);
+  const at::Tensor *draft = tensor_or_none(a[4]), *out = tensor_or_none(a[5]), *count = tensor_or_none(a[6]);
+  const at::Device dev = target.device();
+  const int dt = dtype_of(target);
+  ESA_ASSERT(target.dim() == 2 && (target.stride(1) == 1 || target.size(1) == 1));
+  const int64_t n = target.size(0), vocab = target.size(1), ldt = n > 1 ? target.stride(0) : vocab;
+  ESA_ASSERT(cu.dim() == 1 && cu.size(0) >= 1 && cu.size(0) - 1 <= INT32_MAX);
+  const int64_t n_seq = cu.size(0) - 1;
+  int64_t ldd = vocab;
+  if (draft) {
+    ESA_ASSERT(draft->sizes() == target.sizes() && draft->scalar_type() == target.scalar_type() && draft->device() == dev && (draft->stride(1) == 1 || vocab == 1));
+    if (n > 1) ldd = draft->stride(0);
+  }
+  const int32_t* cp = (const int32_t*)ptr(list_of(a[2], at::kInt, dev, n_seq + 1));
+  const int32_t* tp = (const int32_t*)ptr(list_of(a[1], at::kInt, dev, n));
+  const float* up = (const float*)ptr(list_of(a[3], at::kFloat, dev, n));
+  if (out) list_of(a[5], at::kInt, dev, n);
+  if (count) list_of(a[6], at::kInt, dev, n_seq);
+  on_gpu(target);
+  const c10::DeviceGuard guard(dev);
+  at::Tensor fresh_out, fresh_count;
+  if (!out) fresh_out = new_tensor({n}, at::kInt, dev);
+  if (!count) fresh_count = new_tensor({n_seq}, at::kInt, dev);
+  int32_t *op = (int32_t*)ptr(out ? *out : fresh_out), *np = (int32_t*)ptr(count ? *count : fresh_count);
+  const Scratch ws = scratch(esa_verify_drafts_workspace_bytes((int)n_seq, vocab));
+  void *st = stream_on(dev), *wp = ws.p, *target_p = ptr(target), *draft_p = ptr(draft);
+  const size_t wn = ws.n;
+  launch([&] { return esa_verify_drafts(target_p, ldt, draft_p, ldd, tp, up, cp, n, (int)n_seq, vocab, op, np, dt, wp, wn, st); });
+  return tuple_of({given_or(a[5], std::move(fresh_out)), given_or(a[6], std::move(fresh_count))});
+}
+
 // t0, l_i, l_l
 ESA_ENTRY(segments, 3) {
   int64_t i_end = 0, l_start = 0;
@@ -780,7 +907,8 @@ ESA_ENTRY(set_error_class, 1) {
 PyMethodDef methods[] = {ESA_METHOD(compress), ESA_METHOD(compress_qk), ESA_METHOD(score), ESA_METHOD(select_topk),
                          ESA_METHOD(select_topk_static), ESA_METHOD(score_select_gather), ESA_METHOD(gather_kv),
                          ESA_METHOD(attend_indexed), ESA_METHOD(attend_reencoded), ESA_METHOD(attend), ESA_METHOD(attend_local),
-                         ESA_METHOD(rope), ESA_METHOD(append_paged), ESA_METHOD(attend_paged), ESA_METHOD(segments), ESA_METHOD(set_error_class), {nullptr, nullptr, 0, nullptr}};
+                         ESA_METHOD(rope), ESA_METHOD(append_paged), ESA_METHOD(attend_paged), ESA_METHOD(rope_frequencies), ESA_METHOD(rope_at),
+                         ESA_METHOD(plan_paged), ESA_METHOD(verify_drafts), ESA_METHOD(segments), ESA_METHOD(set_error_class), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", "argument marshalling for libesa", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

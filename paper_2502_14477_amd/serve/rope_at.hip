@@ -1,0 +1,239 @@
+// Rotary encoding of queries and keys at positions that lie on the device (esa_rope_at).
+//
+// Pair j of a token at position p turns by a = p freq[j] in every head: x' = g (x cos a - y sin a), y' = g (y cos a + x sin a).  Angles,
+// their sines and cosines and the products are fp64 with one rounding into the storage type, as esa_rope's are, by a shorter evaluation of the same
+// precision.
+#include "serve.h"
+
+namespace esa {
+namespace serve {
+namespace {
+
+typedef __attribute__((ext_vector_type(2))) double f64x2;
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+
+constexpr int kThreads = 256;
+constexpr int kAhead = 4;      // heads of a thread whose loads are under way together
+
+// Cosine and sine of an angle below 2^38 in magnitude.  Reduced to [-pi/4, pi/4] by a multiple of pi/2 that is held in two parts
+// (the first product is exact in the fma, the second's error is 2^38 2^-107), then the Taylor series: x^17/17! is below 5e-17 of the sine, x^18/18!
+// below 3e-18.
+__device__ __forceinline__ f64x2 turn_of(double angle) {
+  constexpr double kTwoOverPi = 0.63661977236758134308, kPio2 = 1.5707963267948965580, kPio2Low = 6.1232339957367660359e-17;
+  const double k = __builtin_rint(angle * kTwoOverPi);
+  const double x = __builtin_fma(-k, kPio2Low, __builtin_fma(-k, kPio2, angle)), z = x * x;
+  double s = -1.0 / 1307674368000.0;      // 15!
+  s = __builtin_fma(s, z, 1.0 / 6227020800.0);
+  s = __builtin_fma(s, z, -1.0 / 39916800.0);
+  s = __builtin_fma(s, z, 1.0 / 362880.0);
+  s = __builtin_fma(s, z, -1.0 / 5040.0);
+  s = __builtin_fma(s, z, 1.0 / 120.0);
+  s = __builtin_fma(s, z, -1.0 / 6.0);
+  s = __builtin_fma(s * z, x, x);
+  double c = 1.0 / 20922789888000.0;      // 16!
+  c = __builtin_fma(c, z, -1.0 / 87178291200.0);
+  c = __builtin_fma(c, z, 1.0 / 479001600.0);
+  c = __builtin_fma(c, z, -1.0 / 3628800.0);
+  c = __builtin_fma(c, z, 1.0 / 40320.0);
+  c = __builtin_fma(c, z, -1.0 / 720.0);
+  c = __builtin_fma(c, z, 1.0 / 24.0);
+  c = __builtin_fma(c, z, -0.5);
+  c = __builtin_fma(c, z, 1.0);
+  const int quarter = (int)(k - 4.0 * __builtin_floor(k * 0.25));
+  const double a = quarter & 1 ? s : c, b = quarter & 1 ? c : s;
+  return f64x2{quarter == 1 || quarter == 2 ? -a : a, quarter >= 2 ? -b : b};
+}
+
+template <typename T> __device__ __forceinline__ double to_f64(T v);
+template <> __device__ __forceinline__ double to_f64<float>(float v) { return (double)v; }
+template <> __device__ __forceinline__ double to_f64<bf16_t>(bf16_t v) { return (double)bf16_to_f32(v); }
+
+// Rounded into storage, N at a time.
+template <int N> __device__ __forceinline__ void to_storage(const double (&v)[N], float (&o)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = (float)v[i];
+}
+template <int N> __device__ __forceinline__ void to_storage(const double (&v)[N], bf16_t (&o)[N]) {
+  float f[N];
+  narrow_for_bf16(v, f);
+#pragma unroll
+  for (int i = 0; i < N; i += 2) {
+    const uint32_t w = __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2{f[i], f[i + 1]}), bf16x2));
+    o[i] = (bf16_t)w;
+    o[i + 1] = (bf16_t)(w >> 16);
+  }
+}
+
+template <typename T, int N> struct alignas(N * sizeof(T)) Piece {
+  T x[N];
+};
+
+// Where head hh of all sets' lies.
+struct Place {
+  const char* x;
+  char* out;
+};
+__device__ __forceinline__ Place place_of(const RopeArgs& a, int64_t tok, int hh) {
+  const RowSet &f = a.set[0], &g = a.set[1];
+  const bool second = hh >= f.heads;
+  const int64_t h = second ? hh - f.heads : hh;
+  return Place{(second ? g.x : f.x) + tok * (second ? g.x_tok : f.x_tok) + h * (second ? g.x_head : f.x_head),
+               (second ? g.out : f.out) + tok * (second ? g.out_tok : f.out_tok) + h * (second ? g.out_head : f.out_head)};
+}
+
+// A thread owns N pairs: elements of two pieces of N elements, one in each half, or of 2 N neighbours.  N = 1 takes elements one by one, whatever their
+// alignment.
+template <typename T, int N, bool HALVES> struct Pairs {
+  static constexpr bool kSingle = N == 1;
+  T x[N], y[N];
+  __device__ __forceinline__ void load(const char* p, int i, int half) {
+    if constexpr (HALVES || kSingle) {
+      const int step = HALVES ? 1 : 2, gap = HALVES ? half : 1;
+      const Piece<T, N> a = *(const Piece<T, N>*)(p + (int64_t)i * step * (int)sizeof(T)), b = *(const Piece<T, N>*)(p + (int64_t)(i * step + gap) * (int)sizeof(T));
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        x[j] = a.x[j];
+        y[j] = b.x[j];
+      }
+    } else {
+      const Piece<T, N> a = *(const Piece<T, N>*)(p + (int64_t)i * 2 * (int)sizeof(T)), b = *(const Piece<T, N>*)(p + (int64_t)(i * 2 + N) * (int)sizeof(T));
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        x[j] = j < N / 2 ? a.x[2 * j] : b.x[2 * j - N];
+        y[j] = j < N / 2 ? a.x[2 * j + 1] : b.x[2 * j + 1 - N];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(char* p, int i, int half) const {
+    Piece<T, N> a, b;
+    if constexpr (HALVES || kSingle) {
+      const int step = HALVES ? 1 : 2, gap = HALVES ? half : 1;
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        a.x[j] = x[j];
+        b.x[j] = y[j];
+      }
+      *(Piece<T, N>*)(p + (int64_t)i * step * (int)sizeof(T)) = a;
+      *(Piece<T, N>*)(p + (int64_t)(i * step + gap) * (int)sizeof(T)) = b;
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        if (j < N / 2) {
+          a.x[2 * j] = x[j];
+          a.x[2 * j + 1] = y[j];
+        } else {
+          b.x[2 * j - N] = x[j];
+          b.x[2 * j + 1 - N] = y[j];
+        }
+      }
+      *(Piece<T, N>*)(p + (int64_t)i * 2 * (int)sizeof(T)) = a;
+      *(Piece<T, N>*)(p + (int64_t)(i * 2 + N) * (int)sizeof(T)) = b;
+    }
+  }
+  __device__ __forceinline__ void turn(const f64x2 (&cs)[N]) {
+    constexpr int kTogether = N < 4 ? N : 4;      // pairs whose roundings share a branch
+#pragma unroll
+    for (int j0 = 0; j0 < N; j0 += kTogether) {
+      double v[2 * kTogether];
+      T o[2 * kTogether];
+#pragma unroll
+      for (int j = 0; j < kTogether; ++j) {
+        const double a = to_f64<T>(x[j0 + j]), b = to_f64<T>(y[j0 + j]);
+        v[j] = a * cs[j0 + j][0] - b * cs[j0 + j][1];
+        v[kTogether + j] = b * cs[j0 + j][0] + a * cs[j0 + j][1];
+      }
+      to_storage(v, o);
+#pragma unroll
+      for (int j = 0; j < kTogether; ++j) {
+        x[j0 + j] = o[j];
+        y[j0 + j] = o[kTogether + j];
+      }
+    }
+  }
+};
+
+// A workgroup takes `toks` tokens; a thread N pairs of one of them, for every hs-th head.  The tokens' cosines and sines go through LDS.
+template <typename T, int N, bool HALVES>
+__global__ __launch_bounds__(kThreads) void rope_at(RopeArgs a, int toks, int hs) {
+  extern __shared__ f64x2 cs[];                   // [toks][half]
+  const int tid = threadIdx.x;
+  const int64_t tok0 = ((int64_t)blockIdx.y * paged::kGridRow + blockIdx.x) * toks;
+  if (tok0 >= a.n_tok) return;
+  const int n = (int)min((int64_t)toks, a.n_tok - tok0);
+  const int vecs = a.half / N;
+  const int i = tid % vecs * N, rest = tid / vecs, h0 = rest % hs, r = rest / hs;
+  const bool mine = r < n;
+  const int64_t tok = tok0 + (mine ? r : 0);
+  const int p = a.pos[tok];
+  Pairs<T, N, HALVES> v[kAhead];
+  Place at[kAhead];
+  auto request = [&](int hb) {
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      at[u] = place_of(a, tok, hb + u * hs < a.heads ? hb + u * hs : 0);
+      v[u].load(at[u].x, i, a.half);
+    }
+  };
+  request(h0);
+  for (int e = tid; e < n * a.half; e += kThreads) {
+    f64x2 t = turn_of((double)a.pos[tok0 + e / a.half] * a.freq[e % a.half]);
+    t *= a.gain;
+    if (a.transposed) t[1] = -t[1];
+    cs[e] = t;
+  }
+  __syncthreads();
+  if (!mine || p < 0) return;
+  f64x2 t[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) t[j] = cs[r * a.half + i + j];
+  for (int hb = h0; hb < a.heads; hb += hs * kAhead) {
+    if (hb != h0) request(hb);
+#pragma unroll
+    for (int u = 0; u < kAhead; ++u) {
+      if (hb + u * hs >= a.heads) break;
+      v[u].turn(t);
+      v[u].store(at[u].out, i, a.half);
+    }
+  }
+  // what does not turn
+  const int tail = a.rest / N;
+  for (int e = i / N + vecs * h0; e < tail * a.heads; e += vecs * hs) {
+    const Place q = place_of(a, tok, e / tail);
+    const int64_t off = (int64_t)(2 * a.half + e % tail * N) * (int)sizeof(T);
+    *(Piece<T, N>*)(q.out + off) = *(const Piece<T, N>*)(q.x + off);
+  }
+}
+
+template <typename T, int N> int launch_of(const RopeArgs& a, hipStream_t st) {
+  const int vecs = a.half / N;                    // at most 128, of which 256 threads take one or more
+  int hs = (a.heads + kAhead - 1) / kAhead;
+  if (hs > kThreads / vecs) hs = kThreads / vecs;
+  const int toks = kThreads / (vecs * hs);
+  const int64_t groups = ((int64_t)a.n_tok + toks - 1) / toks;
+  const size_t lds = (size_t)toks * a.half * sizeof(f64x2);
+  if (a.pairs == ESA_PAIRS_HALVES)
+    rope_at<T, N, true><<<paged::grid_for(groups), kThreads, lds, st>>>(a, toks, hs);
+  else
+    rope_at<T, N, false><<<paged::grid_for(groups), kThreads, lds, st>>>(a, toks, hs);
+  ESA_LAUNCH_CHECK("rope_at");
+  return ESA_OK;
+}
+
+}  // namespace
+
+int launch_rope_at(const RopeArgs& a, int dtype, hipStream_t st) {
+  const int es = dtype == ESA_F32 ? 4 : 2;
+  // Pieces of 16 or 8 bytes where every row, the pairs and what is behind them allow it.
+  int64_t all = (int64_t)a.half * es | (int64_t)a.rest * es;
+  for (const RowSet& s : a.set) {
+    if (s.heads == 0) continue;
+    all |= (int64_t)(uintptr_t)s.x | (int64_t)(uintptr_t)s.out | s.x_tok | s.x_head | s.out_tok | s.out_head;
+  }
+  const int piece = all % 16 == 0 ? 16 : all % 8 == 0 ? 8 : es;
+  if (dtype == ESA_F32) return piece == 16 ? launch_of<float, 4>(a, st) : piece == 8 ? launch_of<float, 2>(a, st) : launch_of<float, 1>(a, st);
+  return piece == 16 ? launch_of<bf16_t, 8>(a, st) : piece == 8 ? launch_of<bf16_t, 4>(a, st) : launch_of<bf16_t, 1>(a, st);
+}
+
+}  // namespace serve
+}  // namespace esa

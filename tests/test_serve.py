@@ -1,0 +1,212 @@
+"""The calls around the paged cache without a GPU: the header, refusals, frequencies, the oracle against itself."""
+import ctypes
+import math
+import os
+import re
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2502_14477_amd as esa
+from oracle import serve_oracle as orc
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+FAKE, ODD = 4096, 4097            # never dereferenced: every call below fails validation, or has nothing to do
+
+
+def test_header_is_plain_c_and_its_symbols_are_exported():
+    path = os.path.join(ROOT, "include", "esa_serve.h")
+    for lang, std in (("c", "-std=c99"), ("c++", "-std=c++11")):
+        r = subprocess.run(["gcc", "-x", lang, std, "-Wall", "-Wextra", "-Werror", "-pedantic", "-fsyntax-only", path], capture_output=True, text=True)
+        assert r.returncode == 0, r.stderr
+    names = sorted(set(re.findall(r"ESA_API\s+[\w\s\*]+?\b(esa_\w+)\s*\(", open(path).read())))
+    assert names == sorted(esa.SERVE_EXPORTS)
+    raw = ctypes.CDLL(esa.lib_path())
+    for n in names:
+        assert hasattr(raw, n), n
+
+
+def test_the_structures_are_laid_out_as_in_c(tmp_path):
+    src, exe = tmp_path / "layout.c", tmp_path / "layout"
+    kinds = {"esa_rope_rows": esa.RopeRows, "esa_page_state": esa.PageState}
+    lines = "".join('printf("%%zu ", sizeof(%s));' % t + "".join('printf("%%zu ", offsetof(%s, %s));' % (t, f[0]) for f in k._fields_) for t, k in kinds.items())
+    src.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "esa_serve.h"\nint main(void) { %s return 0; }' % lines)
+    subprocess.run(["gcc", "-std=c99", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)], check=True)
+    got = [int(x) for x in subprocess.run([str(exe)], capture_output=True, text=True, check=True).stdout.split()]
+    assert got == [n for k in kinds.values() for n in [ctypes.sizeof(k)] + [getattr(k, f[0]).offset for f in k._fields_]]
+
+
+# ---------------------------------------------------------------- rotation
+@pytest.mark.parametrize("rot", [2, 4, 20, 64, 128, 256])
+@pytest.mark.parametrize("scaling", ["none", "linear", "ntk", "yarn"])
+def test_frequencies(rot, scaling):
+    kind = {"none": 0, "linear": 1, "ntk": 2, "yarn": 3}[scaling]
+    got = esa.esa_rope_frequencies(5e5, rot, kind, 8.0, 32768.0, 32.0, 1.0).numpy()
+    want = orc.frequencies(5e5, rot, scaling, 8.0, 32768.0, 32.0, 1.0)
+    assert got.shape == (rot // 2,)
+    # powers within a step or two, quotients and sums a rounding each
+    assert np.all(np.abs(got - want) <= 2.0 ** -50 * want)
+    if scaling == "ntk" and rot > 2:                              # what the change of base is for
+        assert got[0] == 1.0 and math.isclose(got[-1], 5e5 ** (-(rot - 2) / rot) / 8.0, rel_tol=1e-13)
+
+
+def test_frequencies_refuse():
+    f = (ctypes.c_double * 128)()
+    for args, code in (((0.5, 64, 0, 1, 0, 0, 0), -1), ((float("nan"), 64, 0, 1, 0, 0, 0), -1), ((float("inf"), 64, 0, 1, 0, 0, 0), -1), ((1e4, 0, 0, 1, 0, 0, 0), -1),
+                       ((1e4, 63, 0, 1, 0, 0, 0), -1), ((1e4, 258, 0, 1, 0, 0, 0), -1), ((1e4, 64, 4, 1, 0, 0, 0), -2), ((1e4, 64, -1, 1, 0, 0, 0), -2),
+                       ((1e4, 64, 1, 0.0, 0, 0, 0), -1), ((1e4, 64, 2, float("inf"), 0, 0, 0), -1), ((1e4, 64, 3, 8, 0.0, 32, 1), -1),
+                       ((1e4, 64, 3, 8, 4096, 1, 1), -1), ((1e4, 64, 3, 8, 4096, float("nan"), 1), -1)):
+        assert esa.lib.esa_rope_frequencies(*args, f) == code, args
+    assert esa.lib.esa_rope_frequencies(1e4, 64, 0, 1, 0, 0, 0, None) == -1
+    assert esa.lib.esa_rope_frequencies(1e4, 64, 0, float("nan"), 0, 0, 0, f) == 0      # what the kind does not use is not looked at
+    for bad in ((0.5, 64), (1e4, -2), (1e4, 63)):
+        with pytest.raises(esa.EsaError):
+            esa.esa_rope_frequencies(*bad)
+
+
+def rows(**kw):
+    d = dict(x=FAKE, out=2 * FAKE, x_tok=512, x_head=128, out_tok=512, out_head=128, heads=4)
+    return esa.RopeRows(**{**d, **kw})
+
+
+def rope_at(r=None, n_rows=1, pos=FAKE, n_tok=5, d=128, rot=128, freq=None, pairs=0, gain=1.0, transposed=0, dtype=1):
+    f = (ctypes.c_double * 128)(*(freq or [1.0] * 128))
+    r = r or rows()
+    return esa.lib.esa_rope_at(ctypes.byref(r) if not isinstance(r, ctypes.Array) else r, n_rows, pos, n_tok, d, rot, f, pairs, gain, transposed, dtype, None)
+
+
+def test_rope_at_refuses():
+    for change, code in ((dict(dtype=2), -2), (dict(pairs=2), -2), (dict(rot=130), -2), (dict(rot=63), -2), (dict(rot=0), -2), (dict(d=1026, rot=64), -2),
+                         (dict(d=512, rot=258), -2), (dict(n_rows=0), -1), (dict(n_rows=3), -1), (dict(n_tok=-1), -1), (dict(n_tok=1 << 31), -1),
+                         (dict(gain=float("nan")), -1), (dict(gain=float("inf")), -1), (dict(freq=[65.0]), -1), (dict(freq=[float("nan")]), -1), (dict(pos=None), -1),
+                         (dict(pos=ODD), -1), (dict(r=rows(heads=0)), -1), (dict(r=rows(heads=65536)), -1), (dict(r=rows(x=None)), -1), (dict(r=rows(out=None)), -1),
+                         (dict(r=rows(x=ODD)), -1), (dict(r=rows(x_tok=-512)), -1), (dict(r=rows(x_tok=1 << 60)), -1), (dict(r=rows(out_head=127)), -1),
+                         (dict(r=rows(out_tok=511)), -1), (dict(r=rows(out_tok=128, out_head=128)), -1), (dict(r=rows(out_tok=0)), -1),
+                         (dict(r=rows(out=FAKE, x_tok=1024)), -1), (dict(r=rows(out=FAKE, x_head=256, x_tok=512)), -1)):
+        assert rope_at(**change) == code, change
+        assert b"esa_rope_at" in esa.lib.esa_last_error()
+    assert esa.lib.esa_rope_at(None, 1, FAKE, 5, 128, 128, (ctypes.c_double * 64)(), 0, 1.0, 0, 1, None) == -1
+    assert esa.lib.esa_rope_at(ctypes.byref(rows()), 1, FAKE, 5, 128, 128, None, 0, 1.0, 0, 1, None) == -1
+    two = (esa.RopeRows * 2)(rows(), rows(out_head=64))
+    assert rope_at(r=two, n_rows=2) == -1
+
+
+def test_rope_at_has_nothing_to_do():
+    assert rope_at(r=rows(x=None, out=None), pos=None, n_tok=0) == 0
+
+
+# ---------------------------------------------------------------- plans
+def state(**kw):
+    d = dict(start_in=FAKE, held_in=FAKE, ring_at_in=FAKE, start=FAKE, held=FAKE, ring_at=FAKE, pages=FAKE, pages_ld=8, ring=FAKE, n_seq=3, max_pages=8,
+             n_pages=20, page_size=64)
+    return esa.PageState(**{**d, **kw})
+
+
+def plan(s=None, grow=FAKE, fresh=FAKE, n_tok=7, cu=FAKE, pos=FAKE, slot=FAKE, lack=FAKE, ws=FAKE, ws_bytes=1 << 30):
+    return esa.lib.esa_plan_paged(ctypes.byref(s or state()), grow, fresh, n_tok, cu, pos, slot, lack, ws, ws_bytes, None)
+
+
+def test_plan_refuses():
+    for change, code in ((dict(s=state(page_size=48)), -2), (dict(s=state(page_size=0)), -2), (dict(s=state(n_seq=-1)), -1), (dict(s=state(n_seq=(1 << 24) + 1)), -1),
+                         (dict(s=state(max_pages=0)), -1), (dict(s=state(pages_ld=7)), -1), (dict(s=state(n_pages=0)), -1), (dict(n_tok=-1), -1), (dict(n_tok=1 << 31), -1),
+                         (dict(s=state(max_pages=1 << 25, pages_ld=1 << 25)), -1), (dict(s=state(pages_ld=1 << 40)), -1), (dict(fresh=None), -1), (dict(cu=None), -1),
+                         (dict(pos=None), -1), (dict(slot=None), -1), (dict(slot=FAKE + 4), -1), (dict(lack=None), -1), (dict(grow=ODD), -1), (dict(ws=None), -3),
+                         (dict(ws=ODD), -3), (dict(ws_bytes=64), -3)):
+        assert plan(**change) == code, change
+        assert b"esa_plan_paged" in esa.lib.esa_last_error()
+    for f in ("start_in", "held_in", "ring_at_in", "start", "held", "ring_at", "pages", "ring"):
+        assert plan(s=state(**{f: None})) == -1 and plan(s=state(**{f: ODD})) == -1
+    assert esa.lib.esa_plan_paged(None, None, FAKE, 7, FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 30, None) == -1
+    sizes = [esa.lib.esa_plan_paged_workspace_bytes(n) for n in (-1, 0, 1, 1000, 1 << 24)]
+    assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
+# ---------------------------------------------------------------- drafts
+def verify(target=FAKE, ldt=1000, draft=FAKE, ldd=1000, tokens=FAKE, u=FAKE, cu=FAKE, n_tok=9, n_seq=3, vocab=1000, out=2 * FAKE, count=FAKE, dtype=0, ws=FAKE,
+           ws_bytes=1 << 30):
+    return esa.lib.esa_verify_drafts(target, ldt, draft, ldd, tokens, u, cu, n_tok, n_seq, vocab, out, count, dtype, ws, ws_bytes, None)
+
+
+def test_verify_refuses():
+    for change, code in ((dict(dtype=2), -2), (dict(n_tok=-1), -1), (dict(n_tok=1 << 31), -1), (dict(n_seq=-1), -1), (dict(n_seq=(1 << 24) + 1), -1), (dict(vocab=0), -1),
+                         (dict(vocab=1 << 31), -1), (dict(ldt=999), -1), (dict(ldd=999), -1), (dict(ldt=1 << 60), -1), (dict(target=None), -1), (dict(target=ODD), -1),
+                         (dict(draft=ODD), -1), (dict(tokens=None), -1), (dict(u=None), -1), (dict(cu=None), -1), (dict(out=None), -1), (dict(count=None), -1),
+                         (dict(out=FAKE), -1), (dict(ws=None), -3), (dict(ws=ODD), -3), (dict(ws_bytes=16), -3)):
+        assert verify(**change) == code, change
+        assert b"esa_verify_drafts" in esa.lib.esa_last_error()
+    assert verify(n_seq=0, cu=None, count=None, ws=None) == 0
+
+
+# ---------------------------------------------------------------- the binding
+def ints(*n):
+    return torch.zeros(n, dtype=torch.int32)
+
+
+def test_binding_refuses_what_does_not_fit():
+    q, pos, freq = torch.zeros(5, 4, 64), ints(5), esa.esa_rope_frequencies(1e4, 64)
+    for args, kw in (((q, ints(4), freq), {}), ((q, pos.long(), freq), {}), ((q[0], pos, freq), {}), ((q, pos, freq.float()), {}), ((q, pos, freq[::2]), {}),
+                     ((q, pos, freq), dict(k=q[:4])), ((q, pos, freq), dict(k=q[..., :32])), ((q, pos, freq), dict(k=q.bfloat16())), ((q, pos, freq), dict(out_k=q)),
+                     ((q, torch.zeros(10, dtype=torch.int32)[::2], freq), {}), ((q, pos, freq), {})):
+        with pytest.raises(AssertionError):
+            esa.esa_rope_at(*args, **kw)
+    with pytest.raises(esa.EsaError):
+        esa.esa_rope_at(q.half(), pos, freq)
+    good = dict(new=ints(3), start=ints(3), held=ints(3), pages=ints(3, 4), ring=ints(9), ring_at=ints(2))
+    for bad in (dict(new=ints(2)), dict(start=ints(4)), dict(held=ints(3).long()), dict(pages=ints(12)), dict(pages=ints(4, 3).t()), dict(ring=ints(9).float()),
+                dict(ring_at=ints(3)), dict(grow=ints(2)), dict(out=esa.PagePlan.empty(3, 6, "cpu")), dict(out=esa.PagePlan.empty(2, 7, "cpu")), {}):
+        with pytest.raises(AssertionError):
+            esa.esa_plan_paged(**{**good, **bad}, page_size=16, n_tok=7)
+    p, x, cu, u = torch.zeros(5, 100), ints(5), ints(3), torch.zeros(5)
+    for args, kw in (((p[0], x, cu, u), {}), ((p, x[:4], cu, u), {}), ((p, x, cu.long(), u), {}), ((p, x, cu, u.double()), {}), ((p, x, cu, u), dict(draft=p[:, :99])),
+                     ((p, x, cu, u), dict(draft=p.bfloat16())), ((p, x, cu, u), dict(out=ints(4))), ((p, x, cu, u), dict(count=ints(3))), ((p.t(), x, cu, u), {}),
+                     ((p, x, cu, u), {})):
+        with pytest.raises(AssertionError):
+            esa.esa_verify_drafts(*args, **kw)
+    with pytest.raises(esa.EsaError):
+        esa.esa_verify_drafts(p.half(), x, cu, u)
+
+
+# ---------------------------------------------------------------- the oracle
+def test_oracle_rotation_keeps_lengths_and_its_transposed_is_its_inverse():
+    rng = np.random.default_rng(1)
+    x, pos = rng.standard_normal((6, 3, 40)), [0, 1, 7, 100000, 2 ** 31 - 1, 12]
+    for halves in (True, False):
+        f = orc.frequencies(1e4, 24)
+        y = orc.rope(x, pos, f, halves)
+        assert np.array_equal(y[0], x[0]) and np.array_equal(y[..., 24:], x[..., 24:])
+        assert np.allclose((y ** 2).sum(-1), (x ** 2).sum(-1), rtol=1e-12)
+        assert np.allclose(orc.rope(y, pos, f, halves, transposed=True), x, atol=1e-12)
+        # differences of positions are what scores see
+        a, b = orc.rope(x[:1], [1005], f, halves), orc.rope(x[1:2], [1000], f, halves)
+        c, d = orc.rope(x[:1], [5], f, halves), orc.rope(x[1:2], [0], f, halves)
+        assert np.allclose((a * b).sum(-1), (c * d).sum(-1), atol=1e-10)
+
+
+def test_oracle_pages_are_held_once():
+    rng = np.random.default_rng(2)
+    pool = orc.Pages(5, 40, 60, 16)
+    grow = None
+    for _ in range(60):
+        fresh = rng.integers(0, 40, 5)
+        cu, pos, slot, lack = pool.step(fresh, 120, grow)
+        held = [p for r in pool.rows for p in r]
+        assert sorted(held + pool.free) == list(range(60)) and cu[-1] <= 120
+        used = slot[slot >= 0]
+        assert len(set(used.tolist())) == len(used) and (lack > 0 or np.all((slot >= 0) == (pos >= 0)))
+        grow = np.array([rng.integers(0, n + 1) for n in np.diff(cu)]) - np.where(rng.random(5) < 0.2, pool.start, 0)
+
+
+def test_oracle_verification_draws_from_the_target():
+    """Over all random numbers the first new token is distributed as the target has it, whatever the draft: the point of the procedure."""
+    p, q = np.array([0.5, 0.125, 0.25, 0.125]), np.array([0.125, 0.25, 0.125, 0.5])
+    n = 64
+    grid = (np.arange(n) + 0.5) / n
+    seen = np.zeros(4)
+    for x in range(4):
+        for test in grid:
+            for r in grid:
+                got, _ = orc.verify(np.array([p, p]), [0, x], [0, 2], [r, test], np.array([q, q]))
+                seen[got[0][0]] += q[x] / n / n
+    assert np.all(np.abs(seen - p) <= 4 / n)          # each border of the grid is off by one cell at most
