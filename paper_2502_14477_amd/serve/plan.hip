@@ -9,93 +9,146 @@ namespace esa {
 namespace serve {
 namespace {
 
-constexpr int kScanThreads = 1024;
-constexpr int kWaves = kScanThreads / 64;
+constexpr int kThreads = 1024;
+constexpr int kWaves = kThreads / 64;
 
-// What the rows and pages are filled from.  [n_seq + 1] offsets and [n_seq] numbers a sequence; sums that junk makes longer than 32
-// bits stop at INT32_MAX.
+// What rows and pages are filled from: [n_seq + 1] offsets (those of sequence b end at [b + 1]) and a sequence's numbers.  Sums that
+// junk makes longer than 32 bits stop at INT32_MAX.
+struct alignas(16) Of {
+  int start, had, take, need;      // take: pages taken for the sequences before it
+};
+struct Queue {
+  int first, count, given;         // the free pages, and what is given back and the ring has room for
+};
 struct Offsets {
-  int32_t *row, *give, *take, *need, *had;
-  int32_t* head;      // first free page's place, free pages, pages given back that the ring has room for
+  int32_t *row, *give, *take;
+  Of* of;
 };
-__host__ __device__ inline Offsets offsets_at(void* ws, int n_seq) {
+__host__ __device__ inline size_t offsets_bytes(int n_seq) { return 16 + (size_t)n_seq * sizeof(Of) + 3 * ((size_t)n_seq + 1) * sizeof(int32_t); }
+__host__ __device__ inline Offsets offsets_at(void* p, int n_seq) {
+  Of* of = (Of*)((char*)p + 16);
+  int32_t* ends = (int32_t*)(of + n_seq);
   const size_t n = (size_t)n_seq + 1;
-  int32_t* p = (int32_t*)ws;
-  return Offsets{p + 4, p + 4 + n, p + 4 + 2 * n, p + 4 + 3 * n, p + 4 + 4 * n, p};
+  return Offsets{ends, ends + n, ends + 2 * n, of};
 }
 
-// Sums over the workgroup up to each thread, and of all.  part: [kWaves].
+// Sums that stop at INT32_MAX, of numbers that do not exceed it: what lies beyond is clamped to less in any case, and 32 bits do.
+constexpr uint32_t kMost = INT32_MAX;
+__device__ __forceinline__ uint32_t plus(uint32_t x, uint32_t y) { return min(x + y, kMost); }
+__device__ __forceinline__ uint32_t wave_sums(uint32_t x) {      // of the lanes up to each
+  x = plus(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false));      // row_shr 1, 2, 4, 8
+  x = plus(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false));
+  x = plus(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xF, 0xF, false));
+  x = plus(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xF, 0xF, false));
+  x = plus(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));      // row_bcast 15, 31
+  return plus(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
+}
+// Over the workgroup in front of each thread, and of all.  part: [kWaves].
 struct Scanned {
-  int64_t before, all;
+  uint32_t before, all;
 };
-__device__ __forceinline__ Scanned scan(int64_t x, int64_t* part) {
+template <int N> __device__ __forceinline__ void scan(const uint32_t (&x)[N], Scanned (&s)[N], uint32_t (*part)[kWaves]) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t upto = wave_scan_long(x);
-  __syncthreads();
-  if (lane == 63) part[wave] = upto;
-  __syncthreads();
-  int64_t before = upto - x, all = 0;
+  uint32_t left[N];
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const int64_t v = part[w];
-    before += w < wave ? v : 0;
-    all += v;
+  for (int k = 0; k < N; ++k) {
+    const uint32_t upto = wave_sums(x[k]);
+    left[k] = __shfl_up(upto, 1);
+    if (lane == 63) part[k][wave] = upto;
   }
-  return Scanned{before, all};
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    const uint32_t sums = wave_sums(lane < kWaves ? part[k][lane] : 0);
+    const uint32_t front = wave > 0 ? paged::lane_value(sums, wave - 1) : 0;
+    s[k] = Scanned{plus(front, lane ? left[k] : 0), paged::lane_value(sums, kWaves - 1)};
+  }
 }
-__device__ __forceinline__ int saturated(int64_t x) { return (int)min(x, (int64_t)INT32_MAX); }
 
-// The sequences' lengths and offsets.  One workgroup.
-__device__ void plan_offsets(const PlanArgs& a, const Offsets& o) {
-  __shared__ int64_t part[kWaves];
+// The sequences' lengths and offsets, by one workgroup, EACH of them a thread at a time.
+// `writes`: whether it is the one of them that leaves the call's lengths.
+template <int EACH> __device__ __forceinline__ Queue plan_offsets(const PlanArgs& a, const Offsets& o, bool writes) {
+  __shared__ uint32_t part[3][kWaves];
   const int tid = threadIdx.x;
-  const int first = (int)((uint32_t)max(a.ring_at_in[0], 0) % (uint32_t)a.n_pages), count = min(max(a.ring_at_in[1], 0), a.n_pages);
-  int64_t rows = 0, gives = 0, takes = 0;
-  for (int b0 = 0; b0 < a.n_seq; b0 += kScanThreads) {
-    const int b = b0 + tid;
-    const bool there = b < a.n_seq;
-    const int at = there ? b : 0;
-    int64_t start = (int64_t)a.start_in[at] + (a.grow ? a.grow[at] : 0);
-    const int64_t fresh = there ? max(a.fresh[at], 0) : 0;
-    const int had = min(max(a.held_in[at], 0), a.max_pages);
-    const Scanned r = scan(fresh, part);
-    const int lo = (int)min(rows + r.before, (int64_t)a.n_tok), hi = (int)min(rows + r.before + fresh, (int64_t)a.n_tok);
-    rows += r.all;
-    start = min(max(start, (int64_t)0), (int64_t)(INT32_MAX - (hi - lo)));
-    const int need = (int)min((start + (hi - lo) + (1 << a.page_log2) - 1) >> a.page_log2, (int64_t)a.max_pages);
-    const int64_t give = there ? max(had - need, 0) : 0, take = there ? max(need - had, 0) : 0;
-    const Scanned g = scan(give, part), t = scan(take, part);
-    if (there) {
-      a.start[b] = (int)start;
-      a.cu[b + 1] = hi;
-      o.row[b + 1] = hi;
-      o.give[b + 1] = saturated(gives + g.before + give);
-      o.take[b + 1] = saturated(takes + t.before + take);
-      o.need[b] = need;
-      o.had[b] = had;
+  const int at_in = a.ring_at_in[0], count_in = a.ring_at_in[1];
+  uint32_t rows = 0, gives = 0, takes = 0;
+  for (int r0 = 0; r0 < a.n_seq; r0 += kThreads * EACH) {
+    const int b0 = r0 + tid * EACH;
+    int start[EACH], fresh[EACH], had[EACH], grow[EACH];
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      const int b = min(b0 + j, a.n_seq - 1);
+      start[j] = a.start_in[b];
+      fresh[j] = a.fresh[b];
+      had[j] = a.held_in[b];
+      grow[j] = a.grow ? a.grow[b] : 0;
     }
-    gives += g.all;
-    takes += t.all;
+    uint32_t sum[1] = {0};
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      fresh[j] = b0 + j < a.n_seq ? max(fresh[j], 0) : 0;
+      had[j] = min(max(had[j], 0), a.max_pages);
+      sum[0] = plus(sum[0], fresh[j]);
+    }
+    Scanned s[1];
+    scan<1>(sum, s, part);
+    uint32_t at = plus(rows, s[0].before);
+    rows = plus(rows, s[0].all);
+    int hi[EACH], need[EACH];
+    uint32_t moved[2] = {0, 0};
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      const int lo = (int)min(at, (uint32_t)a.n_tok);
+      at = plus(at, fresh[j]);
+      hi[j] = (int)min(at, (uint32_t)a.n_tok);
+      const int64_t from = (int64_t)start[j] + grow[j];
+      start[j] = (int)min(max(from, (int64_t)0), (int64_t)(INT32_MAX - (hi[j] - lo)));
+      need[j] = (int)min(((uint32_t)start[j] + (uint32_t)(hi[j] - lo) + (1u << a.page_log2) - 1) >> a.page_log2, (uint32_t)a.max_pages);
+      if (b0 + j < a.n_seq) {
+        moved[0] = plus(moved[0], max(had[j] - need[j], 0));
+        moved[1] = plus(moved[1], max(need[j] - had[j], 0));
+      }
+    }
+    Scanned m[2];
+    scan<2>(moved, m, part + 1);
+    uint32_t give = plus(gives, m[0].before), take = plus(takes, m[1].before);
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) {
+      const int b = b0 + j;
+      if (b >= a.n_seq) break;
+      o.of[b] = Of{start[j], had[j], (int)take, need[j]};
+      give = plus(give, max(had[j] - need[j], 0));
+      take = plus(take, max(need[j] - had[j], 0));
+      o.row[b + 1] = hi[j];
+      o.give[b + 1] = (int)give;
+      o.take[b + 1] = (int)take;
+      if (writes) {
+        a.start[b] = start[j];
+        a.cu[b + 1] = hi[j];
+      }
+    }
+    gives = plus(gives, m[0].all);
+    takes = plus(takes, m[1].all);
   }
-  const int given = (int)min(gives, (int64_t)(a.n_pages - count)), free = count + given, taken = (int)min(takes, (int64_t)free);
-  __syncthreads();
-  if (tid == 0) {
-    a.cu[0] = o.row[0] = o.give[0] = o.take[0] = 0;
-    o.head[0] = first;
-    o.head[1] = count;
-    o.head[2] = given;
-    a.ring_at[0] = (int)(((int64_t)first + taken) % a.n_pages);
+  const int first = (int)((uint32_t)max(at_in, 0) % (uint32_t)a.n_pages), count = min(max(count_in, 0), a.n_pages);
+  const int given = min((int)gives, a.n_pages - count), free = count + given, taken = min((int)takes, free);
+  if (tid == 0) o.row[0] = o.give[0] = o.take[0] = 0;
+  if (tid == 0 && writes) {
+    a.cu[0] = 0;
+    const uint32_t next = (uint32_t)first + taken;      // below 2 n_pages
+    a.ring_at[0] = (int)(next >= (uint32_t)a.n_pages ? next - a.n_pages : next);
     a.ring_at[1] = free - taken;
-    a.lack[0] = saturated(takes - taken);
+    a.lack[0] = (int)takes - taken;
   }
   __syncthreads();
-  for (int b = tid; b < a.n_seq; b += kScanThreads) {
-    const int need = o.need[b], had = o.had[b];
-    a.held[b] = need > had ? had + min(o.take[b + 1], free) - min(o.take[b], free) : need;
+  for (int b = tid; writes && b < a.n_seq; b += kThreads) {
+    const Of x = o.of[b];
+    a.held[b] = x.need > x.had ? x.had + (int)min((uint32_t)x.take + (uint32_t)(x.need - x.had), (uint32_t)free) - min(x.take, free) : x.need;
   }
+  return Queue{first, count, given};
 }
 
-// The sequence in which item i falls, of those that end at end[1], end[2], ...: the number of ends up to i.
+// The sequence in which item i falls: the number of ends (end[1], end[2], ...) up to i.
 __device__ __forceinline__ int sequence_of(const int32_t* end, int n_seq, int i) {
   int lo = 0, n = n_seq;
   while (n > 0) {
@@ -106,18 +159,19 @@ __device__ __forceinline__ int sequence_of(const int32_t* end, int n_seq, int i)
   }
   return lo;
 }
-
-struct Queue {
-  int first, count, given;
-};
+// Place x < 3 n_pages round the ring.
+__device__ __forceinline__ int64_t in_ring(const PlanArgs& a, int64_t x) {
+  x -= x >= a.n_pages ? a.n_pages : 0;
+  return x - (x >= a.n_pages ? a.n_pages : 0);
+}
 // The r-th page that is given back.
 __device__ __forceinline__ int given_page(const PlanArgs& a, const Offsets& o, int r) {
   const int b = min(sequence_of(o.give, a.n_seq, r), a.n_seq - 1);
-  return a.pages[(int64_t)b * a.pages_ld + min(o.need[b] + (r - o.give[b]), a.max_pages - 1)];
+  return a.pages[(int64_t)b * a.pages_ld + min(o.of[b].need + (r - o.give[b]), a.max_pages - 1)];
 }
 // The t-th page of the queue, -1 behind its end.
 __device__ __forceinline__ int taken_page(const PlanArgs& a, const Offsets& o, const Queue& q, int64_t t) {
-  if (t < q.count) return a.ring[(q.first + t) % a.n_pages];
+  if (t < q.count) return a.ring[in_ring(a, q.first + t)];
   return t - q.count < q.given ? given_page(a, o, (int)(t - q.count)) : -1;
 }
 
@@ -125,43 +179,93 @@ __device__ __forceinline__ void fill_row(const PlanArgs& a, const Offsets& o, co
   const int b = sequence_of(o.row, a.n_seq, i);
   int pos = -1, page = -1;
   if (b < a.n_seq) {
-    pos = a.start[b] + (i - o.row[b]);
-    const int e = pos >> a.page_log2, had = o.had[b];
-    if (e < a.max_pages) page = e < had ? a.pages[(int64_t)b * a.pages_ld + e] : taken_page(a, o, q, (int64_t)o.take[b] + (e - had));
+    const Of x = o.of[b];
+    pos = x.start + (i - o.row[b]);
+    const int e = pos >> a.page_log2;
+    if (e < a.max_pages) page = e < x.had ? a.pages[(int64_t)b * a.pages_ld + e] : taken_page(a, o, q, (int64_t)x.take + (e - x.had));
   }
   a.pos[i] = pos;
   a.slot[i] = (uint32_t)page < (uint32_t)a.n_pages ? ((int64_t)page << a.page_log2) + (pos & ((1 << a.page_log2) - 1)) : -1;
 }
-// Item m of the pages that are given back and then those that are taken.
-__device__ __forceinline__ void move_page(const PlanArgs& a, const Offsets& o, const Queue& q, int64_t m) {
-  if (m < q.given) {
-    a.ring[(q.first + q.count + m) % a.n_pages] = given_page(a, o, (int)m);
-    return;
+// Pages that are given back, and those that are taken.
+__device__ __forceinline__ void give_page(const PlanArgs& a, const Offsets& o, const Queue& q, int r) {
+  a.ring[in_ring(a, (int64_t)q.first + q.count + r)] = given_page(a, o, r);
+}
+__device__ __forceinline__ void take_page(const PlanArgs& a, const Offsets& o, const Queue& q, int t) {
+  const int b = min(sequence_of(o.take, a.n_seq, t), a.n_seq - 1);
+  const Of x = o.of[b];
+  a.pages[(int64_t)b * a.pages_ld + min(x.had + (t - x.take), a.max_pages - 1)] = taken_page(a, o, q, t);
+}
+
+// Item i of the rows, of the pages that are given back and of those that are taken.
+__device__ __forceinline__ void fill(const PlanArgs& a, const Offsets& o, const Queue& q, int64_t i) {
+  if (i < a.n_tok) return fill_row(a, o, q, (int)i);
+  i -= a.n_tok;
+  if (i < q.given) return give_page(a, o, q, (int)i);
+  take_page(a, o, q, (int)(i - q.given));
+}
+__device__ __forceinline__ int64_t items_of(const PlanArgs& a, const Offsets& o, const Queue& q) { return (int64_t)a.n_tok + q.given + o.take[a.n_seq]; }
+
+// One launch: every workgroup finds the offsets for itself and keeps them in LDS, the first one writes the lengths (which the others must not be
+// reading: more than one only where they do not go on in place).
+template <int EACH> __global__ __launch_bounds__(kThreads) void plan_whole(PlanArgs a) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const Offsets o = offsets_at(lds, a.n_seq);
+  const Queue q = plan_offsets<EACH>(a, o, blockIdx.x == 0);
+  const int64_t n = items_of(a, o, q);
+  for (int64_t i = blockIdx.x * kThreads + threadIdx.x; i < n; i += gridDim.x * kThreads) fill(a, o, q, i);
+}
+
+// Two launches, the offsets in the workspace.
+__global__ __launch_bounds__(kThreads) void plan_lengths(PlanArgs a) {
+  const Queue q = plan_offsets<4>(a, offsets_at(a.ws, a.n_seq), true);
+  if (threadIdx.x == 0) *(Queue*)a.ws = q;
+}
+// ends: of how many sequences there is room for in LDS; all of them or none.
+__global__ __launch_bounds__(kThreads) void plan_fill(PlanArgs a, int ends) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  Offsets o = offsets_at(a.ws, a.n_seq);
+  const Queue q = *(const Queue*)a.ws;
+  if (ends) {
+    int32_t* e = (int32_t*)lds;
+    const int n = a.n_seq + 1;
+    for (int i = threadIdx.x; i < 3 * n; i += kThreads) e[i] = o.row[i];      // give's and take's lie behind them
+    o.row = e;
+    o.give = e + n;
+    o.take = e + 2 * n;
+    __syncthreads();
   }
-  const int t = (int)(m - q.given), b = min(sequence_of(o.take, a.n_seq, t), a.n_seq - 1);
-  a.pages[(int64_t)b * a.pages_ld + min(o.had[b] + (t - o.take[b]), a.max_pages - 1)] = taken_page(a, o, q, t);
+  const int64_t n = items_of(a, o, q);
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) fill(a, o, q, i);
 }
 
-__global__ __launch_bounds__(kScanThreads) void plan_lengths(PlanArgs a) { plan_offsets(a, offsets_at(a.ws, a.n_seq)); }
-
-__global__ __launch_bounds__(256) void plan_fill(PlanArgs a) {
-  const Offsets o = offsets_at(a.ws, a.n_seq);
-  const Queue q = {o.head[0], o.head[1], o.head[2]};
-  const int64_t step = (int64_t)gridDim.x * 256, tid = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  for (int64_t i = tid; i < a.n_tok; i += step) fill_row(a, o, q, (int)i);
-  const int64_t moves = (int64_t)q.given + o.take[a.n_seq];
-  for (int64_t m = tid; m < moves; m += step) move_page(a, o, q, m);
-}
+constexpr int kLdsSeqs = 4096;          // sequences whose offsets a workgroup keeps in LDS
+constexpr int64_t kAlone = 32768;       // rows and entries of the table up to which a workgroup does all
 
 }  // namespace
 
-size_t plan_workspace(int n_seq) { return align_up((4 + 5 * ((size_t)n_seq + 1)) * sizeof(int32_t), 256); }
+size_t plan_workspace(int n_seq) { return align_up(offsets_bytes(n_seq), 256); }
 
 int launch_plan(const PlanArgs& a, hipStream_t st) {
-  plan_lengths<<<dim3(1), kScanThreads, 0, st>>>(a);
+  static OncePerDevice raised;
+  const bool in_place = a.start == a.start_in || a.held == a.held_in || a.ring_at == a.ring_at_in;
+  const bool alone = a.n_seq <= kThreads && (int64_t)a.n_seq * a.max_pages + a.n_tok <= kAlone;
+  const int64_t most = ((int64_t)a.n_tok + kThreads - 1) / kThreads;
+  const unsigned blocks = (unsigned)(most < 32 ? 32 : most > 256 ? 256 : most);
+  if (a.n_seq <= kLdsSeqs && (alone || !in_place)) {
+    const int rc = raise_lds_limit(raised, {(const void*)plan_whole<4>}, offsets_bytes(kLdsSeqs), "plan_whole");
+    if (rc != ESA_OK) return rc;
+    if (a.n_seq <= kThreads)
+      plan_whole<1><<<dim3(alone ? 1 : blocks), kThreads, offsets_bytes(a.n_seq), st>>>(a);
+    else
+      plan_whole<4><<<dim3(blocks), kThreads, offsets_bytes(a.n_seq), st>>>(a);
+    ESA_LAUNCH_CHECK("plan_whole");
+    return ESA_OK;
+  }
+  plan_lengths<<<dim3(1), kThreads, 0, st>>>(a);
   ESA_LAUNCH_CHECK("plan_lengths");
-  const int64_t blocks = ((int64_t)a.n_tok + 255) / 256;
-  plan_fill<<<dim3((unsigned)(blocks < 64 ? 64 : blocks > 1024 ? 1024 : blocks)), 256, 0, st>>>(a);
+  const bool staged = a.n_seq <= kLdsSeqs;
+  plan_fill<<<dim3(blocks), kThreads, staged ? 3 * ((size_t)a.n_seq + 1) * sizeof(int32_t) : 0, st>>>(a, staged ? a.n_seq : 0);
   ESA_LAUNCH_CHECK("plan_fill");
   return ESA_OK;
 }

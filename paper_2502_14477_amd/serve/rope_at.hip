@@ -14,7 +14,7 @@ typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
 constexpr int kThreads = 256;
-constexpr int kAhead = 4;      // heads of a thread whose loads are under way together
+constexpr int64_t kFewItems = 256 * 4 * kThreads;
 
 // Cosine and sine of an angle below 2^38 in magnitude.  Reduced to [-pi/4, pi/4] by a multiple of pi/2 that is held in two parts
 // (the first product is exact in the fma, the second's error is 2^38 2^-107), then the Taylor series: x^17/17! is below 5e-17 of the sine, x^18/18!
@@ -82,54 +82,25 @@ __device__ __forceinline__ Place place_of(const RopeArgs& a, int64_t tok, int hh
                (second ? g.out : f.out) + tok * (second ? g.out_tok : f.out_tok) + h * (second ? g.out_head : f.out_head)};
 }
 
-// A thread owns N pairs: elements of two pieces of N elements, one in each half, or of 2 N neighbours.  N = 1 takes elements one by one, whatever their
-// alignment.
-template <typename T, int N, bool HALVES> struct Pairs {
-  static constexpr bool kSingle = N == 1;
-  T x[N], y[N];
-  __device__ __forceinline__ void load(const char* p, int i, int half) {
-    if constexpr (HALVES || kSingle) {
-      const int step = HALVES ? 1 : 2, gap = HALVES ? half : 1;
-      const Piece<T, N> a = *(const Piece<T, N>*)(p + (int64_t)i * step * (int)sizeof(T)), b = *(const Piece<T, N>*)(p + (int64_t)(i * step + gap) * (int)sizeof(T));
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        x[j] = a.x[j];
-        y[j] = b.x[j];
-      }
-    } else {
-      const Piece<T, N> a = *(const Piece<T, N>*)(p + (int64_t)i * 2 * (int)sizeof(T)), b = *(const Piece<T, N>*)(p + (int64_t)(i * 2 + N) * (int)sizeof(T));
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        x[j] = j < N / 2 ? a.x[2 * j] : b.x[2 * j - N];
-        y[j] = j < N / 2 ? a.x[2 * j + 1] : b.x[2 * j + 1 - N];
-      }
-    }
+// What a thread takes of a head at a time: N pairs, which are two pieces of N elements, one in each half or one behind the other.  N = 1 takes
+// elements one by one, whatever their alignment.  Behind the pairs' come two pieces at a time of what does not turn.
+template <typename T, int N, bool HALVES> struct Pieces {
+  Piece<T, N> a, b;
+  __device__ __forceinline__ void load(const char* p, int at, int gap) {
+    a = *(const Piece<T, N>*)(p + at);
+    b = *(const Piece<T, N>*)(p + at + gap);
   }
-  __device__ __forceinline__ void store(char* p, int i, int half) const {
-    Piece<T, N> a, b;
-    if constexpr (HALVES || kSingle) {
-      const int step = HALVES ? 1 : 2, gap = HALVES ? half : 1;
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        a.x[j] = x[j];
-        b.x[j] = y[j];
-      }
-      *(Piece<T, N>*)(p + (int64_t)i * step * (int)sizeof(T)) = a;
-      *(Piece<T, N>*)(p + (int64_t)(i * step + gap) * (int)sizeof(T)) = b;
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j) {
-        if (j < N / 2) {
-          a.x[2 * j] = x[j];
-          a.x[2 * j + 1] = y[j];
-        } else {
-          b.x[2 * j - N] = x[j];
-          b.x[2 * j + 1 - N] = y[j];
-        }
-      }
-      *(Piece<T, N>*)(p + (int64_t)i * 2 * (int)sizeof(T)) = a;
-      *(Piece<T, N>*)(p + (int64_t)(i * 2 + N) * (int)sizeof(T)) = b;
-    }
+  __device__ __forceinline__ void store(char* p, int at, int gap) const {
+    *(Piece<T, N>*)(p + at) = a;
+    *(Piece<T, N>*)(p + at + gap) = b;
+  }
+  __device__ __forceinline__ T& x(int j) {
+    if constexpr (HALVES || N == 1) return a.x[j];
+    return j < N / 2 ? a.x[2 * j] : b.x[2 * j - N];
+  }
+  __device__ __forceinline__ T& y(int j) {
+    if constexpr (HALVES || N == 1) return b.x[j];
+    return j < N / 2 ? a.x[2 * j + 1] : b.x[2 * j + 1 - N];
   }
   __device__ __forceinline__ void turn(const f64x2 (&cs)[N]) {
     constexpr int kTogether = N < 4 ? N : 4;      // pairs whose roundings share a branch
@@ -139,43 +110,57 @@ template <typename T, int N, bool HALVES> struct Pairs {
       T o[2 * kTogether];
 #pragma unroll
       for (int j = 0; j < kTogether; ++j) {
-        const double a = to_f64<T>(x[j0 + j]), b = to_f64<T>(y[j0 + j]);
-        v[j] = a * cs[j0 + j][0] - b * cs[j0 + j][1];
-        v[kTogether + j] = b * cs[j0 + j][0] + a * cs[j0 + j][1];
+        const double p = to_f64<T>(x(j0 + j)), q = to_f64<T>(y(j0 + j));
+        v[j] = p * cs[j0 + j][0] - q * cs[j0 + j][1];
+        v[kTogether + j] = q * cs[j0 + j][0] + p * cs[j0 + j][1];
       }
       to_storage(v, o);
 #pragma unroll
       for (int j = 0; j < kTogether; ++j) {
-        x[j0 + j] = o[j];
-        y[j0 + j] = o[kTogether + j];
+        x(j0 + j) = o[j];
+        y(j0 + j) = o[kTogether + j];
       }
     }
   }
 };
 
-// A workgroup takes `toks` tokens; a thread N pairs of one of them, for every hs-th head.  The tokens' cosines and sines go through LDS.
-template <typename T, int N, bool HALVES>
-__global__ __launch_bounds__(kThreads) void rope_at(RopeArgs a, int toks, int hs) {
-  extern __shared__ f64x2 cs[];                   // [toks][half]
+// How a launch shares out its rows: a workgroup takes `toks` tokens and hs * AHEAD heads of each, a thread one of a head's `lanes` parts for
+// every hs-th of them.
+struct Split {
+  int toks, hs, lanes, parts;      // parts of a head: those that turn, then those that do not
+};
+
+template <typename T, int N, bool HALVES, int AHEAD>
+__global__ __launch_bounds__(kThreads) void rope_at(RopeArgs a, Split s) {
+  extern __shared__ __attribute__((aligned(16))) f64x2 cs[];                   // [toks][half]
+  constexpr int kSize = N * (int)sizeof(T);
   const int tid = threadIdx.x;
-  const int64_t tok0 = ((int64_t)blockIdx.y * paged::kGridRow + blockIdx.x) * toks;
+  const int64_t tok0 = ((int64_t)blockIdx.y * paged::kGridRow + blockIdx.x) * s.toks;
   if (tok0 >= a.n_tok) return;
-  const int n = (int)min((int64_t)toks, a.n_tok - tok0);
-  const int vecs = a.half / N;
-  const int i = tid % vecs * N, rest = tid / vecs, h0 = rest % hs, r = rest / hs;
+  const int n = (int)min((int64_t)s.toks, a.n_tok - tok0);
+  const int turning = a.half / N;
+  const int lane = tid % s.lanes, rest = tid / s.lanes, h0 = blockIdx.z * (s.hs * AHEAD) + rest % s.hs, r = rest / s.hs;
   const bool mine = r < n;
   const int64_t tok = tok0 + (mine ? r : 0);
   const int p = a.pos[tok];
-  Pairs<T, N, HALVES> v[kAhead];
-  Place at[kAhead];
-  auto request = [&](int hb) {
+  Pieces<T, N, HALVES> v[AHEAD];
+  Place to[AHEAD];
+  int at = 0, gap = 0;
+  auto request = [&](int i) {                     // part i of the thread's heads
+    if (i < turning) {
+      at = i * (HALVES ? kSize : 2 * kSize);
+      gap = HALVES ? a.half * (int)sizeof(T) : kSize;
+    } else {
+      at = 2 * a.half * (int)sizeof(T) + (i - turning) * 2 * kSize;
+      gap = at + kSize < (2 * a.half + a.rest) * (int)sizeof(T) ? kSize : 0;      // a single piece is taken twice
+    }
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      at[u] = place_of(a, tok, hb + u * hs < a.heads ? hb + u * hs : 0);
-      v[u].load(at[u].x, i, a.half);
+    for (int u = 0; u < AHEAD; ++u) {
+      to[u] = place_of(a, tok, min(h0 + u * s.hs, a.heads - 1));
+      v[u].load(to[u].x, at, gap);
     }
   };
-  request(h0);
+  request(lane);
   for (int e = tid; e < n * a.half; e += kThreads) {
     f64x2 t = turn_of((double)a.pos[tok0 + e / a.half] * a.freq[e % a.half]);
     t *= a.gain;
@@ -184,40 +169,44 @@ __global__ __launch_bounds__(kThreads) void rope_at(RopeArgs a, int toks, int hs
   }
   __syncthreads();
   if (!mine || p < 0) return;
-  f64x2 t[N];
+  for (int i = lane; i < s.parts; i += s.lanes) {
+    if (i != lane) request(i);
+    if (i < turning) {
+      f64x2 t[N];
 #pragma unroll
-  for (int j = 0; j < N; ++j) t[j] = cs[r * a.half + i + j];
-  for (int hb = h0; hb < a.heads; hb += hs * kAhead) {
-    if (hb != h0) request(hb);
+      for (int j = 0; j < N; ++j) t[j] = cs[r * a.half + i * N + j];
 #pragma unroll
-    for (int u = 0; u < kAhead; ++u) {
-      if (hb + u * hs >= a.heads) break;
-      v[u].turn(t);
-      v[u].store(at[u].out, i, a.half);
+      for (int u = 0; u < AHEAD; ++u) v[u].turn(t);
     }
-  }
-  // what does not turn
-  const int tail = a.rest / N;
-  for (int e = i / N + vecs * h0; e < tail * a.heads; e += vecs * hs) {
-    const Place q = place_of(a, tok, e / tail);
-    const int64_t off = (int64_t)(2 * a.half + e % tail * N) * (int)sizeof(T);
-    *(Piece<T, N>*)(q.out + off) = *(const Piece<T, N>*)(q.x + off);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (h0 + u * s.hs < a.heads) v[u].store(to[u].out, at, gap);
   }
 }
 
-template <typename T, int N> int launch_of(const RopeArgs& a, hipStream_t st) {
-  const int vecs = a.half / N;                    // at most 128, of which 256 threads take one or more
-  int hs = (a.heads + kAhead - 1) / kAhead;
-  if (hs > kThreads / vecs) hs = kThreads / vecs;
-  const int toks = kThreads / (vecs * hs);
-  const int64_t groups = ((int64_t)a.n_tok + toks - 1) / toks;
-  const size_t lds = (size_t)toks * a.half * sizeof(f64x2);
+template <typename T, int N, int AHEAD> int launch_split(const RopeArgs& a, hipStream_t st) {
+  Split s;
+  s.parts = a.half / N + (a.rest / N + 1) / 2;
+  s.lanes = s.parts < kThreads ? s.parts : kThreads;
+  const int most = kThreads / s.lanes;            // heads' places of a workgroup
+  s.hs = (a.heads + AHEAD - 1) / AHEAD;
+  const int rounds = (s.hs + most - 1) / most;    // workgroups that share a token's heads
+  s.hs = (s.hs + rounds - 1) / rounds;
+  s.toks = most / s.hs;
+  dim3 grid = paged::grid_for(((int64_t)a.n_tok + s.toks - 1) / s.toks);
+  grid.z = rounds;
+  const size_t lds = (size_t)s.toks * a.half * sizeof(f64x2);
   if (a.pairs == ESA_PAIRS_HALVES)
-    rope_at<T, N, true><<<paged::grid_for(groups), kThreads, lds, st>>>(a, toks, hs);
+    rope_at<T, N, true, AHEAD><<<grid, kThreads, lds, st>>>(a, s);
   else
-    rope_at<T, N, false><<<paged::grid_for(groups), kThreads, lds, st>>>(a, toks, hs);
+    rope_at<T, N, false, AHEAD><<<grid, kThreads, lds, st>>>(a, s);
   ESA_LAUNCH_CHECK("rope_at");
   return ESA_OK;
+}
+template <typename T, int N> int launch_of(const RopeArgs& a, hipStream_t st) {
+  // Four heads to a thread share its sines and cosines; one where that leaves compute units without work.
+  const int64_t items = (int64_t)a.n_tok * a.heads * (a.half / N + (a.rest / N + 1) / 2);
+  return items >= kFewItems ? launch_split<T, N, 4>(a, st) : launch_split<T, N, 1>(a, st);
 }
 
 }  // namespace

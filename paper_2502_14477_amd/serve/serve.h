@@ -6,9 +6,6 @@
 namespace esa {
 namespace serve {
 
-using paged::wave_scan;
-using paged::wave_scan_long;
-
 // ---------------------------------------------------------------- rotary positions
 constexpr int kMaxRowSets = 2;
 constexpr int kMaxHalf = 128;

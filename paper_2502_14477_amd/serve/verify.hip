@@ -14,12 +14,29 @@ namespace serve {
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / 64;
 constexpr int kEach = 16;                     // numbers of a chunk a thread
 constexpr int kChunk = kThreads * kEach;
 
-template <typename T> __device__ __forceinline__ double probability(T v);
-template <> __device__ __forceinline__ double probability<float>(float v) { return v > 0.f && v < __builtin_huge_valf() ? (double)v : 0.0; }
-template <> __device__ __forceinline__ double probability<bf16_t>(bf16_t v) { return probability<float>(bf16_to_f32(v)); }
+// Negative numbers, NaN (the maximum's other operand is taken) and infinities count as 0.
+template <typename T> __device__ __forceinline__ float probability(T v);
+template <> __device__ __forceinline__ float probability<float>(float v) {
+  v = fmaxf(v, 0.f);
+  return v < __builtin_huge_valf() ? v : 0.f;
+}
+template <> __device__ __forceinline__ float probability<bf16_t>(bf16_t v) { return probability<float>(bf16_to_f32(v)); }
+
+// N numbers of a row, wherever it begins.
+template <typename T, int N> struct Piece {
+  T x[N];
+};
+template <typename T, int N> __device__ __forceinline__ Piece<T, N> load(const T* p) {
+  Piece<T, N> v;
+  __builtin_memcpy(&v, p, sizeof(v));
+  return v;
+}
+// The largest pieces of a row of that many.
+template <typename T> constexpr int kPiece = 16 / (int)sizeof(T);
 
 // A sequence's rows, clamped.
 struct Rows {
@@ -58,24 +75,50 @@ __device__ __forceinline__ Drawn drawn_of(const VerifyArgs& a, const Rows& s, in
   return Drawn{s.row0 + kept, all ? 0 : a.draft ? 1 : 2, all ? -1 : a.tokens[s.row0 + kept + 1]};
 }
 
-// Weight of token t, and the target's probability of it.
-template <typename T> struct Weight {
-  double w, p;
-};
-template <typename T> __device__ __forceinline__ Weight<T> weight(const Drawn& d, T pv, T qv, int t) {
-  const double p = probability<T>(pv);
-  if (d.mode == 1) return {fmax(p - probability<T>(qv), 0.0), p};
-  return {d.mode == 2 && t == d.token ? fmax(p - 1.0, 0.0) : p, p};
+// Weights of M pieces of N tokens, `step` apart from `first` on: take(number, token, weight); those beyond the vocabulary are 0.  A piece
+// that would reach over a row's end is read as the row's last N numbers, of which those that belong to other pieces do not count (the vocabulary has N or
+// more).  All are requested in front of their first use.
+template <typename T, int N, int M, typename F>
+__device__ __forceinline__ void weights(const VerifyArgs& a, const Drawn& d, int64_t first, int step, F&& take) {
+  const T* pr = (const T*)(a.target + (int64_t)d.row * a.ldt);
+  const int64_t end = (int64_t)a.vocab - N;
+  auto all = [&](auto&& of) {
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      const int64_t want = first + m * step, at = min(want, end);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        const double w = of(m, j, (int)at + j);
+        take(m * N + j, (int)at + j, at + j >= want ? w : 0.0);
+      }
+    }
+  };
+  Piece<T, N> p[M];
+#pragma unroll
+  for (int m = 0; m < M; ++m) p[m] = load<T, N>(pr + min(first + m * step, end));
+  if (d.mode == 1) {
+    const T* qr = (const T*)(a.draft + (int64_t)(d.row + 1) * a.ldd);
+    Piece<T, N> q[M];
+#pragma unroll
+    for (int m = 0; m < M; ++m) q[m] = load<T, N>(qr + min(first + m * step, end));
+    all([&](int m, int j, int) { return fmax((double)probability<T>(p[m].x[j]) - (double)probability<T>(q[m].x[j]), 0.0); });
+  } else {
+    const int without = d.mode == 2 ? d.token : -1;      // the token that was looked up, with a probability of 1
+    all([&](int m, int j, int t) {
+      const double x = probability<T>(p[m].x[j]);
+      return t == without ? fmax(x - 1.0, 0.0) : x;
+    });
+  }
 }
 
 struct Work {
-  double* sums;      // [n_seq][chunks][2]: of w, of p
+  double* sums;      // [n_seq][chunks]
   int32_t* kept;     // [n_seq]
 };
 __host__ __device__ inline int chunks_of(int vocab) { return (int)(((int64_t)vocab + kChunk - 1) / kChunk); }
 __host__ __device__ inline Work work_at(void* ws, int n_seq, int vocab) {
   double* sums = (double*)ws;
-  return Work{sums, (int32_t*)(sums + (size_t)n_seq * chunks_of(vocab) * 2)};
+  return Work{sums, (int32_t*)(sums + (size_t)n_seq * chunks_of(vocab))};
 }
 
 __device__ __forceinline__ double wave_sum(double v) {
@@ -83,43 +126,34 @@ __device__ __forceinline__ double wave_sum(double v) {
   for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
   return v;
 }
+// Of the workgroup, in every thread.
+__device__ __forceinline__ double group_sum(double v, double* part) {
+  v = wave_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = 0.0;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) v += part[i];
+  return v;
+}
 
 // grid (chunks, sequences)
-template <typename T> __global__ __launch_bounds__(kThreads) void verify_sums(VerifyArgs a) {
-  __shared__ double part[kThreads / 64][2];
+template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_sums(VerifyArgs a) {
+  __shared__ double part[kWaves];
   const int tid = threadIdx.x, chunk = blockIdx.x;
+  const Work k = work_at(a.ws, a.n_seq, a.vocab);
   for (int b = blockIdx.y; b < a.n_seq; b += gridDim.y) {
     const Rows s = rows_of(a, b);
-    const Work k = work_at(a.ws, a.n_seq, a.vocab);
     if (s.n == 0) continue;
     const int kept = standing<T>(a, s);
     const Drawn d = drawn_of(a, s, kept);
-    if (chunk == 0 && tid == 0) k.kept[b] = kept;
-    const T* p = (const T*)(a.target + (int64_t)d.row * a.ldt);
-    const T* q = d.mode == 1 ? (const T*)(a.draft + (int64_t)(d.row + 1) * a.ldd) : p;
-    double w = 0.0, all = 0.0;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      const int64_t t = (int64_t)chunk * kChunk + j * kThreads + tid;
-      if (t < a.vocab) {
-        const Weight<T> x = weight<T>(d, p[t], q[t], (int)t);
-        w += x.w;
-        all += x.p;
-      }
-    }
-    w = wave_sum(w);
-    all = wave_sum(all);
-    __syncthreads();
-    if ((tid & 63) == 0) {
-      part[tid >> 6][0] = w;
-      part[tid >> 6][1] = all;
-    }
-    __syncthreads();
-    if (tid < 2) {
-      double v = 0.0;
-#pragma unroll
-      for (int i = 0; i < kThreads / 64; ++i) v += part[i][tid];
-      k.sums[((int64_t)b * gridDim.x + chunk) * 2 + tid] = v;
+    double w = 0.0;
+    weights<T, N, kEach / N>(a, d, (int64_t)chunk * kChunk + tid * N, kThreads * N, [&](int, int, double x) { w += x; });
+    w = group_sum(w, part);
+    if (tid == 0) {
+      k.sums[(int64_t)b * gridDim.x + chunk] = w;
+      if (chunk == 0) k.kept[b] = kept;
     }
   }
 }
@@ -141,19 +175,40 @@ __device__ __forceinline__ Scanned scan(double x, double* part) {
   __syncthreads();
   double all = 0.0, before = 0.0;
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
+  for (int w = 0; w < kWaves; ++w) {
     if (w == wave) before = all;
     all += part[w];
   }
   return Scanned{before + (lane ? left : 0.0), all};
 }
 
+// The first item of which a thread says so (the threads' items ascend), and the last one with any weight: INT32_MAX, -1 where there is none.
+struct Found {
+  int first, last;
+};
+__device__ __forceinline__ Found find(int first, int last, Found* part) {
+  const int wave = threadIdx.x >> 6;
+  const uint64_t f = __ballot(first != INT32_MAX), l = __ballot(last >= 0);
+  const Found mine = {f ? __shfl(first, __ffsll((unsigned long long)f) - 1) : INT32_MAX, l ? __shfl(last, 63 - __clzll((long long)l)) : -1};
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) part[wave] = mine;
+  __syncthreads();
+  Found r = {INT32_MAX, -1};
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) {
+    r.first = min(r.first, part[w].first);
+    r.last = max(r.last, part[w].last);
+  }
+  return r;
+}
+
 // A workgroup a sequence.
-template <typename T> __global__ __launch_bounds__(kThreads) void verify_draw(VerifyArgs a) {
-  __shared__ double part[kThreads / 64];
-  __shared__ int found, last;
-  __shared__ double before;
-  const int tid = threadIdx.x, b = blockIdx.x;
+template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_draw(VerifyArgs a) {
+  __shared__ double part[kWaves];
+  __shared__ Found found[kWaves];
+  __shared__ double at_chunk;
+  const int tid = threadIdx.x, b = paged::block_index();
+  if (b >= a.n_seq) return;
   const Rows s = rows_of(a, b);
   if (s.n == 0) {
     if (tid == 0) a.count[b] = 0;
@@ -161,84 +216,85 @@ template <typename T> __global__ __launch_bounds__(kThreads) void verify_draw(Ve
   }
   const Work k = work_at(a.ws, a.n_seq, a.vocab);
   const int kept = k.kept[b], chunks = chunks_of(a.vocab);
+  const double* sums = k.sums + (int64_t)b * chunks;
+  double mine = sums[min(tid, chunks - 1)];      // of the chunk that the thread's number is, in the first round of them
+  mine = tid < chunks ? mine : 0.0;
+  const float u = a.u[s.row0];
   Drawn d = drawn_of(a, s, kept);
   for (int i = tid; i < s.n; i += kThreads)
     if (i != kept) a.out[s.row0 + i] = i < kept ? a.tokens[s.row0 + i + 1] : -1;
   if (tid == 0) a.count[b] = kept + 1;
-  const float u = a.u[s.row0];
-  const double* sums = k.sums + (int64_t)b * chunks * 2;
-  // the sum of all, of w or else of p
-  double w = 0.0, p = 0.0;
-  for (int c = tid; c < chunks; c += kThreads) {
-    w += sums[2 * c];
-    p += sums[2 * c + 1];
-  }
-  double total = scan(w, part).all;
-  int which = 0;
+  // sums in front of the thread's chunk
+  Scanned y = scan(mine, part);
+  double total = y.all;
+  for (int c = tid + kThreads; c - tid < chunks; c += kThreads) total += group_sum(c < chunks ? sums[c] : 0.0, part);
+  bool again = false;                            // whether the chunks' sums are those of p
   if (!(total > 0.0)) {
-    total = scan(p, part).all;
-    which = 1;
+    if (d.mode == 0) {
+      if (tid == 0) a.out[d.row] = -1;
+      return;
+    }
+    // p itself, of which there are no sums yet: one workgroup reads it all
     d.mode = 0;
-  }
-  if (!(total > 0.0)) {
-    if (tid == 0) a.out[d.row] = -1;
-    return;
+    again = true;
+    for (int c = 0; c < chunks; ++c) {
+      double w = 0.0;
+      weights<T, N, kEach / N>(a, d, (int64_t)c * kChunk + tid * N, kThreads * N, [&](int, int, double x) { w += x; });
+      w = group_sum(w, part);
+      if (tid == 0) k.sums[(int64_t)b * chunks + c] = w;
+      total += w;
+    }
+    if (!(total > 0.0)) {
+      if (tid == 0) a.out[d.row] = -1;
+      return;
+    }
+    __syncthreads();
   }
   const double target = u >= 1.f ? __builtin_huge_val() : u > 0.f ? u * total : 0.0;
-  // the first chunk whose sums pass it, or the last with any
-  if (tid == 0) {
-    found = INT32_MAX;
-    last = -1;
-    before = 0.0;
-  }
+  // the first chunk whose sums pass it, or else the last with any
+  int chunk = -1;
   double base = 0.0;
   for (int c0 = 0; c0 < chunks; c0 += kThreads) {
     const int c = c0 + tid;
-    const double x = c < chunks ? sums[2 * c + which] : 0.0;
-    const Scanned y = scan(x, part);
-    if (x > 0.0) {
-      atomicMax(&last, c);
-      if (base + y.before + x > target) atomicMin(&found, c);
+    if (c0 > 0 || again) {
+      mine = c < chunks ? sums[c] : 0.0;
+      y = scan(mine, part);
     }
-    __syncthreads();
-    if (found == c || (found == INT32_MAX && last == c)) before = base + y.before;
-    __syncthreads();
-    if (found != INT32_MAX) break;
+    const double before = base + y.before;
+    const Found f = find(mine > 0.0 && before + mine > target ? c : INT32_MAX, mine > 0.0 ? c : -1, found);
+    if (f.first != INT32_MAX) chunk = f.first;
+    else if (f.last >= 0) chunk = f.last;
+    if (chunk == c) at_chunk = before;
+    if (f.first != INT32_MAX) break;
     base += y.all;
   }
-  const int chunk = found != INT32_MAX ? found : last;
-  const double start = before;
   __syncthreads();
-  if (tid == 0) {
-    found = INT32_MAX;
-    last = -1;
-  }
-  const T* pr = (const T*)(a.target + (int64_t)d.row * a.ldt);
-  const T* qr = d.mode == 1 ? (const T*)(a.draft + (int64_t)(d.row + 1) * a.ldd) : pr;
-  double x[kEach], mine = 0.0;
-  const int64_t t0 = (int64_t)chunk * kChunk + tid * kEach;
-#pragma unroll
-  for (int j = 0; j < kEach; ++j) {
-    x[j] = t0 + j < a.vocab ? weight<T>(d, pr[t0 + j], qr[t0 + j], (int)(t0 + j)).w : 0.0;
-    mine += x[j];
-  }
-  double sum = start + scan(mine, part).before;
+  double x[kEach], sum = 0.0;
+  int t[kEach];
+  weights<T, N, kEach / N>(a, d, (int64_t)chunk * kChunk + tid * kEach, N, [&](int j, int at, double w) {
+    x[j] = w;
+    t[j] = at;
+    sum += w;
+  });
+  const double start = at_chunk;
+  sum = start + scan(sum, part).before;
+  int first = INT32_MAX, last = -1;
 #pragma unroll
   for (int j = 0; j < kEach; ++j) {
     sum += x[j];
     if (x[j] > 0.0) {
-      atomicMax(&last, (int)(t0 + j));
-      if (sum > target) atomicMin(&found, (int)(t0 + j));
+      last = t[j];
+      if (sum > target && first == INT32_MAX) first = t[j];
     }
   }
-  __syncthreads();
-  if (tid == 0) a.out[d.row] = found != INT32_MAX ? found : last;
+  const Found f = find(first, last, found);
+  if (tid == 0) a.out[d.row] = f.first != INT32_MAX ? f.first : f.last;
 }
 
-template <typename T> int launch_of(const VerifyArgs& a, hipStream_t st) {
-  verify_sums<T><<<dim3((unsigned)chunks_of(a.vocab), (unsigned)(a.n_seq < 65535 ? a.n_seq : 65535)), kThreads, 0, st>>>(a);
+template <typename T, int N> int launch_of(const VerifyArgs& a, hipStream_t st) {
+  verify_sums<T, N><<<dim3((unsigned)chunks_of(a.vocab), (unsigned)(a.n_seq < 65535 ? a.n_seq : 65535)), kThreads, 0, st>>>(a);
   ESA_LAUNCH_CHECK("verify_sums");
-  verify_draw<T><<<dim3((unsigned)a.n_seq), kThreads, 0, st>>>(a);
+  verify_draw<T, N><<<paged::grid_for(a.n_seq), kThreads, 0, st>>>(a);
   ESA_LAUNCH_CHECK("verify_draw");
   return ESA_OK;
 }
@@ -246,10 +302,14 @@ template <typename T> int launch_of(const VerifyArgs& a, hipStream_t st) {
 }  // namespace
 
 size_t verify_workspace(int n_seq, int vocab) {
-  return align_up((size_t)n_seq * (chunks_of(vocab) * 2 * sizeof(double) + sizeof(int32_t)), 256);
+  return align_up((size_t)n_seq * (chunks_of(vocab) * sizeof(double) + sizeof(int32_t)), 256);
 }
 
-int launch_verify(const VerifyArgs& a, int dtype, hipStream_t st) { return dtype == ESA_F32 ? launch_of<float>(a, st) : launch_of<bf16_t>(a, st); }
+// Vocabularies shorter than a piece are read number by number.
+int launch_verify(const VerifyArgs& a, int dtype, hipStream_t st) {
+  if (dtype == ESA_F32) return a.vocab >= kPiece<float> ? launch_of<float, kPiece<float>>(a, st) : launch_of<float, 1>(a, st);
+  return a.vocab >= kPiece<bf16_t> ? launch_of<bf16_t, kPiece<bf16_t>>(a, st) : launch_of<bf16_t, 1>(a, st);
+}
 
 }  // namespace serve
 }  // namespace esa
