@@ -43,26 +43,23 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t x) {      // of the lanes
   x = plus(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));      // row_bcast 15, 31
   return plus(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
 }
-// Over the workgroup in front of each thread, and of all.  part: [kWaves].
-struct Scanned {
-  uint32_t before, all;
-};
-template <int N> __device__ __forceinline__ void scan(const uint32_t (&x)[N], Scanned (&s)[N], uint32_t (*part)[kWaves]) {
+// Over N numbers a thread, of which its wave's j-th are behind its (j - 1)-th: what is in front of each, and all of the workgroup's.  part: [kWaves].
+template <int N> __device__ __forceinline__ uint32_t scan(const uint32_t (&x)[N], uint32_t (&before)[N], uint32_t* part) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t left[N];
+  uint32_t sum = 0;
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const uint32_t upto = wave_sums(x[k]);
-    left[k] = __shfl_up(upto, 1);
-    if (lane == 63) part[k][wave] = upto;
+  for (int j = 0; j < N; ++j) {
+    const uint32_t upto = wave_sums(x[j]), left = __shfl_up(upto, 1);
+    before[j] = plus(sum, lane ? left : 0);
+    sum = plus(sum, paged::lane_value(upto, 63));
   }
+  if (lane == 0) part[wave] = sum;
   __syncthreads();
+  const uint32_t sums = wave_sums(lane < kWaves ? part[lane] : 0);
+  const uint32_t front = wave > 0 ? paged::lane_value(sums, wave - 1) : 0;
 #pragma unroll
-  for (int k = 0; k < N; ++k) {
-    const uint32_t sums = wave_sums(lane < kWaves ? part[k][lane] : 0);
-    const uint32_t front = wave > 0 ? paged::lane_value(sums, wave - 1) : 0;
-    s[k] = Scanned{plus(front, lane ? left[k] : 0), paged::lane_value(sums, kWaves - 1)};
-  }
+  for (int j = 0; j < N; ++j) before[j] = plus(front, before[j]);
+  return paged::lane_value(sums, kWaves - 1);
 }
 
 // The sequences' lengths and offsets, by one workgroup, EACH of them a thread at a time.
@@ -73,62 +70,51 @@ template <int EACH> __device__ __forceinline__ Queue plan_offsets(const PlanArgs
   const int at_in = a.ring_at_in[0], count_in = a.ring_at_in[1];
   uint32_t rows = 0, gives = 0, takes = 0;
   for (int r0 = 0; r0 < a.n_seq; r0 += kThreads * EACH) {
-    const int b0 = r0 + tid * EACH;
-    int start[EACH], fresh[EACH], had[EACH], grow[EACH];
+    const int b0 = r0 + (tid >> 6) * 64 * EACH + (tid & 63);      // the thread's sequences are 64 apart
+    int start[EACH], had[EACH], grow[EACH], need[EACH];
+    uint32_t fresh[EACH], before[EACH], x[EACH], y[EACH];
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
-      const int b = min(b0 + j, a.n_seq - 1);
+      const int b = min(b0 + j * 64, a.n_seq - 1);
       start[j] = a.start_in[b];
-      fresh[j] = a.fresh[b];
+      fresh[j] = max(a.fresh[b], 0);
       had[j] = a.held_in[b];
       grow[j] = a.grow ? a.grow[b] : 0;
     }
-    uint32_t sum[1] = {0};
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) fresh[j] = b0 + j * 64 < a.n_seq ? fresh[j] : 0;
+    const uint32_t all = scan<EACH>(fresh, before, part[0]);
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
-      fresh[j] = b0 + j < a.n_seq ? max(fresh[j], 0) : 0;
+      const uint32_t at = plus(rows, before[j]);
+      const int lo = (int)min(at, (uint32_t)a.n_tok), hi = (int)min(plus(at, fresh[j]), (uint32_t)a.n_tok);
+      fresh[j] = hi;      // from here on the end of the sequence's rows
       had[j] = min(max(had[j], 0), a.max_pages);
-      sum[0] = plus(sum[0], fresh[j]);
+      start[j] = (int)min(max((int64_t)start[j] + grow[j], (int64_t)0), (int64_t)(INT32_MAX - (hi - lo)));
+      need[j] = (int)min(((uint32_t)start[j] + (uint32_t)(hi - lo) + (1u << a.page_log2) - 1) >> a.page_log2, (uint32_t)a.max_pages);
+      const bool there = b0 + j * 64 < a.n_seq;
+      x[j] = there ? max(had[j] - need[j], 0) : 0;
+      y[j] = there ? max(need[j] - had[j], 0) : 0;
     }
-    Scanned s[1];
-    scan<1>(sum, s, part);
-    uint32_t at = plus(rows, s[0].before);
-    rows = plus(rows, s[0].all);
-    int hi[EACH], need[EACH];
-    uint32_t moved[2] = {0, 0};
+    rows = plus(rows, all);
+    uint32_t give[EACH], take[EACH];
+    const uint32_t all_give = scan<EACH>(x, give, part[1]), all_take = scan<EACH>(y, take, part[2]);
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
-      const int lo = (int)min(at, (uint32_t)a.n_tok);
-      at = plus(at, fresh[j]);
-      hi[j] = (int)min(at, (uint32_t)a.n_tok);
-      const int64_t from = (int64_t)start[j] + grow[j];
-      start[j] = (int)min(max(from, (int64_t)0), (int64_t)(INT32_MAX - (hi[j] - lo)));
-      need[j] = (int)min(((uint32_t)start[j] + (uint32_t)(hi[j] - lo) + (1u << a.page_log2) - 1) >> a.page_log2, (uint32_t)a.max_pages);
-      if (b0 + j < a.n_seq) {
-        moved[0] = plus(moved[0], max(had[j] - need[j], 0));
-        moved[1] = plus(moved[1], max(need[j] - had[j], 0));
-      }
-    }
-    Scanned m[2];
-    scan<2>(moved, m, part + 1);
-    uint32_t give = plus(gives, m[0].before), take = plus(takes, m[1].before);
-#pragma unroll
-    for (int j = 0; j < EACH; ++j) {
-      const int b = b0 + j;
+      const int b = b0 + j * 64;
       if (b >= a.n_seq) break;
-      o.of[b] = Of{start[j], had[j], (int)take, need[j]};
-      give = plus(give, max(had[j] - need[j], 0));
-      take = plus(take, max(need[j] - had[j], 0));
-      o.row[b + 1] = hi[j];
-      o.give[b + 1] = (int)give;
-      o.take[b + 1] = (int)take;
+      const uint32_t front = plus(takes, take[j]);
+      o.of[b] = Of{start[j], had[j], (int)front, need[j]};
+      o.row[b + 1] = (int)fresh[j];
+      o.give[b + 1] = (int)plus(plus(gives, give[j]), x[j]);
+      o.take[b + 1] = (int)plus(front, y[j]);
       if (writes) {
         a.start[b] = start[j];
-        a.cu[b + 1] = hi[j];
+        a.cu[b + 1] = (int)fresh[j];
       }
     }
-    gives = plus(gives, m[0].all);
-    takes = plus(takes, m[1].all);
+    gives = plus(gives, all_give);
+    takes = plus(takes, all_take);
   }
   const int first = (int)((uint32_t)max(at_in, 0) % (uint32_t)a.n_pages), count = min(max(count_in, 0), a.n_pages);
   const int given = min((int)gives, a.n_pages - count), free = count + given, taken = min((int)takes, free);
