@@ -8,7 +8,9 @@
 // defaults are in binding.py.
 #include <Python.h>
 
+#include <ATen/EmptyTensor.h>
 #include <ATen/core/Tensor.h>
+#include <ATen/hip/impl/HIPCachingAllocatorMasqueradingAsCUDA.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
@@ -115,6 +117,11 @@ View view_of(const at::Tensor& t, int rank) {
 // ---- outputs and scratch
 at::Tensor new_tensor(at::IntArrayRef shape, at::ScalarType dtype, const at::Device& dev) {
   return at::empty(shape, at::TensorOptions().dtype(dtype).device(dev));
+}
+// The same on the current device, without the way through torch's dispatcher.
+at::Tensor new_here(at::IntArrayRef shape, at::ScalarType dtype) {
+  static c10::Allocator* const allocator = c10::hip::HIPCachingAllocatorMasqueradingAsCUDA::get();
+  return at::Tensor(at::detail::empty_generic(shape, allocator, c10::DispatchKeySet(c10::DispatchKey::CUDA), dtype, std::nullopt));
 }
 PyObject* wrap(at::Tensor t) { return THPVariable_Wrap(std::move(t)); }
 PyObject* wrap_or_none(const at::Tensor& t) {
@@ -804,8 +811,8 @@ ESA_ENTRY(rope_at, 9) {
   on_gpu(q);
   const c10::DeviceGuard guard(q.device());
   at::Tensor fresh_q, fresh_k;
-  if (!oq) fresh_q = new_tensor(q.sizes(), q.scalar_type(), q.device());
-  if (k && !ok) fresh_k = new_tensor(k->sizes(), k->scalar_type(), k->device());
+  if (!oq) fresh_q = new_here(q.sizes(), q.scalar_type());
+  if (k && !ok) fresh_k = new_here(k->sizes(), k->scalar_type());
   esa_rope_rows rows[2] = {rope_rows_of(q, oq ? *oq : fresh_q), {}};
   if (k) rows[1] = rope_rows_of(*k, ok ? *ok : fresh_k);
   void* st = stream_on(q.device());
@@ -878,8 +885,8 @@ ESA_ENTRY(verify_drafts, 7) {
   on_gpu(target);
   const c10::DeviceGuard guard(dev);
   at::Tensor fresh_out, fresh_count;
-  if (!out) fresh_out = new_tensor({n}, at::kInt, dev);
-  if (!count) fresh_count = new_tensor({n_seq}, at::kInt, dev);
+  if (!out) fresh_out = new_here({n}, at::kInt);
+  if (!count) fresh_count = new_here({n_seq}, at::kInt);
   int32_t *op = (int32_t*)ptr(out ? *out : fresh_out), *np = (int32_t*)ptr(count ? *count : fresh_count);
   const Scratch ws = scratch(esa_verify_drafts_workspace_bytes((int)n_seq, vocab));
   void *st = stream_on(dev), *wp = ws.p, *target_p = ptr(target), *draft_p = ptr(draft);

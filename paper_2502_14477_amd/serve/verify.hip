@@ -75,40 +75,49 @@ __device__ __forceinline__ Drawn drawn_of(const VerifyArgs& a, const Rows& s, in
   return Drawn{s.row0 + kept, all ? 0 : a.draft ? 1 : 2, all ? -1 : a.tokens[s.row0 + kept + 1]};
 }
 
-// Weights of M pieces of N tokens, `step` apart from `first` on: take(number, token, weight); those beyond the vocabulary are 0.  A piece
-// that would reach over a row's end is read as the row's last N numbers, of which those that belong to other pieces do not count (the vocabulary has N or
-// more).  All are requested in front of their first use.
-template <typename T, int N, int M, typename F>
-__device__ __forceinline__ void weights(const VerifyArgs& a, const Drawn& d, int64_t first, int step, F&& take) {
-  const T* pr = (const T*)(a.target + (int64_t)d.row * a.ldt);
-  const int64_t end = (int64_t)a.vocab - N;
-  auto all = [&](auto&& of) {
+// The weights of N tokens from `want` on, of which a piece of the row and the draft's are at hand: take(number, token, weight).  A piece that would
+// reach over a row's end is the row's last N numbers, of which those in front of `want` do not count (the vocabulary has N or more).  All lanes
+// of the wave take part.
+template <typename T, int N, typename F>
+__device__ __forceinline__ void piece_weights(const Drawn& d, int64_t want, int64_t end, Piece<T, N> p, Piece<T, N> q, F&& take) {
+  const int at = (int)min(want, end), skip = (int)(want - min(want, end));      // (fewer than 2^31: a chunk's first token is within the row)
+  if (__any(skip > 0)) {
 #pragma unroll
-    for (int m = 0; m < M; ++m) {
-      const int64_t want = first + m * step, at = min(want, end);
+    for (int j = 0; j < N; ++j) p.x[j] = j < skip ? (T)0 : p.x[j];
+  }
+  // the token that was looked up, with a probability of 1, is in few waves
+  const int without = d.token - at;
+  if (d.mode == 1 || (d.mode == 2 && __any((uint32_t)without < (uint32_t)N))) {
 #pragma unroll
-      for (int j = 0; j < N; ++j) {
-        const double w = of(m, j, (int)at + j);
-        take(m * N + j, (int)at + j, at + j >= want ? w : 0.0);
-      }
+    for (int j = 0; j < N; ++j) {
+      const float y = d.mode == 1 ? probability<T>(q.x[j]) : j == without ? 1.f : 0.f;
+      take(j, at + j, fmax((double)probability<T>(p.x[j]) - (double)y, 0.0));
     }
-  };
-  Piece<T, N> p[M];
+  } else {
+#pragma unroll
+    for (int j = 0; j < N; ++j) take(j, at + j, (double)probability<T>(p.x[j]));
+  }
+}
+// M of them, `step` tokens apart from `first` on, all requested in front of their first use.
+template <typename T, int N, int M>
+__device__ __forceinline__ void load_pieces(const VerifyArgs& a, const Drawn& d, int64_t first, int step, Piece<T, N> (&p)[M], Piece<T, N> (&q)[M]) {
+  const int64_t end = (int64_t)a.vocab - N;
+  const T* pr = (const T*)(a.target + (int64_t)d.row * a.ldt);
 #pragma unroll
   for (int m = 0; m < M; ++m) p[m] = load<T, N>(pr + min(first + m * step, end));
   if (d.mode == 1) {
     const T* qr = (const T*)(a.draft + (int64_t)(d.row + 1) * a.ldd);
-    Piece<T, N> q[M];
 #pragma unroll
     for (int m = 0; m < M; ++m) q[m] = load<T, N>(qr + min(first + m * step, end));
-    all([&](int m, int j, int) { return fmax((double)probability<T>(p[m].x[j]) - (double)probability<T>(q[m].x[j]), 0.0); });
-  } else {
-    const int without = d.mode == 2 ? d.token : -1;      // the token that was looked up, with a probability of 1
-    all([&](int m, int j, int t) {
-      const double x = probability<T>(p[m].x[j]);
-      return t == without ? fmax(x - 1.0, 0.0) : x;
-    });
   }
+}
+template <typename T, int N, int M, typename F>
+__device__ __forceinline__ void weights(const VerifyArgs& a, const Drawn& d, int64_t first, int step, F&& take) {
+  Piece<T, N> p[M], q[M];
+  load_pieces<T, N, M>(a, d, first, step, p, q);
+#pragma unroll
+  for (int m = 0; m < M; ++m)
+    piece_weights<T, N>(d, first + m * step, (int64_t)a.vocab - N, p[m], q[m], [&](int j, int t, double w) { take(m * N + j, t, w); });
 }
 
 struct Work {
@@ -121,11 +130,25 @@ __host__ __device__ inline Work work_at(void* ws, int n_seq, int vocab) {
   return Work{sums, (int32_t*)(sums + (size_t)n_seq * chunks_of(vocab))};
 }
 
-__device__ __forceinline__ double wave_sum(double v) {
-#pragma unroll
-  for (int m = 32; m; m >>= 1) v += __shfl_xor(v, m);
-  return v;
+// Sums over the lanes up to each, in the vector unit: shifts within rows of sixteen lanes, then the rows' last lanes passed on.
+template <int CTRL, int ROWS> __device__ __forceinline__ double passed_on(double x) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (uint32_t)u, CTRL, ROWS, 0xF, false), hi = __builtin_amdgcn_update_dpp(0, (uint32_t)(u >> 32), CTRL, ROWS, 0xF, false);
+  return __builtin_bit_cast(double, (uint64_t)lo | (uint64_t)hi << 32);
 }
+__device__ __forceinline__ double wave_sums(double x) {
+  x += passed_on<0x111, 0xF>(x);      // row_shr 1, 2, 4, 8
+  x += passed_on<0x112, 0xF>(x);
+  x += passed_on<0x114, 0xF>(x);
+  x += passed_on<0x118, 0xF>(x);
+  x += passed_on<0x142, 0xA>(x);      // row_bcast 15, 31
+  return x + passed_on<0x143, 0xC>(x);
+}
+__device__ __forceinline__ double lane_double(double x, int lane) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, x);
+  return __builtin_bit_cast(double, (uint64_t)paged::lane_value((uint32_t)u, lane) | (uint64_t)paged::lane_value((uint32_t)(u >> 32), lane) << 32);
+}
+__device__ __forceinline__ double wave_sum(double x) { return lane_double(wave_sums(x), 63); }
 // Of the workgroup, in every thread.
 __device__ __forceinline__ double group_sum(double v, double* part) {
   v = wave_sum(v);
@@ -164,11 +187,7 @@ struct Scanned {
 };
 __device__ __forceinline__ Scanned scan(double x, double* part) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int m = 1; m < 64; m <<= 1) {
-    const double v = __shfl_up(x, m);
-    x += lane >= m ? v : 0.0;
-  }
+  x = wave_sums(x);
   const double left = __shfl_up(x, 1);
   __syncthreads();
   if (lane == 63) part[wave] = x;
@@ -291,7 +310,106 @@ template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_
   if (tid == 0) a.out[d.row] = f.first != INT32_MAX ? f.first : f.last;
 }
 
-template <typename T, int N> int launch_of(const VerifyArgs& a, hipStream_t st) {
+// Where a row is no longer than a workgroup holds in registers, one launch does all: a workgroup of 1024 threads a sequence, M pieces a thread.
+constexpr int kWholeThreads = 1024;
+constexpr int kWholeWaves = kWholeThreads / 64;
+constexpr int kWholeEach = 8;      // numbers of a row a thread
+template <typename T, int N, int M> __global__ __launch_bounds__(kWholeThreads) void verify_whole(VerifyArgs a) {
+  constexpr int kSums = M * kWholeWaves, kLane = (kSums + 63) / 64;      // sums of a wave's pieces in the tokens' order, and how many a lane takes
+  __shared__ double sums[kLane * 64];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = paged::block_index();
+  if (b >= a.n_seq) return;
+  const Rows s = rows_of(a, b);
+  if (s.n == 0) {
+    if (tid == 0) a.count[b] = 0;
+    return;
+  }
+  const int kept = standing<T>(a, s);
+  Drawn d = drawn_of(a, s, kept);
+  const float u = a.u[s.row0];
+  for (int i = tid; i < s.n; i += kWholeThreads)
+    if (i != kept) a.out[s.row0 + i] = i < kept ? a.tokens[s.row0 + i + 1] : -1;
+  if (tid == 0) a.count[b] = kept + 1;
+  if (kSums < kLane * 64 && tid >= kSums && tid < kLane * 64) sums[tid] = 0.0;
+  const int64_t end = (int64_t)a.vocab - N;
+  double mine[kLane], upto[kLane], total;
+  for (;;) {
+    Piece<T, N> p[M], q[M];
+    load_pieces<T, N, M>(a, d, tid * N, kWholeThreads * N, p, q);
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      double w = 0.0;
+      piece_weights<T, N>(d, tid * N + m * (kWholeThreads * N), end, p[m], q[m], [&](int, int, double x) { w += x; });
+      w = wave_sum(w);
+      if (lane == 0) sums[m * kWholeWaves + wave] = w;
+      __builtin_amdgcn_sched_barrier(0);      // (all pieces' numbers in 64 bits at once do not fit the registers)
+    }
+    __syncthreads();
+    // every wave adds them up for itself
+    total = 0.0;
+#pragma unroll
+    for (int e = 0; e < kLane; ++e) {
+      mine[e] = sums[e * 64 + lane];
+      upto[e] = total + wave_sums(mine[e]);
+      total = lane_double(upto[e], 63);
+    }
+    if (total > 0.0 || d.mode == 0) break;
+    d.mode = 0;      // nothing is left: p itself
+    __syncthreads();
+  }
+  if (!(total > 0.0)) {
+    if (tid == 0) a.out[d.row] = -1;
+    return;
+  }
+  const double target = u >= 1.f ? __builtin_huge_val() : u > 0.f ? u * total : 0.0;
+  // the first sum that passes it, or else the last with any
+  int at = -1;
+  double base = 0.0;
+#pragma unroll
+  for (int e = kLane - 1; e >= 0; --e) {
+    const uint64_t past = __ballot(mine[e] > 0.0 && upto[e] > target), any = __ballot(mine[e] > 0.0);
+    const int l = past ? __ffsll((unsigned long long)past) - 1 : at < 0 && any ? 63 - __clzll((long long)any) : -1;
+    if (l >= 0) {
+      at = e * 64 + l;
+      base = l > 0 ? lane_double(upto[e], l - 1) : e > 0 ? lane_double(upto[e > 0 ? e - 1 : 0], 63) : 0.0;
+    }
+  }
+  if (wave != at % kWholeWaves) return;
+  const int first_token = tid * N + at / kWholeWaves * (kWholeThreads * N);
+  Piece<T, N> p[1], q[1];
+  load_pieces<T, N, 1>(a, d, first_token, 0, p, q);
+  double x[N], sum = 0.0;
+  int t[N];
+  piece_weights<T, N>(d, first_token, end, p[0], q[0], [&](int j, int token, double w) {
+    x[j] = w;
+    t[j] = token;
+    sum += w;
+  });
+  const double front = __shfl_up(wave_sums(sum), 1);
+  sum = base + (lane ? front : 0.0);
+  int first = INT32_MAX, last = -1;
+#pragma unroll
+  for (int j = 0; j < N; ++j) {
+    sum += x[j];
+    if (x[j] > 0.0) {
+      last = t[j];
+      if (sum > target && first == INT32_MAX) first = t[j];
+    }
+  }
+  const uint64_t f = __ballot(first != INT32_MAX), l = __ballot(last >= 0);
+  const int token = f ? __shfl(first, __ffsll((unsigned long long)f) - 1) : __shfl(last, 63 - __clzll((long long)l));
+  if (lane == 0) a.out[d.row] = token;
+}
+
+template <typename T, int N, int M> int launch_whole(const VerifyArgs& a, hipStream_t st) {
+  verify_whole<T, N, M><<<paged::grid_for(a.n_seq), kWholeThreads, 0, st>>>(a);
+  ESA_LAUNCH_CHECK("verify_whole");
+  return ESA_OK;
+}
+template <typename T> int launch_of(const VerifyArgs& a, hipStream_t st) {
+  constexpr int N = kPiece<T>;
+  if (a.vocab < N) return launch_whole<T, 1, 1>(a, st);
+  if (a.vocab <= kWholeThreads * kWholeEach) return launch_whole<T, N, kWholeEach / N>(a, st);
   verify_sums<T, N><<<dim3((unsigned)chunks_of(a.vocab), (unsigned)(a.n_seq < 65535 ? a.n_seq : 65535)), kThreads, 0, st>>>(a);
   ESA_LAUNCH_CHECK("verify_sums");
   verify_draw<T, N><<<paged::grid_for(a.n_seq), kThreads, 0, st>>>(a);
@@ -305,11 +423,7 @@ size_t verify_workspace(int n_seq, int vocab) {
   return align_up((size_t)n_seq * (chunks_of(vocab) * sizeof(double) + sizeof(int32_t)), 256);
 }
 
-// Vocabularies shorter than a piece are read number by number.
-int launch_verify(const VerifyArgs& a, int dtype, hipStream_t st) {
-  if (dtype == ESA_F32) return a.vocab >= kPiece<float> ? launch_of<float, kPiece<float>>(a, st) : launch_of<float, 1>(a, st);
-  return a.vocab >= kPiece<bf16_t> ? launch_of<bf16_t, kPiece<bf16_t>>(a, st) : launch_of<bf16_t, 1>(a, st);
-}
+int launch_verify(const VerifyArgs& a, int dtype, hipStream_t st) { return dtype == ESA_F32 ? launch_of<float>(a, st) : launch_of<bf16_t>(a, st); }
 
 }  // namespace serve
 }  // namespace esa
