@@ -3,6 +3,8 @@
 // Pair j of a token at position p turns by a = p freq[j] in every head: x' = g (x cos a - y sin a), y' = g (y cos a + x sin a).  Angles,
 // their sines and cosines and the products are fp64 with one rounding into the storage type, as esa_rope's are, by a shorter evaluation of the same
 // precision.
+#include <type_traits>
+
 #include "serve.h"
 
 namespace esa {
@@ -13,8 +15,7 @@ typedef __attribute__((ext_vector_type(2))) double f64x2;
 typedef __attribute__((ext_vector_type(2))) float f32x2;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 
-constexpr int kThreads = 256;
-constexpr int64_t kFewItems = 256 * 4 * kThreads;
+constexpr int kThreads = 256, kMostThreads = 512;      // of a workgroup: about the former where a token's heads take no more, else up to the latter
 
 // Cosine and sine of an angle below 2^38 in magnitude.  Reduced to [-pi/4, pi/4] by a multiple of pi/2 that is held in two parts
 // (the first product is exact in the fma, the second's error is 2^38 2^-107), then the Taylor series: x^17/17! is below 5e-17 of the sine, x^18/18!
@@ -84,15 +85,20 @@ __device__ __forceinline__ Place place_of(const RopeArgs& a, int64_t tok, int hh
 
 // What a thread takes of a head at a time: N pairs, which are two pieces of N elements, one in each half or one behind the other.  N = 1 takes
 // elements one by one, whatever their alignment.  Behind the pairs' come two pieces at a time of what does not turn.
-template <typename T, int N, bool HALVES> struct Pieces {
+template <typename T, int N, bool HALVES, bool STREAM> struct Pieces {
   Piece<T, N> a, b;
   __device__ __forceinline__ void load(const char* p, int at, int gap) {
     a = *(const Piece<T, N>*)(p + at);
     b = *(const Piece<T, N>*)(p + at + gap);
   }
   __device__ __forceinline__ void store(char* p, int at, int gap) const {
-    *(Piece<T, N>*)(p + at) = a;
-    *(Piece<T, N>*)(p + at + gap) = b;
+    if constexpr (STREAM) {
+      __builtin_nontemporal_store(__builtin_bit_cast(u32x4, a), (u32x4*)(p + at));
+      __builtin_nontemporal_store(__builtin_bit_cast(u32x4, b), (u32x4*)(p + at + gap));
+    } else {
+      *(Piece<T, N>*)(p + at) = a;
+      *(Piece<T, N>*)(p + at + gap) = b;
+    }
   }
   __device__ __forceinline__ T& x(int j) {
     if constexpr (HALVES || N == 1) return a.x[j];
@@ -124,29 +130,28 @@ template <typename T, int N, bool HALVES> struct Pieces {
   }
 };
 
-// How a launch shares out its rows: a workgroup takes `toks` tokens and hs * AHEAD heads of each, a thread one of a head's `lanes` parts for
-// every hs-th of them.
+// How a launch shares out its rows: a workgroup takes `toks` tokens and hs heads of each, a thread one of a head's `lanes` parts.
 struct Split {
   int toks, hs, lanes, parts;      // parts of a head: those that turn, then those that do not
 };
 
-template <typename T, int N, bool HALVES, int AHEAD>
-__global__ __launch_bounds__(kThreads) void rope_at(RopeArgs a, Split s) {
-  extern __shared__ __attribute__((aligned(16))) f64x2 cs[];                   // [toks][half]
+template <typename T, int N, bool HALVES, bool STREAM>
+__global__ __launch_bounds__(kMostThreads) void rope_at(RopeArgs a, Split s) {
+  extern __shared__ __attribute__((aligned(16))) f64x2 cs[];      // [toks][half]
   constexpr int kSize = N * (int)sizeof(T);
   const int tid = threadIdx.x;
   const int64_t tok0 = ((int64_t)blockIdx.y * paged::kGridRow + blockIdx.x) * s.toks;
   if (tok0 >= a.n_tok) return;
   const int n = (int)min((int64_t)s.toks, a.n_tok - tok0);
   const int turning = a.half / N;
-  const int lane = tid % s.lanes, rest = tid / s.lanes, h0 = blockIdx.z * (s.hs * AHEAD) + rest % s.hs, r = rest / s.hs;
-  const bool mine = r < n;
+  const int lane = tid % s.lanes, rest = tid / s.lanes, h = blockIdx.z * s.hs + rest % s.hs, r = rest / s.hs;
+  const bool mine = r < n && h < a.heads;
   const int64_t tok = tok0 + (mine ? r : 0);
   const int p = a.pos[tok];
-  Pieces<T, N, HALVES> v[AHEAD];
-  Place to[AHEAD];
+  const Place to = place_of(a, tok, mine ? h : 0);
+  Pieces<T, N, HALVES, STREAM> v;
   int at = 0, gap = 0;
-  auto request = [&](int i) {                     // part i of the thread's heads
+  auto request = [&](int i) {                     // part i of the thread's head
     if (i < turning) {
       at = i * (HALVES ? kSize : 2 * kSize);
       gap = HALVES ? a.half * (int)sizeof(T) : kSize;
@@ -154,14 +159,10 @@ __global__ __launch_bounds__(kThreads) void rope_at(RopeArgs a, Split s) {
       at = 2 * a.half * (int)sizeof(T) + (i - turning) * 2 * kSize;
       gap = at + kSize < (2 * a.half + a.rest) * (int)sizeof(T) ? kSize : 0;      // a single piece is taken twice
     }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u) {
-      to[u] = place_of(a, tok, min(h0 + u * s.hs, a.heads - 1));
-      v[u].load(to[u].x, at, gap);
-    }
+    v.load(to.x, at, gap);
   };
   request(lane);
-  for (int e = tid; e < n * a.half; e += kThreads) {
+  for (int e = tid; e < n * a.half; e += blockDim.x) {
     f64x2 t = turn_of((double)a.pos[tok0 + e / a.half] * a.freq[e % a.half]);
     t *= a.gain;
     if (a.transposed) t[1] = -t[1];
@@ -175,38 +176,41 @@ __global__ __launch_bounds__(kThreads) void rope_at(RopeArgs a, Split s) {
       f64x2 t[N];
 #pragma unroll
       for (int j = 0; j < N; ++j) t[j] = cs[r * a.half + i * N + j];
-#pragma unroll
-      for (int u = 0; u < AHEAD; ++u) v[u].turn(t);
+      v.turn(t);
     }
-#pragma unroll
-    for (int u = 0; u < AHEAD; ++u)
-      if (h0 + u * s.hs < a.heads) v[u].store(to[u].out, at, gap);
+    v.store(to.out, at, gap);
   }
 }
 
-template <typename T, int N, int AHEAD> int launch_split(const RopeArgs& a, hipStream_t st) {
+template <typename T, int N> int launch_of(const RopeArgs& a, hipStream_t st) {
   Split s;
   s.parts = a.half / N + (a.rest / N + 1) / 2;
   s.lanes = s.parts < kThreads ? s.parts : kThreads;
-  const int most = kThreads / s.lanes;            // heads' places of a workgroup
-  s.hs = (a.heads + AHEAD - 1) / AHEAD;
-  const int rounds = (s.hs + most - 1) / most;    // workgroups that share a token's heads
-  s.hs = (s.hs + rounds - 1) / rounds;
-  s.toks = most / s.hs;
+  const int most = kMostThreads / s.lanes;             // heads' places of a workgroup
+  const int rounds = (a.heads + most - 1) / most;      // workgroups that share a token's heads
+  s.hs = (a.heads + rounds - 1) / rounds;
+  s.toks = kThreads / (s.lanes * s.hs);
+  if (s.toks < 1) s.toks = 1;
   dim3 grid = paged::grid_for(((int64_t)a.n_tok + s.toks - 1) / s.toks);
   grid.z = rounds;
+  const unsigned threads = (unsigned)(s.toks * s.hs * s.lanes + 63) / 64 * 64;
   const size_t lds = (size_t)s.toks * a.half * sizeof(f64x2);
+  // Results that, with what they are made of, are more than the last-level cache holds go past it: what reads them next finds none of them there
+  // in any case.  Projection, rotation and a reader, 32 and 8 heads of 128, less the two others: 40000 tokens 153.3 -> 148.0 us, 16384 65.0 ->
+  // 62.4; but 8192 25.2 -> 28.4, 4096 16.2 -> 19.1.
+  constexpr int64_t kCache = (int64_t)256 << 20;
+  const bool stream = N * sizeof(T) == 16 && (int64_t)a.n_tok * a.heads * (2 * a.half + a.rest) * (int64_t)sizeof(T) * 2 > kCache;
+  auto run = [&](auto halves, auto streams) {
+    rope_at<T, N, decltype(halves)::value, decltype(streams)::value && N * sizeof(T) == 16><<<grid, threads, lds, st>>>(a, s);
+  };
+  using yes = std::true_type;
+  using no = std::false_type;
   if (a.pairs == ESA_PAIRS_HALVES)
-    rope_at<T, N, true, AHEAD><<<grid, kThreads, lds, st>>>(a, s);
+    stream ? run(yes(), yes()) : run(yes(), no());
   else
-    rope_at<T, N, false, AHEAD><<<grid, kThreads, lds, st>>>(a, s);
+    stream ? run(no(), yes()) : run(no(), no());
   ESA_LAUNCH_CHECK("rope_at");
   return ESA_OK;
-}
-template <typename T, int N> int launch_of(const RopeArgs& a, hipStream_t st) {
-  // Four heads to a thread share its sines and cosines; one where that leaves compute units without work.
-  const int64_t items = (int64_t)a.n_tok * a.heads * (a.half / N + (a.rest / N + 1) / 2);
-  return items >= kFewItems ? launch_split<T, N, 4>(a, st) : launch_split<T, N, 1>(a, st);
 }
 
 }  // namespace
