@@ -47,8 +47,11 @@ __device__ __forceinline__ Rows rows_of(const VerifyArgs& a, int b) {
   return Rows{lo, hi - lo};
 }
 
-// Drafts that stand, of a sequence with n >= 1 rows.  The whole wave takes part, a lane to a draft.
-template <typename T> __device__ int standing(const VerifyArgs& a, const Rows& s) {
+// Drafts that stand, of a sequence with n >= 1 rows, and the one that does not (any token where all do).  The whole wave takes part, a lane to a draft.
+struct Standing {
+  int kept, token;
+};
+template <typename T> __device__ __forceinline__ Standing standing(const VerifyArgs& a, const Rows& s) {
   const int lane = threadIdx.x & 63;
   for (int i0 = 1; i0 < s.n; i0 += 64) {
     const int i = i0 + lane;
@@ -60,9 +63,12 @@ template <typename T> __device__ int standing(const VerifyArgs& a, const Rows& s
     const double p = probability<T>(((const T*)(a.target + (row - 1) * a.ldt))[at]);
     const double q = a.draft ? probability<T>(((const T*)(a.draft + row * a.ldd))[at]) : 1.0;
     const uint64_t down = __ballot(i < s.n && !(token && (double)u * q < p));
-    if (down) return i0 - 1 + __ffsll((unsigned long long)down) - 1;
+    if (down) {
+      const int l = __ffsll((unsigned long long)down) - 1;
+      return Standing{i0 - 1 + l, (int)paged::lane_value((uint32_t)x, l)};
+    }
   }
-  return s.n - 1;
+  return Standing{s.n - 1, -1};
 }
 
 // What a sequence draws from.
@@ -70,9 +76,8 @@ struct Drawn {
   int row, mode;      // of the target; 0: p, 1: p - q with the draft's next row, 2: p without the token of the next row
   int token;
 };
-__device__ __forceinline__ Drawn drawn_of(const VerifyArgs& a, const Rows& s, int kept) {
-  const bool all = kept == s.n - 1;
-  return Drawn{s.row0 + kept, all ? 0 : a.draft ? 1 : 2, all ? -1 : a.tokens[s.row0 + kept + 1]};
+__device__ __forceinline__ Drawn drawn_of(const VerifyArgs& a, const Rows& s, const Standing& x) {
+  return Drawn{s.row0 + x.kept, x.kept == s.n - 1 ? 0 : a.draft ? 1 : 2, x.token};
 }
 
 // The weights of N tokens from `want` on, of which a piece of the row and the draft's are at hand: take(number, token, weight).  A piece that would
@@ -169,14 +174,14 @@ template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_
   for (int b = blockIdx.y; b < a.n_seq; b += gridDim.y) {
     const Rows s = rows_of(a, b);
     if (s.n == 0) continue;
-    const int kept = standing<T>(a, s);
-    const Drawn d = drawn_of(a, s, kept);
+    const Standing x = standing<T>(a, s);
+    const Drawn d = drawn_of(a, s, x);
     double w = 0.0;
-    weights<T, N, kEach / N>(a, d, (int64_t)chunk * kChunk + tid * N, kThreads * N, [&](int, int, double x) { w += x; });
+    weights<T, N, kEach / N>(a, d, (int64_t)chunk * kChunk + tid * N, kThreads * N, [&](int, int, double y) { w += y; });
     w = group_sum(w, part);
     if (tid == 0) {
       k.sums[(int64_t)b * gridDim.x + chunk] = w;
-      if (chunk == 0) k.kept[b] = kept;
+      if (chunk == 0) k.kept[b] = x.kept;
     }
   }
 }
@@ -239,7 +244,7 @@ template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_
   double mine = sums[min(tid, chunks - 1)];      // of the chunk that the thread's number is, in the first round of them
   mine = tid < chunks ? mine : 0.0;
   const float u = a.u[s.row0];
-  Drawn d = drawn_of(a, s, kept);
+  Drawn d = drawn_of(a, s, Standing{kept, a.tokens[s.row0 + min(kept + 1, s.n - 1)]});
   for (int i = tid; i < s.n; i += kThreads)
     if (i != kept) a.out[s.row0 + i] = i < kept ? a.tokens[s.row0 + i + 1] : -1;
   if (tid == 0) a.count[b] = kept + 1;
@@ -324,8 +329,9 @@ template <typename T, int N, int M> __global__ __launch_bounds__(kWholeThreads) 
     if (tid == 0) a.count[b] = 0;
     return;
   }
-  const int kept = standing<T>(a, s);
-  Drawn d = drawn_of(a, s, kept);
+  const Standing st = standing<T>(a, s);
+  const int kept = st.kept;
+  Drawn d = drawn_of(a, s, st);
   const float u = a.u[s.row0];
   for (int i = tid; i < s.n; i += kWholeThreads)
     if (i != kept) a.out[s.row0 + i] = i < kept ? a.tokens[s.row0 + i + 1] : -1;
