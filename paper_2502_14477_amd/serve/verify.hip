@@ -116,23 +116,16 @@ __device__ __forceinline__ void load_pieces(const VerifyArgs& a, const Drawn& d,
     for (int m = 0; m < M; ++m) q[m] = load<T, N>(qr + min(first + m * step, end));
   }
 }
-template <typename T, int N, int M, typename F>
-__device__ __forceinline__ void weights(const VerifyArgs& a, const Drawn& d, int64_t first, int step, F&& take) {
-  Piece<T, N> p[M], q[M];
-  load_pieces<T, N, M>(a, d, first, step, p, q);
-#pragma unroll
-  for (int m = 0; m < M; ++m)
-    piece_weights<T, N>(d, first + m * step, (int64_t)a.vocab - N, p[m], q[m], [&](int j, int t, double w) { take(m * N + j, t, w); });
-}
-
+// A row's sums are kept by blocks of 64 pieces, a wave's at a time.
+__host__ __device__ inline int chunks_of(int vocab) { return (int)(((int64_t)vocab + kChunk - 1) / kChunk); }
+template <int N> __host__ __device__ inline int blocks_of(int vocab) { return chunks_of(vocab) * (kChunk / (64 * N)); }
 struct Work {
-  double* sums;      // [n_seq][chunks]
+  double* sums;      // [n_seq][blocks]
   int32_t* kept;     // [n_seq]
 };
-__host__ __device__ inline int chunks_of(int vocab) { return (int)(((int64_t)vocab + kChunk - 1) / kChunk); }
-__host__ __device__ inline Work work_at(void* ws, int n_seq, int vocab) {
+__host__ __device__ inline Work work_at(void* ws, int n_seq, int blocks) {
   double* sums = (double*)ws;
-  return Work{sums, (int32_t*)(sums + (size_t)n_seq * chunks_of(vocab))};
+  return Work{sums, (int32_t*)(sums + (size_t)n_seq * blocks)};
 }
 
 // Sums over the lanes up to each, in the vector unit: shifts within rows of sixteen lanes, then the rows' last lanes passed on.
@@ -154,35 +147,31 @@ __device__ __forceinline__ double lane_double(double x, int lane) {
   return __builtin_bit_cast(double, (uint64_t)paged::lane_value((uint32_t)u, lane) | (uint64_t)paged::lane_value((uint32_t)(u >> 32), lane) << 32);
 }
 __device__ __forceinline__ double wave_sum(double x) { return lane_double(wave_sums(x), 63); }
-// Of the workgroup, in every thread.
-__device__ __forceinline__ double group_sum(double v, double* part) {
-  v = wave_sum(v);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
-  __syncthreads();
-  v = 0.0;
+// A chunk's blocks' sums, by a workgroup.
+template <typename T, int N> __device__ __forceinline__ void chunk_sums(const VerifyArgs& a, const Drawn& d, int chunk, double* sums) {
+  constexpr int M = kEach / N;
+  const int64_t first = (int64_t)chunk * kChunk + threadIdx.x * N;
+  Piece<T, N> p[M], q[M];
+  load_pieces<T, N, M>(a, d, first, kThreads * N, p, q);
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) v += part[i];
-  return v;
+  for (int m = 0; m < M; ++m) {
+    double w = 0.0;
+    piece_weights<T, N>(d, first + m * (kThreads * N), (int64_t)a.vocab - N, p[m], q[m], [&](int, int, double x) { w += x; });
+    w = wave_sums(w);
+    if ((threadIdx.x & 63) == 63) sums[(chunk * M + m) * kWaves + (threadIdx.x >> 6)] = w;
+  }
 }
 
 // grid (chunks, sequences)
 template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_sums(VerifyArgs a) {
-  __shared__ double part[kWaves];
-  const int tid = threadIdx.x, chunk = blockIdx.x;
-  const Work k = work_at(a.ws, a.n_seq, a.vocab);
+  const int chunk = blockIdx.x, blocks = blocks_of<N>(a.vocab);
+  const Work k = work_at(a.ws, a.n_seq, blocks);
   for (int b = blockIdx.y; b < a.n_seq; b += gridDim.y) {
     const Rows s = rows_of(a, b);
     if (s.n == 0) continue;
     const Standing x = standing<T>(a, s);
-    const Drawn d = drawn_of(a, s, x);
-    double w = 0.0;
-    weights<T, N, kEach / N>(a, d, (int64_t)chunk * kChunk + tid * N, kThreads * N, [&](int, int, double y) { w += y; });
-    w = group_sum(w, part);
-    if (tid == 0) {
-      k.sums[(int64_t)b * gridDim.x + chunk] = w;
-      if (chunk == 0) k.kept[b] = x.kept;
-    }
+    chunk_sums<T, N>(a, drawn_of(a, s, x), chunk, k.sums + (int64_t)b * blocks);
+    if (chunk == 0 && threadIdx.x == 0) k.kept[b] = x.kept;
   }
 }
 
@@ -226,93 +215,130 @@ __device__ __forceinline__ Found find(int first, int last, Found* part) {
   return r;
 }
 
-// A workgroup a sequence.
-template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_draw(VerifyArgs a) {
-  __shared__ double part[kWaves];
-  __shared__ Found found[kWaves];
-  __shared__ double at_chunk;
-  const int tid = threadIdx.x, b = paged::block_index();
-  if (b >= a.n_seq) return;
-  const Rows s = rows_of(a, b);
-  if (s.n == 0) {
-    if (tid == 0) a.count[b] = 0;
-    return;
-  }
-  const Work k = work_at(a.ws, a.n_seq, a.vocab);
-  const int kept = k.kept[b], chunks = chunks_of(a.vocab);
-  const double* sums = k.sums + (int64_t)b * chunks;
-  double mine = sums[min(tid, chunks - 1)];      // of the chunk that the thread's number is, in the first round of them
-  mine = tid < chunks ? mine : 0.0;
-  const float u = a.u[s.row0];
-  Drawn d = drawn_of(a, s, Standing{kept, a.tokens[s.row0 + min(kept + 1, s.n - 1)]});
-  for (int i = tid; i < s.n; i += kThreads)
-    if (i != kept) a.out[s.row0 + i] = i < kept ? a.tokens[s.row0 + i + 1] : -1;
-  if (tid == 0) a.count[b] = kept + 1;
-  // sums in front of the thread's chunk
-  Scanned y = scan(mine, part);
-  double total = y.all;
-  for (int c = tid + kThreads; c - tid < chunks; c += kThreads) total += group_sum(c < chunks ? sums[c] : 0.0, part);
-  bool again = false;                            // whether the chunks' sums are those of p
-  if (!(total > 0.0)) {
-    if (d.mode == 0) {
-      if (tid == 0) a.out[d.row] = -1;
-      return;
-    }
-    // p itself, of which there are no sums yet: one workgroup reads it all
-    d.mode = 0;
-    again = true;
-    for (int c = 0; c < chunks; ++c) {
-      double w = 0.0;
-      weights<T, N, kEach / N>(a, d, (int64_t)c * kChunk + tid * N, kThreads * N, [&](int, int, double x) { w += x; });
-      w = group_sum(w, part);
-      if (tid == 0) k.sums[(int64_t)b * chunks + c] = w;
-      total += w;
-    }
-    if (!(total > 0.0)) {
-      if (tid == 0) a.out[d.row] = -1;
-      return;
-    }
-    __syncthreads();
-  }
-  const double target = u >= 1.f ? __builtin_huge_val() : u > 0.f ? u * total : 0.0;
-  // the first chunk whose sums pass it, or else the last with any
-  int chunk = -1;
-  double base = 0.0;
-  for (int c0 = 0; c0 < chunks; c0 += kThreads) {
-    const int c = c0 + tid;
-    if (c0 > 0 || again) {
-      mine = c < chunks ? sums[c] : 0.0;
-      y = scan(mine, part);
-    }
-    const double before = base + y.before;
-    const Found f = find(mine > 0.0 && before + mine > target ? c : INT32_MAX, mine > 0.0 ? c : -1, found);
-    if (f.first != INT32_MAX) chunk = f.first;
-    else if (f.last >= 0) chunk = f.last;
-    if (chunk == c) at_chunk = before;
-    if (f.first != INT32_MAX) break;
-    base += y.all;
-  }
-  __syncthreads();
-  double x[kEach], sum = 0.0;
-  int t[kEach];
-  weights<T, N, kEach / N>(a, d, (int64_t)chunk * kChunk + tid * kEach, N, [&](int j, int at, double w) {
+// The token in a wave's block, of which the lane has N tokens from `want` on, where sums pass the target, `base` being the sum in front of the
+// block; or else the last one with any weight.
+template <typename T, int N> __device__ __forceinline__ int token_in(const VerifyArgs& a, const Drawn& d, int64_t want, double base, double target) {
+  const int lane = threadIdx.x & 63;
+  Piece<T, N> p[1], q[1];
+  load_pieces<T, N, 1>(a, d, want, 0, p, q);
+  double x[N], sum = 0.0;
+  int t[N];
+  piece_weights<T, N>(d, want, (int64_t)a.vocab - N, p[0], q[0], [&](int j, int token, double w) {
     x[j] = w;
-    t[j] = at;
+    t[j] = token;
     sum += w;
   });
-  const double start = at_chunk;
-  sum = start + scan(sum, part).before;
+  const double front = __shfl_up(wave_sums(sum), 1);
+  sum = base + (lane ? front : 0.0);
   int first = INT32_MAX, last = -1;
 #pragma unroll
-  for (int j = 0; j < kEach; ++j) {
+  for (int j = 0; j < N; ++j) {
     sum += x[j];
     if (x[j] > 0.0) {
       last = t[j];
       if (sum > target && first == INT32_MAX) first = t[j];
     }
   }
-  const Found f = find(first, last, found);
-  if (tid == 0) a.out[d.row] = f.first != INT32_MAX ? f.first : f.last;
+  const uint64_t f = __ballot(first != INT32_MAX), l = __ballot(last >= 0);
+  return f ? __shfl(first, __ffsll((unsigned long long)f) - 1) : __shfl(last, 63 - __clzll((long long)l));
+}
+__device__ __forceinline__ double target_of(float u, double total) { return u >= 1.f ? __builtin_huge_val() : u > 0.f ? u * total : 0.0; }
+
+// A workgroup a sequence.
+constexpr int kBlocks = 4;      // blocks' sums a thread in a round
+constexpr int kRound = kThreads * kBlocks;
+template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_draw(VerifyArgs a) {
+  __shared__ double part[kWaves];
+  __shared__ Found found[kWaves];
+  __shared__ double at_block;
+  const int tid = threadIdx.x, b = paged::block_index();
+  if (b >= a.n_seq) return;
+  const int blocks = blocks_of<N>(a.vocab);
+  const Work k = work_at(a.ws, a.n_seq, blocks);
+  double* const sums = k.sums + (int64_t)b * blocks;
+  double x[kBlocks];
+  Scanned y;
+  auto request = [&](int r0) {
+#pragma unroll
+    for (int j = 0; j < kBlocks; ++j) x[j] = sums[min(r0 + tid * kBlocks + j, blocks - 1)];
+  };
+  auto add_up = [&](int r0) {
+    double sum = 0.0;
+#pragma unroll
+    for (int j = 0; j < kBlocks; ++j) {
+      x[j] = r0 + tid * kBlocks + j < blocks ? x[j] : 0.0;
+      sum += x[j];
+    }
+    y = scan(sum, part);
+  };
+  request(0);
+  const Rows s = rows_of(a, b);
+  if (s.n == 0) {
+    if (tid == 0) a.count[b] = 0;
+    return;
+  }
+  const int kept = k.kept[b];
+  const float u = a.u[s.row0];
+  Drawn d = drawn_of(a, s, Standing{kept, a.tokens[s.row0 + min(kept + 1, s.n - 1)]});
+  for (int i = tid; i < s.n; i += kThreads)
+    if (i != kept) a.out[s.row0 + i] = i < kept ? a.tokens[s.row0 + i + 1] : -1;
+  if (tid == 0) a.count[b] = kept + 1;
+  double total = 0.0;
+  bool at_hand = blocks <= kRound;               // whether the first round's sums are those that are looked through
+  for (int r0 = 0; r0 < blocks; r0 += kRound) {
+    if (r0) request(r0);
+    add_up(r0);
+    total += y.all;
+  }
+  if (!(total > 0.0) && d.mode != 0) {
+    // nothing is left: p itself, of which there are no sums yet; one workgroup reads it all
+    d.mode = 0;
+    at_hand = false;
+    for (int c = 0; c < chunks_of(a.vocab); ++c) chunk_sums<T, N>(a, d, c, sums);
+    __syncthreads();
+    for (int r0 = 0; r0 < blocks; r0 += kRound) {
+      request(r0);
+      add_up(r0);
+      total += y.all;
+    }
+  }
+  if (!(total > 0.0)) {
+    if (tid == 0) a.out[d.row] = -1;
+    return;
+  }
+  const double target = target_of(u, total);
+  // the first block whose sums pass it, or else the last with any
+  int block = -1;
+  double base = 0.0;
+  for (int r0 = 0; r0 < blocks; r0 += kRound) {
+    if (!at_hand) {
+      request(r0);
+      add_up(r0);
+    }
+    double before[kBlocks], sum = base + y.before;
+    int first = INT32_MAX, last = -1;
+#pragma unroll
+    for (int j = 0; j < kBlocks; ++j) {
+      before[j] = sum;
+      sum += x[j];
+      if (x[j] > 0.0) {
+        last = r0 + tid * kBlocks + j;
+        if (sum > target && first == INT32_MAX) first = last;
+      }
+    }
+    const Found f = find(first, last, found);
+    if (f.first != INT32_MAX) block = f.first;
+    else if (f.last >= 0) block = f.last;
+#pragma unroll
+    for (int j = 0; j < kBlocks; ++j)
+      if (block == r0 + tid * kBlocks + j) at_block = before[j];
+    if (f.first != INT32_MAX) break;
+    base += y.all;
+  }
+  __syncthreads();
+  if (tid >= 64) return;
+  const int token = token_in<T, N>(a, d, ((int64_t)block * 64 + tid) * N, at_block, target);
+  if (tid == 0) a.out[d.row] = token;
 }
 
 // Where a row is no longer than a workgroup holds in registers, one launch does all: a workgroup of 1024 threads a sequence, M pieces a thread.
@@ -367,7 +393,7 @@ template <typename T, int N, int M> __global__ __launch_bounds__(kWholeThreads) 
     if (tid == 0) a.out[d.row] = -1;
     return;
   }
-  const double target = u >= 1.f ? __builtin_huge_val() : u > 0.f ? u * total : 0.0;
+  const double target = target_of(u, total);
   // the first sum that passes it, or else the last with any
   int at = -1;
   double base = 0.0;
@@ -381,29 +407,7 @@ template <typename T, int N, int M> __global__ __launch_bounds__(kWholeThreads) 
     }
   }
   if (wave != at % kWholeWaves) return;
-  const int first_token = tid * N + at / kWholeWaves * (kWholeThreads * N);
-  Piece<T, N> p[1], q[1];
-  load_pieces<T, N, 1>(a, d, first_token, 0, p, q);
-  double x[N], sum = 0.0;
-  int t[N];
-  piece_weights<T, N>(d, first_token, end, p[0], q[0], [&](int j, int token, double w) {
-    x[j] = w;
-    t[j] = token;
-    sum += w;
-  });
-  const double front = __shfl_up(wave_sums(sum), 1);
-  sum = base + (lane ? front : 0.0);
-  int first = INT32_MAX, last = -1;
-#pragma unroll
-  for (int j = 0; j < N; ++j) {
-    sum += x[j];
-    if (x[j] > 0.0) {
-      last = t[j];
-      if (sum > target && first == INT32_MAX) first = t[j];
-    }
-  }
-  const uint64_t f = __ballot(first != INT32_MAX), l = __ballot(last >= 0);
-  const int token = f ? __shfl(first, __ffsll((unsigned long long)f) - 1) : __shfl(last, 63 - __clzll((long long)l));
+  const int token = token_in<T, N>(a, d, tid * N + at / kWholeWaves * (kWholeThreads * N), base, target);
   if (lane == 0) a.out[d.row] = token;
 }
 
@@ -426,7 +430,7 @@ template <typename T> int launch_of(const VerifyArgs& a, hipStream_t st) {
 }  // namespace
 
 size_t verify_workspace(int n_seq, int vocab) {
-  return align_up((size_t)n_seq * (chunks_of(vocab) * sizeof(double) + sizeof(int32_t)), 256);
+  return align_up((size_t)n_seq * (blocks_of<4>(vocab) * sizeof(double) + sizeof(int32_t)), 256);      // (fp32: bf16 has half as many blocks)
 }
 
 int launch_verify(const VerifyArgs& a, int dtype, hipStream_t st) { return dtype == ESA_F32 ? launch_of<float>(a, st) : launch_of<bf16_t>(a, st); }
