@@ -341,10 +341,12 @@ template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_
   if (tid == 0) a.out[d.row] = token;
 }
 
-// Where a row is no longer than a workgroup holds in registers, one launch does all: a workgroup of 1024 threads a sequence, M pieces a thread.
+// A short row is one workgroup's: a launch does all, M pieces a thread.  Its instructions are then one compute unit's, so that longer rows are quicker in
+// two launches: us a call in a graph, 1 / 16 / 128 / 512 sequences of four drafts, fp32, one launch and two: 8000 tokens 3.8 / 4.5 / 4.9 / 7.0
+// and 6.4 / 7.6 / 8.1 / 12.0 (eight numbers a thread), 16000 5.7 / 5.9 / 6.2 / 13.6 and 6.7 / 7.1 / 8.0 / 15.4 (sixteen), 32000 9.4 / 10.1 /
+// 10.6 / 25.7 and 6.1 / 7.2 / 10.2 / 22.0.
 constexpr int kWholeThreads = 1024;
 constexpr int kWholeWaves = kWholeThreads / 64;
-constexpr int kWholeEach = 8;      // numbers of a row a thread
 template <typename T, int N, int M> __global__ __launch_bounds__(kWholeThreads) void verify_whole(VerifyArgs a) {
   constexpr int kSums = M * kWholeWaves, kLane = (kSums + 63) / 64;      // sums of a wave's pieces in the tokens' order, and how many a lane takes
   __shared__ double sums[kLane * 64];
@@ -419,7 +421,8 @@ template <typename T, int N, int M> int launch_whole(const VerifyArgs& a, hipStr
 template <typename T> int launch_of(const VerifyArgs& a, hipStream_t st) {
   constexpr int N = kPiece<T>;
   if (a.vocab < N) return launch_whole<T, 1, 1>(a, st);
-  if (a.vocab <= kWholeThreads * kWholeEach) return launch_whole<T, N, kWholeEach / N>(a, st);
+  if (a.vocab <= 8 * kWholeThreads) return launch_whole<T, N, 8 / N>(a, st);
+  if (a.vocab <= 16 * kWholeThreads) return launch_whole<T, N, 16 / N>(a, st);
   verify_sums<T, N><<<dim3((unsigned)chunks_of(a.vocab), (unsigned)(a.n_seq < 65535 ? a.n_seq : 65535)), kThreads, 0, st>>>(a);
   ESA_LAUNCH_CHECK("verify_sums");
   verify_draw<T, N><<<paged::grid_for(a.n_seq), kThreads, 0, st>>>(a);
