@@ -202,25 +202,21 @@ template <int EACH> __global__ __launch_bounds__(kThreads) void plan_whole(PlanA
   for (int64_t i = blockIdx.x * kThreads + threadIdx.x; i < n; i += gridDim.x * kThreads) fill(a, o, q, i);
 }
 
-// Two launches, the offsets in the workspace.
+// The lengths that a launch has left aside go to their places: [n_seq] starts, [n_seq] numbers of pages, the ring's two.
+__global__ __launch_bounds__(256) void plan_settle(PlanArgs a, const int32_t* aside) {
+  const int i = blockIdx.x * 256 + threadIdx.x;
+  if (i >= 2 * a.n_seq + 2) return;
+  (i < a.n_seq ? a.start + i : i < 2 * a.n_seq ? a.held + (i - a.n_seq) : a.ring_at + (i - 2 * a.n_seq))[0] = aside[i];
+}
+
+// More sequences than LDS has room for: two launches, the offsets in the workspace.
 __global__ __launch_bounds__(kThreads) void plan_lengths(PlanArgs a) {
   const Queue q = plan_offsets<4>(a, offsets_at(a.ws, a.n_seq), true);
   if (threadIdx.x == 0) *(Queue*)a.ws = q;
 }
-// ends: of how many sequences there is room for in LDS; all of them or none.
-__global__ __launch_bounds__(kThreads) void plan_fill(PlanArgs a, int ends) {
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  Offsets o = offsets_at(a.ws, a.n_seq);
+__global__ __launch_bounds__(kThreads) void plan_fill(PlanArgs a) {
+  const Offsets o = offsets_at(a.ws, a.n_seq);
   const Queue q = *(const Queue*)a.ws;
-  if (ends) {
-    int32_t* e = (int32_t*)lds;
-    const int n = a.n_seq + 1;
-    for (int i = threadIdx.x; i < 3 * n; i += kThreads) e[i] = o.row[i];      // give's and take's lie behind them
-    o.row = e;
-    o.give = e + n;
-    o.take = e + 2 * n;
-    __syncthreads();
-  }
   const int64_t n = items_of(a, o, q);
   for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads) fill(a, o, q, i);
 }
@@ -238,21 +234,30 @@ int launch_plan(const PlanArgs& a, hipStream_t st) {
   const bool alone = a.n_seq <= kThreads && (int64_t)a.n_seq * a.max_pages + a.n_tok <= kAlone;
   const int64_t most = ((int64_t)a.n_tok + kThreads - 1) / kThreads;
   const unsigned blocks = (unsigned)(most < 32 ? 32 : most > 256 ? 256 : most);
-  if (a.n_seq <= kLdsSeqs && (alone || !in_place)) {
-    const int rc = raise_lds_limit(raised, {(const void*)plan_whole<4>}, offsets_bytes(kLdsSeqs), "plan_whole");
-    if (rc != ESA_OK) return rc;
-    if (a.n_seq <= kThreads)
-      plan_whole<1><<<dim3(alone ? 1 : blocks), kThreads, offsets_bytes(a.n_seq), st>>>(a);
-    else
-      plan_whole<4><<<dim3(blocks), kThreads, offsets_bytes(a.n_seq), st>>>(a);
-    ESA_LAUNCH_CHECK("plan_whole");
+  if (a.n_seq > kLdsSeqs) {
+    plan_lengths<<<dim3(1), kThreads, 0, st>>>(a);
+    ESA_LAUNCH_CHECK("plan_lengths");
+    plan_fill<<<dim3(blocks), kThreads, 0, st>>>(a);
+    ESA_LAUNCH_CHECK("plan_fill");
     return ESA_OK;
   }
-  plan_lengths<<<dim3(1), kThreads, 0, st>>>(a);
-  ESA_LAUNCH_CHECK("plan_lengths");
-  const bool staged = a.n_seq <= kLdsSeqs;
-  plan_fill<<<dim3(blocks), kThreads, staged ? 3 * ((size_t)a.n_seq + 1) * sizeof(int32_t) : 0, st>>>(a, staged ? a.n_seq : 0);
-  ESA_LAUNCH_CHECK("plan_fill");
+  const int rc = raise_lds_limit(raised, {(const void*)plan_whole<4>}, offsets_bytes(kLdsSeqs), "plan_whole");
+  if (rc != ESA_OK) return rc;
+  PlanArgs w = a;
+  if (in_place && !alone) {
+    w.start = (int32_t*)a.ws;
+    w.held = w.start + a.n_seq;
+    w.ring_at = w.held + a.n_seq;
+  }
+  if (a.n_seq <= kThreads)
+    plan_whole<1><<<dim3(alone ? 1 : blocks), kThreads, offsets_bytes(a.n_seq), st>>>(w);
+  else
+    plan_whole<4><<<dim3(blocks), kThreads, offsets_bytes(a.n_seq), st>>>(w);
+  ESA_LAUNCH_CHECK("plan_whole");
+  if (in_place && !alone) {
+    plan_settle<<<dim3((2 * a.n_seq + 2 + 255) / 256), 256, 0, st>>>(a, (const int32_t*)a.ws);
+    ESA_LAUNCH_CHECK("plan_settle");
+  }
   return ESA_OK;
 }
 

@@ -234,7 +234,7 @@ class Loop:
 
 PLANS = [  # sequences, entries of a row, pages, page size, rows, most new tokens
     (1, 1, 1, 16, 1, 1), (1, 40, 50, 128, 700, 600), (5, 7, 60, 16, 300, 60), (63, 9, 300, 32, 900, 12), (65, 12, 500, 16, 2000, 33), (1023, 4, 2500, 64, 3000, 5),
-    (1025, 5, 3000, 16, 6000, 9), (2500, 3, 4000, 16, 3000, 3), (7, 300, 900, 16, 20000, 4000)]
+    (1025, 5, 3000, 16, 6000, 9), (2500, 3, 4000, 16, 3000, 3), (5000, 2, 7000, 16, 9000, 4), (7, 300, 900, 16, 20000, 4000)]
 
 
 @pytest.mark.parametrize("shape", PLANS, ids=["x".join(map(str, s)) for s in PLANS])
