@@ -89,7 +89,7 @@ typedef struct {
  *   workspace     esa_plan_paged_workspace_bytes(n_seq) bytes, 256-byte aligned
  * What arrays hold that no sequence of calls leads to (a number of pages above max_pages or n_pages, say) is clamped, the outcome is then
  * unspecified.  n_seq == 0 is a no-op but for cu, lack, pos, slot and ring_at.
- * n_seq at most 2^24, n_tok below 2^31 - 2^16.  Arrays other than those of *_in must not overlap.
+ * n_seq at most 2^24, n_tok below 2^31 - 2^16.  What is written overlaps nothing else, but that start, held and ring_at may be their *_in.
  */
 ESA_API size_t esa_plan_paged_workspace_bytes(int n_seq);
 ESA_API int esa_plan_paged(const esa_page_state* state, const int32_t* grow, const int32_t* fresh, int64_t n_tok, int32_t* cu, int32_t* pos,
@@ -107,7 +107,7 @@ ESA_API int esa_plan_paged(const esa_page_state* state, const int32_t* grow, con
  * having been turned down, or, where there is none, from w = p_a: the lowest t with w_0 + ... + w_t > u[cu[b]] * (w_0 + ... + w_{vocab-1}).
  * Differences, products and sums are fp64; w need not sum to 1.  Probabilities that are negative, infinite or NaN count as 0; where all of
  * w is 0, w = p_a; where that is 0 too the token is -1.  A u that is negative or NaN draws as 0 does, one of
- * 1 or more the last token of positive weight.
+ * 1 or more the last token of positive weight; a draft does not stand by a u that is NaN.
  *   out     [n_tok] int32: the token that follows a row: tokens[i + 1] of rows before a, the drawn one of row a, -1 behind it
  *   count   [n_seq] int32: rows that stand, cu[b] among them, which is the number of new tokens too; 0 for a sequence without rows
  * Rows behind cu[n_seq] are left as they were.  cu ascends from 0 to at most n_tok (other values are clamped, the results are then

@@ -345,7 +345,8 @@ def check_verify(esa, target, tokens, cu, u, draft, rows=None):
 
 
 VERIFIES = [  # sequences, most drafts, vocabulary
-    (1, 0, 1), (1, 4, 2), (3, 3, 63), (17, 5, 1000), (2, 2, 4096), (5, 4, 4097), (2, 150, 300), (4, 3, 50001), (3, 6, 131072), (40, 1, 777)]
+    (1, 0, 1), (1, 4, 2), (3, 3, 63), (17, 5, 1000), (2, 2, 4096), (5, 4, 4097), (2, 150, 300), (4, 3, 50001), (3, 6, 131072), (40, 1, 777), (3, 2, 16384), (2, 2, 16385), (2, 3, 300007),
+    (1, 2, 600001)]
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
@@ -375,12 +376,13 @@ def test_verify(esa, shape, drawn, dtype):
         assert len(seen[0]) > 65
 
 
-def test_verify_counts_what_is_no_probability_as_nothing(esa):
+@pytest.mark.parametrize("vocab", [3, 5000, 50001])
+def test_verify_counts_what_is_no_probability_as_nothing(esa, vocab):
     rng = np.random.default_rng(31)
     for dtype in ("f32", "bf16"):
         for drawn in (True, False):
-            n, vocab = 60, 5000
-            cu, tokens, u = np.arange(0, n + 1, 4), rng.integers(0, 50, n), rng.random(n).astype(np.float32)
+            n = 60
+            cu, tokens, u = np.arange(0, n + 1, 4), rng.integers(0, min(vocab, 50), n), rng.random(n).astype(np.float32)
             p, q = (x[:, rng.permutation(vocab)] for x in distributions(rng, n, vocab))
             for x in (p, q):
                 x[rng.random(x.shape) < 0.2] = float("nan")
@@ -390,10 +392,11 @@ def test_verify_counts_what_is_no_probability_as_nothing(esa):
             check_verify(esa, held(p, dtype), tokens, cu, u, held(q, dtype) if drawn else None)
 
 
-def test_verify_where_nothing_is_left(esa):
+@pytest.mark.parametrize("vocab", [5, 9000, 50001, 300007])
+def test_verify_where_nothing_is_left(esa, vocab):
     """Differences that are nowhere positive: the target's own row; a row without any probability: no token."""
     rng = np.random.default_rng(32)
-    vocab, cu = 9000, [0, 3, 6, 7, 9]
+    cu = [0, 3, 6, 7, 9]
     p = distributions(rng, 9, vocab)[0]
     q = np.ones_like(p)                                           # turns every draft down, and leaves nothing
     tokens, u = rng.integers(0, vocab, 9), np.full(9, 0.999, dtype=np.float32)
@@ -402,12 +405,12 @@ def test_verify_where_nothing_is_left(esa):
     want = check_verify(esa, held(p, "f32"), tokens, cu, u, held(q, "f32"))
     assert want[1] == [-1] and want[2] == [-1]
     p[:] = 0.0
-    p[:, 8999] = 1.0                                              # a draft that was looked up and is sure to be right
-    tokens[:] = 8999
+    p[:, vocab - 1] = 1.0                                              # a draft that was looked up and is sure to be right
+    tokens[:] = vocab - 1
     want = check_verify(esa, held(p, "f32"), tokens, cu, u, None)
-    assert want[0] == [8999] * 3
+    assert want[0] == [vocab - 1] * 3
     u[:] = 1.0                                                    # turned down, and all of p with it: p itself
-    assert check_verify(esa, held(p, "f32"), tokens, cu, u, None)[0] == [8999]
+    assert check_verify(esa, held(p, "f32"), tokens, cu, u, None)[0] == [vocab - 1]
 
 
 def test_verify_tokens_outside_the_vocabulary(esa):
@@ -420,17 +423,18 @@ def test_verify_tokens_outside_the_vocabulary(esa):
             check_verify(esa, held(p, "f32"), tokens, [0, 4, 8], np.linspace(0, 0.9, 8, dtype=np.float32), held(q, "f32") if drawn else None)
 
 
-def test_verify_offsets_of_any_content(esa):
+@pytest.mark.parametrize("vocab", [700, 20000])
+def test_verify_offsets_of_any_content(esa, vocab):
     """cu that does not ascend or leads out of the rows is clamped; nothing outside the outputs is written."""
     rng = np.random.default_rng(34)
-    p, q = (held(x, "f32") for x in distributions(rng, 6, 700))
+    p, q = (held(x, "f32") for x in distributions(rng, 6, vocab))
     for _ in range(20):
         keep = Guarded()
         cu = keep(rng.choice([-2 ** 31, -5, 0, 1, 2, 4, 6, 9, 2 ** 31 - 1], 9))
         out, count = keep(np.zeros(6)), keep(np.zeros(8))
-        esa.esa_verify_drafts(p, keep(rng.integers(-2, 800, 6)), cu, torch.rand(6, device="cuda"), draft=q, out=out, count=count)
+        esa.esa_verify_drafts(p, keep(rng.integers(-2, vocab + 100, 6)), cu, torch.rand(6, device="cuda"), draft=q, out=out, count=count)
         keep.check()
-        assert torch.all((out >= -1) & (out < 700)) and torch.all((count >= 0) & (count <= 6))
+        assert torch.all((out >= -1) & (out < vocab)) and torch.all((count >= 0) & (count <= 6))
 
 
 def test_verify_without_rows(esa):
@@ -449,3 +453,25 @@ def test_verify_far_rows(esa):
     for w, x in zip(whole, (p, q)):
         w.copy_(torch.from_numpy(x))
     check_verify(esa, whole[0], rng.integers(0, 1001, 6), [0, 3, 6], rng.random(6).astype(np.float32), whole[1])
+
+
+@pytest.mark.parametrize("vocab", [40, 16400])
+def test_verify_many_sequences(esa, vocab):
+    """More of them than a launch has workgroups in one dimension of its grid."""
+    n = 70000
+    g = torch.Generator("cuda").manual_seed(5)
+    sure = torch.randint(0, vocab, (n,), generator=g, device="cuda")
+    p = torch.zeros((n, vocab), dtype=torch.bfloat16, device="cuda").scatter_(1, sure[:, None], 1.0)
+    # two rows a sequence: drafts that are sure to stand, or sure not to
+    tokens = torch.where(torch.arange(n, device="cuda") % 4 < 2, sure.roll(1), (sure.roll(1) + 1) % vocab).int()
+    cu = torch.arange(0, n + 1, 2, dtype=torch.int32, device="cuda")
+    u = torch.rand(n, generator=g, device="cuda")
+    out, count = esa.esa_verify_drafts(p, tokens, cu, u)
+    stands = torch.arange(n // 2, device="cuda") % 2 == 0
+    assert torch.equal(count, torch.where(stands, 2, 1).int())
+    want = sure.int().view(-1, 2).clone()
+    want[~stands, 1] = -1
+    assert torch.equal(out.view(-1, 2), want)
+    one = torch.arange(n + 1, dtype=torch.int32, device="cuda")
+    out, count = esa.esa_verify_drafts(p, tokens, one, u)
+    assert torch.equal(out, sure.int()) and torch.all(count == 1)
