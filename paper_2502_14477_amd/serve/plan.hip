@@ -5,17 +5,14 @@
 // the offsets alone.  So no page's number passes through another one's, nothing is atomic, and the outcome does not depend on the order.
 //
 // What bounds it is latency: lengths, three scans of a few hundred cycles, a search in LDS, a table's or ring's entry.  So every workgroup makes the scans
-// for itself (28 bytes a sequence in LDS) and no second launch has to wait for them: 200 sequences 5.6 us in a graph, of which 12000 pages move; two
-// launches, the scans' results by way of memory, 7.7.  One that goes on in place must not overwrite lengths that other workgroups have yet to read: they are
-// left aside, and a launch of 2 us settles them.  Where there is little to move one workgroup does it all (sixteen sequences 4.0 us).
+// for itself (28 bytes a sequence in LDS) and no second launch has to wait for them: 200 sequences 4.8 us in a graph, of which 12000 pages move; two
+// launches, the scans' results by way of memory, took 7.7, one workgroup 15.8.  One that goes on in place must not overwrite lengths that other workgroups
+// have yet to read: they are left aside, and a launch of 2 us settles them.
 #include "serve.h"
 
 namespace esa {
 namespace serve {
 namespace {
-
-constexpr int kThreads = 1024;
-constexpr int kWaves = kThreads / 64;
 
 // What rows and pages are filled from: [n_seq + 1] offsets (those of sequence b end at [b + 1]) and a sequence's numbers.  Sums that
 // junk makes longer than 32 bits stop at INT32_MAX.
@@ -48,8 +45,8 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t x) {      // of the lanes
   x = plus(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));      // row_bcast 15, 31
   return plus(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
 }
-// Over N numbers a thread, of which its wave's j-th are behind its (j - 1)-th: what is in front of each, and all of the workgroup's.  part: [kWaves].
-template <int N> __device__ __forceinline__ uint32_t scan(const uint32_t (&x)[N], uint32_t (&before)[N], uint32_t* part) {
+// Over N numbers a thread, of which its wave's j-th are behind its (j - 1)-th: what is in front of each, and all of the workgroup's.  part: [WAVES].
+template <int WAVES, int N> __device__ __forceinline__ uint32_t scan(const uint32_t (&x)[N], uint32_t (&before)[N], uint32_t* part) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t sum = 0;
 #pragma unroll
@@ -60,21 +57,22 @@ template <int N> __device__ __forceinline__ uint32_t scan(const uint32_t (&x)[N]
   }
   if (lane == 0) part[wave] = sum;
   __syncthreads();
-  const uint32_t sums = wave_sums(lane < kWaves ? part[lane] : 0);
+  const uint32_t sums = wave_sums(lane < WAVES ? part[lane] : 0);
   const uint32_t front = wave > 0 ? paged::lane_value(sums, wave - 1) : 0;
 #pragma unroll
   for (int j = 0; j < N; ++j) before[j] = plus(front, before[j]);
-  return paged::lane_value(sums, kWaves - 1);
+  return paged::lane_value(sums, WAVES - 1);
 }
 
-// The sequences' lengths and offsets, by a workgroup, EACH of them a thread at a time.  writes: whether it is the one that leaves the call's lengths.
+// The sequences' lengths and offsets, by a workgroup of THREADS, EACH of them a thread at a time.  writes: whether it is the one that leaves the call's lengths.
 // (A thread's sequences one behind the other, loads and LDS stores 16 bytes apart: 4000 of them 11.3 us for 9.3.)
-template <int EACH> __device__ __forceinline__ Queue plan_offsets(const PlanArgs& a, const Offsets& o, bool writes) {
+template <int THREADS, int EACH> __device__ __forceinline__ Queue plan_offsets(const PlanArgs& a, const Offsets& o, bool writes) {
+  constexpr int kWaves = THREADS / 64;
   __shared__ uint32_t part[3][kWaves];
   const int tid = threadIdx.x;
   const int at_in = a.ring_at_in[0], count_in = a.ring_at_in[1];
   uint32_t rows = 0, gives = 0, takes = 0;
-  for (int r0 = 0; r0 < a.n_seq; r0 += kThreads * EACH) {
+  for (int r0 = 0; r0 < a.n_seq; r0 += THREADS * EACH) {
     const int b0 = r0 + (tid >> 6) * 64 * EACH + (tid & 63);      // the thread's sequences are 64 apart
     int start[EACH], had[EACH], grow[EACH], need[EACH];
     uint32_t fresh[EACH], before[EACH], x[EACH], y[EACH];
@@ -88,7 +86,7 @@ template <int EACH> __device__ __forceinline__ Queue plan_offsets(const PlanArgs
     }
 #pragma unroll
     for (int j = 0; j < EACH; ++j) fresh[j] = b0 + j * 64 < a.n_seq ? fresh[j] : 0;
-    const uint32_t all = scan<EACH>(fresh, before, part[0]);
+    const uint32_t all = scan<kWaves, EACH>(fresh, before, part[0]);
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
       const uint32_t at = plus(rows, before[j]);
@@ -103,7 +101,7 @@ template <int EACH> __device__ __forceinline__ Queue plan_offsets(const PlanArgs
     }
     rows = plus(rows, all);
     uint32_t give[EACH], take[EACH];
-    const uint32_t all_give = scan<EACH>(x, give, part[1]), all_take = scan<EACH>(y, take, part[2]);
+    const uint32_t all_give = scan<kWaves, EACH>(x, give, part[1]), all_take = scan<kWaves, EACH>(y, take, part[2]);
 #pragma unroll
     for (int j = 0; j < EACH; ++j) {
       const int b = b0 + j * 64;
@@ -132,7 +130,7 @@ template <int EACH> __device__ __forceinline__ Queue plan_offsets(const PlanArgs
     a.lack[0] = (int)takes - taken;
   }
   __syncthreads();
-  for (int b = tid; writes && b < a.n_seq; b += kThreads) {
+  for (int b = tid; writes && b < a.n_seq; b += THREADS) {
     const Of x = o.of[b];
     a.held[b] = x.need > x.had ? x.had + (int)min((uint32_t)x.take + (uint32_t)(x.need - x.had), (uint32_t)free) - min(x.take, free) : x.need;
   }
@@ -198,12 +196,12 @@ __device__ __forceinline__ void fill(const PlanArgs& a, const Offsets& o, const 
 __device__ __forceinline__ int64_t items_of(const PlanArgs& a, const Offsets& o, const Queue& q) { return (int64_t)a.n_tok + q.given + o.take[a.n_seq]; }
 
 // One launch: every workgroup finds the offsets for itself and keeps them in LDS, the first one writes the lengths, which no other may be reading.
-template <int EACH> __global__ __launch_bounds__(kThreads) void plan_whole(PlanArgs a) {
+template <int THREADS, int EACH> __global__ __launch_bounds__(THREADS) void plan_whole(PlanArgs a) {
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const Offsets o = offsets_at(lds, a.n_seq);
-  const Queue q = plan_offsets<EACH>(a, o, blockIdx.x == 0);
+  const Queue q = plan_offsets<THREADS, EACH>(a, o, blockIdx.x == 0);
   const int64_t n = items_of(a, o, q);
-  for (int64_t i = blockIdx.x * kThreads + threadIdx.x; i < n; i += gridDim.x * kThreads) fill(a, o, q, i);
+  for (int64_t i = blockIdx.x * THREADS + threadIdx.x; i < n; i += gridDim.x * THREADS) fill(a, o, q, i);
 }
 
 // The lengths that a launch has left aside go to their places: [n_seq] starts, [n_seq] numbers of pages, the ring's two.
@@ -214,8 +212,9 @@ __global__ __launch_bounds__(256) void plan_settle(PlanArgs a, const int32_t* as
 }
 
 // More sequences than LDS has room for: two launches, the offsets in the workspace.
+constexpr int kThreads = 1024;
 __global__ __launch_bounds__(kThreads) void plan_lengths(PlanArgs a) {
-  const Queue q = plan_offsets<4>(a, offsets_at(a.ws, a.n_seq), true);
+  const Queue q = plan_offsets<kThreads, 4>(a, offsets_at(a.ws, a.n_seq), true);
   if (threadIdx.x == 0) *(Queue*)a.ws = q;
 }
 __global__ __launch_bounds__(kThreads) void plan_fill(PlanArgs a) {
@@ -226,9 +225,14 @@ __global__ __launch_bounds__(kThreads) void plan_fill(PlanArgs a) {
 }
 
 constexpr int kLdsSeqs = 4096;          // sequences whose offsets a workgroup keeps in LDS
-// Rows and entries of the table up to which one workgroup does all (how many pages move is not known on the host): sixteen sequences of up to 1025
-// pages 3.9 us; with more, 200 sequences of which 12000 pages move took one workgroup 15.8 us and take 32 of them 5.6.
-constexpr int64_t kAlone = 32768;
+
+// A launch of `threads` for every row, but for 2^15 at least, as pages are many more than rows at times, and 2^18 at most; or of one workgroup.
+template <int THREADS, int EACH> int launch_whole(const PlanArgs& a, bool alone, hipStream_t st) {
+  const int64_t blocks = ((int64_t)a.n_tok + THREADS - 1) / THREADS, fewest = (1 << 15) / THREADS, most = (1 << 18) / THREADS;
+  plan_whole<THREADS, EACH><<<dim3((unsigned)(alone ? 1 : blocks < fewest ? fewest : blocks > most ? most : blocks)), THREADS, offsets_bytes(a.n_seq), st>>>(a);
+  ESA_LAUNCH_CHECK("plan_whole");
+  return ESA_OK;
+}
 
 }  // namespace
 
@@ -236,34 +240,31 @@ size_t plan_workspace(int n_seq) { return align_up(offsets_bytes(n_seq), 256); }
 
 int launch_plan(const PlanArgs& a, hipStream_t st) {
   static OncePerDevice raised;
-  const bool in_place = a.start == a.start_in || a.held == a.held_in || a.ring_at == a.ring_at_in;
-  const bool alone = a.n_seq <= kThreads && (int64_t)a.n_seq * a.max_pages + a.n_tok <= kAlone;
-  const int64_t most = ((int64_t)a.n_tok + kThreads - 1) / kThreads;
-  const unsigned blocks = (unsigned)(most < 32 ? 32 : most > 256 ? 256 : most);
   if (a.n_seq > kLdsSeqs) {
     plan_lengths<<<dim3(1), kThreads, 0, st>>>(a);
     ESA_LAUNCH_CHECK("plan_lengths");
-    plan_fill<<<dim3(blocks), kThreads, 0, st>>>(a);
+    plan_fill<<<dim3(256), kThreads, 0, st>>>(a);
     ESA_LAUNCH_CHECK("plan_fill");
     return ESA_OK;
   }
-  const int rc = raise_lds_limit(raised, {(const void*)plan_whole<4>}, offsets_bytes(kLdsSeqs), "plan_whole");
-  if (rc != ESA_OK) return rc;
+  // In place one workgroup does all where rows and entries of the table are few (how many pages move is not known on the host): sixteen sequences of
+  // up to 1025 pages 3.3 us, as many workgroups take without being in place; of 1875 pages, with some sequences ended, 5.5 for 4.1 and a settling launch.
+  const bool in_place = a.start == a.start_in || a.held == a.held_in || a.ring_at == a.ring_at_in;
+  const bool alone = in_place && a.n_seq <= 256 && (int64_t)a.n_seq * a.max_pages <= 32768 && a.n_tok <= 2048;
+  const bool aside = in_place && !alone;
   PlanArgs w = a;
-  if (in_place && !alone) {
+  if (aside) {
     w.start = (int32_t*)a.ws;
     w.held = w.start + a.n_seq;
     w.ring_at = w.held + a.n_seq;
   }
-  if (a.n_seq <= kThreads)
-    plan_whole<1><<<dim3(alone ? 1 : blocks), kThreads, offsets_bytes(a.n_seq), st>>>(w);
-  else
-    plan_whole<4><<<dim3(blocks), kThreads, offsets_bytes(a.n_seq), st>>>(w);
-  ESA_LAUNCH_CHECK("plan_whole");
-  if (in_place && !alone) {
-    plan_settle<<<dim3((2 * a.n_seq + 2 + 255) / 256), 256, 0, st>>>(a, (const int32_t*)a.ws);
-    ESA_LAUNCH_CHECK("plan_settle");
-  }
+  int rc = raise_lds_limit(raised, {(const void*)plan_whole<1024, 4>}, offsets_bytes(kLdsSeqs), "plan_whole");
+  // About as many threads as there are sequences: with 1024 of them sixteen sequences took 4.0 us, 200 5.7, 32 prompts 5.2 for 4.4; with 256, each for
+  // sixteen sequences in turn, 4000 took 15.1 us for 9.2; 600 by 1024, 512 or 256 threads 6.07, 5.87, 6.12; 1500 by two or four a thread 7.2 and 8.4.
+  if (rc == ESA_OK) rc = a.n_seq <= 256 ? launch_whole<256, 1>(w, alone, st) : a.n_seq <= 1024 ? launch_whole<512, 2>(w, false, st) : a.n_seq <= 2048 ? launch_whole<1024, 2>(w, false, st) : launch_whole<1024, 4>(w, false, st);
+  if (rc != ESA_OK || !aside) return rc;
+  plan_settle<<<dim3((2 * a.n_seq + 2 + 255) / 256), 256, 0, st>>>(a, (const int32_t*)a.ws);
+  ESA_LAUNCH_CHECK("plan_settle");
   return ESA_OK;
 }
 
