@@ -7,7 +7,8 @@
 // It is a copy with arithmetic, and runs as one: 19787 tokens of 32 and 8 heads of 128 bf16 elements 76 us, 406 MB at 5.3 TB/s, where a copy moves 5.4.
 // A workgroup takes a token (or a few) with all its heads, which share the sines and cosines by way of LDS; a thread turns one piece of 16 bytes of
 // either half, requested in front of the sines.  Four heads to a thread, as many fewer waves, were slower below 16 thousand tokens (1024: 7.3 us
-// for 5.8, sixteen 4.6 for 3.1 in a graph); pieces of 8 bytes are quicker for sixteen tokens (2.8) and slower from 500 on (1024: 7.2, 16384: 100 for 64).
+// for 5.8, sixteen 4.6 for 3.1 in a graph); pieces of 8 bytes are
+// quicker for sixteen tokens (2.8), the same for 250, and slower from 500 on (1024: 7.2, 16384: 100 for 64).
 #include <type_traits>
 
 #include "serve.h"
@@ -218,6 +219,8 @@ template <typename T, int N> int launch_of(const RopeArgs& a, hipStream_t st) {
   return ESA_OK;
 }
 
+constexpr int64_t kFewPieces = 65536;      // (of 16 bytes, two to a thread)
+
 }  // namespace
 
 int launch_rope_at(const RopeArgs& a, int dtype, hipStream_t st) {
@@ -228,7 +231,9 @@ int launch_rope_at(const RopeArgs& a, int dtype, hipStream_t st) {
     if (s.heads == 0) continue;
     all |= (int64_t)(uintptr_t)s.x | (int64_t)(uintptr_t)s.out | s.x_tok | s.x_head | s.out_tok | s.out_head;
   }
-  const int piece = all % 16 == 0 ? 16 : all % 8 == 0 ? 8 : es;
+  int piece = all % 16 == 0 ? 16 : all % 8 == 0 ? 8 : es;
+  // Few rows leave compute units without work: half the instructions to a thread are quicker there.
+  if (piece == 16 && (int64_t)a.n_tok * a.heads * (2 * a.half + a.rest) * es < 32 * kFewPieces) piece = 8;
   if (dtype == ESA_F32) return piece == 16 ? launch_of<float, 4>(a, st) : piece == 8 ? launch_of<float, 2>(a, st) : launch_of<float, 1>(a, st);
   return piece == 16 ? launch_of<bf16_t, 8>(a, st) : piece == 8 ? launch_of<bf16_t, 4>(a, st) : launch_of<bf16_t, 1>(a, st);
 }

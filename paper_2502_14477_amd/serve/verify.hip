@@ -348,13 +348,14 @@ template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_
 }
 
 // A short row is one workgroup's: a launch does all, M pieces a thread.  Its instructions are then one compute unit's, so that longer rows are quicker in
-// two launches: us a call in a graph, 1 / 16 / 128 / 512 sequences of four drafts, fp32, one launch and two: 8000 tokens 3.8 / 4.5 / 4.9 / 7.0
-// and 6.4 / 7.6 / 8.1 / 12.0 (eight numbers a thread), 16000 5.7 / 5.9 / 6.2 / 13.6 and 6.7 / 7.1 / 8.0 / 15.4 (sixteen), 32000 9.4 / 10.1 /
-// 10.6 / 25.7 and 6.1 / 7.2 / 10.2 / 22.0.
-constexpr int kWholeThreads = 1024;
-constexpr int kWholeWaves = kWholeThreads / 64;
-template <typename T, int N, int M> __global__ __launch_bounds__(kWholeThreads) void verify_whole(VerifyArgs a) {
-  constexpr int kSums = M * kWholeWaves, kLane = (kSums + 63) / 64;      // sums of a wave's pieces in the tokens' order, and how many a lane takes
+// two launches.  us a call in a graph, 1 / 16 / 128 / 512 sequences of four drafts, fp32, in one launch and in two:
+//    2000 tokens  3.3 / 3.6 / 3.8 / 4.3 (256 threads; 1024: 4.2 / 4.5 / 4.8 / 6.8)    6.6 / 7.3 / 8.0 / 9.5
+//    8000         3.7 / 4.5 / 4.8 / 6.8 (1024)                                         6.4 / 7.6 / 8.1 / 12.0
+//   16000         5.7 / 5.9 / 6.2 / 13.6 (1024, sixteen numbers each)                  6.7 / 7.1 / 8.0 / 15.4
+//   32000         9.4 / 10.1 / 10.6 / 25.7 (1024, 32 each)                             6.1 / 7.2 / 10.2 / 22.0
+template <typename T, int N, int M, int THREADS> __global__ __launch_bounds__(THREADS) void verify_whole(VerifyArgs a) {
+  constexpr int kWaves = THREADS / 64;
+  constexpr int kSums = M * kWaves, kLane = (kSums + 63) / 64;      // sums of a wave's pieces in the tokens' order, and how many a lane takes
   __shared__ double sums[kLane * 64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = paged::block_index();
   if (b >= a.n_seq) return;
@@ -367,7 +368,7 @@ template <typename T, int N, int M> __global__ __launch_bounds__(kWholeThreads) 
   const int kept = st.kept;
   Drawn d = drawn_of(a, s, st);
   const float u = a.u[s.row0];
-  for (int i = tid; i < s.n; i += kWholeThreads)
+  for (int i = tid; i < s.n; i += THREADS)
     if (i != kept) a.out[s.row0 + i] = i < kept ? a.tokens[s.row0 + i + 1] : -1;
   if (tid == 0) a.count[b] = kept + 1;
   if (kSums < kLane * 64 && tid >= kSums && tid < kLane * 64) sums[tid] = 0.0;
@@ -375,13 +376,13 @@ template <typename T, int N, int M> __global__ __launch_bounds__(kWholeThreads) 
   double mine[kLane], upto[kLane], total;
   for (;;) {
     Piece<T, N> p[M], q[M];
-    load_pieces<T, N, M>(a, d, tid * N, kWholeThreads * N, p, q);
+    load_pieces<T, N, M>(a, d, tid * N, THREADS * N, p, q);
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       double w = 0.0;
-      piece_weights<T, N>(d, tid * N + m * (kWholeThreads * N), end, p[m], q[m], [&](int, int, double x) { w += x; });
+      piece_weights<T, N>(d, tid * N + m * (THREADS * N), end, p[m], q[m], [&](int, int, double x) { w += x; });
       w = wave_sum(w);
-      if (lane == 0) sums[m * kWholeWaves + wave] = w;
+      if (lane == 0) sums[m * kWaves + wave] = w;
       __builtin_amdgcn_sched_barrier(0);      // (all pieces' numbers in 64 bits at once do not fit the registers)
     }
     __syncthreads();
@@ -414,21 +415,23 @@ template <typename T, int N, int M> __global__ __launch_bounds__(kWholeThreads) 
       base = l > 0 ? lane_double(upto[e], l - 1) : e > 0 ? lane_double(upto[e > 0 ? e - 1 : 0], 63) : 0.0;
     }
   }
-  if (wave != at % kWholeWaves) return;
-  const int token = token_in<T, N>(a, d, tid * N + at / kWholeWaves * (kWholeThreads * N), base, target);
+  if (wave != at % kWaves) return;
+  const int token = token_in<T, N>(a, d, tid * N + at / kWaves * (THREADS * N), base, target);
   if (lane == 0) a.out[d.row] = token;
 }
 
-template <typename T, int N, int M> int launch_whole(const VerifyArgs& a, hipStream_t st) {
-  verify_whole<T, N, M><<<paged::grid_for(a.n_seq), kWholeThreads, 0, st>>>(a);
+template <typename T, int N, int M, int THREADS> int launch_whole(const VerifyArgs& a, hipStream_t st) {
+  verify_whole<T, N, M, THREADS><<<paged::grid_for(a.n_seq), THREADS, 0, st>>>(a);
   ESA_LAUNCH_CHECK("verify_whole");
   return ESA_OK;
 }
 template <typename T> int launch_of(const VerifyArgs& a, hipStream_t st) {
   constexpr int N = kPiece<T>;
-  if (a.vocab < N) return launch_whole<T, 1, 1>(a, st);
-  if (a.vocab <= 8 * kWholeThreads) return launch_whole<T, N, 8 / N>(a, st);
-  if (a.vocab <= 16 * kWholeThreads) return launch_whole<T, N, 16 / N>(a, st);
+  if (a.vocab < N) return launch_whole<T, 1, 1, 64>(a, st);
+  if (a.vocab <= 2048) return launch_whole<T, N, 8 / N, 256>(a, st);
+  if (a.vocab <= 4096) return launch_whole<T, N, 8 / N, 512>(a, st);
+  if (a.vocab <= 8192) return launch_whole<T, N, 8 / N, 1024>(a, st);
+  if (a.vocab <= 16384) return launch_whole<T, N, 16 / N, 1024>(a, st);
   verify_sums<T, N><<<dim3((unsigned)chunks_of(a.vocab), (unsigned)(a.n_seq < 65535 ? a.n_seq : 65535)), kThreads, 0, st>>>(a);
   ESA_LAUNCH_CHECK("verify_sums");
   verify_draw<T, N><<<paged::grid_for(a.n_seq), kThreads, 0, st>>>(a);
