@@ -161,6 +161,31 @@ def test_rope_at_far_tokens(esa):
     assert torch.equal(esa.esa_rope_at(x, ints(pos), freq, out_q=x), want)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_rope_at_in_one_buffer(esa, dtype):
+    """Queries and keys of one projection turned where they lie: the values beside them stay; a row that all tokens share."""
+    g = torch.Generator("cuda").manual_seed(6)
+    x = torch.randn((50, 12, 64), generator=g, device="cuda").to(TYPES[dtype])
+    before, pos, freq = x.clone(), torch.arange(50, dtype=torch.int32, device="cuda") * 7, esa.esa_rope_frequencies(1e4, 32)
+    want = esa.esa_rope_at(before[:, :8], pos, freq, k=before[:, 8:10])
+    esa.esa_rope_at(x[:, :8], pos, freq, k=x[:, 8:10], out_q=x[:, :8], out_k=x[:, 8:10])
+    assert torch.equal(x[:, :8], want[0]) and torch.equal(x[:, 8:10], want[1]) and torch.equal(x[:, 10:], before[:, 10:])
+    shared = before[:1].expand(50, 12, 64)
+    assert torch.equal(esa.esa_rope_at(shared, pos, freq), esa.esa_rope_at(shared.contiguous(), pos, freq))
+
+
+def test_rope_at_many_tokens(esa):
+    """More workgroups than one dimension of a grid takes."""
+    n, h, d = 18_000_000, 64, 8
+    x = torch.ones((n, h, d), dtype=torch.bfloat16, device="cuda")
+    pos = torch.arange(n, dtype=torch.int32, device="cuda") % 1000
+    freq = esa.esa_rope_frequencies(1e4, d)
+    esa.esa_rope_at(x, pos, freq, out_q=x)
+    want = esa.esa_rope_at(torch.ones((1000, 1, d), dtype=torch.bfloat16, device="cuda"), pos[:1000], freq)
+    for at in range(0, n, 1_000_000):
+        assert torch.all(x[at:at + 1_000_000].view(1000, 1000, h, d) == want)
+
+
 # ---------------------------------------------------------------- plans
 class Guarded:
     """Arrays with numbers around them that nobody may change."""
