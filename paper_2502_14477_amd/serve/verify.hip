@@ -7,7 +7,7 @@
 //
 // What bounds it is latency (a draft's test is four dependent loads: offsets, token, probabilities, row) and, where sequences are many, HBM.  Rows of
 // up to 16384 tokens are one workgroup's, in one launch (3.8-6.4 us).  Longer ones are cut into chunks of 4096 numbers, a workgroup to each, which finds
-// its sequence's last standing row by itself and leaves the sums of blocks of 64 pieces of 16 bytes; a second launch finds the block in which the
+// its sequence's last standing row by itself and leaves its waves' sums; a second launch finds the block in which the
 // sums pass the drawn number, and in it the token.  Rows are read in pieces of 16 bytes wherever they begin.  In a graph: one sequence of 32000
 // tokens and four drafts 6.7 us, sixteen of 131072 7.7, 128 22.1 (103 MB: the first launch reads 5.5 TB/s).  With loads behind bounds checks and the token
 // found by LDS atomics these were 55, 83 and 117.
@@ -22,13 +22,14 @@ constexpr int kWaves = kThreads / 64;
 constexpr int kEach = 16;                     // numbers of a chunk a thread
 constexpr int kChunk = kThreads * kEach;
 
-// Negative numbers, NaN (the maximum's other operand is taken) and infinities count as 0.
-template <typename T> __device__ __forceinline__ float probability(T v);
-template <> __device__ __forceinline__ float probability<float>(float v) {
-  v = fmaxf(v, 0.f);
-  return v < __builtin_huge_valf() ? v : 0.f;
+template <typename T> __device__ __forceinline__ float number(T v);
+template <> __device__ __forceinline__ float number<float>(float v) { return v; }
+template <> __device__ __forceinline__ float number<bf16_t>(bf16_t v) { return bf16_to_f32(v); }
+// Negative numbers, infinities and NaN count as 0: by their bits, one comparison.
+template <typename T> __device__ __forceinline__ float probability(T v) {
+  const float x = number<T>(v);
+  return __float_as_uint(x) < 0x7F800000u ? x : 0.f;
 }
-template <> __device__ __forceinline__ float probability<bf16_t>(bf16_t v) { return probability<float>(bf16_to_f32(v)); }
 
 // N numbers of a row, wherever it begins.
 template <typename T, int N> struct Piece {
@@ -84,46 +85,57 @@ __device__ __forceinline__ Drawn drawn_of(const VerifyArgs& a, const Rows& s, co
   return Drawn{s.row0 + x.kept, x.kept == s.n - 1 ? 0 : a.draft ? 1 : 2, x.token};
 }
 
-// The weights of N tokens from `want` on, of which a piece of the row and the draft's are at hand: take(number, token, weight).  A piece that would
-// reach over a row's end is the row's last N numbers, of which those in front of `want` do not count (the vocabulary has N or more).  All lanes
-// of the wave take part.
-template <typename T, int N, typename F>
-__device__ __forceinline__ void piece_weights(const Drawn& d, int64_t want, int64_t end, Piece<T, N> p, Piece<T, N> q, F&& take) {
-  const int at = (int)min(want, end), skip = (int)(want - min(want, end));      // (fewer than 2^31: a chunk's first token is within the row)
-  if (__any(skip > 0)) {
+// A piece of a row, and of the draft's: the N numbers from a token on, or, where these would reach over the row's end, the row's last N, of which `skip`
+// belong to the piece in front or to nobody (the vocabulary has N or more).
+template <typename T, int N> struct Pieces {
+  Piece<T, N> p, q;
+  int at, skip;
+};
+// M of them, `step` tokens apart from `first` on, all requested in front of their first use.  WITHIN: none reaches over the row's end.
+template <typename T, int N, int M, bool WITHIN>
+__device__ __forceinline__ void request(const VerifyArgs& a, const Drawn& d, int64_t first, int step, Pieces<T, N> (&x)[M]) {
+  const T* pr = (const T*)(a.target + (int64_t)d.row * a.ldt);
+  const T* qr = (const T*)(a.draft + (int64_t)(d.row + 1) * a.ldd);
+  const int64_t end = (int64_t)a.vocab - N;
 #pragma unroll
-    for (int j = 0; j < N; ++j) p.x[j] = j < skip ? (T)0 : p.x[j];
+  for (int m = 0; m < M; ++m) {
+    const int64_t want = first + m * step, at = WITHIN ? want : min(want, end);
+    x[m].at = (int)at;
+    x[m].skip = WITHIN ? 0 : (int)(want - at);
+    x[m].p = load<T, N>(pr + at);
   }
+  if (d.mode == 1) {
+#pragma unroll
+    for (int m = 0; m < M; ++m) x[m].q = load<T, N>(qr + (WITHIN ? first + m * step : (int64_t)x[m].at));
+  }
+}
+// Its weights: take(number, token, weight).  All lanes of the wave take part.  STRICT: as they are defined.  Otherwise, two instructions a number fewer, an
+// infinite probability of the target has an infinite weight; what is negative or NaN is left by the maximum with the draft's.
+template <bool STRICT, typename T, int N, typename F>
+__device__ __forceinline__ void weigh(const Drawn& d, Pieces<T, N> x, F&& take) {
+  if (__any(x.skip > 0)) {
+#pragma unroll
+    for (int j = 0; j < N; ++j) x.p.x[j] = j < x.skip ? (T)0 : x.p.x[j];
+  }
+  auto of = [](T v) { return STRICT ? probability<T>(v) : number<T>(v); };
   // the token that was looked up, with a probability of 1, is in few waves
-  const int without = (int)((uint32_t)d.token - (uint32_t)at);
+  const int without = (int)((uint32_t)d.token - (uint32_t)x.at);
   if (d.mode == 1 || (d.mode == 2 && __any((uint32_t)without < (uint32_t)N))) {
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const float y = d.mode == 1 ? probability<T>(q.x[j]) : j == without ? 1.f : 0.f;
-      take(j, at + j, fmax((double)probability<T>(p.x[j]) - (double)y, 0.0));
+      const float q = d.mode == 1 ? probability<T>(x.q.x[j]) : j == without ? 1.f : 0.f;
+      take(j, x.at + j, (double)fmaxf(of(x.p.x[j]), q) - (double)q);
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < N; ++j) take(j, at + j, (double)probability<T>(p.x[j]));
-  }
-}
-// M of them, `step` tokens apart from `first` on, all requested in front of their first use.
-template <typename T, int N, int M>
-__device__ __forceinline__ void load_pieces(const VerifyArgs& a, const Drawn& d, int64_t first, int step, Piece<T, N> (&p)[M], Piece<T, N> (&q)[M]) {
-  const int64_t end = (int64_t)a.vocab - N;
-  const T* pr = (const T*)(a.target + (int64_t)d.row * a.ldt);
-#pragma unroll
-  for (int m = 0; m < M; ++m) p[m] = load<T, N>(pr + min(first + m * step, end));
-  if (d.mode == 1) {
-    const T* qr = (const T*)(a.draft + (int64_t)(d.row + 1) * a.ldd);
-#pragma unroll
-    for (int m = 0; m < M; ++m) q[m] = load<T, N>(qr + min(first + m * step, end));
+    for (int j = 0; j < N; ++j) take(j, x.at + j, (double)fmaxf(of(x.p.x[j]), 0.f));
   }
 }
 
-// A row's sums are kept by blocks of 64 pieces, a wave's at a time.
+// A row's sums are kept by blocks, a wave's part of a chunk each.
+constexpr int kBlock = 64 * kEach;
 __host__ __device__ inline int chunks_of(int vocab) { return (int)(((int64_t)vocab + kChunk - 1) / kChunk); }
-template <int N> __host__ __device__ inline int blocks_of(int vocab) { return chunks_of(vocab) * (kChunk / (64 * N)); }
+__host__ __device__ inline int blocks_of(int vocab) { return chunks_of(vocab) * kWaves; }
 struct Work {
   double* sums;      // [n_seq][blocks]
   int32_t* kept;     // [n_seq]
@@ -151,32 +163,34 @@ __device__ __forceinline__ double lane_double(double x, int lane) {
   const uint64_t u = __builtin_bit_cast(uint64_t, x);
   return __builtin_bit_cast(double, (uint64_t)paged::lane_value((uint32_t)u, lane) | (uint64_t)paged::lane_value((uint32_t)(u >> 32), lane) << 32);
 }
-__device__ __forceinline__ double wave_sum(double x) { return lane_double(wave_sums(x), 63); }
 
 // A chunk's blocks' sums, by a workgroup.
-template <typename T, int N> __device__ __forceinline__ void chunk_sums(const VerifyArgs& a, const Drawn& d, int chunk, double* sums) {
+template <bool STRICT, bool WITHIN, typename T, int N> __device__ __forceinline__ void chunk_sums(const VerifyArgs& a, const Drawn& d, int chunk, double* sums) {
   constexpr int M = kEach / N;
-  const int64_t first = (int64_t)chunk * kChunk + threadIdx.x * N;
-  Piece<T, N> p[M], q[M];
-  load_pieces<T, N, M>(a, d, first, kThreads * N, p, q);
+  const int block = chunk * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  Pieces<T, N> x[M];
+  request<T, N, M, WITHIN>(a, d, (int64_t)block * kBlock + lane * N, 64 * N, x);
+  double w = 0.0;
 #pragma unroll
-  for (int m = 0; m < M; ++m) {
-    double w = 0.0;
-    piece_weights<T, N>(d, first + m * (kThreads * N), (int64_t)a.vocab - N, p[m], q[m], [&](int, int, double x) { w += x; });
-    w = wave_sums(w);
-    if ((threadIdx.x & 63) == 63) sums[(chunk * M + m) * kWaves + (threadIdx.x >> 6)] = w;
-  }
+  for (int m = 0; m < M; ++m) weigh<STRICT>(d, x[m], [&](int, int, double y) { w += y; });
+  w = wave_sums(w);
+  if (lane == 63) sums[block] = w;
 }
 
 // grid (chunks, sequences)
 template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_sums(VerifyArgs a) {
-  const int chunk = blockIdx.x, blocks = blocks_of<N>(a.vocab);
+  const int chunk = blockIdx.x, blocks = blocks_of(a.vocab);
   const Work k = work_at(a.ws, a.n_seq, blocks);
   for (int b = blockIdx.y; b < a.n_seq; b += gridDim.y) {
     const Rows s = rows_of(a, b);
     if (s.n == 0) continue;
     const Standing x = standing<T>(a, s);
-    chunk_sums<T, N>(a, drawn_of(a, s, x), chunk, k.sums + (int64_t)b * blocks);
+    const Drawn d = drawn_of(a, s, x);
+    double* sums = k.sums + (int64_t)b * blocks;
+    if ((int64_t)(chunk + 1) * kChunk <= a.vocab)
+      chunk_sums<false, true, T, N>(a, d, chunk, sums);
+    else
+      chunk_sums<false, false, T, N>(a, d, chunk, sums);
     if (chunk == 0 && threadIdx.x == 0) k.kept[b] = x.kept;
   }
 }
@@ -201,14 +215,18 @@ __device__ __forceinline__ Scanned scan(double x, double* part) {
   return Scanned{before + (lane ? left : 0.0), all};
 }
 
-// The first item of which a thread says so (the threads' items ascend), and the last one with any weight: INT32_MAX, -1 where there is none.
+// The first item that passes, and the last one with any weight: INT32_MAX, -1 where there is none.  The threads' items ascend.
 struct Found {
   int first, last;
 };
-__device__ __forceinline__ Found find(int first, int last, Found* part) {
+__device__ __forceinline__ Found in_wave(const Found& x) {
+  const uint64_t f = __ballot(x.first != INT32_MAX), l = __ballot(x.last >= 0);
+  return {f ? (int)paged::lane_value((uint32_t)x.first, __ffsll((unsigned long long)f) - 1) : INT32_MAX,
+          l ? (int)paged::lane_value((uint32_t)x.last, 63 - __clzll((long long)l)) : -1};
+}
+__device__ __forceinline__ Found find(const Found& x, Found* part) {
   const int wave = threadIdx.x >> 6;
-  const uint64_t f = __ballot(first != INT32_MAX), l = __ballot(last >= 0);
-  const Found mine = {f ? __shfl(first, __ffsll((unsigned long long)f) - 1) : INT32_MAX, l ? __shfl(last, 63 - __clzll((long long)l)) : -1};
+  const Found mine = in_wave(x);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) part[wave] = mine;
   __syncthreads();
@@ -221,32 +239,18 @@ __device__ __forceinline__ Found find(int first, int last, Found* part) {
   return r;
 }
 
-// The token in a wave's block, of which the lane has N tokens from `want` on, where sums pass the target, `base` being the sum in front of the
-// block; or else the last one with any weight.
-template <typename T, int N> __device__ __forceinline__ int token_in(const VerifyArgs& a, const Drawn& d, int64_t want, double base, double target) {
-  const int lane = threadIdx.x & 63;
-  Piece<T, N> p[1], q[1];
-  load_pieces<T, N, 1>(a, d, want, 0, p, q);
-  double x[N], sum = 0.0;
-  int t[N];
-  piece_weights<T, N>(d, want, (int64_t)a.vocab - N, p[0], q[0], [&](int j, int token, double w) {
-    x[j] = w;
-    t[j] = token;
-    sum += w;
-  });
-  const double front = __shfl_up(wave_sums(sum), 1);
-  sum = base + (lane ? front : 0.0);
-  int first = INT32_MAX, last = -1;
+// The first of a thread's N tokens where sums pass the target, `sum` being what is in front of them, and the last one with any weight.
+template <int N> __device__ __forceinline__ Found look(const double (&w)[N], int at, double sum, double target) {
+  Found r = {INT32_MAX, -1};
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    sum += x[j];
-    if (x[j] > 0.0) {
-      last = t[j];
-      if (sum > target && first == INT32_MAX) first = t[j];
+    sum += w[j];
+    if (w[j] > 0.0) {
+      r.last = at + j;
+      if (sum > target && r.first == INT32_MAX) r.first = r.last;
     }
   }
-  const uint64_t f = __ballot(first != INT32_MAX), l = __ballot(last >= 0);
-  return f ? __shfl(first, __ffsll((unsigned long long)f) - 1) : __shfl(last, 63 - __clzll((long long)l));
+  return r;
 }
 __device__ __forceinline__ double target_of(float u, double total) { return u >= 1.f ? __builtin_huge_val() : u > 0.f ? u * total : 0.0; }
 
@@ -259,12 +263,12 @@ template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_
   __shared__ double at_block;
   const int tid = threadIdx.x, b = paged::block_index();
   if (b >= a.n_seq) return;
-  const int blocks = blocks_of<N>(a.vocab);
+  const int blocks = blocks_of(a.vocab);
   const Work k = work_at(a.ws, a.n_seq, blocks);
   double* const sums = k.sums + (int64_t)b * blocks;
   double x[kBlocks];
   Scanned y;
-  auto request = [&](int r0) {
+  auto fetch = [&](int r0) {
 #pragma unroll
     for (int j = 0; j < kBlocks; ++j) x[j] = sums[min(r0 + tid * kBlocks + j, blocks - 1)];
   };
@@ -277,7 +281,7 @@ template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_
     }
     y = scan(sum, part);
   };
-  request(0);
+  fetch(0);
   const Rows s = rows_of(a, b);
   if (s.n == 0) {
     if (tid == 0) a.count[b] = 0;
@@ -292,18 +296,20 @@ template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_
   double total = 0.0;
   bool at_hand = blocks <= kRound;               // whether the first round's sums are those that are looked through
   for (int r0 = 0; r0 < blocks; r0 += kRound) {
-    if (r0) request(r0);
+    if (r0) fetch(r0);
     add_up(r0);
     total += y.all;
   }
-  if (!(total > 0.0) && d.mode != 0) {
-    // nothing is left: p itself, of which there are no sums yet; one workgroup reads it all
-    d.mode = 0;
+  // An infinity among the target's probabilities, or nothing left and p itself wanted, of which there are no sums: one workgroup reads it all again.
+  for (bool infinite = !(total < __builtin_huge_val()); infinite || (!(total > 0.0) && d.mode != 0); infinite = false) {
+    if (!infinite) d.mode = 0;
     at_hand = false;
-    for (int c = 0; c < chunks_of(a.vocab); ++c) chunk_sums<T, N>(a, d, c, sums);
     __syncthreads();
+    for (int c = 0; c < chunks_of(a.vocab); ++c) chunk_sums<true, false, T, N>(a, d, c, sums);
+    __syncthreads();
+    total = 0.0;
     for (int r0 = 0; r0 < blocks; r0 += kRound) {
-      request(r0);
+      fetch(r0);
       add_up(r0);
       total += y.all;
     }
@@ -318,33 +324,33 @@ template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_
   double base = 0.0;
   for (int r0 = 0; r0 < blocks; r0 += kRound) {
     if (!at_hand) {
-      request(r0);
+      fetch(r0);
       add_up(r0);
     }
-    double before[kBlocks], sum = base + y.before;
-    int first = INT32_MAX, last = -1;
-#pragma unroll
-    for (int j = 0; j < kBlocks; ++j) {
-      before[j] = sum;
-      sum += x[j];
-      if (x[j] > 0.0) {
-        last = r0 + tid * kBlocks + j;
-        if (sum > target && first == INT32_MAX) first = last;
-      }
-    }
-    const Found f = find(first, last, found);
+    const Found f = find(look<kBlocks>(x, r0 + tid * kBlocks, base + y.before, target), found);
     if (f.first != INT32_MAX) block = f.first;
     else if (f.last >= 0) block = f.last;
+    double before = base + y.before;
 #pragma unroll
-    for (int j = 0; j < kBlocks; ++j)
-      if (block == r0 + tid * kBlocks + j) at_block = before[j];
+    for (int j = 0; j < kBlocks; ++j) {
+      if (block == r0 + tid * kBlocks + j) at_block = before;
+      before += x[j];
+    }
     if (f.first != INT32_MAX) break;
     base += y.all;
   }
   __syncthreads();
-  if (tid >= 64) return;
-  const int token = token_in<T, N>(a, d, ((int64_t)block * 64 + tid) * N, at_block, target);
-  if (tid == 0) a.out[d.row] = token;
+  Pieces<T, N> piece[1];
+  const bool mine = tid < kBlock / N;
+  request<T, N, 1, false>(a, d, (int64_t)block * kBlock + (mine ? tid : 0) * N, 0, piece);
+  double w[N], sum = 0.0;
+  weigh<true>(d, piece[0], [&](int j, int, double v) {
+    w[j] = mine ? v : 0.0;
+    sum += w[j];
+  });
+  sum = at_block + scan(sum, part).before;
+  const Found f = find(look<N>(w, piece[0].at, sum, target), found);
+  if (tid == 0) a.out[d.row] = f.first != INT32_MAX ? f.first : f.last;
 }
 
 // A short row is one workgroup's: a launch does all, M pieces a thread.  Its instructions are then one compute unit's, so that longer rows are quicker in
@@ -372,17 +378,19 @@ template <typename T, int N, int M, int THREADS> __global__ __launch_bounds__(TH
     if (i != kept) a.out[s.row0 + i] = i < kept ? a.tokens[s.row0 + i + 1] : -1;
   if (tid == 0) a.count[b] = kept + 1;
   if (kSums < kLane * 64 && tid >= kSums && tid < kLane * 64) sums[tid] = 0.0;
-  const int64_t end = (int64_t)a.vocab - N;
   double mine[kLane], upto[kLane], total;
-  for (;;) {
-    Piece<T, N> p[M], q[M];
-    load_pieces<T, N, M>(a, d, tid * N, THREADS * N, p, q);
+  for (bool strict = false;;) {
+    Pieces<T, N> x[M];
+    request<T, N, M, false>(a, d, tid * N, THREADS * N, x);
 #pragma unroll
     for (int m = 0; m < M; ++m) {
       double w = 0.0;
-      piece_weights<T, N>(d, tid * N + m * (THREADS * N), end, p[m], q[m], [&](int, int, double x) { w += x; });
-      w = wave_sum(w);
-      if (lane == 0) sums[m * kWaves + wave] = w;
+      if (strict)
+        weigh<true>(d, x[m], [&](int, int, double y) { w += y; });
+      else
+        weigh<false>(d, x[m], [&](int, int, double y) { w += y; });
+      w = wave_sums(w);
+      if (lane == 63) sums[m * kWaves + wave] = w;
       __builtin_amdgcn_sched_barrier(0);      // (all pieces' numbers in 64 bits at once do not fit the registers)
     }
     __syncthreads();
@@ -394,8 +402,12 @@ template <typename T, int N, int M, int THREADS> __global__ __launch_bounds__(TH
       upto[e] = total + wave_sums(mine[e]);
       total = lane_double(upto[e], 63);
     }
-    if (total > 0.0 || d.mode == 0) break;
-    d.mode = 0;      // nothing is left: p itself
+    if (!(total < __builtin_huge_val()))
+      strict = true;
+    else if (total > 0.0 || d.mode == 0)
+      break;
+    else
+      d.mode = 0;      // nothing is left: p itself
     __syncthreads();
   }
   if (!(total > 0.0)) {
@@ -416,8 +428,16 @@ template <typename T, int N, int M, int THREADS> __global__ __launch_bounds__(TH
     }
   }
   if (wave != at % kWaves) return;
-  const int token = token_in<T, N>(a, d, tid * N + at / kWaves * (THREADS * N), base, target);
-  if (lane == 0) a.out[d.row] = token;
+  Pieces<T, N> piece[1];
+  request<T, N, 1, false>(a, d, tid * N + at / kWaves * (THREADS * N), 0, piece);
+  double w[N], sum = 0.0;
+  weigh<true>(d, piece[0], [&](int j, int, double v) {
+    w[j] = v;
+    sum += v;
+  });
+  const double front = __shfl_up(wave_sums(sum), 1);
+  const Found f = in_wave(look<N>(w, piece[0].at, base + (lane ? front : 0.0), target));
+  if (lane == 0) a.out[d.row] = f.first != INT32_MAX ? f.first : f.last;
 }
 
 template <typename T, int N, int M, int THREADS> int launch_whole(const VerifyArgs& a, hipStream_t st) {
@@ -442,7 +462,7 @@ template <typename T> int launch_of(const VerifyArgs& a, hipStream_t st) {
 }  // namespace
 
 size_t verify_workspace(int n_seq, int vocab) {
-  return align_up((size_t)n_seq * (blocks_of<4>(vocab) * sizeof(double) + sizeof(int32_t)), 256);      // (fp32: bf16 has half as many blocks)
+  return align_up((size_t)n_seq * (blocks_of(vocab) * sizeof(double) + sizeof(int32_t)), 256);
 }
 
 int launch_verify(const VerifyArgs& a, int dtype, hipStream_t st) { return dtype == ESA_F32 ? launch_of<float>(a, st) : launch_of<bf16_t>(a, st); }
