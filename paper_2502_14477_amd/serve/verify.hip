@@ -6,7 +6,7 @@
 // outcome is that of the definition but for random numbers that lie within 1e-15 of a border.
 //
 // What bounds it is latency (a draft's test is four dependent loads: offsets, token, probabilities, row) and, where sequences are many, HBM.  Rows of
-// up to 16384 tokens are one workgroup's, in one launch (3.8-6.4 us).  Longer ones are cut into chunks of 4096 numbers, a workgroup to each, which finds
+// up to 16384 tokens are one workgroup's, in one launch (3.8-6.4 us).  Longer ones are cut into chunks, a workgroup to each, which finds
 // its sequence's last standing row by itself and leaves its waves' sums; a second launch finds the block in which the
 // sums pass the drawn number, and in it the token.  Rows are read in pieces of 16 bytes wherever they begin.  In a graph: one sequence of 32000
 // tokens and four drafts 6.7 us, sixteen of 131072 7.7, 128 22.1 (103 MB: the first launch reads 5.5 TB/s).  With loads behind bounds checks and the token
@@ -19,8 +19,6 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
-constexpr int kEach = 16;                     // numbers of a chunk a thread
-constexpr int kChunk = kThreads * kEach;
 
 template <typename T> __device__ __forceinline__ float number(T v);
 template <> __device__ __forceinline__ float number<float>(float v) { return v; }
@@ -132,10 +130,11 @@ __device__ __forceinline__ void weigh(const Drawn& d, Pieces<T, N> x, F&& take) 
   }
 }
 
-// A row's sums are kept by blocks, a wave's part of a chunk each.
-constexpr int kBlock = 64 * kEach;
-__host__ __device__ inline int chunks_of(int vocab) { return (int)(((int64_t)vocab + kChunk - 1) / kChunk); }
-__host__ __device__ inline int blocks_of(int vocab) { return chunks_of(vocab) * kWaves; }
+// A row is cut into chunks of EACH numbers a thread; its sums are kept by blocks, a wave's part of a chunk each.
+template <int EACH> constexpr int kBlock = 64 * EACH;
+template <int EACH> constexpr int kChunk = kThreads * EACH;
+template <int EACH> __host__ __device__ inline int chunks_of(int vocab) { return (int)(((int64_t)vocab + kChunk<EACH> - 1) / kChunk<EACH>); }
+template <int EACH> __host__ __device__ inline int blocks_of(int vocab) { return chunks_of<EACH>(vocab) * kWaves; }
 struct Work {
   double* sums;      // [n_seq][blocks]
   int32_t* kept;     // [n_seq]
@@ -165,11 +164,11 @@ __device__ __forceinline__ double lane_double(double x, int lane) {
 }
 
 // A chunk's blocks' sums, by a workgroup.
-template <bool STRICT, bool WITHIN, typename T, int N> __device__ __forceinline__ void chunk_sums(const VerifyArgs& a, const Drawn& d, int chunk, double* sums) {
-  constexpr int M = kEach / N;
+template <bool STRICT, bool WITHIN, int EACH, typename T, int N> __device__ __forceinline__ void chunk_sums(const VerifyArgs& a, const Drawn& d, int chunk, double* sums) {
+  constexpr int M = EACH / N;
   const int block = chunk * kWaves + (threadIdx.x >> 6), lane = threadIdx.x & 63;
   Pieces<T, N> x[M];
-  request<T, N, M, WITHIN>(a, d, (int64_t)block * kBlock + lane * N, 64 * N, x);
+  request<T, N, M, WITHIN>(a, d, (int64_t)block * kBlock<EACH> + lane * N, 64 * N, x);
   double w = 0.0;
 #pragma unroll
   for (int m = 0; m < M; ++m) weigh<STRICT>(d, x[m], [&](int, int, double y) { w += y; });
@@ -178,8 +177,8 @@ template <bool STRICT, bool WITHIN, typename T, int N> __device__ __forceinline_
 }
 
 // grid (chunks, sequences)
-template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_sums(VerifyArgs a) {
-  const int chunk = blockIdx.x, blocks = blocks_of(a.vocab);
+template <typename T, int N, int EACH> __global__ __launch_bounds__(kThreads) void verify_sums(VerifyArgs a) {
+  const int chunk = blockIdx.x, blocks = blocks_of<EACH>(a.vocab);
   const Work k = work_at(a.ws, a.n_seq, blocks);
   for (int b = blockIdx.y; b < a.n_seq; b += gridDim.y) {
     const Rows s = rows_of(a, b);
@@ -187,10 +186,10 @@ template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_
     const Standing x = standing<T>(a, s);
     const Drawn d = drawn_of(a, s, x);
     double* sums = k.sums + (int64_t)b * blocks;
-    if ((int64_t)(chunk + 1) * kChunk <= a.vocab)
-      chunk_sums<false, true, T, N>(a, d, chunk, sums);
+    if ((int64_t)(chunk + 1) * kChunk<EACH> <= a.vocab)
+      chunk_sums<false, true, EACH, T, N>(a, d, chunk, sums);
     else
-      chunk_sums<false, false, T, N>(a, d, chunk, sums);
+      chunk_sums<false, false, EACH, T, N>(a, d, chunk, sums);
     if (chunk == 0 && threadIdx.x == 0) k.kept[b] = x.kept;
   }
 }
@@ -257,13 +256,13 @@ __device__ __forceinline__ double target_of(float u, double total) { return u >=
 // A workgroup a sequence.
 constexpr int kBlocks = 4;      // blocks' sums a thread in a round
 constexpr int kRound = kThreads * kBlocks;
-template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_draw(VerifyArgs a) {
+template <typename T, int N, int EACH> __global__ __launch_bounds__(kThreads) void verify_draw(VerifyArgs a) {
   __shared__ double part[kWaves];
   __shared__ Found found[kWaves];
   __shared__ double at_block;
   const int tid = threadIdx.x, b = paged::block_index();
   if (b >= a.n_seq) return;
-  const int blocks = blocks_of(a.vocab);
+  const int blocks = blocks_of<EACH>(a.vocab);
   const Work k = work_at(a.ws, a.n_seq, blocks);
   double* const sums = k.sums + (int64_t)b * blocks;
   double x[kBlocks];
@@ -305,7 +304,7 @@ template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_
     if (!infinite) d.mode = 0;
     at_hand = false;
     __syncthreads();
-    for (int c = 0; c < chunks_of(a.vocab); ++c) chunk_sums<true, false, T, N>(a, d, c, sums);
+    for (int c = 0; c < chunks_of<EACH>(a.vocab); ++c) chunk_sums<true, false, EACH, T, N>(a, d, c, sums);
     __syncthreads();
     total = 0.0;
     for (int r0 = 0; r0 < blocks; r0 += kRound) {
@@ -341,8 +340,8 @@ template <typename T, int N> __global__ __launch_bounds__(kThreads) void verify_
   }
   __syncthreads();
   Pieces<T, N> piece[1];
-  const bool mine = tid < kBlock / N;
-  request<T, N, 1, false>(a, d, (int64_t)block * kBlock + (mine ? tid : 0) * N, 0, piece);
+  const bool mine = tid < kBlock<EACH> / N;
+  request<T, N, 1, false>(a, d, (int64_t)block * kBlock<EACH> + (mine ? tid : 0) * N, 0, piece);
   double w[N], sum = 0.0;
   weigh<true>(d, piece[0], [&](int j, int, double v) {
     w[j] = mine ? v : 0.0;
@@ -445,6 +444,13 @@ template <typename T, int N, int M, int THREADS> int launch_whole(const VerifyAr
   ESA_LAUNCH_CHECK("verify_whole");
   return ESA_OK;
 }
+template <typename T, int N, int EACH> int launch_two(const VerifyArgs& a, hipStream_t st) {
+  verify_sums<T, N, EACH><<<dim3((unsigned)chunks_of<EACH>(a.vocab), (unsigned)(a.n_seq < 65535 ? a.n_seq : 65535)), kThreads, 0, st>>>(a);
+  ESA_LAUNCH_CHECK("verify_sums");
+  verify_draw<T, N, EACH><<<paged::grid_for(a.n_seq), kThreads, 0, st>>>(a);
+  ESA_LAUNCH_CHECK("verify_draw");
+  return ESA_OK;
+}
 template <typename T> int launch_of(const VerifyArgs& a, hipStream_t st) {
   constexpr int N = kPiece<T>;
   if (a.vocab < N) return launch_whole<T, 1, 1, 64>(a, st);
@@ -452,17 +458,15 @@ template <typename T> int launch_of(const VerifyArgs& a, hipStream_t st) {
   if (a.vocab <= 4096) return launch_whole<T, N, 8 / N, 512>(a, st);
   if (a.vocab <= 8192) return launch_whole<T, N, 8 / N, 1024>(a, st);
   if (a.vocab <= 16384) return launch_whole<T, N, 16 / N, 1024>(a, st);
-  verify_sums<T, N><<<dim3((unsigned)chunks_of(a.vocab), (unsigned)(a.n_seq < 65535 ? a.n_seq : 65535)), kThreads, 0, st>>>(a);
-  ESA_LAUNCH_CHECK("verify_sums");
-  verify_draw<T, N><<<paged::grid_for(a.n_seq), kThreads, 0, st>>>(a);
-  ESA_LAUNCH_CHECK("verify_draw");
-  return ESA_OK;
+  // Sixteen numbers a thread where that makes more than four workgroups a compute unit, else eight: 16 / 32 / 64 / 200 sequences of 131072 tokens 8.5 /
+  // 10.9 / 15.0 / 30.4 us in a graph with sixteen, 7.7 / 10.5 / 15.1 / 33.4 with eight, 9.3 / 12.1 / 16.1 / 31.6 with 32.
+  return (int64_t)chunks_of<16>(a.vocab) * a.n_seq > 1024 ? launch_two<T, N, 16>(a, st) : launch_two<T, N, 8>(a, st);
 }
 
 }  // namespace
 
 size_t verify_workspace(int n_seq, int vocab) {
-  return align_up((size_t)n_seq * (blocks_of(vocab) * sizeof(double) + sizeof(int32_t)), 256);
+  return align_up((size_t)n_seq * (blocks_of<8>(vocab) * sizeof(double) + sizeof(int32_t)), 256);
 }
 
 int launch_verify(const VerifyArgs& a, int dtype, hipStream_t st) { return dtype == ESA_F32 ? launch_of<float>(a, st) : launch_of<bf16_t>(a, st); }

@@ -370,7 +370,7 @@ def check_verify(esa, target, tokens, cu, u, draft, rows=None):
 
 
 VERIFIES = [  # sequences, most drafts, vocabulary
-    (1, 0, 1), (1, 4, 2), (3, 3, 63), (17, 5, 1000), (2, 2, 4096), (5, 4, 4097), (2, 150, 300), (4, 3, 50001), (3, 6, 131072), (40, 1, 777), (3, 2, 16384), (2, 2, 16385), (2, 3, 300007),
+    (1, 0, 1), (1, 4, 2), (3, 3, 63), (17, 5, 1000), (2, 2, 4096), (5, 4, 4097), (2, 150, 300), (4, 3, 50001), (3, 6, 131072), (40, 1, 777), (300, 1, 17001), (3, 2, 16384), (2, 2, 16385), (2, 3, 300007),
     (1, 2, 600001)]
 
 
@@ -401,12 +401,12 @@ def test_verify(esa, shape, drawn, dtype):
         assert len(seen[0]) > 65
 
 
-@pytest.mark.parametrize("vocab", [3, 5000, 50001])
+@pytest.mark.parametrize("vocab", [3, 5000, 17001, 50001])
 def test_verify_counts_what_is_no_probability_as_nothing(esa, vocab):
     rng = np.random.default_rng(31)
     for dtype in ("f32", "bf16"):
         for drawn in (True, False):
-            n = 60
+            n = 1200 if vocab == 17001 else 60
             cu, tokens, u = np.arange(0, n + 1, 4), rng.integers(0, min(vocab, 50), n), rng.random(n).astype(np.float32)
             p, q = (x[:, rng.permutation(vocab)] for x in distributions(rng, n, vocab))
             for x in (p, q):
