@@ -83,6 +83,8 @@ int esa_rope_at(const esa_rope_rows* rows, int n_rows, const int32_t* pos, int64
     copies = copies || r.x != r.out;
   }
   if (n_tok == 0) return ESA_OK;
+  if (n_rows == 2 && (rows[0].out == rows[1].out || rows[0].out == rows[1].x || rows[1].out == rows[0].x))
+    ESA_FAIL(ESA_EINVAL, "%s: an output over the other's rows", name);
   if (!pos || !aligned(pos, 4)) ESA_FAIL(ESA_EINVAL, "%s: null or misaligned positions", name);
   a.pos = pos;
   for (int j = 0; j < rot / 2; ++j) a.freq[j] = freq[j];

@@ -89,8 +89,8 @@ def test_rope_at_refuses():
         assert b"esa_rope_at" in esa.lib.esa_last_error()
     assert esa.lib.esa_rope_at(None, 1, FAKE, 5, 128, 128, (ctypes.c_double * 64)(), 0, 1.0, 0, 1, None) == -1
     assert esa.lib.esa_rope_at(ctypes.byref(rows()), 1, FAKE, 5, 128, 128, None, 0, 1.0, 0, 1, None) == -1
-    two = (esa.RopeRows * 2)(rows(), rows(out_head=64))
-    assert rope_at(r=two, n_rows=2) == -1
+    for second in (rows(x=3 * FAKE, out=4 * FAKE, out_head=64), rows(x=3 * FAKE), rows(x=2 * FAKE, out=4 * FAKE), rows(x=3 * FAKE, out=FAKE)):
+        assert rope_at(r=(esa.RopeRows * 2)(rows(), second), n_rows=2) == -1
 
 
 def test_rope_at_has_nothing_to_do():
