@@ -28,7 +28,7 @@ extern "C" {
                               to [0, 1]: g f_j + (1 - g) f_j / factor */
 
 /*
- * Host arithmetic (no GPU work): writes the rot/2 angles a position into the HOST array freq.
+ * Host arithmetic (no GPU work): writes the rot/2 angles a position into the HOST array freq, which a program copies to the GPU once.
  *   base >= 1, rot even, 2 to 256; factor positive (not used by ESA_SCALE_NONE); length, fast > slow: ESA_SCALE_YARN only
  */
 ESA_API int esa_rope_frequencies(double base, int rot, int scaling, double factor, double length, double fast, double slow, double* freq);
@@ -50,7 +50,7 @@ typedef struct {
  *            must not overlap one another or another's input
  *   pos      [n_tok] int32
  *   d        2 <= rot <= d <= 1024, rot even, at most 256
- *   freq     HOST array of rot/2 finite numbers of magnitude 64 at most, read before the call returns; gain finite
+ *   freq     [rot/2] float64 on the device, of magnitude 64 at most (angles beyond 2^38 lose their meaning, not more); gain finite
  * Angles, sines, cosines and products are fp64, rounded once into `dtype`.  n_tok == 0 is a no-op.  n_tok below 2^31 - 2^16.
  */
 ESA_API int esa_rope_at(const esa_rope_rows* rows, int n_rows, const int32_t* pos, int64_t n_tok, int d, int rot, const double* freq, int pairs,

@@ -134,7 +134,7 @@ def _load() -> ctypes.CDLL:
     L.esa_rope_frequencies.restype = i32
     L.esa_rope_frequencies.argtypes = [f64, i32, i32, f64, f64, f64, f64, ctypes.POINTER(f64)]
     L.esa_rope_at.restype = i32
-    L.esa_rope_at.argtypes = [ctypes.POINTER(RopeRows), i32, vp, i64, i32, i32, ctypes.POINTER(f64), i32, f64, i32, i32, vp]
+    L.esa_rope_at.argtypes = [ctypes.POINTER(RopeRows), i32, vp, i64, i32, i32, vp, i32, f64, i32, i32, vp]
     L.esa_plan_paged_workspace_bytes.restype = sz
     L.esa_plan_paged_workspace_bytes.argtypes = [i32]
     L.esa_plan_paged.restype = i32
@@ -329,16 +329,16 @@ def esa_attend_paged(q: torch.Tensor, cu: torch.Tensor, start: torch.Tensor, pag
 
 
 def esa_rope_frequencies(base: float, rot: int, scaling: int = ESA_SCALE_NONE, factor: float = 1.0, length: float = 0.0, fast: float = 32.0,
-                         slow: float = 1.0) -> torch.Tensor:
-    """Angles a position of the rot/2 pairs, float64 in host memory: base^(-2j/rot), or scaled for contexts `factor` times as long
+                         slow: float = 1.0, device="cuda") -> torch.Tensor:
+    """Angles a position of the rot/2 pairs, float64, made once per model: base^(-2j/rot), or scaled for contexts `factor` times as long
     (ESA_SCALE_YARN: pairs that make more than `fast` turns in `length` tokens stay, those that make less than `slow` are divided)."""
-    return _native.rope_frequencies(base, rot, scaling, factor, length, fast, slow)
+    return _native.rope_frequencies(base, rot, scaling, factor, length, fast, slow).to(device)
 
 
 def esa_rope_at(q: torch.Tensor, pos: torch.Tensor, freq: torch.Tensor, k: Optional[torch.Tensor] = None, pairs: int = ESA_PAIRS_HALVES,
                 gain: float = 1.0, transposed: bool = False, out_q: Optional[torch.Tensor] = None, out_k: Optional[torch.Tensor] = None):
     """Rotary encoding of q [n_tok, h, d], and k [n_tok, h_kv, d] in the same call, at positions pos [n_tok] int32 on the GPU; tokens and heads may
-    lie in any order of strides.  freq: esa_rope_frequencies' or any float64 in host memory; the first 2 * len(freq) elements of a head
+    lie in any order of strides.  freq: esa_rope_frequencies' or any float64 on the GPU; the first 2 * len(freq) elements of a head
     turn, the others are copied.  transposed=True takes gradients of the outputs to gradients of the inputs.  Rows of negative
     position are left as they are, undefined in a new tensor.  `out_q`, `out_k` may be q and k.  Returns q, or (q, k)."""
     return _native.rope_at(q, pos, freq, k, pairs, gain, transposed, out_q, out_k)

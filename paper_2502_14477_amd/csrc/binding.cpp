@@ -804,7 +804,8 @@ ESA_ENTRY(rope_at, 9) {
   const at::Tensor *k = tensor_or_none(a[3]), *oq = tensor_or_none(a[7]), *ok = tensor_or_none(a[8]);
   ESA_ASSERT(q.dim() == 3 && (!k || (k->dim() == 3 && k->size(0) == q.size(0) && k->size(2) == q.size(2) && k->scalar_type() == q.scalar_type() && k->device() == q.device())));
   ESA_ASSERT(k || !ok);
-  ESA_ASSERT(freq.device().is_cpu() && freq.scalar_type() == at::kDouble && freq.dim() == 1 && freq.is_contiguous() && freq.size(0) <= 65536);
+  ESA_ASSERT(freq.dim() == 1 && freq.size(0) <= 65536);
+  list_of(a[2], at::kDouble, q.device(), freq.size(0));
   const at::Tensor& pos = list_of(a[1], at::kInt, q.device(), q.size(0));
   const int dt = dtype_of(q), pairs = int32_of(a[4]), transposed = true_of(a[6]);
   const double gain = float_of(a[5]);

@@ -18,7 +18,7 @@ struct RowSet {
 struct RopeArgs {
   RowSet set[kMaxRowSets];
   const int32_t* pos;
-  double freq[kMaxHalf];      // angle a position
+  const double* freq;         // angle a position
   double gain;
   int n_tok, heads;           // heads: of all sets
   int half;                   // pairs

@@ -58,11 +58,9 @@ int esa_rope_at(const esa_rope_rows* rows, int n_rows, const int32_t* pos, int64
   if (pairs != ESA_PAIRS_HALVES && pairs != ESA_PAIRS_NEIGHBOURS) ESA_FAIL(ESA_EUNSUPPORTED, "%s: pairs %d", name, pairs);
   if (d < 2 || d > 1024 || rot < 2 || rot > d || rot > 2 * serve::kMaxHalf || rot % 2 != 0)
     ESA_FAIL(ESA_EUNSUPPORTED, "%s: %d of %d elements of a head (even, at most %d, heads of 1024 at most)", name, rot, d, 2 * serve::kMaxHalf);
-  if (!rows || n_rows < 1 || n_rows > serve::kMaxRowSets || n_tok < 0 || n_tok > kMost || !freq)
-    ESA_FAIL(ESA_EINVAL, "%s: bad argument (n_rows=%d n_tok=%lld), or a null one", name, n_rows, (long long)n_tok);
+  if (!rows || n_rows < 1 || n_rows > serve::kMaxRowSets || n_tok < 0 || n_tok > kMost)
+    ESA_FAIL(ESA_EINVAL, "%s: bad argument (n_rows=%d n_tok=%lld), or no rows", name, n_rows, (long long)n_tok);
   if (!std::isfinite(gain)) ESA_FAIL(ESA_EINVAL, "%s: a gain of %g", name, gain);
-  for (int j = 0; j < rot / 2; ++j)
-    if (!(std::fabs(freq[j]) <= 64.0)) ESA_FAIL(ESA_EINVAL, "%s: an angle of %g a position (64 at most)", name, freq[j]);
   const int64_t es = dtype == ESA_F32 ? 4 : 2;
   serve::RopeArgs a = {};
   bool copies = false;
@@ -85,9 +83,9 @@ int esa_rope_at(const esa_rope_rows* rows, int n_rows, const int32_t* pos, int64
   if (n_tok == 0) return ESA_OK;
   if (n_rows == 2 && (rows[0].out == rows[1].out || rows[0].out == rows[1].x || rows[1].out == rows[0].x))
     ESA_FAIL(ESA_EINVAL, "%s: an output over the other's rows", name);
-  if (!pos || !aligned(pos, 4)) ESA_FAIL(ESA_EINVAL, "%s: null or misaligned positions", name);
+  if (!pos || !aligned(pos, 4) || !freq || !aligned(freq, 8)) ESA_FAIL(ESA_EINVAL, "%s: null or misaligned positions or frequencies", name);
   a.pos = pos;
-  for (int j = 0; j < rot / 2; ++j) a.freq[j] = freq[j];
+  a.freq = freq;
   a.gain = gain;
   a.n_tok = (int)n_tok;
   a.half = rot / 2;

@@ -86,7 +86,7 @@ def test_rope_at(esa, shape, kind, halves, dtype):
         got = esa.esa_rope_at(q, ints(pos), freq, k=k, pairs=pairs, gain=gain, transposed=transposed, out_q=oq, out_k=ok)
         assert got[0] is oq and got[1] is ok
         for x, y in ((q, oq), (k, ok)):
-            check_rope(x, y, pos, freq.numpy(), halves, gain, transposed, dtype)
+            check_rope(x, y, pos, freq.cpu().numpy(), halves, gain, transposed, dtype)
             assert torch.all(y[torch.from_numpy(pos < 0).cuda()] == -7.0)        # rows of nobody
     alone = esa.esa_rope_at(q, ints(pos), freq, pairs=pairs, transposed=True)    # one tensor, into a new one
     assert torch.equal(alone[torch.from_numpy(pos >= 0).cuda()], oq[torch.from_numpy(pos >= 0).cuda()])
@@ -135,7 +135,7 @@ def test_rope_at_gradients(esa, halves):
         step = f64(x + e) - f64(x - e)
         tol = 2.0 ** -24 * (np.sum(np.abs(f64(g)) * (np.abs(up) + np.abs(down))) + np.sum(np.abs(back) * np.abs(step)))
         assert abs(by_difference - np.sum(back * step)) <= tol
-    want = orc.rope(f64(g), pos, freq.numpy(), halves, gain, True)
+    want = orc.rope(f64(g), pos, freq.cpu().numpy(), halves, gain, True)
     assert np.all(np.abs(back - want) <= 2.0 ** -24 * np.abs(want) * (1 + 1e-9) + 2.0 ** -40)
 
 
@@ -150,13 +150,27 @@ def test_rope_at_passes_infinities_and_nan(esa):
         assert torch.equal(bad, want)
 
 
+def test_rope_at_frequencies_of_any_content(esa):
+    """Given ones: as they are; what is no number gives none in its own pair, and nothing else."""
+    rng = np.random.default_rng(13)
+    freq = np.array([64.0, -64.0, 1e-300, 0.0, 0.75, float("nan"), float("inf"), 1e300])
+    x = torch.from_numpy(rng.standard_normal((40, 2, 16))).float().cuda()
+    pos = rng.integers(1, 2 ** 31, 40)
+    y = esa.esa_rope_at(x, ints(pos), ints(freq, torch.float64))
+    want = orc.rope(f64(x)[..., [0, 1, 2, 3, 4, 8, 9, 10, 11, 12]], pos, freq[:5])
+    # angles of up to 2^37, rounded to 2^-53 of themselves
+    tol = 2.0 ** -24 * np.abs(want) + 64 * pos.max() * 2.0 ** -53 * 4
+    assert np.all(np.abs(f64(y)[..., [0, 1, 2, 3, 4, 8, 9, 10, 11, 12]] - want) <= tol)
+    assert torch.all(torch.isnan(y[..., [5, 6, 13, 14]]))
+
+
 def test_rope_at_far_tokens(esa):
     """Offsets beyond 32 bits: tokens a gigabyte apart."""
     x = torch.empty((6, 1 << 29), dtype=torch.bfloat16, device="cuda")[:, :256].view(6, 2, 128)
     x.copy_(torch.randn((6, 2, 128), generator=torch.Generator().manual_seed(1)))
     pos = np.arange(6) * 1000
     freq = esa.esa_rope_frequencies(5e5, 128)
-    check_rope(x, esa.esa_rope_at(x, ints(pos), freq), pos, freq.numpy(), True, 1.0, False, "bf16")
+    check_rope(x, esa.esa_rope_at(x, ints(pos), freq), pos, freq.cpu().numpy(), True, 1.0, False, "bf16")
     want = esa.esa_rope_at(x.contiguous(), ints(pos), freq)
     assert torch.equal(esa.esa_rope_at(x, ints(pos), freq, out_q=x), want)
 

@@ -103,7 +103,7 @@ def check_step(server, got, pool, kept_slots, rng_half=2.0 ** -8):
     there = pos >= 0
     for name, w in (("q", server.wq), ("k", server.wk)):
         rows = f64(w)[x]
-        want = orc.rope(rows, pos, server.freq.numpy(), False, 1.125)
+        want = orc.rope(rows, pos, server.freq.cpu().numpy(), False, 1.125)
         assert np.all(np.abs(f64(got[name]) - want)[there] <= (rng_half * np.abs(want) * (1 + 1e-9) + 2.0 ** -40)[there])
         assert np.array_equal(f64(got[name])[~there], rows[~there])
     caches = [f64(c) for c in server.caches]
