@@ -86,12 +86,12 @@ typedef struct {
  *   pos [n_tok]   position of a row, -1 for rows behind cu[n_seq]
  *   slot [n_tok]  int64: page * page_size + pos % page_size, a row's place in an array of one entry a position of the pool; -1 for
  *                 rows behind cu[n_seq] and where there is no page (beyond max_pages, or an entry outside [0, n_pages))
- *   workspace     esa_plan_paged_workspace_bytes(n_seq) bytes, 256-byte aligned
+ *   workspace     esa_plan_paged_workspace_bytes(state) bytes, 256-byte aligned; NULL where that is 0 (up to 4096 sequences, not in place)
  * What arrays hold that no sequence of calls leads to (a number of pages above max_pages or n_pages, say) is clamped, the outcome is then
  * unspecified.  n_seq == 0 is a no-op but for cu, lack, pos, slot and ring_at.
  * n_seq at most 2^24, n_tok below 2^31 - 2^16.  What is written overlaps nothing else, but that start, held and ring_at may be their *_in.
  */
-ESA_API size_t esa_plan_paged_workspace_bytes(int n_seq);
+ESA_API size_t esa_plan_paged_workspace_bytes(const esa_page_state* state);
 ESA_API int esa_plan_paged(const esa_page_state* state, const int32_t* grow, const int32_t* fresh, int64_t n_tok, int32_t* cu, int32_t* pos,
                int64_t* slot, int32_t* lack, void* workspace, size_t ws_bytes, void* stream);
 
@@ -112,7 +112,7 @@ ESA_API int esa_plan_paged(const esa_page_state* state, const int32_t* grow, con
  *   count   [n_seq] int32: rows that stand, cu[b] among them, which is the number of new tokens too; 0 for a sequence without rows
  * Rows behind cu[n_seq] are left as they were.  cu ascends from 0 to at most n_tok (other values are clamped, the results are then
  * unspecified).  dtype is that of target and draft: ESA_F32 or ESA_BF16.
- *   workspace esa_verify_drafts_workspace_bytes(n_seq, vocab) bytes, 256-byte aligned
+ *   workspace esa_verify_drafts_workspace_bytes(n_seq, vocab) bytes, 256-byte aligned; NULL where that is 0 (vocabularies of up to 16384)
  * n_tok == 0: counts are 0.  n_seq == 0 is a no-op.  n_tok and vocab below 2^31 - 2^16, n_seq at most 2^24.  Rows may start at any element; those on 16-byte
  * boundaries are read fastest.
  */

@@ -136,7 +136,7 @@ def _load() -> ctypes.CDLL:
     L.esa_rope_at.restype = i32
     L.esa_rope_at.argtypes = [ctypes.POINTER(RopeRows), i32, vp, i64, i32, i32, vp, i32, f64, i32, i32, vp]
     L.esa_plan_paged_workspace_bytes.restype = sz
-    L.esa_plan_paged_workspace_bytes.argtypes = [i32]
+    L.esa_plan_paged_workspace_bytes.argtypes = [ctypes.POINTER(PageState)]
     L.esa_plan_paged.restype = i32
     L.esa_plan_paged.argtypes = [ctypes.POINTER(PageState), vp, vp, i64, vp, vp, vp, vp, vp, sz, vp]
     L.esa_verify_drafts_workspace_bytes.restype = sz

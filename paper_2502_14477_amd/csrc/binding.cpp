@@ -856,7 +856,9 @@ ESA_ENTRY(plan_paged, 16) {
   s.page_size = int32_of(a[6]);
   on_gpu(pages);
   const c10::DeviceGuard guard(dev);
-  const Scratch ws = scratch(esa_plan_paged_workspace_bytes(s.n_seq));
+  const size_t need = esa_plan_paged_workspace_bytes(&s);
+  Scratch ws = {};
+  if (need > 0) ws = scratch(need);
   void *st = stream_on(dev), *wp = ws.p;
   const size_t wn = ws.n;
   launch([&] { return esa_plan_paged(&s, grow, fresh, n_tok, cu, pos, slot, lack, wp, wn, st); });
@@ -889,7 +891,9 @@ ESA_ENTRY(verify_drafts, 7) {
   if (!out) fresh_out = new_here({n}, at::kInt);
   if (!count) fresh_count = new_here({n_seq}, at::kInt);
   int32_t *op = (int32_t*)ptr(out ? *out : fresh_out), *np = (int32_t*)ptr(count ? *count : fresh_count);
-  const Scratch ws = scratch(esa_verify_drafts_workspace_bytes((int)n_seq, vocab));
+  const size_t need = esa_verify_drafts_workspace_bytes((int)n_seq, vocab);
+  Scratch ws = {};
+  if (need > 0) ws = scratch(need);
   void *st = stream_on(dev), *wp = ws.p, *target_p = ptr(target), *draft_p = ptr(draft);
   const size_t wn = ws.n;
   launch([&] { return esa_verify_drafts(target_p, ldt, draft_p, ldd, tp, up, cp, n, (int)n_seq, vocab, op, np, dt, wp, wn, st); });

@@ -236,7 +236,9 @@ template <int THREADS, int EACH> int launch_whole(const PlanArgs& a, bool alone,
 
 }  // namespace
 
-size_t plan_workspace(int n_seq) { return align_up(offsets_bytes(n_seq), 256); }
+size_t plan_workspace(int n_seq, bool in_place) {
+  return n_seq > kLdsSeqs ? align_up(offsets_bytes(n_seq), 256) : in_place ? align_up((2 * (size_t)n_seq + 2) * sizeof(int32_t), 256) : 0;
+}
 
 int launch_plan(const PlanArgs& a, hipStream_t st) {
   static OncePerDevice raised;

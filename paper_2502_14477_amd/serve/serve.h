@@ -34,9 +34,9 @@ struct PlanArgs {
   int64_t* slot;
   int64_t pages_ld;
   int n_seq, max_pages, n_pages, page_log2, n_tok;
-  void* ws;
+  void* ws;                   // null where plan_workspace is 0
 };
-size_t plan_workspace(int n_seq);
+size_t plan_workspace(int n_seq, bool in_place);
 int launch_plan(const PlanArgs& a, hipStream_t st);
 
 // ---------------------------------------------------------------- drafts
@@ -47,7 +47,7 @@ struct VerifyArgs {
   const float* u;
   int32_t *out, *count;
   int n_tok, n_seq, vocab;
-  void* ws;
+  void* ws;                        // null where verify_workspace is 0
 };
 size_t verify_workspace(int n_seq, int vocab);
 int launch_verify(const VerifyArgs& a, int dtype, hipStream_t st);

@@ -95,7 +95,10 @@ int esa_rope_at(const esa_rope_rows* rows, int n_rows, const int32_t* pos, int64
   return serve::launch_rope_at(a, dtype, (hipStream_t)stream);
 }
 
-size_t esa_plan_paged_workspace_bytes(int n_seq) { return n_seq < 0 || n_seq > kMostSeqs ? 256 : serve::plan_workspace(n_seq); }
+size_t esa_plan_paged_workspace_bytes(const esa_page_state* s) {
+  if (!s || s->n_seq < 0 || s->n_seq > kMostSeqs) return 0;
+  return serve::plan_workspace(s->n_seq, s->start == s->start_in || s->held == s->held_in || s->ring_at == s->ring_at_in);
+}
 
 int esa_plan_paged(const esa_page_state* state, const int32_t* grow, const int32_t* fresh, int64_t n_tok, int32_t* cu, int32_t* pos, int64_t* slot,
                    int32_t* lack, void* workspace, size_t ws_bytes, void* stream) {
@@ -115,8 +118,9 @@ int esa_plan_paged(const esa_page_state* state, const int32_t* grow, const int32
   for (const void* p : sequences)
     if (s.n_seq > 0 && (!p || !aligned(p, 4))) ESA_FAIL(ESA_EINVAL, "%s: null or misaligned pointer", name);
   if (!aligned(grow, 4) || (n_tok > 0 && (!pos || !slot || !aligned(pos, 4) || !aligned(slot, 8)))) ESA_FAIL(ESA_EINVAL, "%s: null or misaligned pointer", name);
-  const size_t need = esa_plan_paged_workspace_bytes(s.n_seq);
-  if (!workspace || !aligned(workspace, 256) || ws_bytes < need) ESA_FAIL(ESA_EWORKSPACE, "%s: workspace needs %zu bytes, 256-byte aligned", name, need);
+  const size_t need = esa_plan_paged_workspace_bytes(state);
+  if (need > 0 && (!workspace || !aligned(workspace, 256) || ws_bytes < need))
+    ESA_FAIL(ESA_EWORKSPACE, "%s: workspace needs %zu bytes, 256-byte aligned", name, need);
   serve::PlanArgs a;
   a.start_in = s.start_in;
   a.held_in = s.held_in;
@@ -143,7 +147,7 @@ int esa_plan_paged(const esa_page_state* state, const int32_t* grow, const int32
 }
 
 size_t esa_verify_drafts_workspace_bytes(int n_seq, int64_t vocab) {
-  return n_seq <= 0 || n_seq > kMostSeqs || vocab <= 0 || vocab > kMost ? 256 : serve::verify_workspace(n_seq, (int)vocab);
+  return n_seq <= 0 || n_seq > kMostSeqs || vocab <= 0 || vocab > kMost ? 0 : serve::verify_workspace(n_seq, (int)vocab);
 }
 
 int esa_verify_drafts(const void* target, int64_t ldt, const void* draft, int64_t ldd, const int32_t* tokens, const float* u, const int32_t* cu,
@@ -164,7 +168,8 @@ int esa_verify_drafts(const void* target, int64_t ldt, const void* draft, int64_
       if (ld < vocab || ld > INT64_MAX / 16 / n_tok) ESA_FAIL(ESA_EINVAL, "%s: rows of %lld elements, %lld apart", name, (long long)vocab, (long long)ld);
   }
   const size_t need = esa_verify_drafts_workspace_bytes(n_seq, vocab);
-  if (!workspace || !aligned(workspace, 256) || ws_bytes < need) ESA_FAIL(ESA_EWORKSPACE, "%s: workspace needs %zu bytes, 256-byte aligned", name, need);
+  if (need > 0 && (!workspace || !aligned(workspace, 256) || ws_bytes < need))
+    ESA_FAIL(ESA_EWORKSPACE, "%s: workspace needs %zu bytes, 256-byte aligned", name, need);
   serve::VerifyArgs a;
   a.target = (const char*)target;
   a.draft = (const char*)draft;

@@ -451,13 +451,14 @@ template <typename T, int N, int EACH> int launch_two(const VerifyArgs& a, hipSt
   ESA_LAUNCH_CHECK("verify_draw");
   return ESA_OK;
 }
+constexpr int kWhole = 16384;      // tokens of a row that one workgroup takes
 template <typename T> int launch_of(const VerifyArgs& a, hipStream_t st) {
   constexpr int N = kPiece<T>;
   if (a.vocab < N) return launch_whole<T, 1, 1, 64>(a, st);
   if (a.vocab <= 2048) return launch_whole<T, N, 8 / N, 256>(a, st);
   if (a.vocab <= 4096) return launch_whole<T, N, 8 / N, 512>(a, st);
   if (a.vocab <= 8192) return launch_whole<T, N, 8 / N, 1024>(a, st);
-  if (a.vocab <= 16384) return launch_whole<T, N, 16 / N, 1024>(a, st);
+  if (a.vocab <= kWhole) return launch_whole<T, N, 16 / N, 1024>(a, st);
   // Sixteen numbers a thread where that makes more than four workgroups a compute unit, else eight: 16 / 32 / 64 / 200 sequences of 131072 tokens 8.5 /
   // 10.9 / 15.0 / 30.4 us in a graph with sixteen, 7.7 / 10.5 / 15.1 / 33.4 with eight, 9.3 / 12.1 / 16.1 / 31.6 with 32.
   return (int64_t)chunks_of<16>(a.vocab) * a.n_seq > 1024 ? launch_two<T, N, 16>(a, st) : launch_two<T, N, 8>(a, st);
@@ -466,7 +467,7 @@ template <typename T> int launch_of(const VerifyArgs& a, hipStream_t st) {
 }  // namespace
 
 size_t verify_workspace(int n_seq, int vocab) {
-  return align_up((size_t)n_seq * (blocks_of<8>(vocab) * sizeof(double) + sizeof(int32_t)), 256);
+  return vocab <= kWhole ? 0 : align_up((size_t)n_seq * (blocks_of<8>(vocab) * sizeof(double) + sizeof(int32_t)), 256);
 }
 
 int launch_verify(const VerifyArgs& a, int dtype, hipStream_t st) { return dtype == ESA_F32 ? launch_of<float>(a, st) : launch_of<bf16_t>(a, st); }

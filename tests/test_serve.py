@@ -117,8 +117,10 @@ def test_plan_refuses():
     for f in ("start_in", "held_in", "ring_at_in", "start", "held", "ring_at", "pages", "ring"):
         assert plan(s=state(**{f: None})) == -1 and plan(s=state(**{f: ODD})) == -1
     assert esa.lib.esa_plan_paged(None, None, FAKE, 7, FAKE, FAKE, FAKE, FAKE, FAKE, 1 << 30, None) == -1
-    sizes = [esa.lib.esa_plan_paged_workspace_bytes(n) for n in (-1, 0, 1, 1000, 1 << 24)]
-    assert all(a <= b for a, b in zip(sizes, sizes[1:]))
+    for aside in ({}, dict(start=8 * FAKE, held=8 * FAKE, ring_at=8 * FAKE)):
+        sizes = [esa.lib.esa_plan_paged_workspace_bytes(ctypes.byref(state(n_seq=n, **aside))) for n in (-1, 0, 1, 1000, 4096, 4097, 1 << 24)]
+        assert all(a <= b for a, b in zip(sizes, sizes[1:])) and (sizes[4] == 0) == bool(aside) and sizes[5] > 0
+    assert esa.lib.esa_plan_paged_workspace_bytes(None) == 0
 
 
 # ---------------------------------------------------------------- drafts
@@ -127,11 +129,15 @@ def verify(target=FAKE, ldt=1000, draft=FAKE, ldd=1000, tokens=FAKE, u=FAKE, cu=
     return esa.lib.esa_verify_drafts(target, ldt, draft, ldd, tokens, u, cu, n_tok, n_seq, vocab, out, count, dtype, ws, ws_bytes, None)
 
 
+LONG = dict(vocab=16385, ldt=16385, ldd=16385)
+
+
 def test_verify_refuses():
+    assert esa.lib.esa_verify_drafts_workspace_bytes(3, 16384) == 0 < esa.lib.esa_verify_drafts_workspace_bytes(3, 16385)
     for change, code in ((dict(dtype=2), -2), (dict(n_tok=-1), -1), (dict(n_tok=1 << 31), -1), (dict(n_seq=-1), -1), (dict(n_seq=(1 << 24) + 1), -1), (dict(vocab=0), -1),
                          (dict(vocab=1 << 31), -1), (dict(ldt=999), -1), (dict(ldd=999), -1), (dict(ldt=1 << 60), -1), (dict(target=None), -1), (dict(target=ODD), -1),
                          (dict(draft=ODD), -1), (dict(tokens=None), -1), (dict(u=None), -1), (dict(cu=None), -1), (dict(out=None), -1), (dict(count=None), -1),
-                         (dict(out=FAKE), -1), (dict(ws=None), -3), (dict(ws=ODD), -3), (dict(ws_bytes=16), -3)):
+                         (dict(out=FAKE), -1), (dict(ws=None, **LONG), -3), (dict(ws=ODD, **LONG), -3), (dict(ws_bytes=16, **LONG), -3)):
         assert verify(**change) == code, change
         assert b"esa_verify_drafts" in esa.lib.esa_last_error()
     assert verify(n_seq=0, cu=None, count=None, ws=None) == 0
