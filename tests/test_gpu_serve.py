@@ -431,6 +431,19 @@ def test_verify_counts_what_is_no_probability_as_nothing(esa, vocab):
             check_verify(esa, held(p, dtype), tokens, cu, u, held(q, dtype) if drawn else None)
 
 
+@pytest.mark.parametrize("vocab", [1000, 20001])
+@pytest.mark.parametrize("power", [-140, -126, 120])
+def test_verify_weights_of_any_size(esa, vocab, power):
+    """Rows that sum to anything: subnormal numbers count, and sums leave fp32's range."""
+    rng = np.random.default_rng(36)
+    n, cu = 24, [0, 4, 8, 12, 16, 20, 24]
+    p, q = (x * 2.0 ** power for x in distributions(rng, n, vocab))
+    tokens = np.array([rng.choice(vocab, p=x / x.sum()) for x in q])
+    for dtype in ("f32", "bf16"):
+        for drawn in (True, False):
+            check_verify(esa, held(np.roll(p, -1, 0), dtype), tokens, cu, rng.random(n).astype(np.float32), held(q, dtype) if drawn else None)
+
+
 @pytest.mark.parametrize("vocab", [5, 9000, 50001, 300007])
 def test_verify_where_nothing_is_left(esa, vocab):
     """Differences that are nowhere positive: the target's own row; a row without any probability: no token."""
