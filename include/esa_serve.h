@@ -76,7 +76,7 @@ typedef struct {
 
 /*
  * Begins a step of fresh[b] new tokens of sequence b: what esa_append_paged and esa_attend_paged read as cu, start and pages.
- *   start[b] = max(start_in[b] + grow[b], 0); grow [n_seq] or NULL: what the step before has left in the cache (esa_verify_drafts'
+ *   start[b] = max(start_in[b] + grow[b], 0), but no position reaches 2^31 - 1; grow [n_seq] or NULL: what the step before has left in the cache (esa_verify_drafts'
  *           count; minus what the sequence has ends it).  Tokens of one step that are not kept are written over by the next.
  *   cu [n_seq + 1]  cu[0] = 0, cu[b + 1] = min(cu[b] + max(fresh[b], 0), n_tok)
  *   With need = min(ceil((start[b] + cu[b + 1] - cu[b]) / page_size), max_pages): entries [need, held_in[b]) are given back, behind

@@ -49,6 +49,7 @@ class Pages:
         for b in range(len(self.rows)):
             self.start[b] = max(self.start[b] + (0 if grow is None else int(grow[b])), 0)
             n = min(max(int(fresh[b]), 0), n_tok - cu[-1])
+            self.start[b] = min(self.start[b], 2 ** 31 - 1 - n)
             cu.append(cu[-1] + n)
             need.append(min(-(-(self.start[b] + n) // self.page), self.max_pages))
         for b, n in enumerate(need):

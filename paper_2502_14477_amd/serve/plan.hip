@@ -34,9 +34,9 @@ __host__ __device__ inline Offsets offsets_at(void* p, int n_seq) {
   return Offsets{ends, ends + n, ends + 2 * n, of};
 }
 
-// Sums that stop at INT32_MAX, of numbers that do not exceed it: what lies beyond is clamped to less in any case, and 32 bits do.
-constexpr uint32_t kMost = INT32_MAX;
-__device__ __forceinline__ uint32_t plus(uint32_t x, uint32_t y) { return min(x + y, kMost); }
+// Sums of numbers below 2^31 that stop at 2^32 - 1 (one instruction): what is beyond 2^31 is clamped to less in any case.
+__device__ __forceinline__ uint32_t plus(uint32_t x, uint32_t y) { return __builtin_elementwise_add_sat(x, y); }
+__device__ __forceinline__ int clamped(uint32_t x) { return (int)min(x, (uint32_t)INT32_MAX); }
 __device__ __forceinline__ uint32_t wave_sums(uint32_t x) {      // of the lanes up to each
   x = plus(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xF, 0xF, false));      // row_shr 1, 2, 4, 8
   x = plus(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xF, 0xF, false));
@@ -45,14 +45,15 @@ __device__ __forceinline__ uint32_t wave_sums(uint32_t x) {      // of the lanes
   x = plus(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xA, 0xF, false));      // row_bcast 15, 31
   return plus(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xC, 0xF, false));
 }
-// Over N numbers a thread, of which its wave's j-th are behind its (j - 1)-th: what is in front of each, and all of the workgroup's.  part: [WAVES].
+// Over N numbers a thread, of which its wave's j-th are behind its (j - 1)-th: what is in front of each, and all of the workgroup's.  part: [WAVES].  (Where
+// a sum has stopped, what is left of it without a number below 2^31 is still 2^31 or more.)
 template <int WAVES, int N> __device__ __forceinline__ uint32_t scan(const uint32_t (&x)[N], uint32_t (&before)[N], uint32_t* part) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   uint32_t sum = 0;
 #pragma unroll
   for (int j = 0; j < N; ++j) {
-    const uint32_t upto = wave_sums(x[j]), left = __shfl_up(upto, 1);
-    before[j] = plus(sum, lane ? left : 0);
+    const uint32_t upto = wave_sums(x[j]);
+    before[j] = plus(sum, upto - x[j]);
     sum = plus(sum, paged::lane_value(upto, 63));
   }
   if (lane == 0) part[wave] = sum;
@@ -107,10 +108,10 @@ template <int THREADS, int EACH> __device__ __forceinline__ Queue plan_offsets(c
       const int b = b0 + j * 64;
       if (b >= a.n_seq) break;
       const uint32_t front = plus(takes, take[j]);
-      o.of[b] = Of{start[j], had[j], (int)front, need[j]};
+      o.of[b] = Of{start[j], had[j], clamped(front), need[j]};
       o.row[b + 1] = (int)fresh[j];
-      o.give[b + 1] = (int)plus(plus(gives, give[j]), x[j]);
-      o.take[b + 1] = (int)plus(front, y[j]);
+      o.give[b + 1] = clamped(plus(plus(gives, give[j]), x[j]));
+      o.take[b + 1] = clamped(plus(front, y[j]));
       if (writes) {
         a.start[b] = start[j];
         a.cu[b + 1] = (int)fresh[j];
@@ -120,14 +121,14 @@ template <int THREADS, int EACH> __device__ __forceinline__ Queue plan_offsets(c
     takes = plus(takes, all_take);
   }
   const int first = (int)((uint32_t)max(at_in, 0) % (uint32_t)a.n_pages), count = min(max(count_in, 0), a.n_pages);
-  const int given = min((int)gives, a.n_pages - count), free = count + given, taken = min((int)takes, free);
+  const int given = min(clamped(gives), a.n_pages - count), free = count + given, taken = min(clamped(takes), free);
   if (tid == 0) o.row[0] = o.give[0] = o.take[0] = 0;
   if (tid == 0 && writes) {
     a.cu[0] = 0;
     const uint32_t next = (uint32_t)first + taken;      // below 2 n_pages
     a.ring_at[0] = (int)(next >= (uint32_t)a.n_pages ? next - a.n_pages : next);
     a.ring_at[1] = free - taken;
-    a.lack[0] = (int)takes - taken;
+    a.lack[0] = clamped(takes) - taken;
   }
   __syncthreads();
   for (int b = tid; writes && b < a.n_seq; b += THREADS) {

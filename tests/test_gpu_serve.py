@@ -309,6 +309,15 @@ def test_plan_beyond_the_table(esa):
     assert (loop.out.slot[:10] >= 0).sum() == 0
 
 
+@pytest.mark.parametrize("n_seq", [70, 700, 3000, 5000])
+def test_plan_of_more_rows_than_there_is_room_for(esa, n_seq):
+    """Numbers whose sums leave 32 bits: rows are those that fit, in order."""
+    loop = Loop(esa, n_seq, 3, 2 * n_seq, 16, 50, seed=8)
+    loop.step([2 ** 31 - 1] * n_seq, None)
+    loop.step([0] * (n_seq - 2) + [7, 2 ** 31 - 1], [2 ** 31 - 1] * n_seq)
+    assert loop.out.cu[-1].item() == 50 and loop.out.lack.item() == n_seq
+
+
 def test_plan_without_sequences_or_rows(esa):
     p = esa.esa_plan_paged(ints([]), ints([]), ints([]), torch.zeros((0, 3), dtype=torch.int32, device="cuda"), ints([4, 5, 6]), ints([2, 1]), 16, 5)
     assert p.cu.tolist() == [0] and p.pos.tolist() == [-1] * 5 and p.slot.tolist() == [-1] * 5 and p.ring_at.tolist() == [2, 1] and p.lack.item() == 0
