@@ -107,8 +107,10 @@ __device__ __forceinline__ void request(const VerifyArgs& a, const Drawn& d, int
     for (int m = 0; m < M; ++m) x[m].q = load<T, N>(qr + (WITHIN ? first + m * step : (int64_t)x[m].at));
   }
 }
-// Its weights: take(number, token, weight).  All lanes of the wave take part.  STRICT: as they are defined.  Otherwise, two instructions a number fewer, an
-// infinite probability of the target has an infinite weight; what is negative or NaN is left by the maximum with the draft's.
+// The larger one, y not being negative: as whole numbers, by which negative ones are less and NaN (of positive sign) stays.
+__device__ __forceinline__ float larger(float x, float y) { return __int_as_float(max(__float_as_int(x), __float_as_int(y))); }
+// Its weights: take(number, token, weight).  All lanes of the wave take part.  STRICT: as they are defined.  Otherwise, two instructions a number fewer,
+// where the target's probability is infinite or NaN the weight may be too, and the sum is.
 template <bool STRICT, typename T, int N, typename F>
 __device__ __forceinline__ void weigh(const Drawn& d, Pieces<T, N> x, F&& take) {
   if (__any(x.skip > 0)) {
@@ -122,11 +124,11 @@ __device__ __forceinline__ void weigh(const Drawn& d, Pieces<T, N> x, F&& take) 
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const float q = d.mode == 1 ? probability<T>(x.q.x[j]) : j == without ? 1.f : 0.f;
-      take(j, x.at + j, (double)fmaxf(of(x.p.x[j]), q) - (double)q);
+      take(j, x.at + j, (double)larger(of(x.p.x[j]), q) - (double)q);
     }
   } else {
 #pragma unroll
-    for (int j = 0; j < N; ++j) take(j, x.at + j, (double)fmaxf(of(x.p.x[j]), 0.f));
+    for (int j = 0; j < N; ++j) take(j, x.at + j, (double)larger(of(x.p.x[j]), 0.f));
   }
 }
 
@@ -299,9 +301,9 @@ template <typename T, int N, int EACH> __global__ __launch_bounds__(kThreads) vo
     add_up(r0);
     total += y.all;
   }
-  // An infinity among the target's probabilities, or nothing left and p itself wanted, of which there are no sums: one workgroup reads it all again.
-  for (bool infinite = !(total < __builtin_huge_val()); infinite || (!(total > 0.0) && d.mode != 0); infinite = false) {
-    if (!infinite) d.mode = 0;
+  // Infinities or NaN among the target's probabilities, or nothing left and p itself wanted, of which there are no sums: one workgroup reads it all again.
+  for (bool bad = !(total < __builtin_huge_val()); bad || (!(total > 0.0) && d.mode != 0); bad = false) {
+    if (!bad) d.mode = 0;
     at_hand = false;
     __syncthreads();
     for (int c = 0; c < chunks_of<EACH>(a.vocab); ++c) chunk_sums<true, false, EACH, T, N>(a, d, c, sums);
