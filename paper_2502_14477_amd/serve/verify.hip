@@ -6,10 +6,10 @@
 // outcome is that of the definition but for random numbers that lie within 1e-15 of a border.
 //
 // What bounds it is latency (a draft's test is four dependent loads: offsets, token, probabilities, row) and, where sequences are many, HBM.  Rows of
-// up to 16384 tokens are one workgroup's, in one launch (3.5 us and more).  Longer ones are cut into chunks, a workgroup to each, which finds
+// up to 16384 tokens are one workgroup's, in one launch (3.3 us and more).  Longer ones are cut into chunks, a workgroup to each, which finds
 // its sequence's last standing row by itself and leaves its waves' sums; a second launch finds the block in which the sums pass the drawn number, and
-// in it the token.  Rows are read in pieces of 16 bytes wherever they begin.  In a graph: one sequence of 32000 tokens and four drafts 6.4 us, sixteen of
-// 131072 7.3, 128 21.5 (103 MB, half of them out of the last-level cache).  With loads behind bounds checks and the token found by LDS atomics these
+// in it the token.  Rows are read in pieces of 16 bytes wherever they begin.  In a graph: one sequence of 32000 tokens and four drafts 6.2 us, sixteen of
+// 131072 7.0, 128 21.4 (103 MB, half of them out of the last-level cache).  With loads behind bounds checks and the token found by LDS atomics these
 // were 55, 83 and 117.  A wave that reads 1024 tokens of either row issues 240 vector instructions, and its SIMD 43 % of the time.
 #include "serve.h"
 
