@@ -58,9 +58,10 @@ __device__ __forceinline__ int page_of(const Batch& a, int n_pages, int b, int p
 }
 
 // ---------------------------------------------------------------- workgroups
-// A launch has fewer than 2^32 threads a dimension: more workgroups than that leaves room for lie in rows of 2^22.  The last row's may have nothing
-// to do.
-constexpr int kGridRow = 1 << 22;
+// A launch has fewer than 2^32 threads a dimension: more workgroups than that leaves room for, of up to 1024 threads, lie in rows of 2^21.  The last
+// row's may have nothing to do.
+constexpr int kGridRow = 1 << 21;
+static_assert((int64_t)kGridRow * 1024 < (int64_t)1 << 32, "threads of a row of workgroups");
 inline dim3 grid_for(int64_t blocks) {
   return blocks <= kGridRow ? dim3((unsigned)blocks) : dim3(kGridRow, (unsigned)((blocks + kGridRow - 1) / kGridRow));
 }
