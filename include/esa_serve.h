@@ -89,7 +89,8 @@ typedef struct {
  *   workspace     esa_plan_paged_workspace_bytes(state) bytes, 256-byte aligned; NULL where that is 0 (up to 4096 sequences, not in place)
  * What arrays hold that no sequence of calls leads to (a number of pages above max_pages or n_pages, say) is clamped, the outcome is then
  * unspecified.  n_seq == 0 is a no-op but for cu, lack, pos, slot and ring_at.
- * n_seq at most 2^24, n_tok below 2^31 - 2^16.  What is written overlaps nothing else, but that start, held and ring_at may be their *_in.
+ * n_seq at most 2^24, n_tok below 2^31 - 2^16.  What is written overlaps nothing else (such a call is refused), but that start, held and ring_at
+ * may be their *_in.
  */
 ESA_API size_t esa_plan_paged_workspace_bytes(const esa_page_state* state);
 ESA_API int esa_plan_paged(const esa_page_state* state, const int32_t* grow, const int32_t* fresh, int64_t n_tok, int32_t* cu, int32_t* pos,

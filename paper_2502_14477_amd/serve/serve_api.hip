@@ -26,6 +26,19 @@ bool strides_ok(int64_t n_tok, int64_t tok, int64_t heads, int64_t head, int64_t
   return outer_n == 1 || outer >= span - (inner_n > 1 ? inner - d : 0);
 }
 
+// Places of an array, and whether two share one; rows `ld` bytes apart, of `width` bytes each.
+struct Span {
+  uintptr_t lo, hi;
+};
+Span span(const void* p, int64_t n, size_t size) { return Span{(uintptr_t)p, (uintptr_t)p + (p ? (size_t)n * size : 0)}; }
+bool meet(const Span& a, const Span& b) { return (a.lo < b.hi) & (b.lo < a.hi) & (a.lo < a.hi) & (b.lo < b.hi); }
+bool meets_rows(const Span& a, const void* rows, int64_t n, int64_t ld, int64_t width) {
+  if (n == 0 || !meet(a, span(rows, (n - 1) * ld + width, 1))) return false;
+  if (a.lo <= (uintptr_t)rows) return true;
+  const uintptr_t at = (a.lo - (uintptr_t)rows) % ld;
+  return at < (uintptr_t)width || at + (a.hi - a.lo) > (uintptr_t)ld;
+}
+
 }  // namespace
 
 extern "C" {
@@ -121,6 +134,18 @@ int esa_plan_paged(const esa_page_state* state, const int32_t* grow, const int32
   const size_t need = esa_plan_paged_workspace_bytes(state);
   if (need > 0 && (!workspace || !aligned(workspace, 256) || ws_bytes < need))
     ESA_FAIL(ESA_EWORKSPACE, "%s: workspace needs %zu bytes, 256-byte aligned", name, need);
+  // What is written lies apart from everything else: workgroups read while others write.  The first three may be what they are made from.
+  const Span made_from[] = {span(s.start_in, s.n_seq, 4), span(s.held_in, s.n_seq, 4), span(s.ring_at_in, 2, 4), span(fresh, s.n_seq, 4), span(grow, s.n_seq, 4)};
+  const Span written[] = {span(s.start, s.n_seq, 4), span(s.held, s.n_seq, 4), span(s.ring_at, 2, 4), span(s.ring, s.n_pages, 4), span(cu, (int64_t)s.n_seq + 1, 4),
+                          span(lack, 1, 4), span(pos, n_tok, 4), span(slot, n_tok, 8), span(workspace, (int64_t)need, 1)};
+  bool over = false;
+  for (int i = 0; i < 9; ++i) {
+    for (int j = 0; j < 5; ++j) over |= meet(written[i], made_from[j]) & !(i < 3 && i == j && written[i].lo == made_from[j].lo);
+    for (int j = 0; j < i; ++j) over |= meet(written[i], written[j]);
+    over |= meets_rows(written[i], s.pages, s.n_seq, s.pages_ld * 4, (int64_t)s.max_pages * 4);
+  }
+  for (const Span& x : made_from) over |= meets_rows(x, s.pages, s.n_seq, s.pages_ld * 4, (int64_t)s.max_pages * 4);
+  if (over) ESA_FAIL(ESA_EINVAL, "%s: an array that is written overlaps another one", name);
   serve::PlanArgs a;
   a.start_in = s.start_in;
   a.held_in = s.held_in;

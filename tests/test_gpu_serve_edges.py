@@ -26,3 +26,31 @@ def test_verify_millions_of_sequences(esa, vocab):
     out, count = esa.esa_verify_drafts(p, torch.zeros(n, dtype=torch.int32, device="cuda"), cu, torch.full((n,), 0.5, device="cuda"))
     assert torch.equal(out, sure.int())
     assert torch.equal(count, rows)
+
+
+def test_plan_in_arrays_that_touch(esa):
+    """One buffer holds everything: arrays one right behind the other, one of them between the table's rows."""
+    n_seq, width, ld, n_pages, n_tok = 3, 5, 9, 20, 60
+    buffer = torch.full((200,), 55, dtype=torch.int32, device="cuda")
+    at = 0
+
+    def take(values):
+        nonlocal at
+        x = buffer[at:at + len(values)]
+        x.copy_(torch.tensor(values, dtype=torch.int32))
+        at += len(values)
+        return x
+
+    pages = buffer[at:at + n_seq * ld].view(n_seq, ld)[:, :width]
+    grow = buffer[at + width:at + width + n_seq]
+    grow.copy_(torch.tensor([0, 2, 1], dtype=torch.int32))
+    at += (n_seq - 1) * ld + width                                # right behind the table's last entry
+    ring, start, held, ring_at, new = take(list(range(n_pages))), take([0, 0, 0]), take([0, 0, 0]), take([4, n_pages]), take([20, 17, 16])
+    cu, pos, lack = take([7] * (n_seq + 1)), take([7] * n_tok), take([7])
+    end = at
+    slot = torch.empty(n_tok, dtype=torch.int64, device="cuda")
+    esa.esa_plan_paged(new, start, held, pages, ring, ring_at, 16, n_tok, grow=grow, out=esa.PagePlan(cu, start, held, ring_at, pos, slot, lack))
+    assert start.tolist() == [0, 2, 1] and held.tolist() == [2, 2, 2] and ring_at.tolist() == [10, 14] and lack.item() == 0
+    assert cu.tolist() == [0, 20, 37, 53] and pages[:, :2].tolist() == [[4, 5], [6, 7], [8, 9]] and torch.all(pages[:, 2:] == 55)
+    assert grow.tolist() == [0, 2, 1] and new.tolist() == [20, 17, 16] and torch.all(buffer[end:] == 55)
+    assert pos[:53].tolist() == list(range(20)) + list(range(2, 19)) + list(range(1, 17)) and torch.all(pos[53:] == -1)
