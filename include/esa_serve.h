@@ -115,7 +115,7 @@ ESA_API int esa_plan_paged(const esa_page_state* state, const int32_t* grow, con
  * unspecified).  dtype is that of target and draft: ESA_F32 or ESA_BF16.
  *   workspace esa_verify_drafts_workspace_bytes(n_seq, vocab) bytes, 256-byte aligned; NULL where that is 0 (vocabularies of up to 16384)
  * n_tok == 0: counts are 0.  n_seq == 0 is a no-op.  n_tok and vocab below 2^31 - 2^16, n_seq at most 2^24.  Rows may start at any element; those on 16-byte
- * boundaries are read fastest.
+ * boundaries are read fastest.  What is written overlaps nothing else (such a call is refused).
  */
 ESA_API size_t esa_verify_drafts_workspace_bytes(int n_seq, int64_t vocab);
 ESA_API int esa_verify_drafts(const void* target, int64_t ldt, const void* draft, int64_t ldd, const int32_t* tokens, const float* u, const int32_t* cu,

@@ -188,13 +188,23 @@ int esa_verify_drafts(const void* target, int64_t ldt, const void* draft, int64_
   if (n_tok > 0) {
     if (!target || !tokens || !u || !out || !aligned(target, es) || !aligned(draft, es) || !aligned(tokens, 4) || !aligned(u, 4) || !aligned(out, 4))
       ESA_FAIL(ESA_EINVAL, "%s: null or misaligned pointer", name);
-    if (tokens == out) ESA_FAIL(ESA_EINVAL, "%s: out over tokens", name);
     for (int64_t ld : {ldt, draft ? ldd : ldt})
       if (ld < vocab || ld > INT64_MAX / 16 / n_tok) ESA_FAIL(ESA_EINVAL, "%s: rows of %lld elements, %lld apart", name, (long long)vocab, (long long)ld);
   }
   const size_t need = esa_verify_drafts_workspace_bytes(n_seq, vocab);
   if (need > 0 && (!workspace || !aligned(workspace, 256) || ws_bytes < need))
     ESA_FAIL(ESA_EWORKSPACE, "%s: workspace needs %zu bytes, 256-byte aligned", name, need);
+  // What is written lies apart from everything else: a sequence's workgroups read while another's write.
+  const Span read[] = {span(tokens, n_tok, 4), span(u, n_tok, 4), span(cu, (int64_t)n_seq + 1, 4)};
+  const Span written[] = {span(out, n_tok, 4), span(count, n_seq, 4), span(workspace, (int64_t)need, 1)};
+  const int64_t width = vocab * (int64_t)es;
+  bool over = false;
+  for (int i = 0; i < 3; ++i) {
+    for (const Span& x : read) over |= meet(written[i], x);
+    for (int j = 0; j < i; ++j) over |= meet(written[i], written[j]);
+    if (n_tok > 0) over |= meets_rows(written[i], target, n_tok, ldt * (int64_t)es, width) || (draft && meets_rows(written[i], draft, n_tok, ldd * (int64_t)es, width));
+  }
+  if (over) ESA_FAIL(ESA_EINVAL, "%s: an array that is written overlaps another one", name);
   serve::VerifyArgs a;
   a.target = (const char*)target;
   a.draft = (const char*)draft;

@@ -65,3 +65,33 @@ def test_plan_refuses_the_table_it_reads():
             p, _ = places()
             p[name] = p["pages"] + 4 * element
             assert plan(p) == -1 and b"overlaps" in esa.lib.esa_last_error(), (name, element)
+
+
+# ---------------------------------------------------------------- drafts
+VERIFY = dict(target=4 * (ROWS - 1) * 20010 + 80000, draft=4 * (ROWS - 1) * 20010 + 80000, tokens=4 * ROWS, u=4 * ROWS, cu=4 * SEQS + 4, out=4 * ROWS, count=4 * SEQS, ws=4096)
+
+
+def verify(**kw):
+    at, p = 1 << 20, {}
+    for name, n in VERIFY.items():
+        p[name] = at
+        at += n + (-n) % 256
+    for name, (other, by) in kw.items():
+        p[name] = p[other] + by
+    return esa.lib.esa_verify_drafts(p["target"], 20010, p["draft"], 20010, p["tokens"], p["u"], p["cu"], ROWS, SEQS, 20000, p["out"], p["count"], 0, p["ws"], 4096, None)
+
+
+@pytest.mark.parametrize("a", ["out", "count"])
+@pytest.mark.parametrize("b", list(VERIFY))
+def test_verify_refuses_arrays_over_one_another(a, b):
+    if a != b:
+        for by in (0, 4 - VERIFY[a], (0 if b == "ws" else VERIFY[b]) - 4):
+            assert verify(**{a: (b, by)}) == -1 and b"esa_verify_drafts" in esa.lib.esa_last_error()
+
+
+def test_verify_refuses_what_lies_over_rows():
+    for rows in ("target", "draft"):
+        for element in (0, 19999, 20008, 6 * 20010 + 19999):      # the first, a row's last, in front of a row and into it, the last
+            assert verify(out=(rows, 4 * element)) == -1 and b"overlaps" in esa.lib.esa_last_error()
+    for name in ("target", "draft", "cu", "tokens", "u"):
+        assert verify(ws=(name, 0)) == -1
