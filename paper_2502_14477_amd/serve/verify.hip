@@ -362,8 +362,9 @@ template <typename T, int N, int EACH> __global__ __launch_bounds__(kThreads) vo
 //   32000         9.4 / 10.1 / 10.6 / 25.7 (1024, 32 each)                             6.1 / 7.2 / 10.2 / 22.0
 template <typename T, int N, int M, int THREADS> __global__ __launch_bounds__(THREADS) void verify_whole(VerifyArgs a) {
   constexpr int kWaves = THREADS / 64;
-  constexpr int kSums = M * kWaves, kLane = (kSums + 63) / 64;      // sums of a wave's pieces in the tokens' order, and how many a lane takes
-  __shared__ double sums[kLane * 64];
+  constexpr int kSums = M * kWaves;      // sums of a wave's pieces in the tokens' order, a lane to each
+  static_assert(kSums <= 64, "a lane to each sum");
+  __shared__ double sums[64];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, b = paged::block_index();
   if (b >= a.n_seq) return;
   const Rows s = rows_of(a, b);
@@ -378,8 +379,8 @@ template <typename T, int N, int M, int THREADS> __global__ __launch_bounds__(TH
   for (int i = tid; i < s.n; i += THREADS)
     if (i != kept) a.out[s.row0 + i] = i < kept ? a.tokens[s.row0 + i + 1] : -1;
   if (tid == 0) a.count[b] = kept + 1;
-  if (kSums < kLane * 64 && tid >= kSums && tid < kLane * 64) sums[tid] = 0.0;
-  double mine[kLane], upto[kLane], total;
+  if (tid >= kSums && tid < 64) sums[tid] = 0.0;
+  double mine, upto, total;
   for (bool strict = false;;) {
     Pieces<T, N> x[M];
     request<T, N, M, false>(a, d, tid * N, THREADS * N, x);
@@ -396,13 +397,9 @@ template <typename T, int N, int M, int THREADS> __global__ __launch_bounds__(TH
     }
     __syncthreads();
     // every wave adds them up for itself
-    total = 0.0;
-#pragma unroll
-    for (int e = 0; e < kLane; ++e) {
-      mine[e] = sums[e * 64 + lane];
-      upto[e] = total + wave_sums(mine[e]);
-      total = lane_double(upto[e], 63);
-    }
+    mine = sums[lane];
+    upto = wave_sums(mine);
+    total = lane_double(upto, 63);
     if (!(total < __builtin_huge_val()))
       strict = true;
     else if (total > 0.0 || d.mode == 0)
@@ -417,17 +414,9 @@ template <typename T, int N, int M, int THREADS> __global__ __launch_bounds__(TH
   }
   const double target = target_of(u, total);
   // the first sum that passes it, or else the last with any
-  int at = -1;
-  double base = 0.0;
-#pragma unroll
-  for (int e = kLane - 1; e >= 0; --e) {
-    const uint64_t past = __ballot(mine[e] > 0.0 && upto[e] > target), any = __ballot(mine[e] > 0.0);
-    const int l = past ? __ffsll((unsigned long long)past) - 1 : at < 0 && any ? 63 - __clzll((long long)any) : -1;
-    if (l >= 0) {
-      at = e * 64 + l;
-      base = l > 0 ? lane_double(upto[e], l - 1) : e > 0 ? lane_double(upto[e > 0 ? e - 1 : 0], 63) : 0.0;
-    }
-  }
+  const uint64_t past = __ballot(mine > 0.0 && upto > target), any = __ballot(mine > 0.0);
+  const int at = past ? __ffsll((unsigned long long)past) - 1 : 63 - __clzll((long long)any);
+  const double base = at > 0 ? lane_double(upto, at - 1) : 0.0;
   if (wave != at % kWaves) return;
   Pieces<T, N> piece[1];
   request<T, N, 1, false>(a, d, tid * N + at / kWaves * (THREADS * N), 0, piece);
