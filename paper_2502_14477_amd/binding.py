@@ -335,13 +335,41 @@ def esa_rope_frequencies(base: float, rot: int, scaling: int = ESA_SCALE_NONE, f
     return _native.rope_frequencies(base, rot, scaling, factor, length, fast, slow).to(device)
 
 
+class _Turn(torch.autograd.Function):
+    """esa_rope_at where gradients are wanted: the map is linear in the rows, and the transposed call is its way back."""
+
+    @staticmethod
+    def forward(ctx, q, k, pos, freq, pairs, gain, transposed, zeros):
+        ctx.save_for_backward(pos, freq)
+        ctx.how = pairs, gain, transposed
+        # rows of negative position have no influence: their gradients are 0
+        out = [torch.zeros(x.shape, dtype=x.dtype, device=x.device) if zeros and x is not None else None for x in (q, k)]
+        got = _native.rope_at(q, pos, freq, k, pairs, gain, transposed, *out)
+        if k is not None:
+            ctx.mark_non_differentiable(*(x for x, needed in zip(got, ctx.needs_input_grad) if not needed))
+        return got
+
+    @staticmethod
+    def backward(ctx, *grads):
+        pos, freq = ctx.saved_tensors
+        pairs, gain, transposed = ctx.how
+        wanted = [(g if g.stride(2) == 1 else g.contiguous()) if needed else None for g, needed in zip(grads, ctx.needs_input_grad)]
+        rows = [g for g in wanted if g is not None]
+        got = _Turn.apply(rows[0], rows[1] if len(rows) > 1 else None, pos, freq, pairs, gain, not transposed, True)
+        back = iter(got if len(rows) > 1 else (got,))
+        wanted = [None if g is None else next(back) for g in wanted]
+        return (*wanted, *[None] * (8 - len(wanted)))
+
+
 def esa_rope_at(q: torch.Tensor, pos: torch.Tensor, freq: torch.Tensor, k: Optional[torch.Tensor] = None, pairs: int = ESA_PAIRS_HALVES,
                 gain: float = 1.0, transposed: bool = False, out_q: Optional[torch.Tensor] = None, out_k: Optional[torch.Tensor] = None):
     """Rotary encoding of q [n_tok, h, d], and k [n_tok, h_kv, d] in the same call, at positions pos [n_tok] int32 on the GPU; tokens and heads may
     lie in any order of strides.  freq: esa_rope_frequencies' or any float64 on the GPU; the first 2 * len(freq) elements of a head
     turn, the others are copied.  transposed=True takes gradients of the outputs to gradients of the inputs.  Rows of negative
-    position are left as they are, undefined in a new tensor.  `out_q`, `out_k` may be q and k.  Returns q, or (q, k)."""
-    return _native.rope_at(q, pos, freq, k, pairs, gain, transposed, out_q, out_k)
+    position are left as they are, undefined in a new tensor.  `out_q`, `out_k` may be q and k.  Returns q, or (q, k).  Where q or k requires a
+    gradient the result has one (pos and freq have to stay as they are until then); outputs are not to be given then."""
+    got = _native.rope_at(q, pos, freq, k, pairs, gain, transposed, out_q, out_k)
+    return got if got is not None else _Turn.apply(q, k, pos, freq, pairs, gain, transposed, False)
 
 
 class PagePlan(NamedTuple):

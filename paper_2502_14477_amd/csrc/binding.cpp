@@ -10,6 +10,7 @@
 
 #include <ATen/EmptyTensor.h>
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/hip/impl/HIPCachingAllocatorMasqueradingAsCUDA.h>
 #include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 #include <ATen/ops/empty.h>
@@ -798,7 +799,8 @@ esa_rope_rows rope_rows_of(const at::Tensor& x, const at::Tensor& out) {
   return esa_rope_rows{ptr(x), ptr(out), s[0], s[1], so[0], so[1], (int)n[1]};
 }
 
-// q, pos, freq, k, pairs, gain, transposed, out_q, out_k
+// q, pos, freq, k, pairs, gain, transposed, out_q, out_k.  None, nothing being done, where the rotation belongs into a graph of gradients: the caller
+// comes again from there.
 ESA_ENTRY(rope_at, 9) {
   const at::Tensor &q = tensor_of(a[0]), &freq = tensor_of(a[2]);
   const at::Tensor *k = tensor_or_none(a[3]), *oq = tensor_or_none(a[7]), *ok = tensor_or_none(a[8]);
@@ -809,6 +811,13 @@ ESA_ENTRY(rope_at, 9) {
   const at::Tensor& pos = list_of(a[1], at::kInt, q.device(), q.size(0));
   const int dt = dtype_of(q), pairs = int32_of(a[4]), transposed = true_of(a[6]);
   const double gain = float_of(a[5]);
+  if (at::GradMode::is_enabled()) {
+    if (freq.requires_grad()) fail_esa(ESA_EUNSUPPORTED, "esa_rope_at: frequencies have no gradient");
+    if (q.requires_grad() || (k && k->requires_grad())) {
+      if (oq || ok) fail_esa(ESA_EINVAL, "esa_rope_at: given outputs would lose the rows' gradient");
+      Py_RETURN_NONE;
+    }
+  }
   on_gpu(q);
   const c10::DeviceGuard guard(q.device());
   at::Tensor fresh_q, fresh_k;
