@@ -54,3 +54,39 @@ def test_plan_in_arrays_that_touch(esa):
     assert cu.tolist() == [0, 20, 37, 53] and pages[:, :2].tolist() == [[4, 5], [6, 7], [8, 9]] and torch.all(pages[:, 2:] == 55)
     assert grow.tolist() == [0, 2, 1] and new.tolist() == [20, 17, 16] and torch.all(buffer[end:] == 55)
     assert pos[:53].tolist() == list(range(20)) + list(range(2, 19)) + list(range(1, 17)) and torch.all(pos[53:] == -1)
+
+
+def test_new_tensors_are_made_where_torch_sees_them(esa):
+    """A dispatch mode sees the outputs being made, and deterministic mode fills them: rows that a call leaves alone hold no number then."""
+    from torch.utils._python_dispatch import TorchDispatchMode
+
+    class Seen(TorchDispatchMode):
+        def __init__(self):
+            super().__init__()
+            self.shapes = []
+
+        def __torch_dispatch__(self, func, types, args=(), kwargs=None):
+            if func is torch.ops.aten.empty.memory_format:
+                self.shapes.append(tuple(args[0]))
+            return func(*args, **(kwargs or {}))
+
+    q, k = torch.ones((3, 2, 8), device="cuda"), torch.ones((3, 1, 8), device="cuda")
+    pos, freq = torch.tensor([4, -1, 0], dtype=torch.int32, device="cuda"), esa.esa_rope_frequencies(1e4, 8)
+    p, cu = torch.full((4, 10), 0.1, device="cuda"), torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    tokens, u = torch.zeros(4, dtype=torch.int32, device="cuda"), torch.full((4,), 0.55, device="cuda")
+    plain = esa.esa_rope_at(q, pos, freq, k=k), esa.esa_verify_drafts(p, tokens, cu, u)
+    with Seen() as seen:
+        watched = esa.esa_rope_at(q, pos, freq, k=k), esa.esa_verify_drafts(p, tokens, cu, u)
+    assert seen.shapes == [(3, 2, 8), (3, 1, 8), (4,), (2,)]
+    was = torch.are_deterministic_algorithms_enabled()
+    torch.use_deterministic_algorithms(True)
+    try:
+        filled = esa.esa_rope_at(q, pos, freq, k=k), esa.esa_verify_drafts(p, tokens, cu, u)
+    finally:
+        torch.use_deterministic_algorithms(was)
+    for got in (watched, filled):
+        for x, y in zip(plain[0], got[0]):
+            assert torch.equal(x[[0, 2]], y[[0, 2]]) and x.device == y.device and x.stride() == y.stride()
+        assert got[1][0][:2].tolist() == plain[1][0][:2].tolist() == [5, 5] and got[1][1].tolist() == [1, 1]
+    assert all(torch.all(torch.isnan(x[1])) for x in filled[0])
+    assert torch.all(filled[1][0][2:] == torch.iinfo(torch.int32).max)
