@@ -203,7 +203,8 @@ template <typename T, int N> int launch_of(const RopeArgs& a, hipStream_t st) {
   const size_t lds = (size_t)s.toks * a.half * sizeof(f64x2);
   // Results that, with what they are made of, are more than the last-level cache holds go past it: what reads them next finds none of them there
   // in any case.  Projection, rotation and a reader, 32 and 8 heads of 128, less the two others: 40000 tokens 153.3 -> 148.0 us, 16384 65.0 ->
-  // 62.4; but 8192 25.2 -> 28.4, 4096 16.2 -> 19.1.
+  // 62.4; but 8192 25.2 -> 28.4, 4096 16.2 -> 19.1.  In place, where rows are half of what is counted here, either store takes the same time (a fill,
+  // the rotation and a reader of 132, 160, 195, 244 MB: 93.1, 106.3, 131.0, 177.0 past the cache, 93.7, 106.7, 131.4, 177.4 not).
   constexpr int64_t kCache = (int64_t)256 << 20;
   const bool stream = N * sizeof(T) == 16 && (int64_t)a.n_tok * a.heads * (2 * a.half + a.rest) * (int64_t)sizeof(T) * 2 > kCache;
   auto run = [&](auto halves, auto streams) {
