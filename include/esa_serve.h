@@ -63,6 +63,8 @@ ESA_API int esa_rope_at(const esa_rope_rows* rows, int n_rows, const int32_t* po
  *   ring_at [2]      place of the first free page, number of them     } repeated with the same outcome)
  *   pages [n_seq][max_pages], row stride pages_ld; ring [n_pages]: free pages, from ring[first] on, round the end
  *   page_size        16, 32, 64 or 128; max_pages * page_size below 2^31 - 2^16
+ * A page is held once, by one sequence: one that several held (esa_attend_paged reads such tables) would come into the ring as often as it is given
+ * back, and be handed out twice.
  * int32 on the device throughout.  A fresh pool: start = held = 0, ring = 0, 1, ... n_pages - 1, ring_at = {0, n_pages}.
  */
 typedef struct {
@@ -77,12 +79,16 @@ typedef struct {
 /*
  * Begins a step of fresh[b] new tokens of sequence b: what esa_append_paged and esa_attend_paged read as cu, start and pages.
  *   start[b] = max(start_in[b] + grow[b], 0), but no position reaches 2^31 - 1; grow [n_seq] or NULL: what the step before has left in the cache (esa_verify_drafts'
- *           count; minus what the sequence has ends it).  Tokens of one step that are not kept are written over by the next.
+ *           count, and rows that were not verified; minus what the sequence has ends it).  Tokens of one step that are not kept are written over by
+ *           the next.
  *   cu [n_seq + 1]  cu[0] = 0, cu[b + 1] = min(cu[b] + max(fresh[b], 0), n_tok)
  *   With need = min(ceil((start[b] + cu[b + 1] - cu[b]) / page_size), max_pages): entries [need, held_in[b]) are given back, behind
  *   the free pages of the ring, sequence by sequence and in the order of the entries; then pages are taken from the front of the ring
  *   for entries [held_in[b], need), in the same order.  Those for which none is left become -1 and are not held; the next
  *   call tries again.  lack[0]: how many they are.  Other entries are left as they were.
+ *   A sequence has all of its step where held[b] * page_size >= start[b] + cu[b + 1] - cu[b].  Where it has not (pages are lacking, or max_pages are too
+ *   few), rows without a slot are stored nowhere, and the step must not count: the next call's grow[b] is 0 and the same tokens come again, or it ends.
+ *   Grown all the same, the sequence would have positions that nothing was written for, and esa_attend_paged reads whatever lies there.
  *   pos [n_tok]   position of a row, -1 for rows behind cu[n_seq]
  *   slot [n_tok]  int64: page * page_size + pos % page_size, a row's place in an array of one entry a position of the pool; -1 for
  *                 rows behind cu[n_seq] and where there is no page (beyond max_pages, or an entry outside [0, n_pages))
@@ -110,7 +116,11 @@ ESA_API int esa_plan_paged(const esa_page_state* state, const int32_t* grow, con
  * w is 0, w = p_a; where that is 0 too the token is -1.  A u that is negative or NaN draws as 0 does, one of
  * 1 or more the last token of positive weight; a draft does not stand by a u that is NaN.
  *   out     [n_tok] int32: the token that follows a row: tokens[i + 1] of rows before a, the drawn one of row a, -1 behind it
- *   count   [n_seq] int32: rows that stand, cu[b] among them, which is the number of new tokens too; 0 for a sequence without rows
+ *   count   [n_seq] int32: rows that stand, cu[b] among them, which is the number of new tokens too (a -1 that was drawn is counted); 0 for a sequence
+ *           without rows
+ * Every row behind a sequence's first one is taken for a draft.  A prompt's tokens are none: of a prompt the last row alone is verified, of one that
+ * goes on in the next step nothing.  In a step that holds prompts cu, target, draft, tokens and u are those of the verified rows, one behind the other,
+ * not the plan's, and a sequence grows by count and its rows that were not verified.
  * Rows behind cu[n_seq] are left as they were.  cu ascends from 0 to at most n_tok (other values are clamped, the results are then
  * unspecified).  dtype is that of target and draft: ESA_F32 or ESA_BF16.
  *   workspace esa_verify_drafts_workspace_bytes(n_seq, vocab) bytes, 256-byte aligned; NULL where that is 0 (vocabularies of up to 16384)

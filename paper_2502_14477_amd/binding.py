@@ -396,7 +396,7 @@ def esa_plan_paged(new: torch.Tensor, start: torch.Tensor, held: torch.Tensor, p
     back to the ring, those that are needed come from it: pages [n_seq, max_pages] and ring are changed in place.  n_tok is the number of
     rows that there is room for.  Returns cu, start and (with pages) what esa_append_paged and esa_attend_paged take, pos as esa_rope_at
     takes it, slot = page * page_size + pos % page_size (-1: none), the next call's held and ring_at, and lack, the pages that were not to be
-    had.  `out` is written into and returned; its start, held and ring_at may be the arguments of these names."""
+    had: a sequence with held[b] * page_size < start[b] + its rows repeats its step (grow[b] = 0).  A page is held once.  `out` is written into and returned; its start, held and ring_at may be the arguments of these names."""
     if out is None:
         out = PagePlan.empty(pages.shape[0], n_tok, pages.device)
     _native.plan_paged(new, start, held, pages, ring, ring_at, page_size, n_tok, grow, *out)
@@ -408,6 +408,7 @@ def esa_verify_drafts(target: torch.Tensor, tokens: torch.Tensor, cu: torch.Tens
     """Rows cu[b] .. cu[b+1] are sequence b's last token and the drafted ones behind it: tokens [n_tok] int32, target [n_tok, vocab] the target's
     probabilities behind each row, draft [n_tok, vocab] those that the row's token was drawn from (None: it was looked up), u [n_tok] fp32 random numbers
     (a drafted row's decides whether it stands, the first row's draws the token behind the last that stands).  Returns (out [n_tok],
-    count [n_seq]) int32: the token behind each row, -1 behind the drawn one, and how many there are.  Rows behind cu[n_seq] are left as they are,
-    undefined in a new tensor."""
+    count [n_seq]) int32: the token behind each row, -1 behind the drawn one (and drawn from a row without any probability), and how many there are.  A prompt's
+    tokens are no drafts: rows that are not verified are left out, by offsets of the others' own.  Rows behind cu[n_seq] are left as they are, undefined in
+    a new tensor."""
     return _native.verify_drafts(target, tokens, cu, u, draft, out, count)
