@@ -7,8 +7,8 @@
 // It is a copy with arithmetic, and runs as one: 19787 tokens of 32 and 8 heads of 128 bf16 elements 72 us, 406 MB at 5.65 TB/s, where a copy moves 5.4.
 // A workgroup takes a token (or a few) with all its heads, which share the sines and cosines by way of LDS; a thread turns one piece of 16 bytes of
 // either half, requested in front of the sines.  Four heads to a thread, as many fewer waves, were slower below 16 thousand tokens (1024: 7.3 us
-// for 5.6, sixteen 4.6 for 2.9 in a graph); pieces of 8 bytes are quicker for sixteen tokens (2.7), the same for 250, and slower from 500 on (1024: 7.2,
-// 16384: 100 for 64).  The frequencies lie on the device: as 1 KB of arguments they cost the host 0.5 to 1.2 us a launch.
+// for 5.8, sixteen 4.6 for 2.9 in a graph); pieces of 8 bytes are quicker for sixteen tokens (2.7), the same for 250, and slower from 500 on (1024: 7.2,
+// 16384: 100 for 64).  As it is 16, 250, 1024 and 16384 tokens take 2.9, 3.6, 6.0 and 52 us.  The frequencies lie on the device: as 1 KB of arguments they cost the host 0.5 to 1.2 us a launch.
 #include <type_traits>
 
 #include "serve.h"

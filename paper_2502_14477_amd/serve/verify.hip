@@ -6,11 +6,12 @@
 // outcome is that of the definition but for random numbers that lie within 1e-15 of a border.
 //
 // What bounds it is latency (a draft's test is four dependent loads: offsets, token, probabilities, row) and, where sequences are many, HBM.  Rows of
-// up to 16384 tokens are one workgroup's, in one launch (3.3 us and more).  Longer ones are cut into chunks, a workgroup to each, which finds
+// up to 16384 tokens are one workgroup's, in one launch (3.6 us and more).  Longer ones are cut into chunks, a workgroup to each, which finds
 // its sequence's last standing row by itself and leaves its waves' sums; a second launch finds the block in which the sums pass the drawn number, and
-// in it the token.  Rows are read in pieces of 16 bytes wherever they begin.  In a graph: one sequence of 32000 tokens and four drafts 6.2 us, sixteen of
-// 131072 7.0, 128 21.4 (103 MB, half of them out of the last-level cache).  With loads behind bounds checks and the token found by LDS atomics these
-// were 55, 83 and 117.  A wave that reads 1024 tokens of either row issues 240 vector instructions, and its SIMD 43 % of the time.
+// in it the token.  Rows are read in pieces of 16 bytes wherever they begin.  In a graph: one sequence of 32000 tokens and four drafts 6.3 us, sixteen of
+// 131072 7.1, 128 21.5 (103 MB, half of them out of the last-level cache).  With loads behind bounds checks and the token found by LDS atomics these
+// were 55, 83 and 117.  A wave that reads 1024 tokens of either row issues 216 vector instructions, its SIMD one in 38 % of its cycles; in bf16 242 and
+// 60 %: there instructions bound it, not bytes (128 sequences 17.7).
 #include "serve.h"
 
 namespace esa {
@@ -355,11 +356,17 @@ template <typename T, int N, int EACH> __global__ __launch_bounds__(kThreads) vo
 }
 
 // A short row is one workgroup's: a launch does all, M pieces a thread.  Its instructions are then one compute unit's, so that longer rows are quicker in
-// two launches.  us a call in a graph, 1 / 16 / 128 / 512 sequences of four drafts, fp32, in one launch and in two:
-//    2000 tokens  3.3 / 3.6 / 3.8 / 4.3 (256 threads; 1024: 4.2 / 4.5 / 4.8 / 6.8)    6.6 / 7.3 / 8.0 / 9.5
-//    8000         3.7 / 4.5 / 4.8 / 6.8 (1024)                                         6.4 / 7.6 / 8.1 / 12.0
-//   16000         5.7 / 5.9 / 6.2 / 13.6 (1024, sixteen numbers each)                  6.7 / 7.1 / 8.0 / 15.4
-//   32000         9.4 / 10.1 / 10.6 / 25.7 (1024, 32 each)                             6.1 / 7.2 / 10.2 / 22.0
+// two launches.  us a call in a graph, 1 / 16 / 128 / 512 sequences of four drafts, in one launch and in two:
+//    fp32   2000 tokens  3.7 / 3.9 / 4.0 / 4.4 (256 threads)                        6.2 / 7.2 / 7.4 / 7.9
+//           4000         3.6 / 4.1 / 4.3 / 4.9 (512)                                6.2 / 7.1 / 7.3 / 8.3
+//           8000         3.9 / 4.5 / 4.8 / 6.8 (1024)                               6.0 / 7.0 / 7.3 / 10.5
+//          16000         5.4 / 5.7 / 5.9 / 15.4 (1024, sixteen numbers each)        6.4 / 7.0 / 7.8 / 16.7
+//          32000         9.4 / 10.1 / 10.6 / 25.7 (a trial of 32 numbers each)      6.0 / 7.0 / 9.5 / 23.8
+//    bf16   2000         3.8 / 4.2 / 4.2 / 4.7                                      6.3 / 7.4 / 7.5 / 8.2
+//           4000         3.6 / 4.3 / 4.4 / 5.2                                      5.8 / 7.2 / 7.4 / 8.4
+//           8000         3.9 / 4.9 / 5.1 / 6.8                                      6.1 / 7.1 / 7.5 / 9.6
+//          16000         5.3 / 5.7 / 6.0 / 10.5                                     6.6 / 7.1 / 7.9 / 12.9
+// (2000 tokens by 1024 threads, fp32: 4.2 / 4.5 / 4.8 / 6.8.)
 template <typename T, int N, int M, int THREADS> __global__ __launch_bounds__(THREADS) void verify_whole(VerifyArgs a) {
   constexpr int kWaves = THREADS / 64;
   constexpr int kSums = M * kWaves;      // sums of a wave's pieces in the tokens' order, a lane to each
@@ -450,8 +457,9 @@ template <typename T> int launch_of(const VerifyArgs& a, hipStream_t st) {
   if (a.vocab <= 4096) return launch_whole<T, N, 8 / N, 512>(a, st);
   if (a.vocab <= 8192) return launch_whole<T, N, 8 / N, 1024>(a, st);
   if (a.vocab <= kWhole) return launch_whole<T, N, 16 / N, 1024>(a, st);
-  // Sixteen numbers a thread where that makes more than four workgroups a compute unit, else eight: 16 / 32 / 64 / 200 sequences of 131072 tokens 8.5 /
-  // 10.9 / 15.0 / 30.4 us in a graph with sixteen, 7.7 / 10.5 / 15.1 / 33.4 with eight, 9.3 / 12.1 / 16.1 / 31.6 with 32.
+  // Sixteen numbers a thread where that makes more than four workgroups a compute unit, else eight: 16 / 32 / 64 / 128 / 200 sequences of 131072 tokens 7.9 /
+  // 10.5 / 16.6 / 23.3 / 31.4 us in a graph with sixteen, 7.4 / 10.2 / 16.4 / 23.6 / 32.6 with eight; in bf16 8.2 / 8.9 / 11.7 / 17.8 / 22.3 and 7.6 / 8.9 /
+  // 12.6 / 19.7 / 25.9.
   return (int64_t)chunks_of<16>(a.vocab) * a.n_seq > 1024 ? launch_two<T, N, 16>(a, st) : launch_two<T, N, 8>(a, st);
 }
 
